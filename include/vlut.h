@@ -385,6 +385,102 @@ int vlut_query_plan(int64_t M, int64_t K, int64_t N, int* out4);
  */
 int vlut_query_lookup_waves(int64_t M, int64_t K, int64_t N);
 
+/*
+ * Between the stacked q|k|v projection of a decoder layer and its output projection: norms of heads and their rotation by position, a paged
+ * cache of keys and values, and attention of a batch whose sequences share a prefix.  Inference only.
+ */
+#define VLUT_TYPE_F32 0
+#define VLUT_TYPE_BF16 1
+#define VLUT_TYPE_F16 2
+#define VLUT_MAX_HEAD_FEATURES 256
+
+/*
+ * Heads of tokens: element (token, head, d) is data[token * token_stride + head * head_stride + d], D features contiguous, strides in elements.
+ * Views of a stacked projection's rows are such tensors.  weight: of the RMS norm ahead of the rotation, fp32, element (head, d) at
+ * weight[head * weight_stride + d] (weight_stride 0: one for all heads), NULL for no norm; of queries and keys that are read only.
+ */
+typedef struct vlut_heads {
+    const void* data;           /* dev; written through where the struct describes an output */
+    const float* weight;        /* dev or NULL */
+    int64_t token_stride, head_stride, weight_stride;
+    int32_t heads, type;        /* type: VLUT_TYPE_* */
+} vlut_heads;
+
+/*
+ * Rotation by position of the first `features` features (even, at most D) of a head, in pairs (i, i + features / 2), or (2i, 2i + 1) where
+ * interleaved != 0: (a, b) -> (a cos - b sin, b cos + a sin) with cos[position * features / 2 + i] and sin likewise.
+ * A position outside [0, rows) makes the rotated features NaN (nothing outside the tables is read).
+ */
+typedef struct vlut_rotation {
+    const float *cos, *sin;     /* dev, fp32 [rows][features / 2] */
+    const int64_t* positions;   /* dev, one for each token */
+    int64_t rows;
+    int32_t features, interleaved;
+} vlut_rotation;
+
+/*
+ * A paged cache: element (page, head, token in the page, d) of the keys is k[page * k_page_stride + head * k_head_stride + token * k_token_stride
+ * + d], of the values likewise; strides in elements, in any order.  page_size: a power of two up to 65536 (VLUT_ERR_UNSUPPORTED otherwise).
+ * type: VLUT_TYPE_BF16 or VLUT_TYPE_F16 (VLUT_ERR_UNSUPPORTED otherwise).
+ */
+typedef struct vlut_cache {
+    void *k, *v;                /* dev */
+    int64_t pages, page_size;
+    int64_t k_page_stride, k_head_stride, k_token_stride;
+    int64_t v_page_stride, v_head_stride, v_token_stride;
+    int32_t heads, type;
+} vlut_cache;
+
+/*
+ * RMS norm of every query and key head and the rotation by position, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * weight   (y = x without a weight), then the rotation (none: rotation NULL);
+ * fp32 throughout, rounded once to the outputs' type.
+ *   N tokens (1 <= N < 2^24), D features: even, 2 <= D <= VLUT_MAX_HEAD_FEATURES; N * all heads < 2^31
+ *   q, k           of one type, any strides and alignment; k NULL (with k_out) for queries alone
+ *   q_out, k_out   of one type; an output may be the input itself (same data, type and strides), else they must not overlap
+ */
+int vlut_norm_rope(const vlut_heads* q, const vlut_heads* k_or_null, float eps, const vlut_rotation* rotation_or_null, int64_t N, int64_t D,
+                   const vlut_heads* q_out, const vlut_heads* k_out_or_null, void* stream);
+
+/*
+ * Keys (after norm and rotation as in vlut_norm_rope) and values (as they are) of N tokens to the slots of a paged cache, converted to the cache's type; the
+ * tokens' queries in the same launch where they are given (to q_out, of the cache's type).
+ *   slots   dev, one for each token: page * page_size + token in the page.  A token whose slot is negative (padding) or past the cache is
+ *           left out; its queries are not.  Slots that occur twice: either token's values, feature by feature.
+ *   k, v, q of one type; k and v have the cache's heads; sizes as in vlut_norm_rope
+ */
+int vlut_append_kv(const vlut_heads* k, const vlut_heads* v, const vlut_heads* q_or_null, float eps, const vlut_rotation* rotation_or_null,
+                   const int64_t* slots, int64_t N, int64_t D, const vlut_cache* cache, const vlut_heads* q_out_or_null, void* stream);
+
+/*
+ * Attention of B sequences with n query tokens each, over a paged cache whose first prefix_len tokens they share.  Query j (of the last
+ * query_lens[b] of sequence b's own_lens[b] own tokens) sees the whole prefix and the own tokens 0 .. own_lens[b] - query_lens[b] + j:
+ *   out[b][j][h] = sum_t softmax_t(scale * q[b][j][h] . k[t][h / G]) v[t][h / G],   G = query heads / key heads.
+ * The prefix is worked on once for all sequences.  A query that sees nothing, and queries from query_lens[b] on, get 0 (and lse -inf).  Keys and
+ * values that a query does not see have no influence on it, NaN and infinities included.
+ *   q, out            B * n tokens: token j of sequence b at b * sequence_stride + j * token_stride; q of the cache's type, out of that type or
+ *                     fp32.  With a 16-bit output the softmax weights are rounded to that type for the product with V; with fp32 they are carried
+ *                     in two such terms.  Scores, sums and partial results are fp32.
+ *   prefix_pages      dev, ceil(prefix_len / page_size) pages of the prefix (may be NULL for prefix_len 0)
+ *   page_table        dev [B][table_stride]: pages of each sequence's own tokens, own token 0 first in page 0 (may be NULL for max_own_len 0);
+ *                     ceil(max_own_len / page_size) of each row are valid where own_lens reaches them
+ *   own_lens          dev [B], 0 <= own_lens[b] <= max_own_len (host: an upper bound that sizes the launch)
+ *   query_lens        dev [B] or NULL (all n)
+ *   lse               dev or NULL, fp32 [B][n][heads]: log of the sum of exp(scale * q . k)
+ *   scale             finite and > 0
+ *   workspace         dev, 16-byte aligned, workspace_bytes >= vlut_shared_prefix_attention_bytes(...); may be NULL when that is 0
+ * D: a multiple of four, 8 <= D <= VLUT_MAX_HEAD_FEATURES, and q, k, v and 16-bit outputs have even strides and dword-aligned data
+ * (VLUT_ERR_UNSUPPORTED otherwise).  Lengths out of range and page numbers outside the cache are found on the device: they read nothing, and
+ * the queries that depend on them get NaN.
+ * vlut_query_shared_prefix_attention: out4 (host) = { query rows per workgroup, parts of the prefix, parts of an own sequence, workgroups }.
+ */
+size_t vlut_shared_prefix_attention_bytes(int64_t B, int64_t n, int64_t q_heads, int64_t k_heads, int64_t D, int64_t prefix_len, int64_t max_own_len);
+int vlut_query_shared_prefix_attention(int64_t B, int64_t n, int64_t q_heads, int64_t k_heads, int64_t D, int64_t prefix_len, int64_t max_own_len, int* out4);
+int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride, const vlut_cache* cache, const int32_t* prefix_pages, int64_t prefix_len,
+                                 const int32_t* page_table, int64_t table_stride, const int32_t* own_lens, int64_t max_own_len,
+                                 const int32_t* query_lens_or_null, int64_t B, int64_t n, int64_t D, float scale, const vlut_heads* out,
+                                 int64_t out_sequence_stride, float* lse_or_null, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

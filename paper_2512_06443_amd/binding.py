@@ -36,9 +36,28 @@ EXPORTS = [
     "vlut_mpgemm_mixed", "vlut_static_scratch_bytes", "vlut_mpgemm_static", "vlut_query_lookup_waves",
     "vlut_query_kernel", "vlut_query_matrix_plan", "vlut_workspace_used", "vlut_workspace_used_g5", "vlut_workspace_used_mixed",
     "vlut_mpgemm_lean", "vlut_mpgemm_g5_lean", "vlut_mpgemm_mixed_lean",
+    "vlut_norm_rope", "vlut_append_kv", "vlut_shared_prefix_attention", "vlut_shared_prefix_attention_bytes",
+    "vlut_query_shared_prefix_attention",
 ]
 
 _lib = None
+
+
+class _Heads(ctypes.Structure):          # vlut_heads
+    _fields_ = [("data", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("weight_stride", ctypes.c_int64), ("heads", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
+class _Rotation(ctypes.Structure):       # vlut_rotation
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("features", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class _Cache(ctypes.Structure):          # vlut_cache
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int64),
+                ("k_page", ctypes.c_int64), ("k_head", ctypes.c_int64), ("k_token", ctypes.c_int64),
+                ("v_page", ctypes.c_int64), ("v_head", ctypes.c_int64), ("v_token", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("type", ctypes.c_int32)]
 
 
 class VlutError(RuntimeError):
@@ -99,6 +118,14 @@ def lib() -> ctypes.CDLL:
         L.vlut_query_matrix_plan.argtypes, L.vlut_query_matrix_plan.restype = [ci, i64, i64, i64, ctypes.POINTER(ci)], ci
         L.vlut_static_scratch_bytes.argtypes, L.vlut_static_scratch_bytes.restype = [], sz
         L.vlut_mpgemm_static.argtypes, L.vlut_mpgemm_static.restype = [p, cf, p, p, i64, i64, i64, p, i64, p, p], ci
+        heads, rotation, cache = (ctypes.POINTER(s) for s in (_Heads, _Rotation, _Cache))
+        L.vlut_norm_rope.argtypes, L.vlut_norm_rope.restype = [heads, heads, cf, rotation, i64, i64, heads, heads, p], ci
+        L.vlut_append_kv.argtypes, L.vlut_append_kv.restype = [heads, heads, heads, cf, rotation, p, i64, i64, cache, heads, p], ci
+        L.vlut_shared_prefix_attention_bytes.argtypes, L.vlut_shared_prefix_attention_bytes.restype = [i64] * 7, sz
+        L.vlut_query_shared_prefix_attention.argtypes = [i64] * 7 + [ctypes.POINTER(ci)]
+        L.vlut_query_shared_prefix_attention.restype = ci
+        L.vlut_shared_prefix_attention.argtypes = [heads, i64, cache, p, i64, p, i64, p, i64, p, i64, i64, i64, cf, heads, i64, p, p, sz, p]
+        L.vlut_shared_prefix_attention.restype = ci
         L.vlut_set_plan.argtypes, L.vlut_set_plan.restype = [ci, ci, ci, ci], ci
         L.vlut_query_plan.argtypes, L.vlut_query_plan.restype = [i64, i64, i64, ctypes.POINTER(ci)], ci
         _load_native(L)
@@ -485,3 +512,166 @@ def mpgemm_g5(packed: torch.Tensor, w_scale: float, a_q: torch.Tensor, a_scale: 
                               0 if workspace is None else workspace.numel() * workspace.element_size(), _stream())
     _check(rc, "vlut_mpgemm_g5")
     return y, acc
+
+
+# ---- between the projections: heads, paged cache, attention over a shared prefix
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _on_gpu(t: torch.Tensor, dim: int, what: str) -> None:
+    """A tensor whose features (its last dimension) are contiguous."""
+    if not t.is_cuda or t.dim() != dim or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what}: a GPU tensor of {dim} dimensions with contiguous features is wanted")
+    if t.dtype not in _TYPES:
+        raise ValueError(f"{what}: fp32, bf16 or fp16 is wanted, not {t.dtype}")
+
+
+def _indices(t: torch.Tensor, dtype: torch.dtype, size: int, what: str) -> None:
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or not t.is_contiguous() or t.numel() < size:
+        raise ValueError(f"{what}: a contiguous {dtype} GPU tensor of {size} values is wanted")
+
+
+def _heads(t: Optional[torch.Tensor], weight: Optional[torch.Tensor] = None, what: str = "heads") -> Optional[_Heads]:
+    """[N][heads][D] and the norm's weight, fp32 [D] or [heads][D]."""
+    if t is None:
+        return None
+    _on_gpu(t, 3, what)
+    if weight is not None and not (weight.is_cuda and weight.dtype == torch.float32 and tuple(weight.shape) in ((t.shape[2],), tuple(t.shape[1:]))
+                                   and (weight.shape[-1] == 1 or weight.stride(-1) == 1)):
+        raise ValueError(f"{what}: the norm's weight is an fp32 GPU tensor [D] or [heads][D]")
+    return _Heads(t.data_ptr(), _ptr(weight), t.stride(0), t.stride(1), weight.stride(0) if weight is not None and weight.dim() == 2 else 0,
+                  t.shape[1], _TYPES[t.dtype])
+
+
+def _rotation(positions, cos, sin, interleaved: bool, N: int) -> Optional[_Rotation]:
+    if cos is None and sin is None and positions is None:
+        return None
+    if cos is None or sin is None or positions is None:
+        raise ValueError("the rotation takes positions, cos and sin, or none of them")
+    for t, what in ((cos, "cos"), (sin, "sin")):
+        if not t.is_cuda or t.dtype != torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.shape != cos.shape:
+            raise ValueError(f"{what}: a contiguous fp32 GPU tensor [positions][features / 2] is wanted")
+    _indices(positions, torch.int64, N, "positions")
+    return _Rotation(cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), cos.shape[0], 2 * cos.shape[1], bool(interleaved))
+
+
+def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, D: int) -> _Cache:
+    """[pages][heads][page_size][D] twice, in any order of the first three in memory."""
+    _on_gpu(k_cache, 4, "k_cache")
+    _on_gpu(v_cache, 4, "v_cache")
+    if k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype or k_cache.shape[3] != D:
+        raise ValueError("k_cache and v_cache: one shape [pages][heads][page_size][D] and one type are wanted")
+    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), k_cache.shape[0], k_cache.shape[2], k_cache.stride(0), k_cache.stride(1), k_cache.stride(2),
+                  v_cache.stride(0), v_cache.stride(1), v_cache.stride(2), k_cache.shape[1], _TYPES[k_cache.dtype])
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
+              sin: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+              eps: float = 1e-6, interleaved: bool = False, dtype: Optional[torch.dtype] = None, q_out: Optional[torch.Tensor] = None,
+              k_out: Optional[torch.Tensor] = None):
+    """Runs vlut_norm_rope: the RMS norm of every head of q [N][heads][D] and k (where a weight is given: fp32 [D] or [heads][D]), then the
+    rotation by the tokens' int64 `positions` with the tables cos and sin, fp32 [rows][features / 2] (where they are given), in one pass.
+    The tensors may be views of a stacked projection's rows.  Returns (q_out, k_out or None) of type `dtype` (default: q's); an output may
+    be the input."""
+    _on_gpu(q, 3, "q")
+    N, _, D = q.shape
+    if dtype is None:
+        dtype = q.dtype if q_out is None else q_out.dtype
+    if k is not None and (k.dim() != 3 or k.shape[0] != N or k.shape[2] != D):
+        raise ValueError("k: [N][heads][D] of q's tokens and features is wanted")
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=dtype, device=q.device)
+    for out, x, what in ((q_out, q, "q_out"), (k_out, k, "k_out")):
+        if (out is None) != (x is None) or (out is not None and out.shape != x.shape):
+            raise ValueError(f"{what}: a tensor of the input's shape is wanted")
+    _check(lib().vlut_norm_rope(_ref(_heads(q, q_weight, "q")), _ref(_heads(k, k_weight, "k")), eps, _ref(_rotation(positions, cos, sin, interleaved, N)),
+                                N, D, _ref(_heads(q_out, what="q_out")), _ref(_heads(k_out, what="k_out")), _stream()), "vlut_norm_rope")
+    return q_out, k_out
+
+
+def append_kv(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+              positions: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
+              k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False, q: Optional[torch.Tensor] = None,
+              q_weight: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
+    """Runs vlut_append_kv: keys (normed and rotated as in `norm_rope`) and values, [N][heads][D], to the int64 `slots` (page * page_size +
+    token in the page; negative: left out) of the caches [pages][heads][page_size][D] (bf16 or fp16).  With q the queries are normed and
+    rotated in the same launch: returns q_out, of the cache's type (None without q)."""
+    _on_gpu(k, 3, "k")
+    N, _, D = k.shape
+    if tuple(v.shape) != tuple(k.shape) or (q is not None and (q.dim() != 3 or q.shape[0] != N or q.shape[2] != D)):
+        raise ValueError("q, k and v: [N][heads][D] of the same tokens and features are wanted")
+    _indices(slots, torch.int64, N, "slots")
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=k_cache.dtype, device=q.device)
+    if (q is None) != (q_out is None) or (q is not None and q_out.shape != q.shape):
+        raise ValueError("q_out: a tensor of q's shape is wanted")
+    _check(lib().vlut_append_kv(_ref(_heads(k, k_weight, "k")), _ref(_heads(v, what="v")), _ref(_heads(q, q_weight, "q")), eps,
+                                _ref(_rotation(positions, cos, sin, interleaved, N)), slots.data_ptr(), N, D, _ref(_cache(k_cache, v_cache, D)),
+                                _ref(_heads(q_out, what="q_out")), _stream()), "vlut_append_kv")
+    return q_out
+
+
+def shared_prefix_attention_bytes(B: int, n: int, q_heads: int, k_heads: int, D: int, prefix_len: int, max_own_len: int) -> int:
+    return lib().vlut_shared_prefix_attention_bytes(B, n, q_heads, k_heads, D, prefix_len, max_own_len)
+
+
+def query_shared_prefix_attention(B: int, n: int, q_heads: int, k_heads: int, D: int, prefix_len: int, max_own_len: int) -> Tuple[int, int, int, int]:
+    """(query rows per workgroup, parts of the prefix, parts of an own sequence, workgroups) of such a call."""
+    out = (ctypes.c_int * 4)()
+    _check(lib().vlut_query_shared_prefix_attention(B, n, q_heads, k_heads, D, prefix_len, max_own_len, out), "vlut_query_shared_prefix_attention")
+    return out[0], out[1], out[2], out[3]
+
+
+def shared_prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, prefix_pages: Optional[torch.Tensor], prefix_len: int,
+                            page_table: Optional[torch.Tensor], own_lens: torch.Tensor, query_lens: Optional[torch.Tensor] = None,
+                            max_own_len: Optional[int] = None, scale: Optional[float] = None, dtype: Optional[torch.dtype] = None,
+                            out: Optional[torch.Tensor] = None, want_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """Runs vlut_shared_prefix_attention: q [B][n][heads][D] (the cache's type) over the first `prefix_len` tokens of `prefix_pages` (int32), which
+    all sequences share, and over each sequence's own `own_lens[b]` tokens (int32 [B]) in the pages of its row of `page_table` (int32
+    [B][pages]); its last `query_lens[b]` (default n) own tokens are the queries', each of which sees up to itself.
+    max_own_len: an upper bound of own_lens (default: what the table's rows hold).  scale: default D ** -0.5.  dtype: fp32 or the
+    cache's (default).  Returns (out [B][n][heads][D], lse fp32 [B][n][heads] or None)."""
+    _on_gpu(q, 4, "q")
+    B, n, Hq, D = q.shape
+    cache = _cache(k_cache, v_cache, D)
+    page_size, Hk = k_cache.shape[2], k_cache.shape[1]
+    table_stride = 0
+    if page_table is not None:
+        if not page_table.is_cuda or page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != B or (
+                page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table: an int32 GPU tensor [B][pages] is wanted")
+        table_stride = page_table.stride(0)
+    room = 0 if page_table is None else page_table.shape[1] * page_size
+    if max_own_len is None:
+        max_own_len = room
+    if max_own_len > room:
+        raise ValueError("max_own_len: more tokens than the rows of page_table hold")
+    if prefix_len > 0:
+        if prefix_pages is None:
+            raise ValueError("prefix_pages: the pages of the prefix are wanted")
+        _indices(prefix_pages, torch.int32, -(-prefix_len // page_size), "prefix_pages")
+    _indices(own_lens, torch.int32, B, "own_lens")
+    if query_lens is not None:
+        _indices(query_lens, torch.int32, B, "query_lens")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype if dtype is None else dtype, device=q.device)
+    _on_gpu(out, 4, "out")
+    if out.shape != q.shape:
+        raise ValueError("out: a tensor of q's shape is wanted")
+    lse = torch.empty((B, n, Hq), dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        nbytes = shared_prefix_attention_bytes(B, n, Hq, Hk, D, prefix_len, max_own_len)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    rows = [_Heads(t.data_ptr(), None, t.stride(1), t.stride(2), 0, Hq, _TYPES[t.dtype]) for t in (q, out)]
+    _check(lib().vlut_shared_prefix_attention(
+        ctypes.byref(rows[0]), q.stride(0), ctypes.byref(cache), _ptr(prefix_pages), prefix_len, _ptr(page_table), table_stride, own_lens.data_ptr(),
+        max_own_len, _ptr(query_lens), B, n, D, D ** -0.5 if scale is None else scale, ctypes.byref(rows[1]), out.stride(0), _ptr(lse),
+        _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()), "vlut_shared_prefix_attention")
+    return out, lse

@@ -4,11 +4,14 @@ from __future__ import annotations
 import os
 import shlex
 import subprocess
+import tempfile
 import warnings
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SRC = os.path.join(_HERE, "csrc", "vlut.hip")
+SOURCES = (SRC, os.path.join(_HERE, "csrc", "attention.hip"))      # the library's translation units
 LIB = os.path.join(_HERE, "libvlut.so")
 TORCH_SRC = os.path.join(_HERE, "csrc", "torch_calls.cpp")
 TORCH_LIB = os.path.join(_HERE, "_vlut_torch.so")
@@ -25,7 +28,7 @@ HIPCC_FLAGS = [
 def build(force: bool = True) -> str:
     """Compiles the library and, where it can, the native form of the binding's calls; returns the library's path.  force=False
     only builds what is missing or stale."""
-    csrc = os.path.dirname(SRC)         # vlut.hip includes the kernel headers next to it
+    csrc = os.path.dirname(SRC)         # the translation units include the kernel headers next to them
     sources = [os.path.join(csrc, f) for f in os.listdir(csrc)] + [os.path.join(INCLUDE, "vlut.h")]
     newest = max(os.path.getmtime(f) for f in sources)
 
@@ -34,7 +37,11 @@ def build(force: bool = True) -> str:
 
     if stale(LIB):
         hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-        _run([hipcc, *HIPCC_FLAGS, "-I", INCLUDE, SRC, "-o", LIB])
+        with tempfile.TemporaryDirectory() as scratch, ThreadPoolExecutor(len(SOURCES)) as pool:
+            objects = [os.path.join(scratch, os.path.basename(src) + ".o") for src in SOURCES]
+            flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+            list(pool.map(lambda so: _run([hipcc, *flags, "-I", INCLUDE, "-c", so[0], "-o", so[1]]), zip(SOURCES, objects)))
+            _run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", *objects, "-o", LIB])
     if stale(TORCH_LIB) or not _built_for_this_torch():
         _build_native()
     return LIB

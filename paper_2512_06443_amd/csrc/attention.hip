@@ -1,0 +1,391 @@
+// Between the projections of a decoder layer, for MI355X (gfx950): norms and rotation of heads, the paged cache, attention over a shared prefix.
+// Kernels and their part of the C ABI; a translation unit of its own, compiled beside vlut.hip and linked with it.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+#include <cstdint>
+
+#include "vlut.h"
+
+#include "common.hip.h"
+#include "launch.hip.h"
+#include "heads_kernel.hip.h"
+#include "attention_kernel.hip.h"
+
+namespace {
+
+bool type_ok(int type) { return type == VLUT_TYPE_F32 || type == VLUT_TYPE_BF16 || type == VLUT_TYPE_F16; }
+int type_bytes(int type) { return type == VLUT_TYPE_F32 ? 4 : 2; }
+bool power_of_two(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
+int log2_of(int64_t v) {
+    int k = 0;
+    while (((int64_t)1 << k) < v) ++k;
+    return k;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Heads
+// ---------------------------------------------------------------------------------------------
+// Vectors of 4, 2 or 1: the widest that divides the pairs and whose loads and stores are aligned everywhere.
+struct Alignment {
+    int vec = 4;
+    void pointer(const void* p, int bytes) {
+        while (vec > 1 && (uintptr_t)p % (uintptr_t)(vec * bytes)) vec /= 2;
+    }
+    void stride(int64_t s) {
+        while (vec > 1 && s % vec) vec /= 2;
+    }
+};
+
+// The checks that norm_rope and append_kv share; fills in p but for where rows go.
+int heads_params(HeadsParams& p, const vlut_heads* const (&in)[3], float eps, const vlut_rotation* rot, int64_t N, int64_t D, Alignment& a) {
+    if (N < 1 || N >= kMaxDim || D < 2 || D > VLUT_MAX_HEAD_FEATURES || D % 2) return VLUT_ERR_SHAPE;
+    if (!(eps >= 0.0f)) return VLUT_ERR_SHAPE;
+    int64_t heads = 0;
+    a.stride(D / 2);
+    int type = -1;
+    for (int i = 0; i < 3; ++i) {
+        p.kind[i] = HeadRows{};
+        if (!in[i]) continue;
+        if (!in[i]->data) return VLUT_ERR_NULL;
+        if (in[i]->heads < 1 || in[i]->heads >= (1 << 16) || !type_ok(in[i]->type) || (type >= 0 && in[i]->type != type)) return VLUT_ERR_SHAPE;
+        type = in[i]->type;
+        heads += in[i]->heads;
+        HeadRows& k = p.kind[i];
+        k.in = in[i]->data;
+        k.in_token = in[i]->token_stride;
+        k.in_head = in[i]->head_stride;
+        k.heads = in[i]->heads;
+        a.pointer(k.in, type_bytes(type));
+        a.stride(k.in_token);
+        a.stride(k.in_head);
+        if (i < 2) {
+            k.weight = in[i]->weight;
+            k.weight_head = in[i]->weight_stride;
+            if (k.weight) {
+                a.pointer(k.weight, 4);
+                a.stride(k.weight_head);
+            }
+        }
+    }
+    p.R = 0;
+    p.cos = p.sin = nullptr;
+    p.positions = nullptr;
+    p.table_rows = 0;
+    p.interleaved = 0;
+    if (rot) {
+        if (!rot->cos || !rot->sin || !rot->positions) return VLUT_ERR_NULL;
+        if (rot->features < 2 || rot->features > D || rot->features % 2 || rot->rows < 1) return VLUT_ERR_SHAPE;
+        p.R = rot->features;
+        p.cos = rot->cos;
+        p.sin = rot->sin;
+        p.positions = rot->positions;
+        p.table_rows = rot->rows;
+        p.interleaved = rot->interleaved != 0;
+        a.pointer(p.cos, 4);
+        a.pointer(p.sin, 4);
+        a.stride(p.R / 2);
+    }
+    p.eps = eps;
+    p.D = (int)D;
+    p.heads = (unsigned)heads;
+    p.slots = nullptr;
+    p.slot_end = 0;
+    p.page_log = 0;
+    if (N * heads >= ((int64_t)1 << 31)) return VLUT_ERR_SHAPE;
+    p.rows = (unsigned)(N * heads);
+    return VLUT_OK;
+}
+
+template <class TI, class TO>
+int launch_heads_t(const HeadsParams& p, int vec, dim3 grid, hipStream_t stream) {
+    if (vec == 4) return launch(heads_kernel<TI, TO, 4>, grid, 256, 0, stream, p);
+    if (vec == 2) return launch(heads_kernel<TI, TO, 2>, grid, 256, 0, stream, p);
+    return launch(heads_kernel<TI, TO, 1>, grid, 256, 0, stream, p);
+}
+template <class TI>
+int launch_heads_out(const HeadsParams& p, int out, int vec, dim3 grid, hipStream_t stream) {
+    if (out == VLUT_TYPE_F32) return launch_heads_t<TI, float>(p, vec, grid, stream);
+    if (out == VLUT_TYPE_BF16) return launch_heads_t<TI, __bf16>(p, vec, grid, stream);
+    return launch_heads_t<TI, _Float16>(p, vec, grid, stream);
+}
+int launch_heads(HeadsParams& p, int in, int out, int vec, hipStream_t stream) {
+    // lanes of a row: enough for its units (at most 64; a lane has two where pairs are single)
+    p.lanes_log = std::min(6, log2_of((p.D + 2 * vec - 1) / (2 * vec)));
+    const unsigned per = 256u >> p.lanes_log;
+    const dim3 grid((p.rows + per - 1) / per);
+    if (in == VLUT_TYPE_F32) return launch_heads_out<float>(p, out, vec, grid, stream);
+    if (in == VLUT_TYPE_BF16) return launch_heads_out<__bf16>(p, out, vec, grid, stream);
+    return launch_heads_out<_Float16>(p, out, vec, grid, stream);
+}
+
+// Rows that go to a tensor of their own.
+int rows_out(HeadRows& k, const vlut_heads* out, int type, Alignment& a) {
+    if (!out || !out->data) return VLUT_ERR_NULL;
+    if (out->heads != k.heads || out->type != type) return VLUT_ERR_SHAPE;
+    k.out = (void*)out->data;
+    k.out_token = out->token_stride;
+    k.out_head = out->head_stride;
+    a.pointer(k.out, type_bytes(type));
+    a.stride(k.out_token);
+    a.stride(k.out_head);
+    return VLUT_OK;
+}
+
+int check_cache(const vlut_cache* c) {
+    if (!c || !c->k || !c->v) return VLUT_ERR_NULL;
+    if (c->type != VLUT_TYPE_BF16 && c->type != VLUT_TYPE_F16) return VLUT_ERR_UNSUPPORTED;
+    if (c->heads < 1 || c->heads >= (1 << 16) || c->pages < 1 || c->page_size < 1) return VLUT_ERR_SHAPE;
+    if (!power_of_two(c->page_size) || c->page_size > 65536) return VLUT_ERR_UNSUPPORTED;
+    return VLUT_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Attention
+// ---------------------------------------------------------------------------------------------
+constexpr int kUnits = 256;            // compute units that a launch is to fill
+
+struct AttendPlan {
+    int MT, DP;                        // tile: 16 * MT rows, 128 for MT = 0
+    int prefix_tiles, prefix_splits, prefix_chunk, prefix_blocks, blocks_per_xcd, own_tiles, own_splits, own_blocks, direct;
+    int64_t rows;
+    size_t o_bytes, ml_bytes;
+};
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t P, int64_t max_own, AttendPlan* out) {
+    if (B < 1 || n < 1 || Hk < 1 || Hq < 1 || Hq >= (1 << 16) || Hq % Hk || B >= kMaxDim || n >= kMaxDim) return VLUT_ERR_SHAPE;
+    if (P < 0 || max_own < 0 || P >= ((int64_t)1 << 30) || max_own >= ((int64_t)1 << 30) || D < 1) return VLUT_ERR_SHAPE;
+    if (D < 8 || D > VLUT_MAX_HEAD_FEATURES || D % 4) return VLUT_ERR_UNSUPPORTED;
+    const int64_t G = Hq / Hk, own_rows = n * G, rows = B * own_rows;
+    if (rows * Hk >= ((int64_t)1 << 30)) return VLUT_ERR_SHAPE;
+    AttendPlan a{};
+    a.rows = rows;
+    a.DP = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
+    const int64_t tile_rows = P > 0 ? rows : own_rows;
+    a.MT = tile_rows <= 16 ? 1 : (tile_rows <= 32 ? 2 : (P > 0 && tile_rows > 64 ? 0 : (a.DP > 128 ? 2 : 4)));
+    if (a.MT == 4 && a.DP > 128) a.MT = 2;
+    const int own_mt = a.MT > 0 ? a.MT : (a.DP > 128 ? 1 : 2);
+    a.own_tiles = (int)ceil_div(own_rows, 16 * own_mt);
+    const int64_t own_steps = ceil_div(max_own, 128), own_units = B * Hk * a.own_tiles * own_steps;
+    int64_t per_own;
+    if (a.MT > 0) {
+        a.prefix_tiles = (int)ceil_div(rows, 16 * a.MT);
+        const int64_t steps = ceil_div(P, 128), units = Hk * a.prefix_tiles * steps + own_units;
+        const int64_t per = std::max<int64_t>(1, ceil_div(units, 2 * kUnits));
+        a.prefix_chunk = (int)(128 * per);
+        per_own = per;
+    } else {
+        a.prefix_tiles = (int)ceil_div(rows, 128);
+        const int64_t keys = many_keys(a.DP), splits = std::min(std::max<int64_t>(1, 2 * kUnits / (Hk * a.prefix_tiles)), ceil_div(P, 256));
+        a.prefix_chunk = (int)(ceil_div(ceil_div(P, splits), keys) * keys);
+        per_own = std::max<int64_t>(1, ceil_div(own_units, 4 * kUnits));
+    }
+    a.prefix_splits = P > 0 ? (int)ceil_div(P, a.prefix_chunk) : 0;
+    a.own_splits = (int)ceil_div(own_steps, per_own);
+    if (a.prefix_splits + a.own_splits == 0) a.own_splits = 1;      // nothing is seen: a workgroup stores that
+    const int64_t prefix_blocks = Hk * a.prefix_tiles * a.prefix_splits;
+    a.blocks_per_xcd = (int)ceil_div(prefix_blocks, 8);
+    const int64_t padded = a.MT == 0 ? 8 * (int64_t)a.blocks_per_xcd : prefix_blocks, own_blocks = B * Hk * a.own_tiles * a.own_splits;
+    if (padded + own_blocks >= ((int64_t)1 << 31)) return VLUT_ERR_SHAPE;
+    a.prefix_blocks = (int)padded;
+    a.own_blocks = (int)own_blocks;
+    a.direct = a.MT > 0 && a.prefix_splits + a.own_splits == 1;
+    if (!a.direct) {
+        const size_t parts = (size_t)(a.prefix_splits + a.own_splits) * (size_t)Hk * (size_t)rows;
+        a.o_bytes = (parts * (size_t)D * 4 + 255) & ~(size_t)255;
+        a.ml_bytes = parts * 8;
+    }
+    *out = a;
+    return VLUT_OK;
+}
+
+bool allow_lds(const void* kfn, int bytes, std::atomic<unsigned>& done_mask) {
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return false;
+    const unsigned bit = (dev >= 0 && dev < 32) ? (1u << dev) : 0u;
+    if (bit && (done_mask.load(std::memory_order_relaxed) & bit)) return true;
+    if (hipFuncSetAttribute(kfn, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    done_mask.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+
+template <class T, int DP, int MT, bool WHOLE>
+int launch_attend_t(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+    static std::atomic<unsigned> done{0};
+    constexpr int lds = MT == 0 ? std::max(2 * many_buffer(DP), few_lds(DP)) : few_lds(DP);
+    auto kfn = attend_kernel<T, DP, MT, WHOLE>;
+    if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
+    return launch(kfn, dim3((unsigned)(a.prefix_blocks + a.own_blocks)), 256, lds, stream, p);
+}
+template <class T, int DP>
+int launch_attend_d(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+    int rc;
+    if (a.MT == 1) rc = launch_attend_t<T, DP, 1, false>(a, p, stream);
+    else if (a.MT == 2) rc = launch_attend_t<T, DP, 2, false>(a, p, stream);
+    else if (a.MT == 0) rc = p.D == DP ? launch_attend_t<T, DP, 0, true>(a, p, stream) : launch_attend_t<T, DP, 0, false>(a, p, stream);
+    else {
+        if constexpr (DP <= 128) rc = launch_attend_t<T, DP, 4, false>(a, p, stream);
+        else rc = VLUT_ERR_UNSUPPORTED;
+    }
+    if (rc != VLUT_OK || a.direct) return rc;
+    constexpr int per = 256 / (DP / 4);
+    return launch(combine_kernel<DP>, dim3((unsigned)ceil_div(a.rows * p.Hk, per)), 256, 0, stream, p);
+}
+template <class T>
+int launch_attend(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+    if (a.DP == 64) return launch_attend_d<T, 64>(a, p, stream);
+    if (a.DP == 128) return launch_attend_d<T, 128>(a, p, stream);
+    return launch_attend_d<T, 256>(a, p, stream);
+}
+
+// Rows that start at a dword.
+bool at_dwords(const void* p, int64_t s0, int64_t s1, int64_t s2, int bytes) {
+    return (uintptr_t)p % 4 == 0 && (bytes == 4 || (s0 % 2 == 0 && s1 % 2 == 0 && s2 % 2 == 0));
+}
+
+}  // namespace
+
+extern "C" {
+
+int vlut_norm_rope(const vlut_heads* q, const vlut_heads* k_or_null, float eps, const vlut_rotation* rotation_or_null, int64_t N, int64_t D,
+                   const vlut_heads* q_out, const vlut_heads* k_out_or_null, void* stream) {
+    if (!q || !q_out || !k_or_null != !k_out_or_null) return VLUT_ERR_NULL;
+    HeadsParams p;
+    Alignment a;
+    const vlut_heads* const in[3] = {q, k_or_null, nullptr};
+    int rc = heads_params(p, in, eps, rotation_or_null, N, D, a);
+    if (rc != VLUT_OK) return rc;
+    if (!type_ok(q_out->type)) return VLUT_ERR_SHAPE;
+    if ((rc = rows_out(p.kind[0], q_out, q_out->type, a)) != VLUT_OK) return rc;
+    if (k_or_null && (rc = rows_out(p.kind[1], k_out_or_null, q_out->type, a)) != VLUT_OK) return rc;
+    return launch_heads(p, q->type, q_out->type, a.vec, (hipStream_t)stream);
+}
+
+int vlut_append_kv(const vlut_heads* k, const vlut_heads* v, const vlut_heads* q_or_null, float eps, const vlut_rotation* rotation_or_null,
+                   const int64_t* slots, int64_t N, int64_t D, const vlut_cache* cache, const vlut_heads* q_out_or_null, void* stream) {
+    if (!k || !v || !slots || !q_or_null != !q_out_or_null) return VLUT_ERR_NULL;
+    int rc = check_cache(cache);
+    if (rc != VLUT_OK) return rc;
+    HeadsParams p;
+    Alignment a;
+    const vlut_heads* const in[3] = {q_or_null, k, v};
+    rc = heads_params(p, in, eps, rotation_or_null, N, D, a);
+    if (rc != VLUT_OK) return rc;
+    if (k->heads != cache->heads || v->heads != cache->heads) return VLUT_ERR_SHAPE;
+    if (q_or_null && (rc = rows_out(p.kind[0], q_out_or_null, cache->type, a)) != VLUT_OK) return rc;
+    for (int i = 1; i < 3; ++i) {
+        HeadRows& r = p.kind[i];
+        r.by_slot = 1;
+        r.out = i == 1 ? cache->k : cache->v;
+        r.out_token = i == 1 ? cache->k_page_stride : cache->v_page_stride;
+        r.out_head = i == 1 ? cache->k_head_stride : cache->v_head_stride;
+        r.out_row = i == 1 ? cache->k_token_stride : cache->v_token_stride;
+        a.pointer(r.out, 2);
+        a.stride(r.out_token);
+        a.stride(r.out_head);
+        a.stride(r.out_row);
+    }
+    p.slots = slots;
+    p.slot_end = cache->pages * cache->page_size;
+    p.page_log = log2_of(cache->page_size);
+    return launch_heads(p, k->type, cache->type, a.vec, (hipStream_t)stream);
+}
+
+size_t vlut_shared_prefix_attention_bytes(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t prefix_len, int64_t max_own_len) {
+    AttendPlan a;
+    return plan_attention(B, n, Hq, Hk, D, prefix_len, max_own_len, &a) == VLUT_OK ? a.o_bytes + a.ml_bytes : 0;
+}
+
+int vlut_query_shared_prefix_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t prefix_len, int64_t max_own_len, int* out4) {
+    if (!out4) return VLUT_ERR_NULL;
+    AttendPlan a;
+    const int rc = plan_attention(B, n, Hq, Hk, D, prefix_len, max_own_len, &a);
+    if (rc != VLUT_OK) return rc;
+    out4[0] = a.MT > 0 ? 16 * a.MT : 128;
+    out4[1] = a.prefix_splits;
+    out4[2] = a.own_splits;
+    out4[3] = a.prefix_blocks + a.own_blocks;
+    return VLUT_OK;
+}
+
+int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride, const vlut_cache* cache, const int32_t* prefix_pages, int64_t prefix_len,
+                                 const int32_t* page_table, int64_t table_stride, const int32_t* own_lens, int64_t max_own_len,
+                                 const int32_t* query_lens_or_null, int64_t B, int64_t n, int64_t D, float scale, const vlut_heads* out,
+                                 int64_t out_sequence_stride, float* lse_or_null, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!q || !out) return VLUT_ERR_NULL;
+    int rc = check_cache(cache);
+    if (rc != VLUT_OK) return rc;
+    AttendPlan a;
+    rc = plan_attention(B, n, q->heads, cache->heads, D, prefix_len, max_own_len, &a);
+    if (rc != VLUT_OK) return rc;
+    if (!q->data || !out->data || !own_lens || (prefix_len > 0 && !prefix_pages) || (max_own_len > 0 && !page_table)) return VLUT_ERR_NULL;
+    if (out->heads != q->heads || q->type != cache->type || (out->type != cache->type && out->type != VLUT_TYPE_F32)) return VLUT_ERR_SHAPE;
+    if (cache->pages >= ((int64_t)1 << 31)) return VLUT_ERR_SHAPE;
+    if (!(scale > 0.0f) || !std::isfinite(scale)) return VLUT_ERR_UNSUPPORTED;
+    if (!at_dwords(q->data, q_sequence_stride, q->token_stride, q->head_stride, 2) ||
+        !at_dwords(cache->k, cache->k_page_stride, cache->k_head_stride, cache->k_token_stride, 2) ||
+        !at_dwords(cache->v, cache->v_page_stride, cache->v_head_stride, cache->v_token_stride, 2) ||
+        !at_dwords(out->data, out_sequence_stride, out->token_stride, out->head_stride, type_bytes(out->type)))
+        return VLUT_ERR_UNSUPPORTED;
+    if (a.o_bytes) {
+        if (!workspace) return VLUT_ERR_NULL;
+        if (workspace_bytes < a.o_bytes + a.ml_bytes) return VLUT_ERR_SMALL_BUFFER;
+        if ((uintptr_t)workspace % 16) return VLUT_ERR_UNSUPPORTED;
+    }
+    AttendParams p{};
+    p.q = q->data;
+    p.k = cache->k;
+    p.v = cache->v;
+    p.q_sequence = q_sequence_stride;
+    p.q_token = q->token_stride;
+    p.q_head = q->head_stride;
+    p.k_page = cache->k_page_stride;
+    p.k_head = cache->k_head_stride;
+    p.k_token = cache->k_token_stride;
+    p.v_page = cache->v_page_stride;
+    p.v_head = cache->v_head_stride;
+    p.v_token = cache->v_token_stride;
+    p.prefix_pages = prefix_pages;
+    p.page_table = page_table;
+    p.own_lens = own_lens;
+    p.query_lens = query_lens_or_null;
+    p.table_stride = table_stride;
+    p.out = (void*)out->data;
+    p.out_sequence = out_sequence_stride;
+    p.out_token = out->token_stride;
+    p.out_head = out->head_stride;
+    p.lse = lse_or_null;
+    p.part_o = (float*)workspace;
+    p.part_ml = (float*)((unsigned char*)workspace + a.o_bytes);
+    p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    p.out_type = out->type;
+    p.exact_p = out->type == VLUT_TYPE_F32;
+    p.B = (int)B;
+    p.n = (int)n;
+    p.Hk = cache->heads;
+    p.G = q->heads / cache->heads;
+    p.D = (int)D;
+    p.page_log = log2_of(cache->page_size);
+    p.pages = (int)cache->pages;
+    p.P = (int)prefix_len;
+    p.max_own = (int)max_own_len;
+    p.prefix_splits = a.prefix_splits;
+    p.prefix_chunk = a.prefix_chunk;
+    p.own_splits = a.own_splits;
+    p.prefix_tiles = a.prefix_tiles;
+    p.own_tiles = a.own_tiles;
+    p.prefix_blocks = a.prefix_blocks;
+    p.blocks_per_xcd = a.blocks_per_xcd;
+    p.rows = (int)a.rows;
+    p.direct = a.direct;
+    return cache->type == VLUT_TYPE_BF16 ? launch_attend<__bf16>(a, p, (hipStream_t)stream) : launch_attend<_Float16>(a, p, (hipStream_t)stream);
+}
+
+}  // extern "C"

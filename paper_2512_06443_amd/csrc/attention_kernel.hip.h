@@ -1,0 +1,580 @@
+// Attention for a batch of sequences that share a prefix, over a paged cache.
+// Part of the translation unit attention.hip (included there, in this order).
+#pragma once
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// For every query row q (a query token and one of its heads) over the keys it sees, s = scale * q . k:
+//   m = max s,  l = sum exp(s - m),  O = sum exp(s - m) v,  output O / l;   nothing seen: 0
+// Parts of the keys are worked out apart and joined: with M = max m_i the sums of exp(m_i - M) l_i and exp(m_i - M) O_i are those of the whole.
+// The parts: the shared prefix, once for the rows of all sequences that read the same key head (B * n * G of them, G query heads to a key
+// head), cut into prefix_splits ranges; and each sequence's own tokens for its n * G rows, cut into own_splits.  One launch works all
+// of them out (a workgroup has one range and one tile of rows), combine_kernel joins them; a single part is stored as the result.
+//
+// Both products run transposed on the matrix cores, S^T = K Q^T and O^T = V^T P^T: a query is a column, so that its m, l and the factor
+// of its O are one number per lane.  The columns of S^T come out with four neighbouring keys in a lane; P^T is taken in with the keys in exactly that
+// order (the order of a sum's terms is free as long as V^T has the same), so that P goes from one product to the next without leaving its
+// registers.  V^T is read out of the row-major V in LDS by transposing reads (ds_read_b64_tr_b16: the 16 lanes of a group give the addresses of 4
+// rows x 16 features, and get four rows of one feature each).
+// Scores, m, l and O are fp32; P is rounded to the cache's type for the second product, with what the rounding left as a second term
+// where the output is fp32.
+// ---------------------------------------------------------------------------------------------
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef i32x4 dword_aligned_i32x4 __attribute__((aligned(4)));     // rows may start at any dword
+typedef float dword_aligned_f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+template <class T>
+struct Number;
+template <>
+struct Number<__bf16> {
+    typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+    static constexpr unsigned kExponents = 0x7f807f80u, kNan = 0x7fc07fc0u;
+};
+template <>
+struct Number<_Float16> {
+    typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+    static constexpr unsigned kExponents = 0x7c007c00u, kNan = 0x7e007e00u;
+};
+#if defined(__HIP_DEVICE_COMPILE__)
+__device__ __forceinline__ f32x4 mfma16(Number<__bf16>::x8 a, Number<__bf16>::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mfma16(Number<_Float16>::x8 a, Number<_Float16>::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma32(Number<__bf16>::x8 a, Number<__bf16>::x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma32(Number<_Float16>::x8 a, Number<_Float16>::x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ s16x4 lds_read_transposed(unsigned at) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at); }
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+#else
+template <class A> inline __device__ f32x4 mfma16(A, A, f32x4 c) { return c; }
+template <class A> inline __device__ f32x16 mfma32(A, A, f32x16 c) { return c; }
+inline __device__ s16x4 lds_read_transposed(unsigned) { return s16x4{}; }
+inline __device__ float exp2_fast(float x) { return x; }
+#endif
+
+struct AttendParams {
+    const void *q, *k, *v;
+    int64_t q_sequence, q_token, q_head;                               // strides in elements
+    int64_t k_page, k_head, k_token, v_page, v_head, v_token;
+    const int32_t *prefix_pages, *page_table, *own_lens, *query_lens;
+    int64_t table_stride;
+    void* out;
+    int64_t out_sequence, out_token, out_head;
+    float* lse;
+    float *part_o, *part_ml;           // [slot][Hk][B n G][D], [slot][Hk][B n G][2]; slots: the prefix' splits, then the own parts'
+    float scale_log2;                  // scale * log2(e): exponentials are powers of two
+    int out_type, exact_p;             // VLUT_TYPE_*; P in two terms
+    int B, n, Hk, G, D, page_log, pages;
+    int P, max_own;
+    int prefix_splits, prefix_chunk;   // keys per split
+    int own_splits;
+    int prefix_tiles, own_tiles;       // tiles of rows
+    int prefix_blocks, blocks_per_xcd;
+    int rows;                          // B n G
+    int direct;                        // a single part: workgroups store the result
+};
+
+constexpr int kFewKeys = 32;           // keys of a wave's step where rows are few
+__host__ __device__ constexpr int few_pitch(int DP) { return DP * 2 + 32; }
+__host__ __device__ constexpr int few_lds(int DP) { return 4 * kFewKeys * few_pitch(DP); }
+__host__ __device__ constexpr int many_keys(int DP) { return DP > 128 ? 32 : 64; }
+__host__ __device__ constexpr int many_k_pitch(int DP) { return DP * 2 + 16; }
+__host__ __device__ constexpr int many_v_pitch(int DP) { return DP * 2 + 64; }
+__host__ __device__ constexpr int many_buffer(int DP) { return many_keys(DP) * (many_k_pitch(DP) + many_v_pitch(DP)); }
+
+// Eight features of a row from feature 8 * chunk on, zeros past D (D >= 8 and a multiple of four).  Nothing past the row is read: a chunk
+// that D ends in is read four features earlier and moved.
+__device__ __forceinline__ int chunk_at(int chunk, int D) { return 8 * chunk >= D ? 0 : min(8 * chunk, D - 8); }
+__device__ __forceinline__ i32x4 chunk_moved(i32x4 x, int chunk, int D) {
+    const int left = D - 8 * chunk;
+    if (left >= 8) return x;
+    return left <= 0 ? i32x4{0, 0, 0, 0} : i32x4{x.z, x.w, 0, 0};
+}
+
+// What a query row sees and where its result goes.  base: own position of the sequence's query 0; bad: lengths that cannot be.
+struct Sequence {
+    int len, queries, base, bad;
+};
+__device__ __forceinline__ Sequence sequence_of(const AttendParams& p, int b) {
+    Sequence s;
+    s.len = p.own_lens[b];
+    s.queries = p.query_lens ? p.query_lens[b] : p.n;
+    s.bad = s.len < 0 || s.len > p.max_own || s.queries < 0 || s.queries > p.n;
+    if (s.bad) s.len = 0;
+    s.base = s.len - s.queries;
+    return s;
+}
+
+// The result of a row from its O / l (dl: 1 / l; 0 where nothing is seen).
+__device__ __forceinline__ void store_result(const AttendParams& p, int64_t at, const f32x4& o) {
+    if (p.out_type == VLUT_TYPE_F32) *(dword_aligned_f32x4*)((float*)p.out + at) = o;
+    else if (p.out_type == VLUT_TYPE_BF16) {
+        typedef __bf16 x4 __attribute__((ext_vector_type(4), aligned(4)));
+        *(x4*)((__bf16*)p.out + at) = x4{(__bf16)o.x, (__bf16)o.y, (__bf16)o.z, (__bf16)o.w};
+    } else {
+        typedef _Float16 x4 __attribute__((ext_vector_type(4), aligned(4)));
+        *(x4*)((_Float16*)p.out + at) = x4{(_Float16)o.x, (_Float16)o.y, (_Float16)o.z, (_Float16)o.w};
+    }
+}
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f; }
+
+// Page of a key of a list of pages; -1 for a number that is no page of the cache.
+__device__ __forceinline__ int page_of(const AttendParams& p, const int32_t* pages, int key) {
+    const int id = pages[key >> p.page_log];
+    return (unsigned)id < (unsigned)p.pages ? id : -1;
+}
+
+// One range of keys for up to 16 * MT query rows, few enough that memory is what bounds it: the four waves take 32 keys in turn, each on its
+// own (K straight to registers, V through a piece of LDS of its own, no barrier), and join at the end.  The next 32 keys are on their way
+// while the present ones are worked on.
+template <class T, int DP, int MT>
+__device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, bool own, const Sequence& seq, int slot,
+                           unsigned char* lds) {
+    typedef typename Number<T>::x8 x8;
+    constexpr int KS = DP / 32, CH = DP / 8, PER = 64 / CH, VI = kFewKeys / PER, PITCH = few_pitch(DP);
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int l16 = lane & 15, grp = lane >> 4;
+    unsigned char* const mine = lds + wave * kFewKeys * PITCH;
+    const unsigned mine_at = lds_base_of(mine);
+    const int nG = p.n * p.G;
+
+    x8 q[MT][KS];
+    int limit[MT], query[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int row = min(row0 + 16 * mt + l16, row_end - 1);
+        const int b = row / nG, in_seq = row - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
+        const T* src = (const T*)p.q + b * p.q_sequence + j * p.q_token + (int64_t)(h * p.G + g) * p.q_head;
+        query[mt] = j;
+        limit[mt] = own ? min(end_key, seq.base + j + 1) : end_key;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int chunk = 4 * ks + grp;
+            q[mt][ks] = __builtin_bit_cast(x8, chunk_moved(*(const dword_aligned_i32x4*)(src + chunk_at(chunk, p.D)), chunk, p.D));
+        }
+    }
+    // keys below `all_see` are seen by every row of the tile
+    const int j_first = (row0 % nG) / p.G, j_last = own ? ((row_end - 1 < row0 + 16 * MT - 1 ? row_end - 1 : row0 + 16 * MT - 1) % nG) / p.G : 0;
+    const int all_see = own ? min(end_key, seq.base + j_first + 1) : end_key;
+
+    float m[MT], l[MT];
+    f32x4 o[MT][DP / 16];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        m[mt] = -__builtin_inff();
+        l[mt] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < DP / 16; ++dt) o[mt][dt] = f32x4{0, 0, 0, 0};
+    }
+
+    const T* const kh = (const T*)p.k + h * p.k_head;
+    const T* const vh = (const T*)p.v + h * p.v_head;
+    const int mask = (1 << p.page_log) - 1, last = end_key - 1;
+    const int v_chunk = lane % CH, v_key = lane / CH;
+    i32x4 kr[2][KS], vr[VI];
+    // (keys past the range read its last one: its scores are masked, its V is zeroed)
+    auto load = [&](int kt, int page) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int key = min(kt + 16 * t + l16, last), id = __shfl(page, 16 * t + l16);
+            const T* src = kh + (int64_t)max(id, 0) * p.k_page + (key & mask) * p.k_token;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int chunk = 4 * ks + grp;
+                kr[t][ks] = *(const dword_aligned_i32x4*)(src + chunk_at(chunk, p.D));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VI; ++i) {
+            const int k_in = PER * i + v_key, key = min(kt + k_in, last), id = __shfl(page, k_in);
+            const T* src = vh + (int64_t)max(id, 0) * p.v_page + (key & mask) * p.v_token;
+            vr[i] = *(const dword_aligned_i32x4*)(src + chunk_at(v_chunk, p.D));
+        }
+    };
+    auto look_up = [&](int kt) { return page_of(p, pages, min(kt + (lane & 31), last)); };
+
+    int kt = first_key + kFewKeys * wave;
+    int page = 0, next_page = 0;
+    if (kt < end_key) {
+        page = look_up(kt);
+        next_page = look_up(kt + 4 * kFewKeys);
+        load(kt, page);
+    }
+    for (; kt < end_key; kt += 4 * kFewKeys) {
+        const bool some_masked = kt + kFewKeys > all_see;
+        // V to LDS, zeros for keys past the range
+        unsigned odd = 0;
+#pragma unroll
+        for (int i = 0; i < VI; ++i) {
+            i32x4 x = chunk_moved(vr[i], v_chunk, p.D);
+            if (some_masked) {
+                if (kt + PER * i + v_key >= end_key) x = i32x4{0, 0, 0, 0};
+                constexpr unsigned E = Number<T>::kExponents;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) odd |= ((x[w] & (E & 0xffff0000u)) == (E & 0xffff0000u)) | ((x[w] & (E & 0xffffu)) == (E & 0xffffu));
+            }
+            *(i32x4*)(mine + (PER * i + v_key) * PITCH + 16 * v_chunk) = x;
+        }
+        x8 kf[2][KS];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) kf[t][ks] = __builtin_bit_cast(x8, chunk_moved(kr[t][ks], 4 * ks + grp, p.D));
+        if (__any(page < 0)) {                      // a number that is no page: not read, and whoever sees its keys gets NaN
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                if (__shfl(page, 16 * t + l16) < 0) {
+                    constexpr int N = (int)Number<T>::kNan;
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) kf[t][ks] = __builtin_bit_cast(x8, i32x4{N, N, N, N});
+                }
+        }
+        f32x4 s[MT][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[mt][t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) s[mt][t] = mfma16(kf[t][ks], q[mt][ks], s[mt][t]);
+            }
+        if (kt + 4 * kFewKeys < end_key) {
+            load(kt + 4 * kFewKeys, next_page);
+            page = next_page;
+            next_page = look_up(kt + 8 * kFewKeys);
+        }
+        x8 pf[MT], pf_rest[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            if (some_masked) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (kt + 16 * t + 4 * grp + i >= limit[mt]) s[mt][t][i] = -__builtin_inff();
+            }
+            float top = fmaxf(fmaxf(fmaxf(s[mt][0].x, s[mt][0].y), fmaxf(s[mt][0].z, s[mt][0].w)), fmaxf(fmaxf(s[mt][1].x, s[mt][1].y), fmaxf(s[mt][1].z, s[mt][1].w)));
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float now = fmaxf(m[mt], top * p.scale_log2), shift = now == -__builtin_inff() ? 0.0f : now;
+            const float factor = exp2_fast(m[mt] - shift);
+            m[mt] = now;
+            l[mt] *= factor;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float e = exp2_fast(__builtin_fmaf(s[mt][t][i], p.scale_log2, -shift));
+                    l[mt] += e;
+                    pf[mt][4 * t + i] = (T)e;
+                    pf_rest[mt][4 * t + i] = (T)(e - (float)(T)e);
+                }
+#pragma unroll
+            for (int dt = 0; dt < DP / 16; ++dt) o[mt][dt] *= factor;
+        }
+        if (some_masked && __any(odd)) {
+            // An infinity or NaN among the values, and rows that do not see all of them: 0 * inf would reach those too.  One query after the other,
+            // with the values that it does not see zeroed and its own columns alone kept.
+            for (int j = own ? j_first : 0; j <= j_last; ++j) {
+                const int see = own ? min(end_key, seq.base + j + 1) : end_key;
+#pragma unroll
+                for (int dt = 0; dt < DP / 16; ++dt) {
+                    const unsigned at = mine_at + (4 * grp + (l16 >> 2)) * PITCH + 32 * dt + 8 * (l16 & 3);
+                    s16x4 v0 = lds_read_transposed(at), v1 = lds_read_transposed(at + 16 * PITCH);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (kt + 4 * grp + i >= see) v0[i] = 0;
+                        if (kt + 16 + 4 * grp + i >= see) v1[i] = 0;
+                    }
+                    const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        f32x4 t = mfma16(vf, pf[mt], o[mt][dt]);
+                        if (p.exact_p) t = mfma16(vf, pf_rest[mt], t);
+                        if (!own || query[mt] == j) o[mt][dt] = t;
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int dt = 0; dt < DP / 16; ++dt) {
+                const unsigned at = mine_at + (4 * grp + (l16 >> 2)) * PITCH + 32 * dt + 8 * (l16 & 3);
+                const s16x4 v0 = lds_read_transposed(at), v1 = lds_read_transposed(at + 16 * PITCH);
+                const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    o[mt][dt] = mfma16(vf, pf[mt], o[mt][dt]);
+                    if (p.exact_p) o[mt][dt] = mfma16(vf, pf_rest[mt], o[mt][dt]);
+                }
+            }
+        }
+    }
+
+    // The waves' parts: 16 rows at a time through LDS, thread t joins features (t % 16) * DP / 16 .. of row t / 16.
+    constexpr int OP = DP + 4, F4 = DP / 64;                       // floats per row; vectors of four per thread
+    float* const all_o = (float*)lds;                              // [wave][16][OP]
+    float* const all_ml = all_o + 4 * 16 * OP;                     // [wave][16][2]
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        float sum = l[mt];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        __syncthreads();
+#pragma unroll
+        for (int dt = 0; dt < DP / 16; ++dt) *(f32x4*)(all_o + (wave * 16 + l16) * OP + 16 * dt + 4 * grp) = o[mt][dt];
+        if (grp == 0) {
+            all_ml[(wave * 16 + l16) * 2] = m[mt];
+            all_ml[(wave * 16 + l16) * 2 + 1] = sum;
+        }
+        __syncthreads();
+        const int r = (int)threadIdx.x >> 4, part = (int)threadIdx.x & 15, row = row0 + 16 * mt + r;
+        if (row < row_end) {
+            float top = -__builtin_inff(), total = 0.0f, f[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, all_ml[(w * 16 + r) * 2]);
+            const float shift = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                f[w] = exp2_fast(all_ml[(w * 16 + r) * 2] - shift);
+                total += f[w] * all_ml[(w * 16 + r) * 2 + 1];
+            }
+            const int b = row / nG, in_seq = row - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
+            const Sequence its = own || !p.direct ? seq : sequence_of(p, b);
+            if (its.bad) total = __builtin_nanf("");
+            const bool real = its.bad || j < its.queries;
+            const float inverse = p.direct ? (total == 0.0f || !real ? 0.0f : 1.0f / total) : 1.0f;
+            const int64_t part_row = ((int64_t)slot * p.Hk + h) * p.rows + row;
+#pragma unroll
+            for (int v = 0; v < F4; ++v) {
+                const int d = (part + 16 * v) * 4;
+                f32x4 x = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) x += *(f32x4*)(all_o + (w * 16 + r) * OP + d) * f[w];
+                if (d >= p.D) continue;
+                if (p.direct) {
+                    if (total == 0.0f || !real) x = f32x4{0, 0, 0, 0};
+                    else x = x * inverse;
+                    store_result(p, b * p.out_sequence + j * p.out_token + (int64_t)(h * p.G + g) * p.out_head + d, x);
+                } else *(f32x4*)(p.part_o + part_row * p.D + d) = x;
+            }
+            if (part == 0) {
+                if (!p.direct) {
+                    p.part_ml[part_row * 2] = its.bad ? __builtin_nanf("") : top;
+                    p.part_ml[part_row * 2 + 1] = total;
+                } else if (p.lse) p.lse[((int64_t)b * p.n + j) * p.Hk * p.G + h * p.G + g] = real ? lse_of(top, total) : -__builtin_inff();
+            }
+        }
+    }
+}
+
+// One range of the prefix for 128 query rows, many enough that the matrix cores are what bounds it: K and V of 64 keys (32 where D is
+// over 128) in LDS for all four waves, which have 32 rows each.  Two buffers: the next keys travel to registers while the present ones are
+// worked on, and are stored behind them; one barrier per step.
+template <class T, int DP, bool WHOLE>
+__device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, int slot, unsigned char* lds) {
+    typedef typename Number<T>::x8 x8;
+    constexpr int KEYS = many_keys(DP), KT = KEYS / 32, KS = DP / 16, CH = DP / 8, PER = 256 / CH, LI = KEYS / PER;
+    constexpr int KP = many_k_pitch(DP), VP = many_v_pitch(DP);
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
+    const int nG = p.n * p.G;
+    const int row = row0 + 32 * wave + l32, real_row = min(row, row_end - 1);
+    const int b = real_row / nG, in_seq = real_row - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
+
+    x8 q[KS];
+    {
+        const T* src = (const T*)p.q + b * p.q_sequence + j * p.q_token + (int64_t)(h * p.G + g) * p.q_head;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int chunk = 2 * ks + half;
+            q[ks] = __builtin_bit_cast(x8, chunk_moved(*(const dword_aligned_i32x4*)(src + chunk_at(chunk, p.D)), chunk, p.D));
+        }
+    }
+    float m = -__builtin_inff(), l = 0.0f;
+    f32x16 o[DP / 32];
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+
+    const T* const kh = (const T*)p.k + h * p.k_head;
+    const T* const vh = (const T*)p.v + h * p.v_head;
+    const int mask = (1 << p.page_log) - 1, last = end_key - 1;
+    const int chunk = tid % CH, key_in = tid / CH, at = WHOLE ? 8 * chunk : chunk_at(chunk, p.D);
+    i32x4 kr[LI], vr[LI];
+    int ids[LI];
+    auto look_up = [&](int kt) {
+#pragma unroll
+        for (int i = 0; i < LI; ++i) ids[i] = page_of(p, pages, min(kt + PER * i + key_in, last));
+    };
+    auto load = [&](int kt) {
+#pragma unroll
+        for (int i = 0; i < LI; ++i) {
+            const int key = min(kt + PER * i + key_in, last), in_page = key & mask;
+            kr[i] = *(const dword_aligned_i32x4*)(kh + (int64_t)max(ids[i], 0) * p.k_page + in_page * p.k_token + at);
+            vr[i] = *(const dword_aligned_i32x4*)(vh + (int64_t)max(ids[i], 0) * p.v_page + in_page * p.v_token + at);
+        }
+    };
+    int bad = 0;                       // a bit for each loaded key that is in no page
+    auto store = [&](int kt, unsigned char* to) {
+#pragma unroll
+        for (int i = 0; i < LI; ++i) {
+            i32x4 x = kr[i], y = vr[i];
+            if constexpr (!WHOLE) {
+                x = chunk_moved(x, chunk, p.D);
+                y = chunk_moved(y, chunk, p.D);
+            }
+            if (bad >> i & 1) {
+                constexpr int N = (int)Number<T>::kNan;
+                x = i32x4{N, N, N, N};
+            }
+            if (kt + KEYS > end_key && kt + PER * i + key_in >= end_key) y = i32x4{0, 0, 0, 0};
+            *(i32x4*)(to + (PER * i + key_in) * KP + 16 * chunk) = x;
+            *(i32x4*)(to + KEYS * KP + (PER * i + key_in) * VP + 16 * chunk) = y;
+        }
+    };
+    auto keep_bad = [&]() {
+        bad = 0;
+#pragma unroll
+        for (int i = 0; i < LI; ++i) bad |= ids[i] < 0 ? 1 << i : 0;
+    };
+
+    look_up(first_key);
+    load(first_key);
+    keep_bad();
+    look_up(first_key + KEYS);
+    store(first_key, lds);
+    int turn = 0;
+    for (int kt = first_key; kt < end_key; kt += KEYS, turn ^= 1) {
+        wg_barrier_lds();
+        const unsigned char* const buf = lds + turn * many_buffer(DP);
+        const unsigned v_at = lds_base_of((void*)(buf + KEYS * KP)) + (4 * half + (l16 >> 2)) * VP + 32 * ((lane >> 4) & 1) + 8 * (l16 & 3);
+        const bool more = kt + KEYS < end_key;
+        if (more) {
+            load(kt + KEYS);
+            keep_bad();
+            look_up(kt + 2 * KEYS);
+        }
+        f32x16 s[KT];
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s[t] = mfma32(__builtin_bit_cast(x8, *(const i32x4*)(buf + (32 * t + l32) * KP + 32 * ks + 16 * half)), q[ks], s[t]);
+        }
+        if (kt + KEYS > end_key) {
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (kt + 32 * t + (i & 3) + 8 * (i >> 2) + 4 * half >= end_key) s[t][i] = -__builtin_inff();
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = fmaxf(m, top * p.scale_log2), shift = now == -__builtin_inff() ? 0.0f : now;
+        if (__any(now > m)) {
+            const float factor = exp2_fast(m - shift);
+            l *= factor;
+#pragma unroll
+            for (int dt = 0; dt < DP / 32; ++dt) o[dt] *= factor;
+        }
+        m = now;
+#pragma unroll
+        for (int st = 0; st < 2 * KT; ++st) {
+            x8 pf, rest;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float e = exp2_fast(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], p.scale_log2, -shift));
+                l += e;
+                pf[i] = (T)e;
+                rest[i] = (T)(e - (float)(T)e);
+            }
+#pragma unroll
+            for (int dt = 0; dt < DP / 32; ++dt) {
+                const s16x4 v0 = lds_read_transposed(v_at + 16 * st * VP + 64 * dt), v1 = lds_read_transposed(v_at + (16 * st + 8) * VP + 64 * dt);
+                const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+                o[dt] = mfma32(vf, pf, o[dt]);
+                if (p.exact_p) o[dt] = mfma32(vf, rest, o[dt]);
+            }
+        }
+        if (more) store(kt + KEYS, lds + (turn ^ 1) * many_buffer(DP));
+    }
+    l += __shfl_xor(l, 32);
+    if (row >= row_end) return;
+    const int64_t part_row = ((int64_t)slot * p.Hk + h) * p.rows + row;
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int d = 32 * dt + 8 * i + 4 * half;
+            if (d < p.D) *(f32x4*)(p.part_o + part_row * p.D + d) = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+        }
+    if (half == 0) {
+        p.part_ml[part_row * 2] = m;
+        p.part_ml[part_row * 2 + 1] = l;
+    }
+}
+
+// MT > 0: 16 * MT rows of the prefix per workgroup; 0: 128, WHOLE where D fills DP.
+template <class T, int DP, int MT, bool WHOLE>
+__global__ void __launch_bounds__(256, (DP > 128 && MT != 1) || MT == 4 ? 1 : 2) attend_kernel(const AttendParams p) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    constexpr int OWN = MT > 0 ? MT : (DP > 128 ? 1 : 2);
+    int i = (int)blockIdx.x;
+    if (i < p.prefix_blocks) {
+        // Workgroups go to the 8 XCDs in turn; those of one range of keys, which differ in their rows alone, are given to one XCD (one L2).
+        if constexpr (MT == 0) i = (i & 7) * p.blocks_per_xcd + (i >> 3);
+        const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
+        if (h >= p.Hk) return;
+        const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
+        if constexpr (MT == 0) attend_many<T, DP, WHOLE>(p, p.prefix_pages, h, first, end, tile * 128, p.rows, split, lds);
+        else attend_few<T, DP, OWN>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, lds);
+        return;
+    }
+    i -= p.prefix_blocks;
+    const int tile = i % p.own_tiles, split = i / p.own_tiles % p.own_splits, bh = i / p.own_tiles / p.own_splits, h = bh % p.Hk, b = bh / p.Hk;
+    const Sequence seq = sequence_of(p, b);
+    const int steps = (seq.len + 127) / 128, per = (steps + p.own_splits - 1) / p.own_splits;
+    const int first = min(split * per * 128, seq.len), end = min(first + per * 128, seq.len);
+    const int nG = p.n * p.G, row0 = b * nG + tile * 16 * OWN;
+    attend_few<T, DP, OWN>(p, p.page_table + b * p.table_stride, h, first, end, row0, (b + 1) * nG, true, seq, p.prefix_splits + split, lds);
+}
+
+// The parts of every row joined: DP / 4 threads per row, four features each.
+template <int DP>
+__global__ void __launch_bounds__(256) combine_kernel(const AttendParams p) {
+    constexpr int PER_ROW = DP / 4;
+    const int row = (int)(blockIdx.x * (256 / PER_ROW) + threadIdx.x / PER_ROW);
+    const int64_t all = (int64_t)p.Hk * p.rows;
+    const int d = (int)(threadIdx.x % PER_ROW) * 4;
+    if (row >= all || d >= p.D) return;
+    const int slots = p.prefix_splits + p.own_splits;
+    float top = -__builtin_inff(), total = 0.0f;
+    for (int s = 0; s < slots; ++s) top = fmaxf(top, p.part_ml[(s * all + row) * 2]);
+    const float shift = top == -__builtin_inff() ? 0.0f : top;
+    f32x4 x = f32x4{0, 0, 0, 0};
+    for (int s = 0; s < slots; ++s) {
+        const float m = p.part_ml[(s * all + row) * 2];
+        if (m == -__builtin_inff()) continue;
+        const float f = exp2_fast(m - shift);
+        total += f * p.part_ml[(s * all + row) * 2 + 1];
+        x += *(const f32x4*)(p.part_o + (s * all + row) * p.D + d) * f;
+    }
+    const int h = row / p.rows, in_head = row - h * p.rows, nG = p.n * p.G;
+    const int b = in_head / nG, in_seq = in_head - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
+    const Sequence seq = sequence_of(p, b);
+    const bool real = seq.bad || j < seq.queries;
+    if (seq.bad) total = __builtin_nanf("");
+    if (!real || total == 0.0f) x = f32x4{0, 0, 0, 0};
+    else x = x * (1.0f / total);
+    store_result(p, b * p.out_sequence + j * p.out_token + (int64_t)(h * p.G + g) * p.out_head + d, x);
+    if (p.lse && d == 0) p.lse[((int64_t)b * p.n + j) * p.Hk * p.G + h * p.G + g] = real ? lse_of(top, total) : -__builtin_inff();
+}
+
+}  // namespace

@@ -1,0 +1,171 @@
+// Norms of query and key heads, the rotation by position, and the way of keys and values into a paged cache: one pass over the heads.
+// Part of the translation unit attention.hip (included there, in this order).
+#pragma once
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// A row is one head of one token, D features:
+//   y = x / sqrt(mean(x^2) + eps) * w          (without a weight: y = x)
+//   (a, b) -> (a cos - b sin, b cos + a sin)   for the R / 2 pairs of the first R features, (i, i + R/2) or (2i, 2i + 1)
+// all in fp32, rounded once where it is stored.  The rows of a token are its query heads, then its key heads, then its value heads (which
+// are only converted); each goes to a tensor or, by the token's slot, into a page.
+// A unit is two vectors of VEC features that rotate with each other (or, past R, two neighbouring ones), and a lane has one unit (two
+// of VEC = 1): a pair never leaves its lane, and the only exchange is the sum of squares over the row's 2^lanes_log lanes.
+// ---------------------------------------------------------------------------------------------
+struct HeadRows {              // what the rows of one kind (queries, keys, values) are read from and written to; strides in elements
+    const void* in;
+    const float* weight;       // null: no norm
+    void* out;
+    int64_t in_token, in_head, weight_head;
+    int64_t out_token, out_head;       // out_token: of a page where the rows go by slots
+    int64_t out_row;                   // of a token inside its page
+    int heads, by_slot;
+};
+
+struct HeadsParams {
+    HeadRows kind[3];
+    const float *cos, *sin;
+    const int64_t *positions, *slots;
+    int64_t table_rows, slot_end;
+    float eps;
+    unsigned rows, heads;      // all rows; heads of all kinds per token
+    int D, R, interleaved, lanes_log, page_log;
+};
+
+template <class T, int N>
+using Vec = T __attribute__((ext_vector_type(N)));
+template <class T, int N>
+struct LoadVec {
+    typedef Vec<T, N> type;
+};
+template <class T>
+struct LoadVec<T, 1> {
+    typedef T type;
+};
+
+template <class T, int N>
+__device__ __forceinline__ void load_floats(float (&v)[N], const T* p) {
+    typedef typename LoadVec<T, N>::type L;
+    const L x = *(const L*)p;
+    if constexpr (N == 1) v[0] = (float)x;
+    else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = (float)x[i];
+    }
+}
+template <class T, int N>
+__device__ __forceinline__ void store_floats(T* p, const float (&v)[N]) {
+    typedef typename LoadVec<T, N>::type L;
+    L x;
+    if constexpr (N == 1) x = (T)v[0];
+    else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = (T)v[i];
+    }
+    *(L*)p = x;
+}
+
+template <class TI, class TO, int VEC>
+__global__ void __launch_bounds__(256) heads_kernel(const HeadsParams p) {
+    constexpr int UNITS = VEC == 1 ? 2 : 1;         // of a lane: D <= 256 has at most 128 units of one pair
+    const int lane = (int)threadIdx.x & ((1 << p.lanes_log) - 1);
+    const unsigned row = blockIdx.x * (256u >> p.lanes_log) + (threadIdx.x >> p.lanes_log);
+    const bool alive = row < p.rows;
+    const unsigned r = alive ? row : p.rows - 1;    // (the exchange below wants every lane)
+    const unsigned token = r / p.heads;
+    int head = (int)(r - token * p.heads), which = 0;
+    if (head >= p.kind[0].heads) {
+        head -= p.kind[0].heads;
+        which = 1;
+        if (head >= p.kind[1].heads) {
+            head -= p.kind[1].heads;
+            which = 2;
+        }
+    }
+    const HeadRows k = which == 0 ? p.kind[0] : (which == 1 ? p.kind[1] : p.kind[2]);
+    const bool rotated = which < 2 && p.R > 0;
+    int64_t position = 0;
+    bool placed = true;                             // inside the rotation's tables
+    if (rotated) {
+        position = p.positions[token];
+        placed = position >= 0 && position < p.table_rows;
+        position = placed ? position : 0;
+    }
+    int64_t to = (int64_t)token * k.out_token;
+    bool kept = alive;
+    if (k.by_slot) {
+        const int64_t slot = p.slots[token];
+        kept = alive && slot >= 0 && slot < p.slot_end;
+        to = (slot >> p.page_log) * k.out_token + (slot & ((1 << p.page_log) - 1)) * k.out_row;
+    }
+    const TI* in = (const TI*)k.in + (int64_t)token * k.in_token + head * k.in_head;
+    const int half = p.R / 2, rotating = half / VEC, units = p.D / (2 * VEC);
+    float x[UNITS][2][VEC];
+    int at[UNITS][2];
+    float squares = 0.0f;
+#pragma unroll
+    for (int s = 0; s < UNITS; ++s) {
+        const int u = lane + (s << p.lanes_log);
+        if (u < rotating && !p.interleaved) {
+            at[s][0] = u * VEC;
+            at[s][1] = half + u * VEC;
+        } else {
+            at[s][0] = u * 2 * VEC;
+            at[s][1] = at[s][0] + VEC;
+        }
+        if (u >= units) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            load_floats<TI, VEC>(x[s][h], in + at[s][h]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) squares += x[s][h][i] * x[s][h][i];
+        }
+    }
+    for (int m = 1 << p.lanes_log >> 1; m; m >>= 1) squares += __shfl_xor(squares, m);
+    const float inverse = 1.0f / sqrtf(squares / (float)p.D + p.eps);
+#pragma unroll
+    for (int s = 0; s < UNITS; ++s) {
+        const int u = lane + (s << p.lanes_log);
+        if (u >= units || !kept) continue;
+        if (k.weight) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float w[VEC];
+                load_floats<float, VEC>(w, k.weight + head * k.weight_head + at[s][h]);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) x[s][h][i] = x[s][h][i] * inverse * w[i];
+            }
+        }
+        if (rotated && u < rotating) {
+            float c[VEC], n[VEC];
+            load_floats<float, VEC>(c, p.cos + position * half + u * VEC);
+            load_floats<float, VEC>(n, p.sin + position * half + u * VEC);
+            if (!placed) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) c[i] = n[i] = __builtin_nanf("");
+            }
+            if (p.interleaved && VEC > 1) {
+                float* const flat = &x[s][0][0];    // pairs of neighbours through both vectors
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float a = flat[2 * i], b = flat[2 * i + 1];
+                    flat[2 * i] = a * c[i] - b * n[i];
+                    flat[2 * i + 1] = b * c[i] + a * n[i];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float a = x[s][0][i], b = x[s][1][i];
+                    x[s][0][i] = a * c[i] - b * n[i];
+                    x[s][1][i] = b * c[i] + a * n[i];
+                }
+            }
+        }
+        TO* const out = (TO*)k.out + to + head * k.out_head;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) store_floats<TO, VEC>(out + at[s][h], x[s][h]);
+    }
+}
+
+}  // namespace

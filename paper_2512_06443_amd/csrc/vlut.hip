@@ -29,6 +29,7 @@
 
 // The kernels, one header per kernel family; this file holds the host side (launch plans, launches, the C ABI).
 #include "common.hip.h"
+#include "launch.hip.h"
 #include "prepare_kernels.hip.h"
 #include "lookup_kernel.hip.h"
 #include "mfma_kernel.hip.h"
@@ -82,18 +83,6 @@ bool allow_dynamic_lds(const void* kfn, int bytes, std::atomic<unsigned>& done_m
     if (hipFuncSetAttribute(kfn, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) return false;
     done_mask.fetch_or(bit, std::memory_order_relaxed);
     return true;
-}
-
-// A launch by the runtime's call itself: <<< >>> (hipLaunchKernelGGL) hands the same arguments over through a thread's stack of
-// configurations first, 2.35 us of the host against 2.15.
-template <class T>
-struct AsIs { using type = T; };
-template <class... Args>
-int launch(void (*kfn)(Args...), dim3 grid, int threads, int lds, hipStream_t stream, typename AsIs<Args>::type... args) {
-    void* list[] = {(void*)&args...};
-    if (hipLaunchKernel((const void*)kfn, grid, dim3((unsigned)threads), list, (size_t)lds, stream) == hipSuccess) return VLUT_OK;
-    (void)hipGetLastError();                     // (reported here: not once more to whoever asks next)
-    return VLUT_ERR_DEVICE;
 }
 
 struct Plan {
