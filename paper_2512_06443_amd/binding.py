@@ -147,6 +147,8 @@ _NATIVE_ORDER = ("vlut_quantize_act", "vlut_mpgemm_lean", "vlut_workspace_used",
                  "vlut_packed_weight_bytes", "vlut_pack_weights_g5", "vlut_packed_weight_bytes_g5", "vlut_pack_weights_mixed",
                  "vlut_packed_weight_bytes_mixed")
 
+_NATIVE_ATTENTION_ORDER = ("vlut_norm_rope", "vlut_append_kv", "vlut_shared_prefix_attention", "vlut_shared_prefix_attention_bytes")
+
 
 def built_for() -> str:
     """What NATIVE_PATH is compiled against: it holds layouts and key numbers of torch's headers, and a file for others may load all the same."""
@@ -165,7 +167,8 @@ def _load_native(L: ctypes.CDLL) -> None:
         return
     if getattr(mod, "built_for", None) != built_for():      # (whose symbols are all here)
         return
-    mod.bind(*[ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in _NATIVE_ORDER])
+    for bind, order in ((mod.bind, _NATIVE_ORDER), (mod.bind_attention, _NATIVE_ATTENTION_ORDER)):
+        bind(*[ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in order])
     _native = mod
 
 
@@ -577,6 +580,10 @@ def norm_rope(q: torch.Tensor, k: Optional[torch.Tensor] = None, positions: Opti
     rotation by the tokens' int64 `positions` with the tables cos and sin, fp32 [rows][features / 2] (where they are given), in one pass.
     The tensors may be views of a stacked projection's rows.  Returns (q_out, k_out or None) of type `dtype` (default: q's); an output may
     be the input."""
+    if _native is not None:
+        r = _native.norm_rope(q, k, positions, cos, sin, q_weight, k_weight, eps, interleaved, dtype, q_out, k_out)
+        if r is not None:
+            return _outputs(r, "vlut_norm_rope")
     _on_gpu(q, 3, "q")
     N, _, D = q.shape
     if dtype is None:
@@ -602,6 +609,10 @@ def append_kv(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_cache: to
     """Runs vlut_append_kv: keys (normed and rotated as in `norm_rope`) and values, [N][heads][D], to the int64 `slots` (page * page_size +
     token in the page; negative: left out) of the caches [pages][heads][page_size][D] (bf16 or fp16).  With q the queries are normed and
     rotated in the same launch: returns q_out, of the cache's type (None without q)."""
+    if _native is not None:
+        r = _native.append_kv(k, v, slots, k_cache, v_cache, positions, cos, sin, k_weight, eps, interleaved, q, q_weight, q_out)
+        if r is not None:
+            return _outputs(r, "vlut_append_kv")[0]
     _on_gpu(k, 3, "k")
     N, _, D = k.shape
     if tuple(v.shape) != tuple(k.shape) or (q is not None and (q.dim() != 3 or q.shape[0] != N or q.shape[2] != D)):
@@ -637,6 +648,11 @@ def shared_prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     [B][pages]); its last `query_lens[b]` (default n) own tokens are the queries', each of which sees up to itself.
     max_own_len: an upper bound of own_lens (default: what the table's rows hold).  scale: default D ** -0.5.  dtype: fp32 or the
     cache's (default).  Returns (out [B][n][heads][D], lse fp32 [B][n][heads] or None)."""
+    if _native is not None:
+        r = _native.shared_prefix_attention(q, k_cache, v_cache, prefix_pages, prefix_len, page_table, own_lens, query_lens, max_own_len, scale, dtype,
+                                            out, want_lse, workspace)
+        if r is not None:
+            return _outputs(r, "vlut_shared_prefix_attention")
     _on_gpu(q, 4, "q")
     B, n, Hq, D = q.shape
     cache = _cache(k_cache, v_cache, D)

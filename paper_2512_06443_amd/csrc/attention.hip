@@ -224,16 +224,17 @@ int launch_attend_t(const AttendPlan& a, const AttendParams& p, hipStream_t stre
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
     return launch(kfn, dim3((unsigned)(a.prefix_blocks + a.own_blocks)), 256, lds, stream, p);
 }
+template <class T, int DP, bool WHOLE>
+int launch_attend_w(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+    if (a.MT == 1) return launch_attend_t<T, DP, 1, WHOLE>(a, p, stream);
+    if (a.MT == 2) return launch_attend_t<T, DP, 2, WHOLE>(a, p, stream);
+    if (a.MT == 0) return launch_attend_t<T, DP, 0, WHOLE>(a, p, stream);
+    if constexpr (DP <= 128) return launch_attend_t<T, DP, 4, WHOLE>(a, p, stream);
+    return VLUT_ERR_UNSUPPORTED;
+}
 template <class T, int DP>
 int launch_attend_d(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
-    int rc;
-    if (a.MT == 1) rc = launch_attend_t<T, DP, 1, false>(a, p, stream);
-    else if (a.MT == 2) rc = launch_attend_t<T, DP, 2, false>(a, p, stream);
-    else if (a.MT == 0) rc = p.D == DP ? launch_attend_t<T, DP, 0, true>(a, p, stream) : launch_attend_t<T, DP, 0, false>(a, p, stream);
-    else {
-        if constexpr (DP <= 128) rc = launch_attend_t<T, DP, 4, false>(a, p, stream);
-        else rc = VLUT_ERR_UNSUPPORTED;
-    }
+    const int rc = p.D == DP ? launch_attend_w<T, DP, true>(a, p, stream) : launch_attend_w<T, DP, false>(a, p, stream);
     if (rc != VLUT_OK || a.direct) return rc;
     constexpr int per = 256 / (DP / 4);
     return launch(combine_kernel<DP>, dim3((unsigned)ceil_div(a.rows * p.Hk, per)), 256, 0, stream, p);

@@ -85,8 +85,11 @@ __host__ __device__ constexpr int many_buffer(int DP) { return many_keys(DP) * (
 
 // Eight features of a row from feature 8 * chunk on, zeros past D (D >= 8 and a multiple of four).  Nothing past the row is read: a chunk
 // that D ends in is read four features earlier and moved.
-__device__ __forceinline__ int chunk_at(int chunk, int D) { return 8 * chunk >= D ? 0 : min(8 * chunk, D - 8); }
+template <bool WHOLE>
+__device__ __forceinline__ int chunk_at(int chunk, int D) { return WHOLE ? 8 * chunk : (8 * chunk >= D ? 0 : min(8 * chunk, D - 8)); }
+template <bool WHOLE>
 __device__ __forceinline__ i32x4 chunk_moved(i32x4 x, int chunk, int D) {
+    if constexpr (WHOLE) return x;
     const int left = D - 8 * chunk;
     if (left >= 8) return x;
     return left <= 0 ? i32x4{0, 0, 0, 0} : i32x4{x.z, x.w, 0, 0};
@@ -128,7 +131,7 @@ __device__ __forceinline__ int page_of(const AttendParams& p, const int32_t* pag
 // One range of keys for up to 16 * MT query rows, few enough that memory is what bounds it: the four waves take 32 keys in turn, each on its
 // own (K straight to registers, V through a piece of LDS of its own, no barrier), and join at the end.  The next 32 keys are on their way
 // while the present ones are worked on.
-template <class T, int DP, int MT>
+template <class T, int DP, int MT, bool WHOLE>
 __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, bool own, const Sequence& seq, int slot,
                            unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
@@ -140,23 +143,21 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
     const int nG = p.n * p.G;
 
     x8 q[MT][KS];
-    int limit[MT], query[MT];
+    int limit[MT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         const int row = min(row0 + 16 * mt + l16, row_end - 1);
         const int b = row / nG, in_seq = row - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
         const T* src = (const T*)p.q + b * p.q_sequence + j * p.q_token + (int64_t)(h * p.G + g) * p.q_head;
-        query[mt] = j;
         limit[mt] = own ? min(end_key, seq.base + j + 1) : end_key;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const int chunk = 4 * ks + grp;
-            q[mt][ks] = __builtin_bit_cast(x8, chunk_moved(*(const dword_aligned_i32x4*)(src + chunk_at(chunk, p.D)), chunk, p.D));
+            q[mt][ks] = __builtin_bit_cast(x8, chunk_moved<WHOLE>(*(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(chunk, p.D)), chunk, p.D));
         }
     }
     // keys below `all_see` are seen by every row of the tile
-    const int j_first = (row0 % nG) / p.G, j_last = own ? ((row_end - 1 < row0 + 16 * MT - 1 ? row_end - 1 : row0 + 16 * MT - 1) % nG) / p.G : 0;
-    const int all_see = own ? min(end_key, seq.base + j_first + 1) : end_key;
+    const int all_see = own ? min(end_key, seq.base + (row0 % nG) / p.G + 1) : end_key;
 
     float m[MT], l[MT];
     f32x4 o[MT][DP / 16];
@@ -182,14 +183,14 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 const int chunk = 4 * ks + grp;
-                kr[t][ks] = *(const dword_aligned_i32x4*)(src + chunk_at(chunk, p.D));
+                kr[t][ks] = *(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(chunk, p.D));
             }
         }
 #pragma unroll
         for (int i = 0; i < VI; ++i) {
             const int k_in = PER * i + v_key, key = min(kt + k_in, last), id = __shfl(page, k_in);
             const T* src = vh + (int64_t)max(id, 0) * p.v_page + (key & mask) * p.v_token;
-            vr[i] = *(const dword_aligned_i32x4*)(src + chunk_at(v_chunk, p.D));
+            vr[i] = *(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(v_chunk, p.D));
         }
     };
     auto look_up = [&](int kt) { return page_of(p, pages, min(kt + (lane & 31), last)); };
@@ -207,7 +208,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
         unsigned odd = 0;
 #pragma unroll
         for (int i = 0; i < VI; ++i) {
-            i32x4 x = chunk_moved(vr[i], v_chunk, p.D);
+            i32x4 x = chunk_moved<WHOLE>(vr[i], v_chunk, p.D);
             if (some_masked) {
                 if (kt + PER * i + v_key >= end_key) x = i32x4{0, 0, 0, 0};
                 constexpr unsigned E = Number<T>::kExponents;
@@ -220,7 +221,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) kf[t][ks] = __builtin_bit_cast(x8, chunk_moved(kr[t][ks], 4 * ks + grp, p.D));
+            for (int ks = 0; ks < KS; ++ks) kf[t][ks] = __builtin_bit_cast(x8, chunk_moved<WHOLE>(kr[t][ks], 4 * ks + grp, p.D));
         if (__any(page < 0)) {                      // a number that is no page: not read, and whoever sees its keys gets NaN
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -274,39 +275,42 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
             for (int dt = 0; dt < DP / 16; ++dt) o[mt][dt] *= factor;
         }
         if (some_masked && __any(odd)) {
-            // An infinity or NaN among the values, and rows that do not see all of them: 0 * inf would reach those too.  One query after the other,
-            // with the values that it does not see zeroed and its own columns alone kept.
-            for (int j = own ? j_first : 0; j <= j_last; ++j) {
-                const int see = own ? min(end_key, seq.base + j + 1) : end_key;
+            // An infinity or NaN among the values, and rows that do not see all of them: 0 * inf would reach those too.  Such values are added
+            // to the rows that see them one by one and taken out of V.  P goes to the ends of V's rows for that, which are free.
 #pragma unroll
-                for (int dt = 0; dt < DP / 16; ++dt) {
-                    const unsigned at = mine_at + (4 * grp + (l16 >> 2)) * PITCH + 32 * dt + 8 * (l16 & 3);
-                    s16x4 v0 = lds_read_transposed(at), v1 = lds_read_transposed(at + 16 * PITCH);
+            for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (kt + 4 * grp + i >= see) v0[i] = 0;
-                        if (kt + 16 + 4 * grp + i >= see) v1[i] = 0;
-                    }
-                    const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+                for (int e = 0; e < 8; ++e) *(T*)(mine + (16 * (e >> 2) + 4 * grp + (e & 3)) * PITCH + 2 * DP + 2 * l16) = pf[mt][e];
+                __builtin_amdgcn_wave_barrier();
+                for (int key = 0; key < kFewKeys && kt + key < end_key; ++key) {
+                    const bool seen = kt + key < limit[mt];
+                    const float weight = (float)*(const T*)(mine + key * PITCH + 2 * DP + 2 * l16);
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        f32x4 t = mfma16(vf, pf[mt], o[mt][dt]);
-                        if (p.exact_p) t = mfma16(vf, pf_rest[mt], t);
-                        if (!own || query[mt] == j) o[mt][dt] = t;
-                    }
+                    for (int dt = 0; dt < DP / 16; ++dt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = (float)*(const T*)(mine + key * PITCH + 32 * dt + 8 * grp + 2 * i);
+                            if (seen && !(fabsf(x) < __builtin_inff())) o[mt][dt][i] += weight * x;
+                        }
                 }
+                __builtin_amdgcn_wave_barrier();
             }
-        } else {
-#pragma unroll
-            for (int dt = 0; dt < DP / 16; ++dt) {
-                const unsigned at = mine_at + (4 * grp + (l16 >> 2)) * PITCH + 32 * dt + 8 * (l16 & 3);
-                const s16x4 v0 = lds_read_transposed(at), v1 = lds_read_transposed(at + 16 * PITCH);
-                const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    o[mt][dt] = mfma16(vf, pf[mt], o[mt][dt]);
-                    if (p.exact_p) o[mt][dt] = mfma16(vf, pf_rest[mt], o[mt][dt]);
+            for (int i = 0; i < VI; ++i)
+                for (int e = 0; e < 8; ++e) {
+                    T* const x = (T*)(mine + (PER * i + v_key) * PITCH + 16 * v_chunk) + e;
+                    if (!(fabsf((float)*x) < __builtin_inff())) *x = (T)0.0f;
                 }
+            __builtin_amdgcn_wave_barrier();
+        }
+#pragma unroll
+        for (int dt = 0; dt < DP / 16; ++dt) {
+            const unsigned at = mine_at + (4 * grp + (l16 >> 2)) * PITCH + 32 * dt + 8 * (l16 & 3);
+            const s16x4 v0 = lds_read_transposed(at), v1 = lds_read_transposed(at + 16 * PITCH);
+            const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                o[mt][dt] = mfma16(vf, pf[mt], o[mt][dt]);
+                if (p.exact_p) o[mt][dt] = mfma16(vf, pf_rest[mt], o[mt][dt]);
             }
         }
     }
@@ -388,7 +392,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const int chunk = 2 * ks + half;
-            q[ks] = __builtin_bit_cast(x8, chunk_moved(*(const dword_aligned_i32x4*)(src + chunk_at(chunk, p.D)), chunk, p.D));
+            q[ks] = __builtin_bit_cast(x8, chunk_moved<WHOLE>(*(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(chunk, p.D)), chunk, p.D));
         }
     }
     float m = -__builtin_inff(), l = 0.0f;
@@ -401,7 +405,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
     const T* const kh = (const T*)p.k + h * p.k_head;
     const T* const vh = (const T*)p.v + h * p.v_head;
     const int mask = (1 << p.page_log) - 1, last = end_key - 1;
-    const int chunk = tid % CH, key_in = tid / CH, at = WHOLE ? 8 * chunk : chunk_at(chunk, p.D);
+    const int chunk = tid % CH, key_in = tid / CH, at = chunk_at<WHOLE>(chunk, p.D);
     i32x4 kr[LI], vr[LI];
     int ids[LI];
     auto look_up = [&](int kt) {
@@ -420,11 +424,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
     auto store = [&](int kt, unsigned char* to) {
 #pragma unroll
         for (int i = 0; i < LI; ++i) {
-            i32x4 x = kr[i], y = vr[i];
-            if constexpr (!WHOLE) {
-                x = chunk_moved(x, chunk, p.D);
-                y = chunk_moved(y, chunk, p.D);
-            }
+            i32x4 x = chunk_moved<WHOLE>(kr[i], chunk, p.D), y = chunk_moved<WHOLE>(vr[i], chunk, p.D);
             if (bad >> i & 1) {
                 constexpr int N = (int)Number<T>::kNan;
                 x = i32x4{N, N, N, N};
@@ -521,29 +521,37 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
     }
 }
 
-// MT > 0: 16 * MT rows of the prefix per workgroup; 0: 128, WHOLE where D fills DP.
+// MT > 0: 16 * MT rows of the prefix per workgroup; 0: 128.  WHOLE: D is DP.
 template <class T, int DP, int MT, bool WHOLE>
-__global__ void __launch_bounds__(256, (DP > 128 && MT != 1) || MT == 4 ? 1 : 2) attend_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(256, DP > 128 || MT == 4 ? 1 : 2) attend_kernel(const AttendParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     constexpr int OWN = MT > 0 ? MT : (DP > 128 ? 1 : 2);
-    int i = (int)blockIdx.x;
-    if (i < p.prefix_blocks) {
-        // Workgroups go to the 8 XCDs in turn; those of one range of keys, which differ in their rows alone, are given to one XCD (one L2).
-        if constexpr (MT == 0) i = (i & 7) * p.blocks_per_xcd + (i >> 3);
-        const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
-        if (h >= p.Hk) return;
-        const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
-        if constexpr (MT == 0) attend_many<T, DP, WHOLE>(p, p.prefix_pages, h, first, end, tile * 128, p.rows, split, lds);
-        else attend_few<T, DP, OWN>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, lds);
-        return;
+    const bool own = (int)blockIdx.x >= p.prefix_blocks;
+    int i = (int)blockIdx.x - (own ? p.prefix_blocks : 0);
+    // Workgroups go to the 8 XCDs in turn; those of one range of the prefix, which differ in their rows alone, are given to one XCD (one L2).
+    if (MT == 0 && !own) i = (i & 7) * p.blocks_per_xcd + (i >> 3);
+    const int tiles = own ? p.own_tiles : p.prefix_tiles, splits = own ? p.own_splits : p.prefix_splits;
+    const int tile = i % tiles, rest = i / tiles, split = rest % splits, bh = rest / splits, h = own ? bh % p.Hk : bh, b = own ? bh / p.Hk : 0;
+    if (h >= p.Hk) return;
+    int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
+    if constexpr (MT == 0) {
+        if (!own) {
+            attend_many<T, DP, WHOLE>(p, p.prefix_pages, h, first, end, tile * 128, p.rows, split, lds);
+            return;
+        }
     }
-    i -= p.prefix_blocks;
-    const int tile = i % p.own_tiles, split = i / p.own_tiles % p.own_splits, bh = i / p.own_tiles / p.own_splits, h = bh % p.Hk, b = bh / p.Hk;
-    const Sequence seq = sequence_of(p, b);
-    const int steps = (seq.len + 127) / 128, per = (steps + p.own_splits - 1) / p.own_splits;
-    const int first = min(split * per * 128, seq.len), end = min(first + per * 128, seq.len);
-    const int nG = p.n * p.G, row0 = b * nG + tile * 16 * OWN;
-    attend_few<T, DP, OWN>(p, p.page_table + b * p.table_stride, h, first, end, row0, (b + 1) * nG, true, seq, p.prefix_splits + split, lds);
+    Sequence seq{};
+    int row0 = tile * 16 * OWN, row_end = p.rows;
+    if (own) {
+        seq = sequence_of(p, b);
+        const int steps = (seq.len + 127) / 128, per = (steps + p.own_splits - 1) / p.own_splits, nG = p.n * p.G;
+        first = min(split * per * 128, seq.len);
+        end = min(first + per * 128, seq.len);
+        row0 += b * nG;
+        row_end = (b + 1) * nG;
+    }
+    attend_few<T, DP, OWN, WHOLE>(p, own ? p.page_table + b * p.table_stride : p.prefix_pages, h, first, end, row0, row_end, own, seq,
+                                  own ? p.prefix_splits + split : split, lds);
 }
 
 // The parts of every row joined: DP / 4 threads per row, four features each.

@@ -249,24 +249,35 @@ PyObject* py_pack_weights_mixed(PyObject*, PyObject* const* o, Py_ssize_t n) {
     return pack(o, n, g_api.packed_weight_bytes_mixed, g_api.pack_weights_mixed);
 }
 
-// bind(addresses): the functions of the loaded library, as whole numbers in the order of Api
-PyObject* py_bind(PyObject*, PyObject* const* o, Py_ssize_t n) {
-    void* address[kApiCount];
-    if (n != kApiCount) {
+// Whole numbers that are addresses of functions; an error is set otherwise.
+bool addresses(PyObject* const* o, Py_ssize_t n, void** address, int count) {
+    if (n != count) {
         PyErr_SetString(PyExc_TypeError, "bind: one address for each function");
-        return nullptr;
+        return false;
     }
-    for (int i = 0; i < kApiCount; ++i) {
+    for (int i = 0; i < count; ++i) {
         address[i] = PyLong_AsVoidPtr(o[i]);
         if (!address[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: null address");
-            return nullptr;
+            return false;
         }
     }
+    return true;
+}
+// bind(addresses): the functions of the loaded library, as whole numbers in the order of Api
+PyObject* py_bind(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    void* address[kApiCount];
+    if (!addresses(o, n, address, kApiCount)) return nullptr;
     std::memcpy((void*)&g_api, address, sizeof(g_api));
     g_bound = true;
     Py_RETURN_NONE;
 }
+
+}  // namespace
+
+#include "attention_calls.h"
+
+namespace {
 
 PyMethodDef kMethods[] = {
     {"bind", (PyCFunction)(void (*)(void))py_bind, METH_FASTCALL, nullptr},
@@ -278,6 +289,10 @@ PyMethodDef kMethods[] = {
     {"pack_weights", (PyCFunction)(void (*)(void))py_pack_weights, METH_FASTCALL, nullptr},
     {"pack_weights_g5", (PyCFunction)(void (*)(void))py_pack_weights_g5, METH_FASTCALL, nullptr},
     {"pack_weights_mixed", (PyCFunction)(void (*)(void))py_pack_weights_mixed, METH_FASTCALL, nullptr},
+    {"bind_attention", (PyCFunction)(void (*)(void))py_bind_attention, METH_FASTCALL, nullptr},
+    {"norm_rope", (PyCFunction)(void (*)(void))py_norm_rope, METH_FASTCALL, nullptr},
+    {"append_kv", (PyCFunction)(void (*)(void))py_append_kv, METH_FASTCALL, nullptr},
+    {"shared_prefix_attention", (PyCFunction)(void (*)(void))py_shared_prefix_attention, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_vlut_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
