@@ -6,6 +6,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "vlut.h"
 
@@ -148,7 +149,8 @@ int check_cache(const vlut_cache* c) {
 constexpr int kUnits = 256;            // compute units that a launch is to fill
 
 struct AttendPlan {
-    int MT, DP;                        // tile: 16 * MT rows, 128 for MT = 0
+    int MT, own_mt, DP;                // tile: 16 * MT rows, 128 for MT = 0
+    int own_share, own_step;
     int prefix_tiles, prefix_splits, prefix_chunk, prefix_blocks, blocks_per_xcd, own_tiles, own_splits, own_blocks, direct;
     int64_t rows;
     size_t o_bytes, ml_bytes;
@@ -165,16 +167,17 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     AttendPlan a{};
     a.rows = rows;
     a.DP = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
-    const int64_t tile_rows = P > 0 ? rows : own_rows;
-    a.MT = tile_rows <= 16 ? 1 : (tile_rows <= 32 ? 2 : (P > 0 && tile_rows > 64 ? 0 : (a.DP > 128 ? 2 : 4)));
-    if (a.MT == 4 && a.DP > 128) a.MT = 2;
-    const int own_mt = a.MT > 0 ? a.MT : (a.DP > 128 ? 1 : 2);
-    a.own_tiles = (int)ceil_div(own_rows, 16 * own_mt);
-    const int64_t own_steps = ceil_div(max_own, 128), own_units = B * Hk * a.own_tiles * own_steps;
+    a.own_mt = own_rows <= 16 ? 1 : 2;
+    a.MT = P == 0 ? a.own_mt : (rows <= 16 ? 1 : (rows <= 64 ? 2 : 0));
+    a.own_tiles = (int)ceil_div(own_rows, 16 * a.own_mt);
+    const int64_t own_units = B * Hk * a.own_tiles;
+    a.own_share = own_units >= 4 * 2 * kUnits ? 1 : 4;
+    a.own_step = a.own_share * kFewKeys;
+    const int64_t own_steps = ceil_div(max_own, a.own_step), own_all = own_units * own_steps;
     int64_t per_own;
     if (a.MT > 0) {
         a.prefix_tiles = (int)ceil_div(rows, 16 * a.MT);
-        const int64_t steps = ceil_div(P, 128), units = Hk * a.prefix_tiles * steps + own_units;
+        const int64_t steps = ceil_div(P, 128), units = Hk * a.prefix_tiles * steps + own_all / (4 / a.own_share);
         const int64_t per = std::max<int64_t>(1, ceil_div(units, 2 * kUnits));
         a.prefix_chunk = (int)(128 * per);
         per_own = per;
@@ -182,14 +185,15 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
         a.prefix_tiles = (int)ceil_div(rows, 128);
         const int64_t keys = many_keys(a.DP), splits = std::min(std::max<int64_t>(1, 2 * kUnits / (Hk * a.prefix_tiles)), ceil_div(P, 256));
         a.prefix_chunk = (int)(ceil_div(ceil_div(P, splits), keys) * keys);
-        per_own = std::max<int64_t>(1, ceil_div(own_units, 4 * kUnits));
+        per_own = std::max<int64_t>(1, ceil_div(own_all / (4 / a.own_share), 4 * kUnits));
     }
+    if (a.own_share == 1) per_own = std::max<int64_t>(per_own, own_steps);
     a.prefix_splits = P > 0 ? (int)ceil_div(P, a.prefix_chunk) : 0;
     a.own_splits = (int)ceil_div(own_steps, per_own);
     if (a.prefix_splits + a.own_splits == 0) a.own_splits = 1;      // nothing is seen: a workgroup stores that
     const int64_t prefix_blocks = Hk * a.prefix_tiles * a.prefix_splits;
     a.blocks_per_xcd = (int)ceil_div(prefix_blocks, 8);
-    const int64_t padded = a.MT == 0 ? 8 * (int64_t)a.blocks_per_xcd : prefix_blocks, own_blocks = B * Hk * a.own_tiles * a.own_splits;
+    const int64_t padded = 8 * (int64_t)a.blocks_per_xcd, own_blocks = ceil_div(own_units * a.own_splits, 4 / a.own_share);
     if (padded + own_blocks >= ((int64_t)1 << 31)) return VLUT_ERR_SHAPE;
     a.prefix_blocks = (int)padded;
     a.own_blocks = (int)own_blocks;
@@ -216,28 +220,27 @@ bool allow_lds(const void* kfn, int bytes, std::atomic<unsigned>& done_mask) {
     return true;
 }
 
-template <class T, int DP, int MT, bool WHOLE>
+template <class T, int DP, int MT, int OWN, bool WHOLE>
 int launch_attend_t(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
     static std::atomic<unsigned> done{0};
     constexpr int lds = MT == 0 ? std::max(2 * many_buffer(DP), few_lds(DP)) : few_lds(DP);
-    auto kfn = attend_kernel<T, DP, MT, WHOLE>;
+    auto kfn = attend_kernel<T, DP, MT, OWN, WHOLE>;
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
     return launch(kfn, dim3((unsigned)(a.prefix_blocks + a.own_blocks)), 256, lds, stream, p);
 }
 template <class T, int DP, bool WHOLE>
 int launch_attend_w(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
-    if (a.MT == 1) return launch_attend_t<T, DP, 1, WHOLE>(a, p, stream);
-    if (a.MT == 2) return launch_attend_t<T, DP, 2, WHOLE>(a, p, stream);
-    if (a.MT == 0) return launch_attend_t<T, DP, 0, WHOLE>(a, p, stream);
-    if constexpr (DP <= 128) return launch_attend_t<T, DP, 4, WHOLE>(a, p, stream);
-    return VLUT_ERR_UNSUPPORTED;
+    if (a.MT == 1) return launch_attend_t<T, DP, 1, 1, WHOLE>(a, p, stream);
+    if (a.MT == 2) return a.own_mt == 1 ? launch_attend_t<T, DP, 2, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 2, 2, WHOLE>(a, p, stream);
+    return a.own_mt == 1 ? launch_attend_t<T, DP, 0, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 0, 2, WHOLE>(a, p, stream);
 }
 template <class T, int DP>
 int launch_attend_d(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
     const int rc = p.D == DP ? launch_attend_w<T, DP, true>(a, p, stream) : launch_attend_w<T, DP, false>(a, p, stream);
     if (rc != VLUT_OK || a.direct) return rc;
-    constexpr int per = 256 / (DP / 4);
-    return launch(combine_kernel<DP>, dim3((unsigned)ceil_div(a.rows * p.Hk, per)), 256, 0, stream, p);
+    constexpr int groups = 256 / (DP / 4);
+    const int lanes_log = std::min(log2_of(groups), log2_of(ceil_div(a.prefix_splits + a.own_splits, 4)));
+    return launch(combine_kernel<DP>, dim3((unsigned)ceil_div(a.rows * p.Hk, groups >> lanes_log)), 256, 0, stream, p, lanes_log);
 }
 template <class T>
 int launch_attend(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
@@ -380,6 +383,8 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
     p.prefix_splits = a.prefix_splits;
     p.prefix_chunk = a.prefix_chunk;
     p.own_splits = a.own_splits;
+    p.own_share = a.own_share;
+    p.own_step = a.own_step;
     p.prefix_tiles = a.prefix_tiles;
     p.own_tiles = a.own_tiles;
     p.prefix_blocks = a.prefix_blocks;

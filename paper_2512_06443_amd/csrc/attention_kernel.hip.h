@@ -68,7 +68,7 @@ struct AttendParams {
     int B, n, Hk, G, D, page_log, pages;
     int P, max_own;
     int prefix_splits, prefix_chunk;   // keys per split
-    int own_splits;
+    int own_splits, own_share, own_step;   // waves to a range; its keys are a multiple of own_step but for the end
     int prefix_tiles, own_tiles;       // tiles of rows
     int prefix_blocks, blocks_per_xcd;
     int rows;                          // B n G
@@ -128,19 +128,29 @@ __device__ __forceinline__ int page_of(const AttendParams& p, const int32_t* pag
     return (unsigned)id < (unsigned)p.pages ? id : -1;
 }
 
-// One range of keys for up to 16 * MT query rows, few enough that memory is what bounds it: the four waves take 32 keys in turn, each on its
-// own (K straight to registers, V through a piece of LDS of its own, no barrier), and join at the end.  The next 32 keys are on their way
-// while the present ones are worked on.
+// The compiler waits for what it loaded ahead of a loop again in every turn of it, and so for the loads of that turn: `x` is there from here on.
+template <class V>
+__device__ __forceinline__ void arrived(V& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    i32x4 y = __builtin_bit_cast(i32x4, x);
+    asm volatile("" : "+v"(y));
+    x = __builtin_bit_cast(V, y);
+#endif
+}
+
+// One range of keys for up to 16 * MT query rows, few enough that memory is what bounds it.  A wave takes 32 keys a step (K straight to registers, V
+// through a piece of LDS of its own, no barrier); the next 32 are on their way while the present ones are worked on.  `share` waves
+// have the range in turn: 4, which join at the end through LDS, or 1 where ranges are short and many.
 template <class T, int DP, int MT, bool WHOLE>
 __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, bool own, const Sequence& seq, int slot,
-                           unsigned char* lds) {
+                           int share, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
     constexpr int KS = DP / 32, CH = DP / 8, PER = 64 / CH, VI = kFewKeys / PER, PITCH = few_pitch(DP);
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int l16 = lane & 15, grp = lane >> 4;
     unsigned char* const mine = lds + wave * kFewKeys * PITCH;
     const unsigned mine_at = lds_base_of(mine);
-    const int nG = p.n * p.G;
+    const int nG = p.n * p.G, stride = share * kFewKeys;
 
     x8 q[MT][KS];
     int limit[MT];
@@ -175,17 +185,16 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
     const int v_chunk = lane % CH, v_key = lane / CH;
     i32x4 kr[2][KS], vr[VI];
     // (keys past the range read its last one: its scores are masked, its V is zeroed)
-    auto load = [&](int kt, int page) {
+    auto load_k = [&](int kt, int page) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int key = min(kt + 16 * t + l16, last), id = __shfl(page, 16 * t + l16);
             const T* src = kh + (int64_t)max(id, 0) * p.k_page + (key & mask) * p.k_token;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int chunk = 4 * ks + grp;
-                kr[t][ks] = *(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(chunk, p.D));
-            }
+            for (int ks = 0; ks < KS; ++ks) kr[t][ks] = *(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(4 * ks + grp, p.D));
         }
+    };
+    auto load_v = [&](int kt, int page) {
 #pragma unroll
         for (int i = 0; i < VI; ++i) {
             const int k_in = PER * i + v_key, key = min(kt + k_in, last), id = __shfl(page, k_in);
@@ -195,15 +204,20 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
     };
     auto look_up = [&](int kt) { return page_of(p, pages, min(kt + (lane & 31), last)); };
 
-    int kt = first_key + kFewKeys * wave;
+    int kt = first_key + (share > 1 ? kFewKeys * wave : 0);
     int page = 0, next_page = 0;
     if (kt < end_key) {
         page = look_up(kt);
-        next_page = look_up(kt + 4 * kFewKeys);
-        load(kt, page);
+        next_page = look_up(kt + stride);
+        load_v(kt, page);
+        load_k(kt, page);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) arrived(q[mt][ks]);
     }
-    for (; kt < end_key; kt += 4 * kFewKeys) {
-        const bool some_masked = kt + kFewKeys > all_see;
+    for (; kt < end_key; kt += stride) {
+        const bool some_masked = kt + kFewKeys > all_see, more = kt + stride < end_key;
         // V to LDS, zeros for keys past the range
         unsigned odd = 0;
 #pragma unroll
@@ -216,6 +230,12 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                 for (int w = 0; w < 4; ++w) odd |= ((x[w] & (E & 0xffff0000u)) == (E & 0xffff0000u)) | ((x[w] & (E & 0xffffu)) == (E & 0xffffu));
             }
             *(i32x4*)(mine + (PER * i + v_key) * PITCH + 16 * v_chunk) = x;
+        }
+        // (in the order in which they are waited for: the page after the next, V, K)
+        int page_after = 0;
+        if (more) {
+            page_after = look_up(kt + 2 * stride);
+            load_v(kt + stride, next_page);
         }
         x8 kf[2][KS];
 #pragma unroll
@@ -240,11 +260,9 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) s[mt][t] = mfma16(kf[t][ks], q[mt][ks], s[mt][t]);
             }
-        if (kt + 4 * kFewKeys < end_key) {
-            load(kt + 4 * kFewKeys, next_page);
-            page = next_page;
-            next_page = look_up(kt + 8 * kFewKeys);
-        }
+        if (more) load_k(kt + stride, next_page);
+        page = next_page;
+        next_page = page_after;
         x8 pf[MT], pf_rest[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -310,26 +328,58 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
                 o[mt][dt] = mfma16(vf, pf[mt], o[mt][dt]);
-                if (p.exact_p) o[mt][dt] = mfma16(vf, pf_rest[mt], o[mt][dt]);
+                o[mt][dt] = mfma16(vf, pf_rest[mt], o[mt][dt]);
             }
         }
     }
 
-    // The waves' parts: 16 rows at a time through LDS, thread t joins features (t % 16) * DP / 16 .. of row t / 16.
+    // Where a row's result goes, in four features a thread; f is the factor of what is stored (the parts' sums are stored as they are).
+    auto store = [&](int row, int d, f32x4 x, float top, float total) {
+        const int b = row / nG, in_seq = row - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
+        const int64_t part_row = ((int64_t)slot * p.Hk + h) * p.rows + row;
+        if (!p.direct) {
+            if (own && seq.bad) top = total = __builtin_nanf("");
+            if (d < p.D) *(f32x4*)(p.part_o + part_row * p.D + d) = x;
+            if (d == 0) {
+                p.part_ml[part_row * 2] = top;
+                p.part_ml[part_row * 2 + 1] = total;
+            }
+            return;
+        }
+        const Sequence its = own ? seq : sequence_of(p, b);
+        if (its.bad) total = __builtin_nanf("");
+        const bool real = its.bad || j < its.queries;
+        x = !real || total == 0.0f ? f32x4{0, 0, 0, 0} : x * (1.0f / total);
+        if (d < p.D) store_result(p, b * p.out_sequence + j * p.out_token + (int64_t)(h * p.G + g) * p.out_head + d, x);
+        if (d == 0 && p.lse) p.lse[((int64_t)b * p.n + j) * p.Hk * p.G + h * p.G + g] = real ? lse_of(top, total) : -__builtin_inff();
+    };
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        l[mt] += __shfl_xor(l[mt], 16);
+        l[mt] += __shfl_xor(l[mt], 32);
+    }
+    if (share == 1) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int row = row0 + 16 * mt + l16;
+            if (row < row_end)
+#pragma unroll
+                for (int dt = 0; dt < DP / 16; ++dt) store(row, 16 * dt + 4 * grp, o[mt][dt], m[mt], l[mt]);
+        }
+        return;
+    }
+    // The waves' parts: 16 rows at a time through LDS, thread t joins features of row t / 16.
     constexpr int OP = DP + 4, F4 = DP / 64;                       // floats per row; vectors of four per thread
     float* const all_o = (float*)lds;                              // [wave][16][OP]
     float* const all_ml = all_o + 4 * 16 * OP;                     // [wave][16][2]
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        float sum = l[mt];
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
         __syncthreads();
 #pragma unroll
         for (int dt = 0; dt < DP / 16; ++dt) *(f32x4*)(all_o + (wave * 16 + l16) * OP + 16 * dt + 4 * grp) = o[mt][dt];
         if (grp == 0) {
             all_ml[(wave * 16 + l16) * 2] = m[mt];
-            all_ml[(wave * 16 + l16) * 2 + 1] = sum;
+            all_ml[(wave * 16 + l16) * 2 + 1] = l[mt];
         }
         __syncthreads();
         const int r = (int)threadIdx.x >> 4, part = (int)threadIdx.x & 15, row = row0 + 16 * mt + r;
@@ -343,30 +393,13 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                 f[w] = exp2_fast(all_ml[(w * 16 + r) * 2] - shift);
                 total += f[w] * all_ml[(w * 16 + r) * 2 + 1];
             }
-            const int b = row / nG, in_seq = row - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
-            const Sequence its = own || !p.direct ? seq : sequence_of(p, b);
-            if (its.bad) total = __builtin_nanf("");
-            const bool real = its.bad || j < its.queries;
-            const float inverse = p.direct ? (total == 0.0f || !real ? 0.0f : 1.0f / total) : 1.0f;
-            const int64_t part_row = ((int64_t)slot * p.Hk + h) * p.rows + row;
 #pragma unroll
             for (int v = 0; v < F4; ++v) {
                 const int d = (part + 16 * v) * 4;
                 f32x4 x = f32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) x += *(f32x4*)(all_o + (w * 16 + r) * OP + d) * f[w];
-                if (d >= p.D) continue;
-                if (p.direct) {
-                    if (total == 0.0f || !real) x = f32x4{0, 0, 0, 0};
-                    else x = x * inverse;
-                    store_result(p, b * p.out_sequence + j * p.out_token + (int64_t)(h * p.G + g) * p.out_head + d, x);
-                } else *(f32x4*)(p.part_o + part_row * p.D + d) = x;
-            }
-            if (part == 0) {
-                if (!p.direct) {
-                    p.part_ml[part_row * 2] = its.bad ? __builtin_nanf("") : top;
-                    p.part_ml[part_row * 2 + 1] = total;
-                } else if (p.lse) p.lse[((int64_t)b * p.n + j) * p.Hk * p.G + h * p.G + g] = real ? lse_of(top, total) : -__builtin_inff();
+                store(row, d, x, top, total);
             }
         }
     }
@@ -444,6 +477,8 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
     load(first_key);
     keep_bad();
     look_up(first_key + KEYS);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) arrived(q[ks]);
     store(first_key, lds);
     int turn = 0;
     for (int kt = first_key; kt < end_key; kt += KEYS, turn ^= 1) {
@@ -485,24 +520,28 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
             for (int dt = 0; dt < DP / 32; ++dt) o[dt] *= factor;
         }
         m = now;
+        auto weigh = [&](auto terms) {
 #pragma unroll
-        for (int st = 0; st < 2 * KT; ++st) {
-            x8 pf, rest;
+            for (int st = 0; st < 2 * KT; ++st) {
+                x8 pf, rest;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float e = exp2_fast(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], p.scale_log2, -shift));
-                l += e;
-                pf[i] = (T)e;
-                rest[i] = (T)(e - (float)(T)e);
+                for (int i = 0; i < 8; ++i) {
+                    const float e = exp2_fast(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], p.scale_log2, -shift));
+                    l += e;
+                    pf[i] = (T)e;
+                    if constexpr (terms.value > 1) rest[i] = (T)(e - (float)(T)e);
+                }
+#pragma unroll
+                for (int dt = 0; dt < DP / 32; ++dt) {
+                    const s16x4 v0 = lds_read_transposed(v_at + 16 * st * VP + 64 * dt), v1 = lds_read_transposed(v_at + (16 * st + 8) * VP + 64 * dt);
+                    const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+                    o[dt] = mfma32(vf, pf, o[dt]);
+                    if constexpr (terms.value > 1) o[dt] = mfma32(vf, rest, o[dt]);
+                }
             }
-#pragma unroll
-            for (int dt = 0; dt < DP / 32; ++dt) {
-                const s16x4 v0 = lds_read_transposed(v_at + 16 * st * VP + 64 * dt), v1 = lds_read_transposed(v_at + (16 * st + 8) * VP + 64 * dt);
-                const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-                o[dt] = mfma32(vf, pf, o[dt]);
-                if (p.exact_p) o[dt] = mfma32(vf, rest, o[dt]);
-            }
-        }
+        };
+        if (p.exact_p) weigh(std::integral_constant<int, 2>());
+        else weigh(std::integral_constant<int, 1>());
         if (more) store(kt + KEYS, lds + (turn ^ 1) * many_buffer(DP));
     }
     l += __shfl_xor(l, 32);
@@ -521,66 +560,101 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
     }
 }
 
-// MT > 0: 16 * MT rows of the prefix per workgroup; 0: 128.  WHOLE: D is DP.
-template <class T, int DP, int MT, bool WHOLE>
-__global__ void __launch_bounds__(256, DP > 128 || MT == 4 ? 1 : 2) attend_kernel(const AttendParams p) {
+// MT > 0: 16 * MT rows of the prefix per workgroup; 0: 128.  OWN: 16 * OWN rows of a sequence.  WHOLE: D is DP.
+template <class T, int DP, int MT, int OWN, bool WHOLE>
+__global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(const AttendParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
-    constexpr int OWN = MT > 0 ? MT : (DP > 128 ? 1 : 2);
     const bool own = (int)blockIdx.x >= p.prefix_blocks;
-    int i = (int)blockIdx.x - (own ? p.prefix_blocks : 0);
-    // Workgroups go to the 8 XCDs in turn; those of one range of the prefix, which differ in their rows alone, are given to one XCD (one L2).
-    if (MT == 0 && !own) i = (i & 7) * p.blocks_per_xcd + (i >> 3);
-    const int tiles = own ? p.own_tiles : p.prefix_tiles, splits = own ? p.own_splits : p.prefix_splits;
-    const int tile = i % tiles, rest = i / tiles, split = rest % splits, bh = rest / splits, h = own ? bh % p.Hk : bh, b = own ? bh / p.Hk : 0;
-    if (h >= p.Hk) return;
-    int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
-    if constexpr (MT == 0) {
-        if (!own) {
-            attend_many<T, DP, WHOLE>(p, p.prefix_pages, h, first, end, tile * 128, p.rows, split, lds);
-            return;
-        }
+    if (!own) {
+        // Workgroups go to the 8 XCDs in turn; those of one range of the prefix, which differ in their rows alone, are given to one XCD (one L2).
+        const int i = ((int)blockIdx.x & 7) * p.blocks_per_xcd + ((int)blockIdx.x >> 3);
+        const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
+        if (h >= p.Hk) return;
+        const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
+        if constexpr (MT == 0) attend_many<T, DP, WHOLE>(p, p.prefix_pages, h, first, end, tile * 128, p.rows, split, lds);
+        else attend_few<T, DP, MT, WHOLE>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, 4, lds);
+        return;
     }
-    Sequence seq{};
-    int row0 = tile * 16 * OWN, row_end = p.rows;
-    if (own) {
-        seq = sequence_of(p, b);
-        const int steps = (seq.len + 127) / 128, per = (steps + p.own_splits - 1) / p.own_splits, nG = p.n * p.G;
-        first = min(split * per * 128, seq.len);
-        end = min(first + per * 128, seq.len);
-        row0 += b * nG;
-        row_end = (b + 1) * nG;
-    }
-    attend_few<T, DP, OWN, WHOLE>(p, own ? p.page_table + b * p.table_stride : p.prefix_pages, h, first, end, row0, row_end, own, seq,
-                                  own ? p.prefix_splits + split : split, lds);
+    int i = (int)blockIdx.x - p.prefix_blocks;
+    if (p.own_share == 1) i = i * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int tile = i % p.own_tiles, rest = i / p.own_tiles, split = rest % p.own_splits, bh = rest / p.own_splits, h = bh % p.Hk, b = bh / p.Hk;
+    if (b >= p.B) return;
+    const Sequence seq = sequence_of(p, b);
+    const int steps = (seq.len + p.own_step - 1) / p.own_step, per = (steps + p.own_splits - 1) / p.own_splits, nG = p.n * p.G;
+    const int first = min(split * per * p.own_step, seq.len), end = min(first + per * p.own_step, seq.len);
+    attend_few<T, DP, OWN, WHOLE>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq, p.prefix_splits + split,
+                                  p.own_share, lds);
 }
 
-// The parts of every row joined: DP / 4 threads per row, four features each.
+// The parts of every row joined.  DP / 4 threads have four features each of a row's part, 2^lanes_log such groups share a row's parts, and
+// the rest of the workgroup has other rows.  A group takes four parts at a time, loads ahead of sums, and the groups meet in LDS.
 template <int DP>
-__global__ void __launch_bounds__(256) combine_kernel(const AttendParams p) {
-    constexpr int PER_ROW = DP / 4;
-    const int row = (int)(blockIdx.x * (256 / PER_ROW) + threadIdx.x / PER_ROW);
+__global__ void __launch_bounds__(256) combine_kernel(const AttendParams p, const int lanes_log) {
+    constexpr int PER = DP / 4, GROUPS = 256 / PER;
+    __shared__ f32x4 parts[GROUPS][PER];
+    __shared__ float tops[GROUPS], totals[GROUPS];
+    const int group = (int)threadIdx.x / PER, d = (int)(threadIdx.x % PER) * 4, lanes = 1 << lanes_log;
     const int64_t all = (int64_t)p.Hk * p.rows;
-    const int d = (int)(threadIdx.x % PER_ROW) * 4;
-    if (row >= all || d >= p.D) return;
+    const int row = (int)blockIdx.x * (GROUPS >> lanes_log) + (group >> lanes_log), at_row = min(row, (int)all - 1), at_d = min(d, p.D - 4);
     const int slots = p.prefix_splits + p.own_splits;
     float top = -__builtin_inff(), total = 0.0f;
-    for (int s = 0; s < slots; ++s) top = fmaxf(top, p.part_ml[(s * all + row) * 2]);
-    const float shift = top == -__builtin_inff() ? 0.0f : top;
     f32x4 x = f32x4{0, 0, 0, 0};
-    for (int s = 0; s < slots; ++s) {
-        const float m = p.part_ml[(s * all + row) * 2];
-        if (m == -__builtin_inff()) continue;
-        const float f = exp2_fast(m - shift);
-        total += f * p.part_ml[(s * all + row) * 2 + 1];
-        x += *(const f32x4*)(p.part_o + (s * all + row) * p.D + d) * f;
+    for (int s0 = group & (lanes - 1); s0 < slots; s0 += 4 * lanes) {
+        float m[4], l[4];
+        f32x4 o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int s = s0 + i * lanes;
+            const int64_t at = min(s, slots - 1) * all + at_row;
+            m[i] = p.part_ml[at * 2];
+            l[i] = p.part_ml[at * 2 + 1];
+            o[i] = *(const f32x4*)(p.part_o + at * p.D + at_d);
+            if (s >= slots) {
+                m[i] = -__builtin_inff();
+                l[i] = 0.0f;
+                o[i] = f32x4{0, 0, 0, 0};
+            }
+        }
+        const float now = fmaxf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), top), shift = now == -__builtin_inff() ? 0.0f : now;
+        const float factor = exp2_fast(top - shift);
+        x *= factor;
+        total *= factor;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float f = exp2_fast(m[i] - shift);
+            total += f * l[i];
+            x += o[i] * f;
+        }
+        top = now;
     }
+    if (lanes > 1) {
+        parts[group][d / 4] = x;
+        if (d == 0) {
+            tops[group] = top;
+            totals[group] = total;
+        }
+        __syncthreads();
+        if (group & (lanes - 1)) return;
+        float now = top;
+        for (int g = 1; g < lanes; ++g) now = fmaxf(now, tops[group + g]);
+        const float shift = now == -__builtin_inff() ? 0.0f : now;
+        const float factor = exp2_fast(top - shift);
+        x *= factor;
+        total *= factor;
+        for (int g = 1; g < lanes; ++g) {
+            const float f = exp2_fast(tops[group + g] - shift);
+            total += f * totals[group + g];
+            x += parts[group + g][d / 4] * f;
+        }
+        top = now;
+    }
+    if (row >= all || d >= p.D) return;
     const int h = row / p.rows, in_head = row - h * p.rows, nG = p.n * p.G;
     const int b = in_head / nG, in_seq = in_head - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
     const Sequence seq = sequence_of(p, b);
     const bool real = seq.bad || j < seq.queries;
     if (seq.bad) total = __builtin_nanf("");
-    if (!real || total == 0.0f) x = f32x4{0, 0, 0, 0};
-    else x = x * (1.0f / total);
+    x = !real || total == 0.0f ? f32x4{0, 0, 0, 0} : x * (1.0f / total);
     store_result(p, b * p.out_sequence + j * p.out_token + (int64_t)(h * p.G + g) * p.out_head + d, x);
     if (p.lse && d == 0) p.lse[((int64_t)b * p.n + j) * p.Hk * p.G + h * p.G + g] = real ? lse_of(top, total) : -__builtin_inff();
 }
