@@ -11,7 +11,7 @@ from concurrent.futures import ThreadPoolExecutor
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SRC = os.path.join(_HERE, "csrc", "vlut.hip")
-SOURCES = (SRC, os.path.join(_HERE, "csrc", "attention.hip"))      # the library's translation units
+SOURCES = (SRC, *(os.path.join(_HERE, "csrc", f"attention{part}.hip") for part in ("", "_bf16", "_f16")))       # the library's translation units
 LIB = os.path.join(_HERE, "libvlut.so")
 TORCH_SRC = os.path.join(_HERE, "csrc", "torch_calls.cpp")
 TORCH_LIB = os.path.join(_HERE, "_vlut_torch.so")

@@ -1,21 +1,21 @@
 // Between the projections of a decoder layer, for MI355X (gfx950): norms and rotation of heads, the paged cache, attention over a shared prefix.
-// Kernels and their part of the C ABI; a translation unit of its own, compiled beside vlut.hip and linked with it.
+// The heads' kernels, the host side of the attention, and their part of the C ABI; a translation unit beside vlut.hip, as those of the attention's kernels.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 #include <cmath>
 #include <cstdint>
-#include <type_traits>
 
 #include "vlut.h"
 
+#include "attention_params.h"
 #include "common.hip.h"
 #include "launch.hip.h"
 #include "heads_kernel.hip.h"
-#include "attention_kernel.hip.h"
 
 namespace {
+
+using namespace vlut_attention;
 
 bool type_ok(int type) { return type == VLUT_TYPE_F32 || type == VLUT_TYPE_BF16 || type == VLUT_TYPE_F16; }
 int type_bytes(int type) { return type == VLUT_TYPE_F32 ? 4 : 2; }
@@ -148,14 +148,6 @@ int check_cache(const vlut_cache* c) {
 // ---------------------------------------------------------------------------------------------
 constexpr int kUnits = 256;            // compute units that a launch is to fill
 
-struct AttendPlan {
-    int MT, own_mt, DP;                // tile: 16 * MT rows, 128 for MT = 0
-    int own_share, own_step;
-    int prefix_tiles, prefix_splits, prefix_chunk, prefix_blocks, blocks_per_xcd, own_tiles, own_splits, own_blocks, direct;
-    int64_t rows;
-    size_t o_bytes, ml_bytes;
-};
-
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t P, int64_t max_own, AttendPlan* out) {
@@ -205,48 +197,6 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     }
     *out = a;
     return VLUT_OK;
-}
-
-bool allow_lds(const void* kfn, int bytes, std::atomic<unsigned>& done_mask) {
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return false;
-    const unsigned bit = (dev >= 0 && dev < 32) ? (1u << dev) : 0u;
-    if (bit && (done_mask.load(std::memory_order_relaxed) & bit)) return true;
-    if (hipFuncSetAttribute(kfn, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) {
-        (void)hipGetLastError();
-        return false;
-    }
-    done_mask.fetch_or(bit, std::memory_order_relaxed);
-    return true;
-}
-
-template <class T, int DP, int MT, int OWN, bool WHOLE>
-int launch_attend_t(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
-    static std::atomic<unsigned> done{0};
-    constexpr int lds = MT == 0 ? std::max(2 * many_buffer(DP), few_lds(DP)) : few_lds(DP);
-    auto kfn = attend_kernel<T, DP, MT, OWN, WHOLE>;
-    if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
-    return launch(kfn, dim3((unsigned)(a.prefix_blocks + a.own_blocks)), 256, lds, stream, p);
-}
-template <class T, int DP, bool WHOLE>
-int launch_attend_w(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
-    if (a.MT == 1) return launch_attend_t<T, DP, 1, 1, WHOLE>(a, p, stream);
-    if (a.MT == 2) return a.own_mt == 1 ? launch_attend_t<T, DP, 2, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 2, 2, WHOLE>(a, p, stream);
-    return a.own_mt == 1 ? launch_attend_t<T, DP, 0, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 0, 2, WHOLE>(a, p, stream);
-}
-template <class T, int DP>
-int launch_attend_d(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
-    const int rc = p.D == DP ? launch_attend_w<T, DP, true>(a, p, stream) : launch_attend_w<T, DP, false>(a, p, stream);
-    if (rc != VLUT_OK || a.direct) return rc;
-    constexpr int groups = 256 / (DP / 4);
-    const int lanes_log = std::min(log2_of(groups), log2_of(ceil_div(a.prefix_splits + a.own_splits, 4)));
-    return launch(combine_kernel<DP>, dim3((unsigned)ceil_div(a.rows * p.Hk, groups >> lanes_log)), 256, 0, stream, p, lanes_log);
-}
-template <class T>
-int launch_attend(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
-    if (a.DP == 64) return launch_attend_d<T, 64>(a, p, stream);
-    if (a.DP == 128) return launch_attend_d<T, 128>(a, p, stream);
-    return launch_attend_d<T, 256>(a, p, stream);
 }
 
 // Rows that start at a dword.
@@ -370,7 +320,6 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
     p.part_ml = (float*)((unsigned char*)workspace + a.o_bytes);
     p.scale_log2 = (float)((double)scale * 1.4426950408889634);
     p.out_type = out->type;
-    p.exact_p = out->type == VLUT_TYPE_F32;
     p.B = (int)B;
     p.n = (int)n;
     p.Hk = cache->heads;
@@ -378,6 +327,8 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
     p.D = (int)D;
     p.page_log = log2_of(cache->page_size);
     p.pages = (int)cache->pages;
+    // (eight keys at most, whose offsets from the first have to fit 32 bits)
+    p.page_groups = cache->page_size >= 8 && std::max(std::abs(cache->k_token_stride), std::abs(cache->v_token_stride)) < (1 << 26);
     p.P = (int)prefix_len;
     p.max_own = (int)max_own_len;
     p.prefix_splits = a.prefix_splits;
@@ -391,7 +342,7 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
     p.blocks_per_xcd = a.blocks_per_xcd;
     p.rows = (int)a.rows;
     p.direct = a.direct;
-    return cache->type == VLUT_TYPE_BF16 ? launch_attend<__bf16>(a, p, (hipStream_t)stream) : launch_attend<_Float16>(a, p, (hipStream_t)stream);
+    return cache->type == VLUT_TYPE_BF16 ? launch_bf16(a, p, (hipStream_t)stream) : launch_f16(a, p, (hipStream_t)stream);
 }
 
 }  // extern "C"

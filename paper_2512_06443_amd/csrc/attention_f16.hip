@@ -1,0 +1,16 @@
+// The attention's kernels over a cache of type f16: a translation unit of its own for the time it takes to compile.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cstdint>
+
+#include "vlut.h"
+
+#include "attention_params.h"
+#include "common.hip.h"
+#include "launch.hip.h"
+#include "attention_kernel.hip.h"
+#include "attention_launch.hip.h"
+
+int vlut_attention::launch_f16(const AttendPlan& a, const AttendParams& p, hipStream_t stream) { return launch_attend<_Float16>(a, p, stream); }

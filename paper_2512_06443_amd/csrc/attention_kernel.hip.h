@@ -1,8 +1,10 @@
 // Attention for a batch of sequences that share a prefix, over a paged cache.
-// Part of the translation unit attention.hip (included there, in this order).
+// Part of the translation units attention_bf16.hip and attention_f16.hip (included there, in this order).
 #pragma once
 
 namespace {
+
+using namespace vlut_attention;
 
 // ---------------------------------------------------------------------------------------------
 // For every query row q (a query token and one of its heads) over the keys it sees, s = scale * q . k:
@@ -52,36 +54,6 @@ template <class A> inline __device__ f32x16 mfma32(A, A, f32x16 c) { return c; }
 inline __device__ s16x4 lds_read_transposed(unsigned) { return s16x4{}; }
 inline __device__ float exp2_fast(float x) { return x; }
 #endif
-
-struct AttendParams {
-    const void *q, *k, *v;
-    int64_t q_sequence, q_token, q_head;                               // strides in elements
-    int64_t k_page, k_head, k_token, v_page, v_head, v_token;
-    const int32_t *prefix_pages, *page_table, *own_lens, *query_lens;
-    int64_t table_stride;
-    void* out;
-    int64_t out_sequence, out_token, out_head;
-    float* lse;
-    float *part_o, *part_ml;           // [slot][Hk][B n G][D], [slot][Hk][B n G][2]; slots: the prefix' splits, then the own parts'
-    float scale_log2;                  // scale * log2(e): exponentials are powers of two
-    int out_type, exact_p;             // VLUT_TYPE_*; P in two terms
-    int B, n, Hk, G, D, page_log, pages;
-    int P, max_own;
-    int prefix_splits, prefix_chunk;   // keys per split
-    int own_splits, own_share, own_step;   // waves to a range; its keys are a multiple of own_step but for the end
-    int prefix_tiles, own_tiles;       // tiles of rows
-    int prefix_blocks, blocks_per_xcd;
-    int rows;                          // B n G
-    int direct;                        // a single part: workgroups store the result
-};
-
-constexpr int kFewKeys = 32;           // keys of a wave's step where rows are few
-__host__ __device__ constexpr int few_pitch(int DP) { return DP * 2 + 32; }
-__host__ __device__ constexpr int few_lds(int DP) { return 4 * kFewKeys * few_pitch(DP); }
-__host__ __device__ constexpr int many_keys(int DP) { return DP > 128 ? 32 : 64; }
-__host__ __device__ constexpr int many_k_pitch(int DP) { return DP * 2 + 16; }
-__host__ __device__ constexpr int many_v_pitch(int DP) { return DP * 2 + 64; }
-__host__ __device__ constexpr int many_buffer(int DP) { return many_keys(DP) * (many_k_pitch(DP) + many_v_pitch(DP)); }
 
 // Eight features of a row from feature 8 * chunk on, zeros past D (D >= 8 and a multiple of four).  Nothing past the row is read: a chunk
 // that D ends in is read four features earlier and moved.
@@ -135,6 +107,12 @@ __device__ __forceinline__ void arrived(V& x) {
     i32x4 y = __builtin_bit_cast(i32x4, x);
     asm volatile("" : "+v"(y));
     x = __builtin_bit_cast(V, y);
+#endif
+}
+
+__device__ __forceinline__ void arrived_scalar(int& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+s"(x));
 #endif
 }
 
@@ -408,11 +386,17 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 // One range of the prefix for 128 query rows, many enough that the matrix cores are what bounds it: K and V of 64 keys (32 where D is
 // over 128) in LDS for all four waves, which have 32 rows each.  Two buffers: the next keys travel to registers while the present ones are
 // worked on, and are stored behind them; one barrier per step.
-template <class T, int DP, bool WHOLE>
+// What the vector units have to do beside the matrix instructions is kept short:
+//   - a wave's load covers GK neighbouring keys.  Where pages hold as many, they share their page, and addresses are worked out once per
+//     wave (p.page_groups; else a thread works out its own);
+//   - O is not multiplied with every new maximum.  m is the exponentials' reference, at most kSlack (powers of two) below the maximum: only when
+//     a score passes that, O and l are brought down, and the scores worked out again (which leaves O's registers alone on the usual way).
+template <class T, int DP, int TERMS, bool WHOLE>
 __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, int slot, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
-    constexpr int KEYS = many_keys(DP), KT = KEYS / 32, KS = DP / 16, CH = DP / 8, PER = 256 / CH, LI = KEYS / PER;
+    constexpr int KEYS = many_keys(DP), KT = KEYS / 32, KS = DP / 16, CH = DP / 8, PER = 256 / CH, LI = KEYS / PER, GK = PER / 4;
     constexpr int KP = many_k_pitch(DP), VP = many_v_pitch(DP);
+    constexpr float kSlack = 8.0f;             // (P is at most 2^8: inside fp16)
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int nG = p.n * p.G;
@@ -438,44 +422,62 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
     const T* const kh = (const T*)p.k + h * p.k_head;
     const T* const vh = (const T*)p.v + h * p.v_head;
     const int mask = (1 << p.page_log) - 1, last = end_key - 1;
-    const int chunk = tid % CH, key_in = tid / CH, at = chunk_at<WHOLE>(chunk, p.D);
+    const int chunk = lane % CH, group_key = lane / CH, at = chunk_at<WHOLE>(chunk, p.D);
+    const unsigned k_lane = 2u * (unsigned)(group_key * (int)p.k_token + at), v_lane = 2u * (unsigned)(group_key * (int)p.v_token + at);
     i32x4 kr[LI], vr[LI];
-    int ids[LI];
+    int ids[LI], bad = 0;                      // the next keys' pages; a bit for each loaded key that is in none
+    // (keys past the range: another row of the last one's page, or the last one; its scores are masked, its V is zeroed)
+    auto key_of = [&](int kt, int i) { return p.page_groups ? min(kt + PER * i + GK * wave, last & ~(GK - 1)) : min(kt + PER * i + GK * wave + group_key, last); };
     auto look_up = [&](int kt) {
 #pragma unroll
-        for (int i = 0; i < LI; ++i) ids[i] = page_of(p, pages, min(kt + PER * i + key_in, last));
+        for (int i = 0; i < LI; ++i) ids[i] = page_of(p, pages, key_of(kt, i));
     };
     auto load = [&](int kt) {
-#pragma unroll
-        for (int i = 0; i < LI; ++i) {
-            const int key = min(kt + PER * i + key_in, last), in_page = key & mask;
-            kr[i] = *(const dword_aligned_i32x4*)(kh + (int64_t)max(ids[i], 0) * p.k_page + in_page * p.k_token + at);
-            vr[i] = *(const dword_aligned_i32x4*)(vh + (int64_t)max(ids[i], 0) * p.v_page + in_page * p.v_token + at);
-        }
-    };
-    int bad = 0;                       // a bit for each loaded key that is in no page
-    auto store = [&](int kt, unsigned char* to) {
-#pragma unroll
-        for (int i = 0; i < LI; ++i) {
-            i32x4 x = chunk_moved<WHOLE>(kr[i], chunk, p.D), y = chunk_moved<WHOLE>(vr[i], chunk, p.D);
-            if (bad >> i & 1) {
-                constexpr int N = (int)Number<T>::kNan;
-                x = i32x4{N, N, N, N};
-            }
-            if (kt + KEYS > end_key && kt + PER * i + key_in >= end_key) y = i32x4{0, 0, 0, 0};
-            *(i32x4*)(to + (PER * i + key_in) * KP + 16 * chunk) = x;
-            *(i32x4*)(to + KEYS * KP + (PER * i + key_in) * VP + 16 * chunk) = y;
-        }
-    };
-    auto keep_bad = [&]() {
         bad = 0;
+        if (p.page_groups) {
 #pragma unroll
-        for (int i = 0; i < LI; ++i) bad |= ids[i] < 0 ? 1 << i : 0;
+            for (int i = 0; i < LI; ++i) {
+                const int in_page = key_of(kt, i) & mask, id = __builtin_amdgcn_readfirstlane(ids[i]);
+                bad |= id < 0 ? 1 << i : 0;
+                const T* const kb = kh + max(id, 0) * p.k_page + in_page * p.k_token;
+                const T* const vb = vh + max(id, 0) * p.v_page + in_page * p.v_token;
+                kr[i] = *(const dword_aligned_i32x4*)((const unsigned char*)kb + k_lane);
+                vr[i] = *(const dword_aligned_i32x4*)((const unsigned char*)vb + v_lane);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < LI; ++i) {
+                const int in_page = key_of(kt, i) & mask;
+                bad |= ids[i] < 0 ? 1 << i : 0;
+                kr[i] = *(const dword_aligned_i32x4*)(kh + max(ids[i], 0) * p.k_page + in_page * p.k_token + at);
+                vr[i] = *(const dword_aligned_i32x4*)(vh + max(ids[i], 0) * p.v_page + in_page * p.v_token + at);
+            }
+        }
+    };
+    const int to_key = GK * wave + group_key;
+    auto store = [&](int kt, unsigned char* to) {
+        if (__any(bad)) {
+#pragma unroll
+            for (int i = 0; i < LI; ++i)
+                if (bad >> i & 1) {
+                    constexpr int N = (int)Number<T>::kNan;
+                    kr[i] = i32x4{N, N, N, N};
+                }
+        }
+        if (kt + KEYS > end_key) {
+#pragma unroll
+            for (int i = 0; i < LI; ++i)
+                if (kt + PER * i + to_key >= end_key) vr[i] = i32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < LI; ++i) {
+            *(i32x4*)(to + (PER * i + to_key) * KP + 16 * chunk) = chunk_moved<WHOLE>(kr[i], chunk, p.D);
+            *(i32x4*)(to + KEYS * KP + (PER * i + to_key) * VP + 16 * chunk) = chunk_moved<WHOLE>(vr[i], chunk, p.D);
+        }
     };
 
     look_up(first_key);
     load(first_key);
-    keep_bad();
     look_up(first_key + KEYS);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) arrived(q[ks]);
@@ -488,39 +490,42 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         const bool more = kt + KEYS < end_key;
         if (more) {
             load(kt + KEYS);
-            keep_bad();
             look_up(kt + 2 * KEYS);
         }
         f32x16 s[KT];
+        float shift;
+        for (;;) {
 #pragma unroll
-        for (int t = 0; t < KT; ++t) {
+            for (int t = 0; t < KT; ++t) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+                for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s[t] = mfma32(__builtin_bit_cast(x8, *(const i32x4*)(buf + (32 * t + l32) * KP + 32 * ks + 16 * half)), q[ks], s[t]);
-        }
-        if (kt + KEYS > end_key) {
+                for (int ks = 0; ks < KS; ++ks) s[t] = mfma32(__builtin_bit_cast(x8, *(const i32x4*)(buf + (32 * t + l32) * KP + 32 * ks + 16 * half)), q[ks], s[t]);
+            }
+            if (kt + KEYS > end_key) {
+                int left = end_key - kt;
+                arrived_scalar(left);          // (or its comparisons are made in every step, ahead of this loop)
+#pragma unroll
+                for (int t = 0; t < KT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (32 * t + (i & 3) + 8 * (i >> 2) + 4 * half >= left) s[t][i] = -__builtin_inff();
+            }
+            float top = s[0][0];
 #pragma unroll
             for (int t = 0; t < KT; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (kt + 32 * t + (i & 3) + 8 * (i >> 2) + 4 * half >= end_key) s[t][i] = -__builtin_inff();
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int t = 0; t < KT; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float now = fmaxf(m, top * p.scale_log2), shift = now == -__builtin_inff() ? 0.0f : now;
-        if (__any(now > m)) {
-            const float factor = exp2_fast(m - shift);
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+            top = fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
+            shift = m == -__builtin_inff() ? 0.0f : m;
+            if (!__any(top > m + kSlack)) break;
+            const float now = fmaxf(m, top), factor = exp2_fast(m - (now == -__builtin_inff() ? 0.0f : now));
+            m = now;
             l *= factor;
 #pragma unroll
             for (int dt = 0; dt < DP / 32; ++dt) o[dt] *= factor;
         }
-        m = now;
-        auto weigh = [&](auto terms) {
+        {
 #pragma unroll
             for (int st = 0; st < 2 * KT; ++st) {
                 x8 pf, rest;
@@ -529,19 +534,17 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
                     const float e = exp2_fast(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], p.scale_log2, -shift));
                     l += e;
                     pf[i] = (T)e;
-                    if constexpr (terms.value > 1) rest[i] = (T)(e - (float)(T)e);
+                    if constexpr (TERMS > 1) rest[i] = (T)(e - (float)(T)e);
                 }
 #pragma unroll
                 for (int dt = 0; dt < DP / 32; ++dt) {
                     const s16x4 v0 = lds_read_transposed(v_at + 16 * st * VP + 64 * dt), v1 = lds_read_transposed(v_at + (16 * st + 8) * VP + 64 * dt);
                     const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
                     o[dt] = mfma32(vf, pf, o[dt]);
-                    if constexpr (terms.value > 1) o[dt] = mfma32(vf, rest, o[dt]);
+                    if constexpr (TERMS > 1) o[dt] = mfma32(vf, rest, o[dt]);
                 }
             }
-        };
-        if (p.exact_p) weigh(std::integral_constant<int, 2>());
-        else weigh(std::integral_constant<int, 1>());
+        }
         if (more) store(kt + KEYS, lds + (turn ^ 1) * many_buffer(DP));
     }
     l += __shfl_xor(l, 32);
@@ -560,7 +563,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
     }
 }
 
-// MT > 0: 16 * MT rows of the prefix per workgroup; 0: 128.  OWN: 16 * OWN rows of a sequence.  WHOLE: D is DP.
+// MT > 0: 16 * MT rows of the prefix per workgroup; 0 and -1: 128, with P in one term or two.  OWN: 16 * OWN rows of a sequence.  WHOLE: D is DP.
 template <class T, int DP, int MT, int OWN, bool WHOLE>
 __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(const AttendParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
@@ -571,7 +574,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(const Att
         const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
         if (h >= p.Hk) return;
         const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
-        if constexpr (MT == 0) attend_many<T, DP, WHOLE>(p, p.prefix_pages, h, first, end, tile * 128, p.rows, split, lds);
+        if constexpr (MT <= 0) attend_many<T, DP, 1 - MT, WHOLE>(p, p.prefix_pages, h, first, end, tile * 128, p.rows, split, lds);
         else attend_few<T, DP, MT, WHOLE>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, 4, lds);
         return;
     }

@@ -1,0 +1,55 @@
+// What the host side of the attention (attention.hip) and its kernels (attention_kernel.hip.h, compiled once for each type of the cache) share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "vlut.h"
+
+namespace vlut_attention {
+
+struct AttendParams {
+    const void *q, *k, *v;
+    int64_t q_sequence, q_token, q_head;                               // strides in elements
+    int64_t k_page, k_head, k_token, v_page, v_head, v_token;
+    const int32_t *prefix_pages, *page_table, *own_lens, *query_lens;
+    int64_t table_stride;
+    void* out;
+    int64_t out_sequence, out_token, out_head;
+    float* lse;
+    float *part_o, *part_ml;           // [slot][Hk][B n G][D], [slot][Hk][B n G][2]; slots: the prefix' splits, then the own parts'
+    float scale_log2;                  // scale * log2(e): exponentials are powers of two
+    int out_type;                      // VLUT_TYPE_*
+    int B, n, Hk, G, D, page_log, pages;
+    int P, max_own;
+    int prefix_splits, prefix_chunk;   // keys per split
+    int own_splits, own_share, own_step;   // waves to a range; its keys are a multiple of own_step but for the end
+    int prefix_tiles, own_tiles;       // tiles of rows
+    int prefix_blocks, blocks_per_xcd;
+    int rows;                          // B n G
+    int page_groups;                   // the keys of a wave's load share their page
+    int direct;                        // a single part: workgroups store the result
+};
+
+constexpr int kFewKeys = 32;           // keys of a wave's step where rows are few
+__host__ __device__ constexpr int few_pitch(int DP) { return DP * 2 + 32; }
+__host__ __device__ constexpr int few_lds(int DP) { return 4 * kFewKeys * few_pitch(DP); }
+__host__ __device__ constexpr int many_keys(int DP) { return DP > 128 ? 32 : 64; }
+__host__ __device__ constexpr int many_k_pitch(int DP) { return DP * 2 + 16; }
+__host__ __device__ constexpr int many_v_pitch(int DP) { return DP * 2 + 64; }
+__host__ __device__ constexpr int many_buffer(int DP) { return many_keys(DP) * (many_k_pitch(DP) + many_v_pitch(DP)); }
+
+struct AttendPlan {
+    int MT, own_mt, DP;                // tile: 16 * MT rows, 128 for MT = 0
+    int own_share, own_step;
+    int prefix_tiles, prefix_splits, prefix_chunk, prefix_blocks, blocks_per_xcd, own_tiles, own_splits, own_blocks, direct;
+    int64_t rows;
+    size_t o_bytes, ml_bytes;
+};
+
+__attribute__((visibility("hidden"))) int launch_bf16(const AttendPlan& a, const AttendParams& p, hipStream_t stream);
+__attribute__((visibility("hidden"))) int launch_f16(const AttendPlan& a, const AttendParams& p, hipStream_t stream);
+
+}  // namespace vlut_attention
