@@ -327,8 +327,10 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
     p.D = (int)D;
     p.page_log = log2_of(cache->page_size);
     p.pages = (int)cache->pages;
-    // (eight keys at most, whose offsets from the first have to fit 32 bits)
-    p.page_groups = cache->page_size >= 8 && std::max(std::abs(cache->k_token_stride), std::abs(cache->v_token_stride)) < (1 << 26);
+    // (eight keys at most; strides and the offsets inside a page have to fit 31 bits, in bytes)
+    p.page_groups = cache->page_size >= 8;
+    for (int64_t s : {cache->k_page_stride, cache->v_page_stride}) p.page_groups = p.page_groups && s >= 0 && s < ((int64_t)1 << 31);
+    for (int64_t s : {cache->k_token_stride, cache->v_token_stride}) p.page_groups = p.page_groups && s >= 0 && s < ((int64_t)1 << 30) / cache->page_size;
     p.P = (int)prefix_len;
     p.max_own = (int)max_own_len;
     p.prefix_splits = a.prefix_splits;

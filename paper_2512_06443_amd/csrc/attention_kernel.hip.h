@@ -22,6 +22,7 @@ using namespace vlut_attention;
 // Scores, m, l and O are fp32; P is rounded to the cache's type for the second product, with what the rounding left as a second term
 // where the output is fp32.
 // ---------------------------------------------------------------------------------------------
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -94,11 +95,9 @@ __device__ __forceinline__ void store_result(const AttendParams& p, int64_t at, 
 }
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f; }
 
-// Page of a key of a list of pages; -1 for a number that is no page of the cache.
-__device__ __forceinline__ int page_of(const AttendParams& p, const int32_t* pages, int key) {
-    const int id = pages[key >> p.page_log];
-    return (unsigned)id < (unsigned)p.pages ? id : -1;
-}
+// Whether a number out of a list of pages is one of the cache's.  Asked where the page is used: asked where it is loaded, it would wait for the keys
+// and values that have been asked for before it.
+__device__ __forceinline__ bool is_page(const AttendParams& p, int id) { return (unsigned)id < (unsigned)p.pages; }
 
 // The compiler waits for what it loaded ahead of a loop again in every turn of it, and so for the loads of that turn: `x` is there from here on.
 template <class V>
@@ -167,7 +166,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int key = min(kt + 16 * t + l16, last), id = __shfl(page, 16 * t + l16);
-            const T* src = kh + (int64_t)max(id, 0) * p.k_page + (key & mask) * p.k_token;
+            const T* src = kh + (is_page(p, id) ? id : 0) * p.k_page + (key & mask) * p.k_token;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) kr[t][ks] = *(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(4 * ks + grp, p.D));
         }
@@ -176,11 +175,11 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
         for (int i = 0; i < VI; ++i) {
             const int k_in = PER * i + v_key, key = min(kt + k_in, last), id = __shfl(page, k_in);
-            const T* src = vh + (int64_t)max(id, 0) * p.v_page + (key & mask) * p.v_token;
+            const T* src = vh + (is_page(p, id) ? id : 0) * p.v_page + (key & mask) * p.v_token;
             vr[i] = *(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(v_chunk, p.D));
         }
     };
-    auto look_up = [&](int kt) { return page_of(p, pages, min(kt + (lane & 31), last)); };
+    auto look_up = [&](int kt) { return pages[min(kt + (lane & 31), last) >> p.page_log]; };
 
     int kt = first_key + (share > 1 ? kFewKeys * wave : 0);
     int page = 0, next_page = 0;
@@ -195,7 +194,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
             for (int ks = 0; ks < KS; ++ks) arrived(q[mt][ks]);
     }
     for (; kt < end_key; kt += stride) {
-        const bool some_masked = kt + kFewKeys > all_see, more = kt + stride < end_key;
+        const bool some_masked = kt + kFewKeys > all_see;
         // V to LDS, zeros for keys past the range
         unsigned odd = 0;
 #pragma unroll
@@ -209,21 +208,19 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
             }
             *(i32x4*)(mine + (PER * i + v_key) * PITCH + 16 * v_chunk) = x;
         }
-        // (in the order in which they are waited for: the page after the next, V, K)
-        int page_after = 0;
-        if (more) {
-            page_after = look_up(kt + 2 * stride);
-            load_v(kt + stride, next_page);
-        }
+        // What comes next, in the order in which it is waited for: the page after the next, V, K.  Also behind the last step, from its last key: in a
+        // branch, registers that are loaded on one way alone would be copied, and waited for, where the ways meet.
+        const int page_after = look_up(kt + 2 * stride);
+        load_v(kt + stride, next_page);
         x8 kf[2][KS];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) kf[t][ks] = __builtin_bit_cast(x8, chunk_moved<WHOLE>(kr[t][ks], 4 * ks + grp, p.D));
-        if (__any(page < 0)) {                      // a number that is no page: not read, and whoever sees its keys gets NaN
+        if (__any(!is_page(p, page))) {             // a number that is no page: not read, and whoever sees its keys gets NaN
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-                if (__shfl(page, 16 * t + l16) < 0) {
+                if (!is_page(p, __shfl(page, 16 * t + l16))) {
                     constexpr int N = (int)Number<T>::kNan;
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) kf[t][ks] = __builtin_bit_cast(x8, i32x4{N, N, N, N});
@@ -238,7 +235,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) s[mt][t] = mfma16(kf[t][ks], q[mt][ks], s[mt][t]);
             }
-        if (more) load_k(kt + stride, next_page);
+        load_k(kt + stride, next_page);
         page = next_page;
         next_page = page_after;
         x8 pf[MT], pf_rest[MT];
@@ -291,7 +288,9 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                 }
                 __builtin_amdgcn_wave_barrier();
             }
+#pragma unroll 1
             for (int i = 0; i < VI; ++i)
+#pragma unroll 1
                 for (int e = 0; e < 8; ++e) {
                     T* const x = (T*)(mine + (PER * i + v_key) * PITCH + 16 * v_chunk) + e;
                     if (!(fabsf((float)*x) < __builtin_inff())) *x = (T)0.0f;
@@ -311,25 +310,33 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
         }
     }
 
-    // Where a row's result goes, in four features a thread; f is the factor of what is stored (the parts' sums are stored as they are).
-    auto store = [&](int row, int d, f32x4 x, float top, float total) {
-        const int b = row / nG, in_seq = row - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
-        const int64_t part_row = ((int64_t)slot * p.Hk + h) * p.rows + row;
+    // A row's result from threads that have some of its features each: the part as it is, or O / l.
+    struct Row {
+        int64_t at;
+        float factor;
+        bool real;
+    };
+    auto begin_row = [&](int row, float top, float total, bool first) {
+        Row r;
         if (!p.direct) {
-            if (own && seq.bad) top = total = __builtin_nanf("");
-            if (d < p.D) *(f32x4*)(p.part_o + part_row * p.D + d) = x;
-            if (d == 0) {
-                p.part_ml[part_row * 2] = top;
-                p.part_ml[part_row * 2 + 1] = total;
-            }
-            return;
+            const int64_t part = ((int64_t)h * p.rows + row) * (p.prefix_splits + p.own_splits) + slot;
+            r.at = part * p.D;
+            if (first) *(f32x2*)(p.part_ml + part * 2) = own && seq.bad ? f32x2{__builtin_nanf(""), __builtin_nanf("")} : f32x2{top, total};
+            return r;
         }
+        const int b = row / nG, in_seq = row - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
         const Sequence its = own ? seq : sequence_of(p, b);
         if (its.bad) total = __builtin_nanf("");
-        const bool real = its.bad || j < its.queries;
-        x = !real || total == 0.0f ? f32x4{0, 0, 0, 0} : x * (1.0f / total);
-        if (d < p.D) store_result(p, b * p.out_sequence + j * p.out_token + (int64_t)(h * p.G + g) * p.out_head + d, x);
-        if (d == 0 && p.lse) p.lse[((int64_t)b * p.n + j) * p.Hk * p.G + h * p.G + g] = real ? lse_of(top, total) : -__builtin_inff();
+        r.real = (its.bad || j < its.queries) && total != 0.0f;
+        r.factor = 1.0f / total;
+        r.at = b * p.out_sequence + j * p.out_token + (int64_t)(h * p.G + g) * p.out_head;
+        if (first && p.lse) p.lse[((int64_t)b * p.n + j) * p.Hk * p.G + h * p.G + g] = r.real ? lse_of(top, total) : -__builtin_inff();
+        return r;
+    };
+    auto put = [&](const Row& r, int d, f32x4 x) {
+        if (d >= p.D) return;
+        if (!p.direct) *(f32x4*)(p.part_o + r.at + d) = x;
+        else store_result(p, r.at + d, r.real ? x * r.factor : f32x4{0, 0, 0, 0});
     };
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -340,9 +347,10 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const int row = row0 + 16 * mt + l16;
-            if (row < row_end)
+            if (row >= row_end) continue;
+            const Row r = begin_row(row, m[mt], l[mt], grp == 0);
 #pragma unroll
-                for (int dt = 0; dt < DP / 16; ++dt) store(row, 16 * dt + 4 * grp, o[mt][dt], m[mt], l[mt]);
+            for (int dt = 0; dt < DP / 16; ++dt) put(r, 16 * dt + 4 * grp, o[mt][dt]);
         }
         return;
     }
@@ -371,13 +379,14 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                 f[w] = exp2_fast(all_ml[(w * 16 + r) * 2] - shift);
                 total += f[w] * all_ml[(w * 16 + r) * 2 + 1];
             }
+            const Row to = begin_row(row, top, total, part == 0);
 #pragma unroll
             for (int v = 0; v < F4; ++v) {
                 const int d = (part + 16 * v) * 4;
                 f32x4 x = f32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) x += *(f32x4*)(all_o + (w * 16 + r) * OP + d) * f[w];
-                store(row, d, x, top, total);
+                put(to, d, x);
             }
         }
     }
@@ -430,17 +439,18 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
     auto key_of = [&](int kt, int i) { return p.page_groups ? min(kt + PER * i + GK * wave, last & ~(GK - 1)) : min(kt + PER * i + GK * wave + group_key, last); };
     auto look_up = [&](int kt) {
 #pragma unroll
-        for (int i = 0; i < LI; ++i) ids[i] = page_of(p, pages, key_of(kt, i));
+        for (int i = 0; i < LI; ++i) ids[i] = pages[key_of(kt, i) >> p.page_log];
     };
     auto load = [&](int kt) {
         bad = 0;
         if (p.page_groups) {
 #pragma unroll
             for (int i = 0; i < LI; ++i) {
-                const int in_page = key_of(kt, i) & mask, id = __builtin_amdgcn_readfirstlane(ids[i]);
-                bad |= id < 0 ? 1 << i : 0;
-                const T* const kb = kh + max(id, 0) * p.k_page + in_page * p.k_token;
-                const T* const vb = vh + max(id, 0) * p.v_page + in_page * p.v_token;
+                const int in_page = key_of(kt, i) & mask, named = __builtin_amdgcn_readfirstlane(ids[i]), id = is_page(p, named) ? named : 0;
+                bad |= is_page(p, named) ? 0 : 1 << i;
+                // (strides are below 2^31 here, and so are offsets inside a page)
+                const T* const kb = kh + ((int64_t)id * (int)p.k_page + in_page * (int)p.k_token);
+                const T* const vb = vh + ((int64_t)id * (int)p.v_page + in_page * (int)p.v_token);
                 kr[i] = *(const dword_aligned_i32x4*)((const unsigned char*)kb + k_lane);
                 vr[i] = *(const dword_aligned_i32x4*)((const unsigned char*)vb + v_lane);
             }
@@ -448,9 +458,10 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
 #pragma unroll
             for (int i = 0; i < LI; ++i) {
                 const int in_page = key_of(kt, i) & mask;
-                bad |= ids[i] < 0 ? 1 << i : 0;
-                kr[i] = *(const dword_aligned_i32x4*)(kh + max(ids[i], 0) * p.k_page + in_page * p.k_token + at);
-                vr[i] = *(const dword_aligned_i32x4*)(vh + max(ids[i], 0) * p.v_page + in_page * p.v_token + at);
+                const int64_t id = is_page(p, ids[i]) ? ids[i] : 0;
+                bad |= is_page(p, ids[i]) ? 0 : 1 << i;
+                kr[i] = *(const dword_aligned_i32x4*)(kh + id * p.k_page + in_page * p.k_token + at);
+                vr[i] = *(const dword_aligned_i32x4*)(vh + id * p.v_page + in_page * p.v_token + at);
             }
         }
     };
@@ -487,11 +498,8 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         wg_barrier_lds();
         const unsigned char* const buf = lds + turn * many_buffer(DP);
         const unsigned v_at = lds_base_of((void*)(buf + KEYS * KP)) + (4 * half + (l16 >> 2)) * VP + 32 * ((lane >> 4) & 1) + 8 * (l16 & 3);
-        const bool more = kt + KEYS < end_key;
-        if (more) {
-            load(kt + KEYS);
-            look_up(kt + 2 * KEYS);
-        }
+        load(kt + KEYS);                       // (behind the last step too, from the last keys)
+        look_up(kt + 2 * KEYS);
         f32x16 s[KT];
         float shift;
         for (;;) {
@@ -499,9 +507,11 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
             for (int t = 0; t < KT; ++t) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) s[t] = mfma32(__builtin_bit_cast(x8, *(const i32x4*)(buf + (32 * t + l32) * KP + 32 * ks + 16 * half)), q[ks], s[t]);
             }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int t = 0; t < KT; ++t) s[t] = mfma32(__builtin_bit_cast(x8, *(const i32x4*)(buf + (32 * t + l32) * KP + 32 * ks + 16 * half)), q[ks], s[t]);
             if (kt + KEYS > end_key) {
                 int left = end_key - kt;
                 arrived_scalar(left);          // (or its comparisons are made in every step, ahead of this loop)
@@ -545,11 +555,11 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
                 }
             }
         }
-        if (more) store(kt + KEYS, lds + (turn ^ 1) * many_buffer(DP));
+        if (kt + KEYS < end_key) store(kt + KEYS, lds + (turn ^ 1) * many_buffer(DP));
     }
     l += __shfl_xor(l, 32);
     if (row >= row_end) return;
-    const int64_t part_row = ((int64_t)slot * p.Hk + h) * p.rows + row;
+    const int64_t part_row = ((int64_t)h * p.rows + row) * (p.prefix_splits + p.own_splits) + slot;
 #pragma unroll
     for (int dt = 0; dt < DP / 32; ++dt)
 #pragma unroll
@@ -597,8 +607,8 @@ __global__ void __launch_bounds__(256) combine_kernel(const AttendParams p, cons
     __shared__ f32x4 parts[GROUPS][PER];
     __shared__ float tops[GROUPS], totals[GROUPS];
     const int group = (int)threadIdx.x / PER, d = (int)(threadIdx.x % PER) * 4, lanes = 1 << lanes_log;
-    const int64_t all = (int64_t)p.Hk * p.rows;
-    const int row = (int)blockIdx.x * (GROUPS >> lanes_log) + (group >> lanes_log), at_row = min(row, (int)all - 1), at_d = min(d, p.D - 4);
+    const int all = p.Hk * p.rows;
+    const int row = (int)blockIdx.x * (GROUPS >> lanes_log) + (group >> lanes_log), at_row = min(row, all - 1), at_d = min(d, p.D - 4);
     const int slots = p.prefix_splits + p.own_splits;
     float top = -__builtin_inff(), total = 0.0f;
     f32x4 x = f32x4{0, 0, 0, 0};
@@ -608,7 +618,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const AttendParams p, cons
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int s = s0 + i * lanes;
-            const int64_t at = min(s, slots - 1) * all + at_row;
+            const int64_t at = (int64_t)at_row * slots + min(s, slots - 1);
             m[i] = p.part_ml[at * 2];
             l[i] = p.part_ml[at * 2 + 1];
             o[i] = *(const f32x4*)(p.part_o + at * p.D + at_d);
