@@ -150,7 +150,8 @@ constexpr int kUnits = 256;            // compute units that a launch is to fill
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t P, int64_t max_own, AttendPlan* out) {
+// grouped: the keys of a wave's load share their page, as the kernel for many rows wants it.
+int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t P, int64_t max_own, bool grouped, AttendPlan* out) {
     if (B < 1 || n < 1 || Hk < 1 || Hq < 1 || Hq >= (1 << 16) || Hq % Hk || B >= kMaxDim || n >= kMaxDim) return VLUT_ERR_SHAPE;
     if (P < 0 || max_own < 0 || P >= ((int64_t)1 << 30) || max_own >= ((int64_t)1 << 30) || D < 1) return VLUT_ERR_SHAPE;
     if (D < 8 || D > VLUT_MAX_HEAD_FEATURES || D % 4) return VLUT_ERR_UNSUPPORTED;
@@ -160,24 +161,25 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     a.rows = rows;
     a.DP = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
     a.own_mt = own_rows <= 16 ? 1 : 2;
-    a.MT = P == 0 ? a.own_mt : (rows <= 16 ? 1 : (rows <= 64 ? 2 : 0));
+    a.MT = P == 0 ? a.own_mt : (rows <= 16 ? 1 : (rows <= 64 || !grouped ? 2 : 0));
+    a.waves = a.MT == 0 && a.DP <= 128 && rows > 128 ? 8 : 4;
     a.own_tiles = (int)ceil_div(own_rows, 16 * a.own_mt);
     const int64_t own_units = B * Hk * a.own_tiles;
-    a.own_share = own_units >= 4 * 2 * kUnits ? 1 : 4;
+    a.own_share = own_units >= 4 * 2 * kUnits ? 1 : a.waves;
     a.own_step = a.own_share * kFewKeys;
     const int64_t own_steps = ceil_div(max_own, a.own_step), own_all = own_units * own_steps;
     int64_t per_own;
     if (a.MT > 0) {
         a.prefix_tiles = (int)ceil_div(rows, 16 * a.MT);
-        const int64_t steps = ceil_div(P, 128), units = Hk * a.prefix_tiles * steps + own_all / (4 / a.own_share);
+        const int64_t steps = ceil_div(P, 128), units = Hk * a.prefix_tiles * steps + own_all / (a.waves / a.own_share);
         const int64_t per = std::max<int64_t>(1, ceil_div(units, 2 * kUnits));
         a.prefix_chunk = (int)(128 * per);
         per_own = per;
     } else {
-        a.prefix_tiles = (int)ceil_div(rows, 128);
-        const int64_t keys = many_keys(a.DP), splits = std::min(std::max<int64_t>(1, 2 * kUnits / (Hk * a.prefix_tiles)), ceil_div(P, 256));
+        a.prefix_tiles = (int)ceil_div(rows, 32 * a.waves);
+        const int64_t keys = many_keys(a.DP), splits = std::min(std::max<int64_t>(1, 8 / a.waves * kUnits / (Hk * a.prefix_tiles)), ceil_div(P, 256));
         a.prefix_chunk = (int)(ceil_div(ceil_div(P, splits), keys) * keys);
-        per_own = std::max<int64_t>(1, ceil_div(own_all / (4 / a.own_share), 4 * kUnits));
+        per_own = std::max<int64_t>(1, ceil_div(own_all / (a.waves / a.own_share), 16 / a.waves * kUnits));
     }
     if (a.own_share == 1) per_own = std::max<int64_t>(per_own, own_steps);
     a.prefix_splits = P > 0 ? (int)ceil_div(P, a.prefix_chunk) : 0;
@@ -185,7 +187,7 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     if (a.prefix_splits + a.own_splits == 0) a.own_splits = 1;      // nothing is seen: a workgroup stores that
     const int64_t prefix_blocks = Hk * a.prefix_tiles * a.prefix_splits;
     a.blocks_per_xcd = (int)ceil_div(prefix_blocks, 8);
-    const int64_t padded = 8 * (int64_t)a.blocks_per_xcd, own_blocks = ceil_div(own_units * a.own_splits, 4 / a.own_share);
+    const int64_t padded = 8 * (int64_t)a.blocks_per_xcd, own_blocks = ceil_div(own_units * a.own_splits, a.waves / a.own_share);
     if (padded + own_blocks >= ((int64_t)1 << 31)) return VLUT_ERR_SHAPE;
     a.prefix_blocks = (int)padded;
     a.own_blocks = (int)own_blocks;
@@ -197,6 +199,14 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     }
     *out = a;
     return VLUT_OK;
+}
+
+// The keys of a wave's load (eight at most) share their page, and strides and the offsets inside a page fit 31 bits, in bytes.
+bool grouped_keys(const vlut_cache& c) {
+    bool ok = c.page_size >= 8;
+    for (int64_t s : {c.k_page_stride, c.v_page_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30);
+    for (int64_t s : {c.k_token_stride, c.v_token_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) / std::max<int64_t>(c.page_size, 8);
+    return ok;
 }
 
 // Rows that start at a dword.
@@ -253,16 +263,21 @@ int vlut_append_kv(const vlut_heads* k, const vlut_heads* v, const vlut_heads* q
 }
 
 size_t vlut_shared_prefix_attention_bytes(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t prefix_len, int64_t max_own_len) {
-    AttendPlan a;
-    return plan_attention(B, n, Hq, Hk, D, prefix_len, max_own_len, &a) == VLUT_OK ? a.o_bytes + a.ml_bytes : 0;
+    size_t most = 0;                   // (of any cache)
+    for (bool grouped : {false, true}) {
+        AttendPlan a;
+        if (plan_attention(B, n, Hq, Hk, D, prefix_len, max_own_len, grouped, &a) != VLUT_OK) return 0;
+        most = std::max(most, a.o_bytes + a.ml_bytes);
+    }
+    return most;
 }
 
 int vlut_query_shared_prefix_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t prefix_len, int64_t max_own_len, int* out4) {
     if (!out4) return VLUT_ERR_NULL;
     AttendPlan a;
-    const int rc = plan_attention(B, n, Hq, Hk, D, prefix_len, max_own_len, &a);
+    const int rc = plan_attention(B, n, Hq, Hk, D, prefix_len, max_own_len, true, &a);
     if (rc != VLUT_OK) return rc;
-    out4[0] = a.MT > 0 ? 16 * a.MT : 128;
+    out4[0] = a.MT > 0 ? 16 * a.MT : 32 * a.waves;
     out4[1] = a.prefix_splits;
     out4[2] = a.own_splits;
     out4[3] = a.prefix_blocks + a.own_blocks;
@@ -277,7 +292,7 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
     int rc = check_cache(cache);
     if (rc != VLUT_OK) return rc;
     AttendPlan a;
-    rc = plan_attention(B, n, q->heads, cache->heads, D, prefix_len, max_own_len, &a);
+    rc = plan_attention(B, n, q->heads, cache->heads, D, prefix_len, max_own_len, grouped_keys(*cache), &a);
     if (rc != VLUT_OK) return rc;
     if (!q->data || !out->data || !own_lens || (prefix_len > 0 && !prefix_pages) || (max_own_len > 0 && !page_table)) return VLUT_ERR_NULL;
     if (out->heads != q->heads || q->type != cache->type || (out->type != cache->type && out->type != VLUT_TYPE_F32)) return VLUT_ERR_SHAPE;
@@ -327,10 +342,6 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
     p.D = (int)D;
     p.page_log = log2_of(cache->page_size);
     p.pages = (int)cache->pages;
-    // (eight keys at most; strides and the offsets inside a page have to fit 31 bits, in bytes)
-    p.page_groups = cache->page_size >= 8;
-    for (int64_t s : {cache->k_page_stride, cache->v_page_stride}) p.page_groups = p.page_groups && s >= 0 && s < ((int64_t)1 << 31);
-    for (int64_t s : {cache->k_token_stride, cache->v_token_stride}) p.page_groups = p.page_groups && s >= 0 && s < ((int64_t)1 << 30) / cache->page_size;
     p.P = (int)prefix_len;
     p.max_own = (int)max_own_len;
     p.prefix_splits = a.prefix_splits;

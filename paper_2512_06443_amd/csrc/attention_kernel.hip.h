@@ -36,11 +36,13 @@ template <>
 struct Number<__bf16> {
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     static constexpr unsigned kExponents = 0x7f807f80u, kNan = 0x7fc07fc0u;
+    static constexpr float kSlack = 24.0f;
 };
 template <>
 struct Number<_Float16> {
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     static constexpr unsigned kExponents = 0x7c007c00u, kNan = 0x7e007e00u;
+    static constexpr float kSlack = 15.0f;             // (weights below 2^15 are inside the type)
 };
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ f32x4 mfma16(Number<__bf16>::x8 a, Number<__bf16>::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -117,8 +119,8 @@ __device__ __forceinline__ void arrived_scalar(int& x) {
 
 // One range of keys for up to 16 * MT query rows, few enough that memory is what bounds it.  A wave takes 32 keys a step (K straight to registers, V
 // through a piece of LDS of its own, no barrier); the next 32 are on their way while the present ones are worked on.  `share` waves
-// have the range in turn: 4, which join at the end through LDS, or 1 where ranges are short and many.
-template <class T, int DP, int MT, bool WHOLE>
+// have the range in turn: all NW, which join at the end through LDS, or 1 where ranges are short and many.
+template <class T, int DP, int MT, int NW, bool WHOLE>
 __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, bool own, const Sequence& seq, int slot,
                            int share, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
@@ -357,7 +359,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
     // The waves' parts: 16 rows at a time through LDS, thread t joins features of row t / 16.
     constexpr int OP = DP + 4, F4 = DP / 64;                       // floats per row; vectors of four per thread
     float* const all_o = (float*)lds;                              // [wave][16][OP]
-    float* const all_ml = all_o + 4 * 16 * OP;                     // [wave][16][2]
+    float* const all_ml = all_o + NW * 16 * OP;                    // [wave][16][2]
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         __syncthreads();
@@ -369,13 +371,13 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
         }
         __syncthreads();
         const int r = (int)threadIdx.x >> 4, part = (int)threadIdx.x & 15, row = row0 + 16 * mt + r;
-        if (row < row_end) {
-            float top = -__builtin_inff(), total = 0.0f, f[4];
+        if (r < 16 && row < row_end) {
+            float top = -__builtin_inff(), total = 0.0f, f[NW];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) top = fmaxf(top, all_ml[(w * 16 + r) * 2]);
+            for (int w = 0; w < NW; ++w) top = fmaxf(top, all_ml[(w * 16 + r) * 2]);
             const float shift = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
+            for (int w = 0; w < NW; ++w) {
                 f[w] = exp2_fast(all_ml[(w * 16 + r) * 2] - shift);
                 total += f[w] * all_ml[(w * 16 + r) * 2 + 1];
             }
@@ -385,35 +387,53 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                 const int d = (part + 16 * v) * 4;
                 f32x4 x = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int w = 0; w < 4; ++w) x += *(f32x4*)(all_o + (w * 16 + r) * OP + d) * f[w];
+                for (int w = 0; w < NW; ++w) x += *(f32x4*)(all_o + (w * 16 + r) * OP + d) * f[w];
                 put(to, d, x);
             }
         }
     }
 }
 
-// One range of the prefix for 128 query rows, many enough that the matrix cores are what bounds it: K and V of 64 keys (32 where D is
-// over 128) in LDS for all four waves, which have 32 rows each.  Two buffers: the next keys travel to registers while the present ones are
+// The order of a stretch of code with MFMAS matrix instructions: AHEAD reads of LDS in front, then READS of them, VALU vector instructions and EXPS
+// exponentials behind each matrix instruction.  Left to itself the compiler reads what an instruction needs right before it and waits.
+template <int MFMAS, int READS, int AHEAD, int VALU, int EXPS>
+__device__ __forceinline__ void in_turn() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (AHEAD > 0) __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+    if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x402, 4 * (VALU + EXPS), 0);
+#pragma unroll
+    for (int i = 0; i < MFMAS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+        if constexpr (VALU > 0) {
+            __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
+            __builtin_amdgcn_sched_group_barrier(0x400, EXPS, 0);
+        }
+    }
+#endif
+}
+
+// One range of the prefix for 32 * NW query rows, many enough that the matrix cores are what bounds it: K and V of 64 keys (32 where D is
+// over 128) in LDS for all NW waves, which have 32 rows each.  Two buffers: the next keys travel to registers while the present ones are
 // worked on, and are stored behind them; one barrier per step.
 // What the vector units have to do beside the matrix instructions is kept short:
-//   - a wave's load covers GK neighbouring keys.  Where pages hold as many, they share their page, and addresses are worked out once per
-//     wave (p.page_groups; else a thread works out its own);
-//   - O is not multiplied with every new maximum.  m is the exponentials' reference, at most kSlack (powers of two) below the maximum: only when
-//     a score passes that, O and l are brought down, and the scores worked out again (which leaves O's registers alone on the usual way).
-template <class T, int DP, int TERMS, bool WHOLE>
+//   - a wave's load covers GK neighbouring keys, which share their page (the host sees to it): addresses are worked out once per wave;
+//   - O is not multiplied with every new maximum: m is the maximum of the first step's scores, and weights are powers of two of the scores above it.
+//     Where a later score is kSlack or more above that, the range is begun again, with the largest of all its scores, which a sweep over K
+//     finds.  (Multiplying where it is needed, in a branch, costs as much as always: O's registers are copied where the ways meet.)
+template <class T, int DP, int TERMS, int NW, bool WHOLE>
 __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, int slot, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
-    constexpr int KEYS = many_keys(DP), KT = KEYS / 32, KS = DP / 16, CH = DP / 8, PER = 256 / CH, LI = KEYS / PER, GK = PER / 4;
+    constexpr int KEYS = many_keys(DP), KT = KEYS / 32, KS = DP / 16, CH = DP / 8, PER = 64 * NW / CH, LI = KEYS / PER, GK = 64 / CH;
     constexpr int KP = many_k_pitch(DP), VP = many_v_pitch(DP);
-    constexpr float kSlack = 8.0f;             // (P is at most 2^8: inside fp16)
+    constexpr float kSlack = Number<T>::kSlack;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
-    const int nG = p.n * p.G;
-    const int row = row0 + 32 * wave + l32, real_row = min(row, row_end - 1);
-    const int b = real_row / nG, in_seq = real_row - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
+    const int nG = p.n * p.G, row = row0 + 32 * wave + l32;
 
     x8 q[KS];
     {
+        const int real = min(row, row_end - 1), b = real / nG, in_seq = real - b * nG, j = in_seq / p.G, g = in_seq - j * p.G;
         const T* src = (const T*)p.q + b * p.q_sequence + j * p.q_token + (int64_t)(h * p.G + g) * p.q_head;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -421,53 +441,36 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
             q[ks] = __builtin_bit_cast(x8, chunk_moved<WHOLE>(*(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(chunk, p.D)), chunk, p.D));
         }
     }
-    float m = -__builtin_inff(), l = 0.0f;
-    f32x16 o[DP / 32];
-#pragma unroll
-    for (int dt = 0; dt < DP / 32; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
 
     const T* const kh = (const T*)p.k + h * p.k_head;
     const T* const vh = (const T*)p.v + h * p.v_head;
-    const int mask = (1 << p.page_log) - 1, last = end_key - 1;
-    const int chunk = lane % CH, group_key = lane / CH, at = chunk_at<WHOLE>(chunk, p.D);
-    const unsigned k_lane = 2u * (unsigned)(group_key * (int)p.k_token + at), v_lane = 2u * (unsigned)(group_key * (int)p.v_token + at);
+    const int mask = (1 << p.page_log) - 1, last_group = (end_key - 1) & ~(GK - 1);
+    const int chunk = lane % CH, to_key = GK * wave + lane / CH;
+    const unsigned at = 2u * (unsigned)chunk_at<WHOLE>(chunk, p.D), k_lane = (unsigned)(lane / CH) * 2u * (unsigned)p.k_token + at, v_lane = (unsigned)(lane / CH) * 2u * (unsigned)p.v_token + at;
+    const unsigned to_k = (unsigned)(to_key * KP + 16 * chunk), to_v = (unsigned)(KEYS * KP + to_key * VP + 16 * chunk);
     i32x4 kr[LI], vr[LI];
-    int ids[LI], bad = 0;                      // the next keys' pages; a bit for each loaded key that is in none
-    // (keys past the range: another row of the last one's page, or the last one; its scores are masked, its V is zeroed)
-    auto key_of = [&](int kt, int i) { return p.page_groups ? min(kt + PER * i + GK * wave, last & ~(GK - 1)) : min(kt + PER * i + GK * wave + group_key, last); };
+    int ids[LI], bad = 0;                      // the next keys' pages; a bit for each loaded group that is in none
+    // (groups past the range read the last one: scores are masked, V is zeroed)
+    auto group = [&](int kt, int i) { return min(kt + PER * i + GK * wave, last_group); };
     auto look_up = [&](int kt) {
 #pragma unroll
-        for (int i = 0; i < LI; ++i) ids[i] = pages[key_of(kt, i) >> p.page_log];
+        for (int i = 0; i < LI; ++i) ids[i] = pages[group(kt, i) >> p.page_log];
     };
     auto load = [&](int kt) {
         bad = 0;
-        if (p.page_groups) {
 #pragma unroll
-            for (int i = 0; i < LI; ++i) {
-                const int in_page = key_of(kt, i) & mask, named = __builtin_amdgcn_readfirstlane(ids[i]), id = is_page(p, named) ? named : 0;
-                bad |= is_page(p, named) ? 0 : 1 << i;
-                // (strides are below 2^31 here, and so are offsets inside a page)
-                const T* const kb = kh + ((int64_t)id * (int)p.k_page + in_page * (int)p.k_token);
-                const T* const vb = vh + ((int64_t)id * (int)p.v_page + in_page * (int)p.v_token);
-                kr[i] = *(const dword_aligned_i32x4*)((const unsigned char*)kb + k_lane);
-                vr[i] = *(const dword_aligned_i32x4*)((const unsigned char*)vb + v_lane);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < LI; ++i) {
-                const int in_page = key_of(kt, i) & mask;
-                const int64_t id = is_page(p, ids[i]) ? ids[i] : 0;
-                bad |= is_page(p, ids[i]) ? 0 : 1 << i;
-                kr[i] = *(const dword_aligned_i32x4*)(kh + id * p.k_page + in_page * p.k_token + at);
-                vr[i] = *(const dword_aligned_i32x4*)(vh + id * p.v_page + in_page * p.v_token + at);
-            }
+        for (int i = 0; i < LI; ++i) {
+            const unsigned in_page = (unsigned)(group(kt, i) & mask), named = (unsigned)__builtin_amdgcn_readfirstlane(ids[i]);
+            const bool page = named < (unsigned)p.pages;
+            bad |= page ? 0 : 1 << i;
+            // (strides are below 2^31 bytes here, and so are offsets inside a page)
+            const uint64_t id = page ? named : 0u;
+            kr[i] = *(const dword_aligned_i32x4*)((const unsigned char*)kh + (id * (unsigned)p.k_page * 2u + in_page * 2u * (unsigned)p.k_token) + k_lane);
+            vr[i] = *(const dword_aligned_i32x4*)((const unsigned char*)vh + (id * (unsigned)p.v_page * 2u + in_page * 2u * (unsigned)p.v_token) + v_lane);
         }
     };
-    const int to_key = GK * wave + group_key;
     auto store = [&](int kt, unsigned char* to) {
-        if (__any(bad)) {
+        if (bad) {
 #pragma unroll
             for (int i = 0; i < LI; ++i)
                 if (bad >> i & 1) {
@@ -482,100 +485,133 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         }
 #pragma unroll
         for (int i = 0; i < LI; ++i) {
-            *(i32x4*)(to + (PER * i + to_key) * KP + 16 * chunk) = chunk_moved<WHOLE>(kr[i], chunk, p.D);
-            *(i32x4*)(to + KEYS * KP + (PER * i + to_key) * VP + 16 * chunk) = chunk_moved<WHOLE>(vr[i], chunk, p.D);
+            *(i32x4*)(to + to_k + PER * i * KP) = chunk_moved<WHOLE>(kr[i], chunk, p.D);
+            *(i32x4*)(to + to_v + PER * i * VP) = chunk_moved<WHOLE>(vr[i], chunk, p.D);
         }
     };
 
-    look_up(first_key);
-    load(first_key);
-    look_up(first_key + KEYS);
+    // All keys of the range, in steps: use(kt, K and V in LDS) between two barriers each.
+    auto sweep = [&](auto use) {
+        look_up(first_key);
+        load(first_key);
+        look_up(first_key + KEYS);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) arrived(q[ks]);
-    store(first_key, lds);
-    int turn = 0;
-    for (int kt = first_key; kt < end_key; kt += KEYS, turn ^= 1) {
-        wg_barrier_lds();
-        const unsigned char* const buf = lds + turn * many_buffer(DP);
-        const unsigned v_at = lds_base_of((void*)(buf + KEYS * KP)) + (4 * half + (l16 >> 2)) * VP + 32 * ((lane >> 4) & 1) + 8 * (l16 & 3);
-        load(kt + KEYS);                       // (behind the last step too, from the last keys)
-        look_up(kt + 2 * KEYS);
-        f32x16 s[KT];
-        float shift;
-        for (;;) {
+        for (int ks = 0; ks < KS; ++ks) arrived(q[ks]);
+        store(first_key, lds);
+        int turn = 0;
+        for (int kt = first_key; kt < end_key; kt += KEYS, turn ^= 1) {
+            wg_barrier_lds();
+            load(kt + KEYS);                   // (behind the last step too, from the last keys)
+            look_up(kt + 2 * KEYS);
+            use(kt, lds + turn * many_buffer(DP));
+            if (kt + KEYS < end_key) store(kt + KEYS, lds + (turn ^ 1) * many_buffer(DP));
+        }
+    };
+    f32x16 s[KT], o[DP / 32];
+    float top, m = 0.0f, l;                    // top: the largest score of a step, times scale_log2
+    auto score = [&](int kt, const unsigned char* buf) {
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
+        for (int t = 0; t < KT; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
-            }
+            for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int t = 0; t < KT; ++t) s[t] = mfma32(__builtin_bit_cast(x8, *(const i32x4*)(buf + (32 * t + l32) * KP + 32 * ks + 16 * half)), q[ks], s[t]);
-            if (kt + KEYS > end_key) {
-                int left = end_key - kt;
-                arrived_scalar(left);          // (or its comparisons are made in every step, ahead of this loop)
-#pragma unroll
-                for (int t = 0; t < KT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (32 * t + (i & 3) + 8 * (i >> 2) + 4 * half >= left) s[t][i] = -__builtin_inff();
-            }
-            float top = s[0][0];
+            for (int t = 0; t < KT; ++t) s[t] = mfma32(__builtin_bit_cast(x8, *(const i32x4*)(buf + (32 * t + l32) * KP + 32 * ks + 16 * half)), q[ks], s[t]);
+        in_turn<KS * KT, 1, 6, 0, 0>();
+        if (kt + KEYS > end_key) {
+            int left = end_key - kt;
+            arrived_scalar(left);              // (or its comparisons are made in every step, ahead of the branch)
 #pragma unroll
             for (int t = 0; t < KT; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-            top = fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
-            shift = m == -__builtin_inff() ? 0.0f : m;
-            if (!__any(top > m + kSlack)) break;
-            const float now = fmaxf(m, top), factor = exp2_fast(m - (now == -__builtin_inff() ? 0.0f : now));
-            m = now;
-            l *= factor;
-#pragma unroll
-            for (int dt = 0; dt < DP / 32; ++dt) o[dt] *= factor;
+                for (int i = 0; i < 16; ++i)
+                    if (32 * t + (i & 3) + 8 * (i >> 2) + 4 * half >= left) s[t][i] = -__builtin_inff();
         }
-        {
+        top = s[0][0];
 #pragma unroll
-            for (int st = 0; st < 2 * KT; ++st) {
-                x8 pf, rest;
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
+    };
+    int* const again = (int*)(lds + 2 * many_buffer(DP));
+    if (tid == 0) *again = 0;                  // (the sweep's first barrier is between this and what follows)
+    for (bool known = false;;) {
+        bool over = false;
+        l = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] = 0.0f;
+        sweep([&](int kt, const unsigned char* buf) {
+            const unsigned v_at = lds_base_of((void*)(buf + KEYS * KP)) + (4 * half + (l16 >> 2)) * VP + 32 * ((lane >> 4) & 1) + 8 * (l16 & 3);
+            score(kt, buf);
+            m = kt == first_key && !known ? top : m;
+            const float shift = m == -__builtin_inff() ? 0.0f : m;
+            over = over || top > m + kSlack;
+            // Sixteen keys at a time; the weights and V of the next are made and read while the matrix cores are on these.
+            x8 vf[DP / 32], pf, rest, next, next_rest;
+            auto weigh = [&](int st, x8& w, x8& w_rest) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float e = exp2_fast(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], p.scale_log2, -shift));
                     l += e;
-                    pf[i] = (T)e;
-                    if constexpr (TERMS > 1) rest[i] = (T)(e - (float)(T)e);
+                    w[i] = (T)e;
+                    if constexpr (TERMS > 1) w_rest[i] = (T)(e - (float)(T)e);
                 }
+            };
+            auto read_v = [&](int st, int dt) {
+                const s16x4 v0 = lds_read_transposed(v_at + 16 * st * VP + 64 * dt), v1 = lds_read_transposed(v_at + (16 * st + 8) * VP + 64 * dt);
+                return __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+            };
+#pragma unroll
+            for (int dt = 0; dt < DP / 32; ++dt) vf[dt] = read_v(0, dt);
+            __builtin_amdgcn_sched_barrier(0);
+            weigh(0, pf, rest);
+#pragma unroll
+            for (int st = 0; st < 2 * KT; ++st) {
+                if (st + 1 < 2 * KT) weigh(st + 1, next, next_rest);
 #pragma unroll
                 for (int dt = 0; dt < DP / 32; ++dt) {
-                    const s16x4 v0 = lds_read_transposed(v_at + 16 * st * VP + 64 * dt), v1 = lds_read_transposed(v_at + (16 * st + 8) * VP + 64 * dt);
-                    const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-                    o[dt] = mfma32(vf, pf, o[dt]);
-                    if constexpr (TERMS > 1) o[dt] = mfma32(vf, rest, o[dt]);
+                    o[dt] = mfma32(vf[dt], pf, o[dt]);
+                    if constexpr (TERMS > 1) o[dt] = mfma32(vf[dt], rest, o[dt]);
+                    if (st + 1 < 2 * KT) vf[dt] = read_v(st + 1, dt);
                 }
+                pf = next;
+                rest = next_rest;
             }
-        }
-        if (kt + KEYS < end_key) store(kt + KEYS, lds + (turn ^ 1) * many_buffer(DP));
+            in_turn<2 * KT * (DP / 32) * TERMS, 2 / TERMS, 0, 20 / (DP / 32), 8 / (DP / 32)>();
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if (over) *again = 1;
+        __syncthreads();
+        if (!*again) break;                    // (never twice: m is the largest score then)
+        known = true;
+        m = -__builtin_inff();
+        sweep([&](int kt, const unsigned char* buf) {
+            score(kt, buf);
+            m = fmaxf(m, top);
+        });
+        __syncthreads();
+        if (tid == 0) *again = 0;
     }
     l += __shfl_xor(l, 32);
     if (row >= row_end) return;
-    const int64_t part_row = ((int64_t)h * p.rows + row) * (p.prefix_splits + p.own_splits) + slot;
+    const int64_t part = ((int64_t)h * p.rows + row) * (p.prefix_splits + p.own_splits) + slot;
 #pragma unroll
     for (int dt = 0; dt < DP / 32; ++dt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int d = 32 * dt + 8 * i + 4 * half;
-            if (d < p.D) *(f32x4*)(p.part_o + part_row * p.D + d) = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+            if (d < p.D) *(f32x4*)(p.part_o + part * p.D + d) = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
         }
-    if (half == 0) {
-        p.part_ml[part_row * 2] = m;
-        p.part_ml[part_row * 2 + 1] = l;
-    }
+    if (half == 0) *(f32x2*)(p.part_ml + part * 2) = f32x2{m, l};
 }
 
-// MT > 0: 16 * MT rows of the prefix per workgroup; 0 and -1: 128, with P in one term or two.  OWN: 16 * OWN rows of a sequence.  WHOLE: D is DP.
-template <class T, int DP, int MT, int OWN, bool WHOLE>
-__global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(const AttendParams p) {
+// MT > 0: 16 * MT rows of the prefix per workgroup; 0: 32 for each of its NW waves, with P in TERMS terms.  OWN: 16 * OWN rows of a sequence.  WHOLE: D is DP.
+template <class T, int DP, int MT, int NW, int TERMS, int OWN, bool WHOLE>
+__global__ void __launch_bounds__(64 * NW, DP > 128 ? NW / 4 : 2) attend_kernel(const AttendParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     const bool own = (int)blockIdx.x >= p.prefix_blocks;
     if (!own) {
@@ -584,18 +620,18 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) attend_kernel(const Att
         const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
         if (h >= p.Hk) return;
         const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
-        if constexpr (MT <= 0) attend_many<T, DP, 1 - MT, WHOLE>(p, p.prefix_pages, h, first, end, tile * 128, p.rows, split, lds);
-        else attend_few<T, DP, MT, WHOLE>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, 4, lds);
+        if constexpr (MT == 0) attend_many<T, DP, TERMS, NW, WHOLE>(p, p.prefix_pages, h, first, end, tile * 32 * NW, p.rows, split, lds);
+        else attend_few<T, DP, MT, NW, WHOLE>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, NW, lds);
         return;
     }
     int i = (int)blockIdx.x - p.prefix_blocks;
-    if (p.own_share == 1) i = i * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (p.own_share == 1) i = i * NW + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int tile = i % p.own_tiles, rest = i / p.own_tiles, split = rest % p.own_splits, bh = rest / p.own_splits, h = bh % p.Hk, b = bh / p.Hk;
     if (b >= p.B) return;
     const Sequence seq = sequence_of(p, b);
     const int steps = (seq.len + p.own_step - 1) / p.own_step, per = (steps + p.own_splits - 1) / p.own_splits, nG = p.n * p.G;
     const int first = min(split * per * p.own_step, seq.len), end = min(first + per * p.own_step, seq.len);
-    attend_few<T, DP, OWN, WHOLE>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq, p.prefix_splits + split,
+    attend_few<T, DP, OWN, NW, WHOLE>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq, p.prefix_splits + split,
                                   p.own_share, lds);
 }
 

@@ -24,20 +24,26 @@ bool allow_lds(const void* kfn, int bytes, std::atomic<unsigned>& done_mask) {
     return true;
 }
 
-template <class T, int DP, int MT, int OWN, bool WHOLE>
+template <class T, int DP, int MT, int NW, int TERMS, int OWN, bool WHOLE>
 int launch_attend_t(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
     static std::atomic<unsigned> done{0};
-    constexpr int lds = MT <= 0 ? std::max(2 * many_buffer(DP), few_lds(DP)) : few_lds(DP);
-    auto kfn = attend_kernel<T, DP, MT, OWN, WHOLE>;
+    constexpr int lds = MT == 0 ? std::max(2 * many_buffer(DP) + 16, few_lds(DP, NW)) : few_lds(DP, NW);
+    auto kfn = attend_kernel<T, DP, MT, NW, TERMS, OWN, WHOLE>;
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
-    return launch(kfn, dim3((unsigned)(a.prefix_blocks + a.own_blocks)), 256, lds, stream, p);
+    return launch(kfn, dim3((unsigned)(a.prefix_blocks + a.own_blocks)), 64 * NW, lds, stream, p);
+}
+template <class T, int DP, int NW, bool WHOLE>
+int launch_attend_many(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+    if (p.out_type == VLUT_TYPE_F32) return a.own_mt == 1 ? launch_attend_t<T, DP, 0, NW, 2, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 0, NW, 2, 2, WHOLE>(a, p, stream);
+    return a.own_mt == 1 ? launch_attend_t<T, DP, 0, NW, 1, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 0, NW, 1, 2, WHOLE>(a, p, stream);
 }
 template <class T, int DP, bool WHOLE>
 int launch_attend_w(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
-    if (a.MT == 1) return launch_attend_t<T, DP, 1, 1, WHOLE>(a, p, stream);
-    if (a.MT == 2) return a.own_mt == 1 ? launch_attend_t<T, DP, 2, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 2, 2, WHOLE>(a, p, stream);
-    if (p.out_type == VLUT_TYPE_F32) return a.own_mt == 1 ? launch_attend_t<T, DP, -1, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, -1, 2, WHOLE>(a, p, stream);
-    return a.own_mt == 1 ? launch_attend_t<T, DP, 0, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 0, 2, WHOLE>(a, p, stream);
+    if (a.MT == 1) return launch_attend_t<T, DP, 1, 4, 0, 1, WHOLE>(a, p, stream);
+    if (a.MT == 2) return a.own_mt == 1 ? launch_attend_t<T, DP, 2, 4, 0, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 2, 4, 0, 2, WHOLE>(a, p, stream);
+    if constexpr (DP <= 128)
+        if (a.waves == 8) return launch_attend_many<T, DP, 8, WHOLE>(a, p, stream);
+    return launch_attend_many<T, DP, 4, WHOLE>(a, p, stream);
 }
 template <class T, int DP>
 int launch_attend_d(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {

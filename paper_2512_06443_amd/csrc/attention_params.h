@@ -29,20 +29,19 @@ struct AttendParams {
     int prefix_tiles, own_tiles;       // tiles of rows
     int prefix_blocks, blocks_per_xcd;
     int rows;                          // B n G
-    int page_groups;                   // the keys of a wave's load share their page
     int direct;                        // a single part: workgroups store the result
 };
 
 constexpr int kFewKeys = 32;           // keys of a wave's step where rows are few
 __host__ __device__ constexpr int few_pitch(int DP) { return DP * 2 + 32; }
-__host__ __device__ constexpr int few_lds(int DP) { return 4 * kFewKeys * few_pitch(DP); }
+__host__ __device__ constexpr int few_lds(int DP, int waves) { return waves * kFewKeys * few_pitch(DP); }
 __host__ __device__ constexpr int many_keys(int DP) { return DP > 128 ? 32 : 64; }
 __host__ __device__ constexpr int many_k_pitch(int DP) { return DP * 2 + 16; }
 __host__ __device__ constexpr int many_v_pitch(int DP) { return DP * 2 + 64; }
 __host__ __device__ constexpr int many_buffer(int DP) { return many_keys(DP) * (many_k_pitch(DP) + many_v_pitch(DP)); }
 
 struct AttendPlan {
-    int MT, own_mt, DP;                // tile: 16 * MT rows, 128 for MT = 0
+    int MT, waves, own_mt, DP;         // tile: 16 * MT rows, 32 for each of the waves for MT = 0
     int own_share, own_step;
     int prefix_tiles, prefix_splits, prefix_chunk, prefix_blocks, blocks_per_xcd, own_tiles, own_splits, own_blocks, direct;
     int64_t rows;

@@ -143,7 +143,7 @@ def test_against_64_bits(B, name, dtype):
 
 def test_every_tile_is_among_the_cases(B):
     rows = {B.query_shared_prefix_attention(c["B"], c["n"], c["Hq"], c["Hk"], c["D"], c["P"], max(c["lens"]))[0] for c in CASES.values()}
-    assert rows == {16, 32, 128}
+    assert rows == {16, 32, 128, 256}
 
 
 def test_scale_and_large_scores(B):
