@@ -150,7 +150,7 @@ constexpr int kUnits = 256;            // compute units that a launch is to fill
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// grouped: the keys of a wave's load share their page, as the kernel for many rows wants it.
+// grouped: 16 keys share their page, as the kernel for many rows wants it.
 int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t P, int64_t max_own, bool grouped, AttendPlan* out) {
     if (B < 1 || n < 1 || Hk < 1 || Hq < 1 || Hq >= (1 << 16) || Hq % Hk || B >= kMaxDim || n >= kMaxDim) return VLUT_ERR_SHAPE;
     if (P < 0 || max_own < 0 || P >= ((int64_t)1 << 30) || max_own >= ((int64_t)1 << 30) || D < 1) return VLUT_ERR_SHAPE;
@@ -158,6 +158,7 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     const int64_t G = Hq / Hk, own_rows = n * G, rows = B * own_rows;
     if (rows * Hk >= ((int64_t)1 << 30)) return VLUT_ERR_SHAPE;
     AttendPlan a{};
+    a.grouped = grouped;
     a.rows = rows;
     a.DP = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
     a.own_mt = own_rows <= 16 ? 1 : 2;
@@ -165,32 +166,30 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     a.waves = a.MT == 0 && a.DP <= 128 && rows > 128 ? 8 : 4;
     a.own_tiles = (int)ceil_div(own_rows, 16 * a.own_mt);
     const int64_t own_units = B * Hk * a.own_tiles;
-    a.own_share = own_units >= 4 * 2 * kUnits ? 1 : a.waves;
+    const int64_t slots = kUnits * few_waves(a.DP, a.MT == 0 ? a.own_mt : a.MT);            // workgroups of four waves that run at once
+    a.own_share = own_units >= 4 * slots ? 1 : 4;
     a.own_step = a.own_share * kFewKeys;
-    const int64_t own_steps = ceil_div(max_own, a.own_step), own_all = own_units * own_steps;
+    const int64_t own_steps = ceil_div(max_own, a.own_step), own_all = ceil_div(own_units * own_steps, 4 / a.own_share);
     int64_t per_own;
     if (a.MT > 0) {
         a.prefix_tiles = (int)ceil_div(rows, 16 * a.MT);
-        const int64_t steps = ceil_div(P, 128), units = Hk * a.prefix_tiles * steps + own_all / (a.waves / a.own_share);
-        const int64_t per = std::max<int64_t>(1, ceil_div(units, 2 * kUnits));
+        const int64_t units = Hk * a.prefix_tiles * ceil_div(P, 128) + own_all, per = std::max<int64_t>(1, ceil_div(units, slots));
         a.prefix_chunk = (int)(128 * per);
         per_own = per;
     } else {
         a.prefix_tiles = (int)ceil_div(rows, 32 * a.waves);
         const int64_t keys = many_keys(a.DP), splits = std::min(std::max<int64_t>(1, 8 / a.waves * kUnits / (Hk * a.prefix_tiles)), ceil_div(P, 256));
         a.prefix_chunk = (int)(ceil_div(ceil_div(P, splits), keys) * keys);
-        per_own = std::max<int64_t>(1, ceil_div(own_all / (a.waves / a.own_share), 16 / a.waves * kUnits));
+        per_own = std::max<int64_t>(1, ceil_div(own_all, slots));
     }
     if (a.own_share == 1) per_own = std::max<int64_t>(per_own, own_steps);
     a.prefix_splits = P > 0 ? (int)ceil_div(P, a.prefix_chunk) : 0;
     a.own_splits = (int)ceil_div(own_steps, per_own);
     if (a.prefix_splits + a.own_splits == 0) a.own_splits = 1;      // nothing is seen: a workgroup stores that
-    const int64_t prefix_blocks = Hk * a.prefix_tiles * a.prefix_splits;
-    a.blocks_per_xcd = (int)ceil_div(prefix_blocks, 8);
-    const int64_t padded = 8 * (int64_t)a.blocks_per_xcd, own_blocks = ceil_div(own_units * a.own_splits, a.waves / a.own_share);
-    if (padded + own_blocks >= ((int64_t)1 << 31)) return VLUT_ERR_SHAPE;
-    a.prefix_blocks = (int)padded;
-    a.own_blocks = (int)own_blocks;
+    const int64_t ranges = B * Hk * a.own_splits, prefix_blocks = Hk * a.prefix_tiles * a.prefix_splits;
+    if (ranges * a.own_tiles + prefix_blocks + 64 >= ((int64_t)1 << 30)) return VLUT_ERR_SHAPE;
+    a.prefix_per_xcd = (int)ceil_div(prefix_blocks, 8);
+    a.own_per_xcd = (int)ceil_div(ceil_div(ranges, 8) * a.own_tiles, 4 / a.own_share);
     a.direct = a.MT > 0 && a.prefix_splits + a.own_splits == 1;
     if (!a.direct) {
         const size_t parts = (size_t)(a.prefix_splits + a.own_splits) * (size_t)Hk * (size_t)rows;
@@ -201,11 +200,11 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     return VLUT_OK;
 }
 
-// The keys of a wave's load (eight at most) share their page, and strides and the offsets inside a page fit 31 bits, in bytes.
+// Sixteen keys share their page, and strides and the offsets inside a page fit 31 bits, in bytes.
 bool grouped_keys(const vlut_cache& c) {
-    bool ok = c.page_size >= 8;
+    bool ok = c.page_size >= 16;
     for (int64_t s : {c.k_page_stride, c.v_page_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30);
-    for (int64_t s : {c.k_token_stride, c.v_token_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) / std::max<int64_t>(c.page_size, 8);
+    for (int64_t s : {c.k_token_stride, c.v_token_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) / std::max<int64_t>(c.page_size, 16);
     return ok;
 }
 
@@ -280,7 +279,7 @@ int vlut_query_shared_prefix_attention(int64_t B, int64_t n, int64_t Hq, int64_t
     out4[0] = a.MT > 0 ? 16 * a.MT : 32 * a.waves;
     out4[1] = a.prefix_splits;
     out4[2] = a.own_splits;
-    out4[3] = a.prefix_blocks + a.own_blocks;
+    out4[3] = 8 * (a.prefix_per_xcd + a.own_per_xcd);
     return VLUT_OK;
 }
 
@@ -351,8 +350,8 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
     p.own_step = a.own_step;
     p.prefix_tiles = a.prefix_tiles;
     p.own_tiles = a.own_tiles;
-    p.prefix_blocks = a.prefix_blocks;
-    p.blocks_per_xcd = a.blocks_per_xcd;
+    p.prefix_per_xcd = a.prefix_per_xcd;
+    p.own_per_xcd = a.own_per_xcd;
     p.rows = (int)a.rows;
     p.direct = a.direct;
     return cache->type == VLUT_TYPE_BF16 ? launch_bf16(a, p, (hipStream_t)stream) : launch_f16(a, p, (hipStream_t)stream);

@@ -119,8 +119,8 @@ __device__ __forceinline__ void arrived_scalar(int& x) {
 
 // One range of keys for up to 16 * MT query rows, few enough that memory is what bounds it.  A wave takes 32 keys a step (K straight to registers, V
 // through a piece of LDS of its own, no barrier); the next 32 are on their way while the present ones are worked on.  `share` waves
-// have the range in turn: all NW, which join at the end through LDS, or 1 where ranges are short and many.
-template <class T, int DP, int MT, int NW, bool WHOLE>
+// have the range in turn: 4, which join at the end through LDS, or 1 where ranges are short and many.
+template <class T, int DP, int MT, bool WHOLE, bool GROUPED>
 __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, bool own, const Sequence& seq, int slot,
                            int share, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
@@ -163,28 +163,57 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
     const int mask = (1 << p.page_log) - 1, last = end_key - 1;
     const int v_chunk = lane % CH, v_key = lane / CH;
     i32x4 kr[2][KS], vr[VI];
-    // (keys past the range read its last one: its scores are masked, its V is zeroed)
-    auto load_k = [&](int kt, int page) {
+    // Pages of 32 keys, and their rows.  GROUPED: every 16 keys share a page, whose number a wave has two of (Pages), and addresses are worked out
+    // once per wave; else a lane looks up one key's.  Keys past the range read its last one or another row of that one's page: scores are
+    // masked, V is zeroed.
+    struct Pages {
+        int id[GROUPED ? 2 : 1];
+    };
+    const unsigned k_lane = GROUPED ? 2u * (unsigned)l16 * (unsigned)p.k_token : 0u;
+    const unsigned v_lane = GROUPED ? 2u * ((unsigned)v_key * (unsigned)p.v_token + (unsigned)chunk_at<WHOLE>(v_chunk, p.D)) : 0u;
+    auto look_up = [&](int kt) {
+        Pages g;
+        if constexpr (GROUPED) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) g.id[t] = pages[min(kt + 16 * t, last & ~15) >> p.page_log];
+        } else g.id[0] = pages[min(kt + (lane & 31), last) >> p.page_log];
+        return g;
+    };
+    // the first row of 16 keys that share a page
+    auto rows_of = [&](const T* of, int64_t page_stride, int64_t token_stride, int kt, int t, const Pages& g) {
+        const unsigned named = (unsigned)__builtin_amdgcn_readfirstlane(g.id[GROUPED ? t : 0]), id = is_page(p, (int)named) ? named : 0u;
+        return (const unsigned char*)of + ((uint64_t)id * 2u * (unsigned)page_stride + (unsigned)(min(kt + 16 * t, last & ~15) & mask) * 2u * (unsigned)token_stride);
+    };
+    auto load_k = [&](int kt, const Pages& g) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int key = min(kt + 16 * t + l16, last), id = __shfl(page, 16 * t + l16);
-            const T* src = kh + (is_page(p, id) ? id : 0) * p.k_page + (key & mask) * p.k_token;
+            if constexpr (GROUPED) {
+                const unsigned char* const src = rows_of(kh, p.k_page, p.k_token, kt, t, g);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) kr[t][ks] = *(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(4 * ks + grp, p.D));
+                for (int ks = 0; ks < KS; ++ks) kr[t][ks] = *(const dword_aligned_i32x4*)(src + (k_lane + 2u * (unsigned)chunk_at<WHOLE>(4 * ks + grp, p.D)));
+            } else {
+                const int key = min(kt + 16 * t + l16, last), id = __shfl(g.id[0], 16 * t + l16);
+                const T* src = kh + (is_page(p, id) ? id : 0) * p.k_page + (key & mask) * p.k_token;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) kr[t][ks] = *(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(4 * ks + grp, p.D));
+            }
         }
     };
-    auto load_v = [&](int kt, int page) {
+    auto load_v = [&](int kt, const Pages& g) {
 #pragma unroll
         for (int i = 0; i < VI; ++i) {
-            const int k_in = PER * i + v_key, key = min(kt + k_in, last), id = __shfl(page, k_in);
-            const T* src = vh + (is_page(p, id) ? id : 0) * p.v_page + (key & mask) * p.v_token;
-            vr[i] = *(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(v_chunk, p.D));
+            if constexpr (GROUPED)
+                vr[i] = *(const dword_aligned_i32x4*)(rows_of(vh, p.v_page, p.v_token, kt, PER * i / 16, g) + (unsigned)(PER * i % 16) * 2u * (unsigned)p.v_token + v_lane);
+            else {
+                const int k_in = PER * i + v_key, key = min(kt + k_in, last), id = __shfl(g.id[0], k_in);
+                const T* src = vh + (is_page(p, id) ? id : 0) * p.v_page + (key & mask) * p.v_token;
+                vr[i] = *(const dword_aligned_i32x4*)(src + chunk_at<WHOLE>(v_chunk, p.D));
+            }
         }
     };
-    auto look_up = [&](int kt) { return pages[min(kt + (lane & 31), last) >> p.page_log]; };
 
     int kt = first_key + (share > 1 ? kFewKeys * wave : 0);
-    int page = 0, next_page = 0;
+    Pages page, next_page;
     if (kt < end_key) {
         page = look_up(kt);
         next_page = look_up(kt + stride);
@@ -200,29 +229,36 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
         // V to LDS, zeros for keys past the range
         unsigned odd = 0;
 #pragma unroll
-        for (int i = 0; i < VI; ++i) {
-            i32x4 x = chunk_moved<WHOLE>(vr[i], v_chunk, p.D);
-            if (some_masked) {
-                if (kt + PER * i + v_key >= end_key) x = i32x4{0, 0, 0, 0};
-                constexpr unsigned E = Number<T>::kExponents;
+        for (int i = 0; i < VI; ++i) vr[i] = chunk_moved<WHOLE>(vr[i], v_chunk, p.D);
+        if (some_masked) {
+            constexpr unsigned E = Number<T>::kExponents;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) odd |= ((x[w] & (E & 0xffff0000u)) == (E & 0xffff0000u)) | ((x[w] & (E & 0xffffu)) == (E & 0xffffu));
+            for (int i = 0; i < VI; ++i) {
+                if (kt + PER * i + v_key >= end_key) vr[i] = i32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) odd |= ((vr[i][w] & (E & 0xffff0000u)) == (E & 0xffff0000u)) | ((vr[i][w] & (E & 0xffffu)) == (E & 0xffffu));
             }
-            *(i32x4*)(mine + (PER * i + v_key) * PITCH + 16 * v_chunk) = x;
         }
+#pragma unroll
+        for (int i = 0; i < VI; ++i) *(i32x4*)(mine + (PER * i + v_key) * PITCH + 16 * v_chunk) = vr[i];
         // What comes next, in the order in which it is waited for: the page after the next, V, K.  Also behind the last step, from its last key: in a
         // branch, registers that are loaded on one way alone would be copied, and waited for, where the ways meet.
-        const int page_after = look_up(kt + 2 * stride);
+        const Pages page_after = look_up(kt + 2 * stride);
         load_v(kt + stride, next_page);
         x8 kf[2][KS];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) kf[t][ks] = __builtin_bit_cast(x8, chunk_moved<WHOLE>(kr[t][ks], 4 * ks + grp, p.D));
-        if (__any(!is_page(p, page))) {             // a number that is no page: not read, and whoever sees its keys gets NaN
+        // A number that is no page: not read, and whoever sees its keys gets NaN
+        const auto no_page = [&](int t) {
+            if constexpr (GROUPED) return !is_page(p, __builtin_amdgcn_readfirstlane(page.id[t]));
+            else return !is_page(p, __shfl(page.id[0], 16 * t + l16));
+        };
+        if (GROUPED ? no_page(0) || no_page(1) : __any(!is_page(p, page.id[0]))) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-                if (!is_page(p, __shfl(page, 16 * t + l16))) {
+                if (no_page(t)) {
                     constexpr int N = (int)Number<T>::kNan;
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) kf[t][ks] = __builtin_bit_cast(x8, i32x4{N, N, N, N});
@@ -244,11 +280,12 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             if (some_masked) {
+                const int seen = limit[mt] - kt - 4 * grp;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (kt + 16 * t + 4 * grp + i >= limit[mt]) s[mt][t][i] = -__builtin_inff();
+                        if (16 * t + i >= seen) s[mt][t][i] = -__builtin_inff();
             }
             float top = fmaxf(fmaxf(fmaxf(s[mt][0].x, s[mt][0].y), fmaxf(s[mt][0].z, s[mt][0].w)), fmaxf(fmaxf(s[mt][1].x, s[mt][1].y), fmaxf(s[mt][1].z, s[mt][1].w)));
             top = fmaxf(top, __shfl_xor(top, 16));
@@ -359,7 +396,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
     // The waves' parts: 16 rows at a time through LDS, thread t joins features of row t / 16.
     constexpr int OP = DP + 4, F4 = DP / 64;                       // floats per row; vectors of four per thread
     float* const all_o = (float*)lds;                              // [wave][16][OP]
-    float* const all_ml = all_o + NW * 16 * OP;                    // [wave][16][2]
+    float* const all_ml = all_o + 4 * 16 * OP;                     // [wave][16][2]
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         __syncthreads();
@@ -371,13 +408,13 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
         }
         __syncthreads();
         const int r = (int)threadIdx.x >> 4, part = (int)threadIdx.x & 15, row = row0 + 16 * mt + r;
-        if (r < 16 && row < row_end) {
-            float top = -__builtin_inff(), total = 0.0f, f[NW];
+        if (row < row_end) {
+            float top = -__builtin_inff(), total = 0.0f, f[4];
 #pragma unroll
-            for (int w = 0; w < NW; ++w) top = fmaxf(top, all_ml[(w * 16 + r) * 2]);
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, all_ml[(w * 16 + r) * 2]);
             const float shift = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
-            for (int w = 0; w < NW; ++w) {
+            for (int w = 0; w < 4; ++w) {
                 f[w] = exp2_fast(all_ml[(w * 16 + r) * 2] - shift);
                 total += f[w] * all_ml[(w * 16 + r) * 2 + 1];
             }
@@ -387,7 +424,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                 const int d = (part + 16 * v) * 4;
                 f32x4 x = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int w = 0; w < NW; ++w) x += *(f32x4*)(all_o + (w * 16 + r) * OP + d) * f[w];
+                for (int w = 0; w < 4; ++w) x += *(f32x4*)(all_o + (w * 16 + r) * OP + d) * f[w];
                 put(to, d, x);
             }
         }
@@ -522,11 +559,12 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         if (kt + KEYS > end_key) {
             int left = end_key - kt;
             arrived_scalar(left);              // (or its comparisons are made in every step, ahead of the branch)
+            const int seen = left - 4 * half;
 #pragma unroll
             for (int t = 0; t < KT; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (32 * t + (i & 3) + 8 * (i >> 2) + 4 * half >= left) s[t][i] = -__builtin_inff();
+                    if (32 * t + (i & 3) + 8 * (i >> 2) >= seen) s[t][i] = -__builtin_inff();
         }
         top = s[0][0];
 #pragma unroll
@@ -549,7 +587,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
             score(kt, buf);
             m = kt == first_key && !known ? top : m;
             const float shift = m == -__builtin_inff() ? 0.0f : m;
-            over = over || top > m + kSlack;
+            over |= top > m + kSlack;          // (no branch here)
             // Sixteen keys at a time; the weights and V of the next are made and read while the matrix cores are on these.
             x8 vf[DP / 32], pf, rest, next, next_rest;
             auto weigh = [&](int st, x8& w, x8& w_rest) {
@@ -597,42 +635,61 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         if (tid == 0) *again = 0;
     }
     l += __shfl_xor(l, 32);
-    if (row >= row_end) return;
-    const int64_t part = ((int64_t)h * p.rows + row) * (p.prefix_splits + p.own_splits) + slot;
+    // O turned through the wave's piece of LDS (nobody reads the buffers any more), 32 features at a time, so that a store has whole lines.
+    constexpr int TP = 36;                     // floats from row to row
+    float* const turned = (float*)lds + wave * 32 * TP;
+    const int64_t stride = p.prefix_splits + p.own_splits, part0 = ((int64_t)h * p.rows + row0 + 32 * wave) * stride + slot;
+    const int rows_here = row_end - row0 - 32 * wave;
 #pragma unroll
-    for (int dt = 0; dt < DP / 32; ++dt)
+    for (int dt = 0; dt < DP / 32; ++dt) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *(f32x4*)(turned + l32 * TP + 8 * i + 4 * half) = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int d = 32 * dt + 8 * i + 4 * half;
-            if (d < p.D) *(f32x4*)(p.part_o + part * p.D + d) = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+            const int r = 8 * i + (lane >> 3), d = 32 * dt + 4 * (lane & 7);
+            const f32x4 x = *(const f32x4*)(turned + r * TP + 4 * (lane & 7));
+            if (r < rows_here && d < p.D) *(f32x4*)(p.part_o + (part0 + r * stride) * p.D + d) = x;
         }
-    if (half == 0) *(f32x2*)(p.part_ml + part * 2) = f32x2{m, l};
+        __builtin_amdgcn_wave_barrier();
+    }
+    if (half == 0 && row < row_end) *(f32x2*)(p.part_ml + (part0 + l32 * stride) * 2) = f32x2{m, l};
 }
 
-// MT > 0: 16 * MT rows of the prefix per workgroup; 0: 32 for each of its NW waves, with P in TERMS terms.  OWN: 16 * OWN rows of a sequence.  WHOLE: D is DP.
-template <class T, int DP, int MT, int NW, int TERMS, int OWN, bool WHOLE>
-__global__ void __launch_bounds__(64 * NW, DP > 128 ? NW / 4 : 2) attend_kernel(const AttendParams p) {
+// Few rows: ranges of the prefix for 16 * MT rows, and of the sequences' own tokens for 16 * OWN.  WHOLE: D is DP.  GROUPED: 16 keys share a page.
+// Workgroups go to the 8 XCDs in turn; those of one range, which differ in their rows alone, are given to one XCD (one L2).
+template <class T, int DP, int MT, int OWN, bool WHOLE, bool GROUPED>
+__global__ void __launch_bounds__(256, few_waves(DP, MT)) attend_few_kernel(const AttendParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
-    const bool own = (int)blockIdx.x >= p.prefix_blocks;
-    if (!own) {
-        // Workgroups go to the 8 XCDs in turn; those of one range of the prefix, which differ in their rows alone, are given to one XCD (one L2).
-        const int i = ((int)blockIdx.x & 7) * p.blocks_per_xcd + ((int)blockIdx.x >> 3);
+    const int xcd = (int)blockIdx.x & 7, place = (int)blockIdx.x >> 3;
+    if (place < p.prefix_per_xcd) {
+        const int i = xcd * p.prefix_per_xcd + place;
         const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
         if (h >= p.Hk) return;
         const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
-        if constexpr (MT == 0) attend_many<T, DP, TERMS, NW, WHOLE>(p, p.prefix_pages, h, first, end, tile * 32 * NW, p.rows, split, lds);
-        else attend_few<T, DP, MT, NW, WHOLE>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, NW, lds);
+        attend_few<T, DP, MT, WHOLE, GROUPED>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, 4, lds);
         return;
     }
-    int i = (int)blockIdx.x - p.prefix_blocks;
-    if (p.own_share == 1) i = i * NW + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int tile = i % p.own_tiles, rest = i / p.own_tiles, split = rest % p.own_splits, bh = rest / p.own_splits, h = bh % p.Hk, b = bh / p.Hk;
+    // (sequences differ in length, so that their ranges go round; the tiles of a range stay together)
+    const int own_place = (place - p.prefix_per_xcd) * (p.own_share == 1 ? 4 : 1) + (p.own_share == 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0);
+    const int tile = own_place % p.own_tiles, rest = own_place / p.own_tiles * 8 + xcd, split = rest % p.own_splits, bh = rest / p.own_splits, h = bh % p.Hk, b = bh / p.Hk;
     if (b >= p.B) return;
     const Sequence seq = sequence_of(p, b);
     const int steps = (seq.len + p.own_step - 1) / p.own_step, per = (steps + p.own_splits - 1) / p.own_splits, nG = p.n * p.G;
     const int first = min(split * per * p.own_step, seq.len), end = min(first + per * p.own_step, seq.len);
-    attend_few<T, DP, OWN, NW, WHOLE>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq, p.prefix_splits + split,
-                                  p.own_share, lds);
+    attend_few<T, DP, OWN, WHOLE, GROUPED>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq,
+                                           p.prefix_splits + split, p.own_share, lds);
+}
+
+// Many rows: ranges of the prefix for 32 rows of each of NW waves, with P in TERMS terms.  XCDs as above.
+template <class T, int DP, int NW, int TERMS, bool WHOLE>
+__global__ void __launch_bounds__(64 * NW, DP > 128 ? NW / 4 : 2) attend_many_kernel(const AttendParams p) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int i = ((int)blockIdx.x & 7) * p.prefix_per_xcd + ((int)blockIdx.x >> 3);
+    const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
+    if (h >= p.Hk) return;
+    const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
+    attend_many<T, DP, TERMS, NW, WHOLE>(p, p.prefix_pages, h, first, end, tile * 32 * NW, p.rows, split, lds);
 }
 
 // The parts of every row joined.  DP / 4 threads have four features each of a row's part, 2^lanes_log such groups share a row's parts, and

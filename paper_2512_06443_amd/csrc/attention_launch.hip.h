@@ -24,26 +24,43 @@ bool allow_lds(const void* kfn, int bytes, std::atomic<unsigned>& done_mask) {
     return true;
 }
 
-template <class T, int DP, int MT, int NW, int TERMS, int OWN, bool WHOLE>
-int launch_attend_t(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+template <class T, int DP, int MT, int OWN, bool WHOLE, bool GROUPED>
+int launch_few_t(const AttendParams& p, hipStream_t stream) {
     static std::atomic<unsigned> done{0};
-    constexpr int lds = MT == 0 ? std::max(2 * many_buffer(DP) + 16, few_lds(DP, NW)) : few_lds(DP, NW);
-    auto kfn = attend_kernel<T, DP, MT, NW, TERMS, OWN, WHOLE>;
+    constexpr int lds = few_lds(DP);
+    auto kfn = attend_few_kernel<T, DP, MT, OWN, WHOLE, GROUPED>;
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
-    return launch(kfn, dim3((unsigned)(a.prefix_blocks + a.own_blocks)), 64 * NW, lds, stream, p);
+    return launch(kfn, dim3(8u * (unsigned)(p.prefix_per_xcd + p.own_per_xcd)), 256, lds, stream, p);
+}
+template <class T, int DP, int MT, int OWN, bool WHOLE>
+int launch_few(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+    return a.grouped ? launch_few_t<T, DP, MT, OWN, WHOLE, true>(p, stream) : launch_few_t<T, DP, MT, OWN, false, false>(p, stream);
+}
+template <class T, int DP, int NW, int TERMS, bool WHOLE>
+int launch_many(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+    static std::atomic<unsigned> done{0};
+    constexpr int lds = 2 * many_buffer(DP) + 16;
+    auto kfn = attend_many_kernel<T, DP, NW, TERMS, WHOLE>;
+    if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
+    return launch(kfn, dim3(8u * (unsigned)a.prefix_per_xcd), 64 * NW, lds, stream, p);
 }
 template <class T, int DP, int NW, bool WHOLE>
-int launch_attend_many(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
-    if (p.out_type == VLUT_TYPE_F32) return a.own_mt == 1 ? launch_attend_t<T, DP, 0, NW, 2, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 0, NW, 2, 2, WHOLE>(a, p, stream);
-    return a.own_mt == 1 ? launch_attend_t<T, DP, 0, NW, 1, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 0, NW, 1, 2, WHOLE>(a, p, stream);
+int launch_many_terms(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+    return p.out_type == VLUT_TYPE_F32 ? launch_many<T, DP, NW, 2, WHOLE>(a, p, stream) : launch_many<T, DP, NW, 1, WHOLE>(a, p, stream);
 }
 template <class T, int DP, bool WHOLE>
 int launch_attend_w(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
-    if (a.MT == 1) return launch_attend_t<T, DP, 1, 4, 0, 1, WHOLE>(a, p, stream);
-    if (a.MT == 2) return a.own_mt == 1 ? launch_attend_t<T, DP, 2, 4, 0, 1, WHOLE>(a, p, stream) : launch_attend_t<T, DP, 2, 4, 0, 2, WHOLE>(a, p, stream);
+    if (a.MT == 1) return launch_few<T, DP, 1, 1, WHOLE>(a, p, stream);
+    if (a.MT == 2) return a.own_mt == 1 ? launch_few<T, DP, 2, 1, WHOLE>(a, p, stream) : launch_few<T, DP, 2, 2, WHOLE>(a, p, stream);
+    if (a.own_per_xcd > 0) {                   // the sequences' own tokens alone
+        AttendParams own = p;
+        own.prefix_per_xcd = 0;
+        const int rc = a.own_mt == 1 ? launch_few<T, DP, 1, 1, WHOLE>(a, own, stream) : launch_few<T, DP, 2, 2, WHOLE>(a, own, stream);
+        if (rc != VLUT_OK) return rc;
+    }
     if constexpr (DP <= 128)
-        if (a.waves == 8) return launch_attend_many<T, DP, 8, WHOLE>(a, p, stream);
-    return launch_attend_many<T, DP, 4, WHOLE>(a, p, stream);
+        if (a.waves == 8) return launch_many_terms<T, DP, 8, WHOLE>(a, p, stream);
+    return launch_many_terms<T, DP, 4, WHOLE>(a, p, stream);
 }
 template <class T, int DP>
 int launch_attend_d(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {

@@ -27,23 +27,24 @@ struct AttendParams {
     int prefix_splits, prefix_chunk;   // keys per split
     int own_splits, own_share, own_step;   // waves to a range; its keys are a multiple of own_step but for the end
     int prefix_tiles, own_tiles;       // tiles of rows
-    int prefix_blocks, blocks_per_xcd;
+    int prefix_per_xcd, own_per_xcd;   // workgroups
     int rows;                          // B n G
     int direct;                        // a single part: workgroups store the result
 };
 
 constexpr int kFewKeys = 32;           // keys of a wave's step where rows are few
 __host__ __device__ constexpr int few_pitch(int DP) { return DP * 2 + 32; }
-__host__ __device__ constexpr int few_lds(int DP, int waves) { return waves * kFewKeys * few_pitch(DP); }
+__host__ __device__ constexpr int few_lds(int DP) { return 4 * kFewKeys * few_pitch(DP); }
+__host__ __device__ constexpr int few_waves(int DP, int MT) { return DP > 128 ? 1 : (MT > 1 || DP > 64 ? 2 : 4); }   // of a SIMD
 __host__ __device__ constexpr int many_keys(int DP) { return DP > 128 ? 32 : 64; }
 __host__ __device__ constexpr int many_k_pitch(int DP) { return DP * 2 + 16; }
 __host__ __device__ constexpr int many_v_pitch(int DP) { return DP * 2 + 64; }
 __host__ __device__ constexpr int many_buffer(int DP) { return many_keys(DP) * (many_k_pitch(DP) + many_v_pitch(DP)); }
 
 struct AttendPlan {
-    int MT, waves, own_mt, DP;         // tile: 16 * MT rows, 32 for each of the waves for MT = 0
-    int own_share, own_step;
-    int prefix_tiles, prefix_splits, prefix_chunk, prefix_blocks, blocks_per_xcd, own_tiles, own_splits, own_blocks, direct;
+    int MT, waves, own_mt, DP;         // tile of the prefix: 16 * MT rows; MT = 0: 32 for each of the waves, by a kernel of its own
+    int own_share, own_step, grouped;
+    int prefix_tiles, prefix_splits, prefix_chunk, prefix_per_xcd, own_tiles, own_splits, own_per_xcd, direct;
     int64_t rows;
     size_t o_bytes, ml_bytes;
 };
