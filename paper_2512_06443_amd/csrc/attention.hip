@@ -17,6 +17,8 @@ namespace {
 
 using namespace vlut_attention;
 
+constexpr int kUnits = 256;            // compute units that a launch is to fill
+
 bool type_ok(int type) { return type == VLUT_TYPE_F32 || type == VLUT_TYPE_BF16 || type == VLUT_TYPE_F16; }
 int type_bytes(int type) { return type == VLUT_TYPE_F32 ? 4 : 2; }
 bool power_of_two(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
@@ -96,30 +98,39 @@ int heads_params(HeadsParams& p, const vlut_heads* const (&in)[3], float eps, co
     p.slot_end = 0;
     p.page_log = 0;
     if (N * heads >= ((int64_t)1 << 31)) return VLUT_ERR_SHAPE;
-    p.rows = (unsigned)(N * heads);
+    p.tokens = (unsigned)N;
     return VLUT_OK;
 }
 
 template <class TI, class TO>
-int launch_heads_t(const HeadsParams& p, int vec, dim3 grid, hipStream_t stream) {
-    if (vec == 4) return launch(heads_kernel<TI, TO, 4>, grid, 256, 0, stream, p);
-    if (vec == 2) return launch(heads_kernel<TI, TO, 2>, grid, 256, 0, stream, p);
-    return launch(heads_kernel<TI, TO, 1>, grid, 256, 0, stream, p);
+int launch_heads_t(const HeadsParams& p, int vec, int together, dim3 grid, hipStream_t stream) {
+    if (vec == 4) return together == 4 ? launch(heads_kernel<TI, TO, 4, 4>, grid, 256, 0, stream, p) : launch(heads_kernel<TI, TO, 4, 1>, grid, 256, 0, stream, p);
+    if (vec == 2) return together == 4 ? launch(heads_kernel<TI, TO, 2, 4>, grid, 256, 0, stream, p) : launch(heads_kernel<TI, TO, 2, 1>, grid, 256, 0, stream, p);
+    return launch(heads_kernel<TI, TO, 1, 1>, grid, 256, 0, stream, p);
 }
 template <class TI>
-int launch_heads_out(const HeadsParams& p, int out, int vec, dim3 grid, hipStream_t stream) {
-    if (out == VLUT_TYPE_F32) return launch_heads_t<TI, float>(p, vec, grid, stream);
-    if (out == VLUT_TYPE_BF16) return launch_heads_t<TI, __bf16>(p, vec, grid, stream);
-    return launch_heads_t<TI, _Float16>(p, vec, grid, stream);
+int launch_heads_out(const HeadsParams& p, int out, int vec, int together, dim3 grid, hipStream_t stream) {
+    if (out == VLUT_TYPE_F32) return launch_heads_t<TI, float>(p, vec, together, grid, stream);
+    if (out == VLUT_TYPE_BF16) return launch_heads_t<TI, __bf16>(p, vec, together, grid, stream);
+    return launch_heads_t<TI, _Float16>(p, vec, together, grid, stream);
 }
 int launch_heads(HeadsParams& p, int in, int out, int vec, hipStream_t stream) {
     // lanes of a row: enough for its units (at most 64; a lane has two where pairs are single)
     p.lanes_log = std::min(6, log2_of((p.D + 2 * vec - 1) / (2 * vec)));
     const unsigned per = 256u >> p.lanes_log;
-    const dim3 grid((p.rows + per - 1) / per);
-    if (in == VLUT_TYPE_F32) return launch_heads_out<float>(p, out, vec, grid, stream);
-    if (in == VLUT_TYPE_BF16) return launch_heads_out<__bf16>(p, out, vec, grid, stream);
-    return launch_heads_out<_Float16>(p, out, vec, grid, stream);
+    // Four heads together where that leaves every unit eight workgroups (HEADS_FIGURES)
+    const int together = vec > 1 && (uint64_t)p.tokens * p.heads >= 4ull * 8 * kUnits * per ? 4 : 1;
+    unsigned blocks = 0;
+    for (HeadRows& k : p.kind) {
+        k.groups_of_token = (unsigned)((k.heads + together - 1) / together);
+        k.groups = p.tokens * k.groups_of_token;
+        blocks += (k.groups + per - 1) / per;
+        k.end_block = blocks;
+    }
+    const dim3 grid(blocks);
+    if (in == VLUT_TYPE_F32) return launch_heads_out<float>(p, out, vec, together, grid, stream);
+    if (in == VLUT_TYPE_BF16) return launch_heads_out<__bf16>(p, out, vec, together, grid, stream);
+    return launch_heads_out<_Float16>(p, out, vec, together, grid, stream);
 }
 
 // Rows that go to a tensor of their own.
@@ -146,12 +157,11 @@ int check_cache(const vlut_cache* c) {
 // ---------------------------------------------------------------------------------------------
 // Attention
 // ---------------------------------------------------------------------------------------------
-constexpr int kUnits = 256;            // compute units that a launch is to fill
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// grouped: 16 keys share their page, as the kernel for many rows wants it.
-int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t P, int64_t max_own, bool grouped, AttendPlan* out) {
+// grouped: 16 keys share their page, as the kernel for many rows wants it.  neighbours: a token's heads are neighbours in memory.
+int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t P, int64_t max_own, bool grouped, bool neighbours, AttendPlan* out) {
     if (B < 1 || n < 1 || Hk < 1 || Hq < 1 || Hq >= (1 << 16) || Hq % Hk || B >= kMaxDim || n >= kMaxDim) return VLUT_ERR_SHAPE;
     if (P < 0 || max_own < 0 || P >= ((int64_t)1 << 30) || max_own >= ((int64_t)1 << 30) || D < 1) return VLUT_ERR_SHAPE;
     if (D < 8 || D > VLUT_MAX_HEAD_FEATURES || D % 4) return VLUT_ERR_UNSUPPORTED;
@@ -159,37 +169,47 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     if (rows * Hk >= ((int64_t)1 << 30)) return VLUT_ERR_SHAPE;
     AttendPlan a{};
     a.grouped = grouped;
+    a.own_heads_together = neighbours ? (int)Hk : 1;
     a.rows = rows;
     a.DP = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
     a.own_mt = own_rows <= 16 ? 1 : 2;
-    a.MT = P == 0 ? a.own_mt : (rows <= 16 ? 1 : (rows <= 64 || !grouped ? 2 : 0));
+    // Tiles of 16 or 32 rows whose waves share the keys, or, where the prefix' products are many, a launch of its own with 32 rows a wave.  us, by tiles /
+    // that launch (8 key heads of 128 features, bf16): 128 rows a head, 1500 keys 17.2 / 22.3, 4096 22.2 / 25.9, 9000 29.3 / 31.4, 32768 63 / 47;
+    // 256 rows, 1024 keys 15.9 / 25.1, 4096 29.9 / 31.1; 1024 rows, 500 keys 24 / 31, 1000 32 / 38.
+    a.MT = P == 0 ? a.own_mt : (rows <= 16 ? 1 : (rows <= 64 || !grouped || rows * P * Hk <= 10000000 ? 2 : 0));
     a.waves = a.MT == 0 && a.DP <= 128 && rows > 128 ? 8 : 4;
     a.own_tiles = (int)ceil_div(own_rows, 16 * a.own_mt);
     const int64_t own_units = B * Hk * a.own_tiles;
     const int64_t slots = kUnits * few_waves(a.DP, a.MT == 0 ? a.own_mt : a.MT);            // workgroups of four waves that run at once
-    a.own_share = own_units >= 4 * slots ? 1 : 4;
+    // Waves to a range of own tokens: as many as have a step in it and as leave the workgroups of all ranges room at once.  (24 sequences of 150
+    // to 300 tokens, 32 heads of 100, a range a head: 4 waves 31.7 us, in two rounds; 2 waves, in one, 25.8 us.)
+    a.own_share = 4;
+    while (a.own_share > 1 && (kFewKeys * a.own_share / 2 >= max_own || own_units * a.own_share > 4 * slots)) a.own_share /= 2;
     a.own_step = a.own_share * kFewKeys;
-    const int64_t own_steps = ceil_div(max_own, a.own_step), own_all = ceil_div(own_units * own_steps, 4 / a.own_share);
+    const int64_t own_steps = ceil_div(max_own, a.own_step);
+    const auto own_blocks = [&](int64_t splits) { return ceil_div(ceil_div(B * splits * Hk / a.own_heads_together, 8) * a.own_heads_together * a.own_tiles, 4 / a.own_share) * 8; };
     int64_t per_own;
-    if (a.MT > 0) {
+    if (a.MT > 0) {                            // steps per range: the fewest with which all workgroups run at once
         a.prefix_tiles = (int)ceil_div(rows, 16 * a.MT);
-        const int64_t units = Hk * a.prefix_tiles * ceil_div(P, 128) + own_all, per = std::max<int64_t>(1, ceil_div(units, slots));
+        const int64_t steps = ceil_div(P, 128), most = std::max(steps, own_steps);
+        const auto blocks = [&](int64_t per) { return ceil_div(Hk * a.prefix_tiles * ceil_div(steps, per), 8) * 8 + own_blocks(ceil_div(own_steps, per)); };
+        int64_t per = std::max<int64_t>(1, ceil_div(Hk * a.prefix_tiles * steps + ceil_div(own_units * own_steps, 4 / a.own_share), slots));
+        for (int more = 0; more < 8 && per < most && blocks(per) > slots; ++more) ++per;
         a.prefix_chunk = (int)(128 * per);
-        per_own = per;
+        per_own = own_blocks(1) >= slots ? std::max<int64_t>(1, own_steps) : per;
     } else {
         a.prefix_tiles = (int)ceil_div(rows, 32 * a.waves);
         const int64_t keys = many_keys(a.DP), splits = std::min(std::max<int64_t>(1, 8 / a.waves * kUnits / (Hk * a.prefix_tiles)), ceil_div(P, 256));
         a.prefix_chunk = (int)(ceil_div(ceil_div(P, splits), keys) * keys);
-        per_own = std::max<int64_t>(1, ceil_div(own_all, slots));
+        per_own = std::max<int64_t>(1, ceil_div(own_steps, std::max<int64_t>(1, slots / own_blocks(1))));
     }
-    if (a.own_share == 1) per_own = std::max<int64_t>(per_own, own_steps);
     a.prefix_splits = P > 0 ? (int)ceil_div(P, a.prefix_chunk) : 0;
     a.own_splits = (int)ceil_div(own_steps, per_own);
     if (a.prefix_splits + a.own_splits == 0) a.own_splits = 1;      // nothing is seen: a workgroup stores that
     const int64_t ranges = B * Hk * a.own_splits, prefix_blocks = Hk * a.prefix_tiles * a.prefix_splits;
     if (ranges * a.own_tiles + prefix_blocks + 64 >= ((int64_t)1 << 30)) return VLUT_ERR_SHAPE;
     a.prefix_per_xcd = (int)ceil_div(prefix_blocks, 8);
-    a.own_per_xcd = (int)ceil_div(ceil_div(ranges, 8) * a.own_tiles, 4 / a.own_share);
+    a.own_per_xcd = (int)(own_blocks(a.own_splits) / 8);
     a.direct = a.MT > 0 && a.prefix_splits + a.own_splits == 1;
     if (!a.direct) {
         const size_t parts = (size_t)(a.prefix_splits + a.own_splits) * (size_t)Hk * (size_t)rows;
@@ -263,9 +283,9 @@ int vlut_append_kv(const vlut_heads* k, const vlut_heads* v, const vlut_heads* q
 
 size_t vlut_shared_prefix_attention_bytes(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t prefix_len, int64_t max_own_len) {
     size_t most = 0;                   // (of any cache)
-    for (bool grouped : {false, true}) {
+    for (int kind = 0; kind < 4; ++kind) {
         AttendPlan a;
-        if (plan_attention(B, n, Hq, Hk, D, prefix_len, max_own_len, grouped, &a) != VLUT_OK) return 0;
+        if (plan_attention(B, n, Hq, Hk, D, prefix_len, max_own_len, kind & 1, kind & 2, &a) != VLUT_OK) return 0;
         most = std::max(most, a.o_bytes + a.ml_bytes);
     }
     return most;
@@ -274,7 +294,7 @@ size_t vlut_shared_prefix_attention_bytes(int64_t B, int64_t n, int64_t Hq, int6
 int vlut_query_shared_prefix_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t prefix_len, int64_t max_own_len, int* out4) {
     if (!out4) return VLUT_ERR_NULL;
     AttendPlan a;
-    const int rc = plan_attention(B, n, Hq, Hk, D, prefix_len, max_own_len, true, &a);
+    const int rc = plan_attention(B, n, Hq, Hk, D, prefix_len, max_own_len, true, false, &a);
     if (rc != VLUT_OK) return rc;
     out4[0] = a.MT > 0 ? 16 * a.MT : 32 * a.waves;
     out4[1] = a.prefix_splits;
@@ -291,7 +311,7 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
     int rc = check_cache(cache);
     if (rc != VLUT_OK) return rc;
     AttendPlan a;
-    rc = plan_attention(B, n, q->heads, cache->heads, D, prefix_len, max_own_len, grouped_keys(*cache), &a);
+    rc = plan_attention(B, n, q->heads, cache->heads, D, prefix_len, max_own_len, grouped_keys(*cache), cache->k_head_stride < cache->k_token_stride, &a);
     if (rc != VLUT_OK) return rc;
     if (!q->data || !out->data || !own_lens || (prefix_len > 0 && !prefix_pages) || (max_own_len > 0 && !page_table)) return VLUT_ERR_NULL;
     if (out->heads != q->heads || q->type != cache->type || (out->type != cache->type && out->type != VLUT_TYPE_F32)) return VLUT_ERR_SHAPE;
@@ -347,6 +367,7 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
     p.prefix_chunk = a.prefix_chunk;
     p.own_splits = a.own_splits;
     p.own_share = a.own_share;
+    p.own_heads_together = a.own_heads_together;
     p.own_step = a.own_step;
     p.prefix_tiles = a.prefix_tiles;
     p.own_tiles = a.own_tiles;

@@ -117,12 +117,33 @@ __device__ __forceinline__ void arrived_scalar(int& x) {
 #endif
 }
 
+// The order of a stretch of code that ends here: AHEAD reads of LDS in front, then, GROUPS times, MFMAS matrix instructions, READS reads, VALU vector
+// instructions and EXPS exponentials.  Left to itself the compiler reads what an instruction needs right before it and waits, or all that is needed
+// far ahead, in registers that others want.
+template <int GROUPS, int MFMAS, int READS, int AHEAD, int VALU, int EXPS>
+__device__ __forceinline__ void in_turn() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (AHEAD > 0) __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+    if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x402, 4 * (VALU + EXPS), 0);
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, MFMAS, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+        if constexpr (VALU > 0) {
+            __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
+            __builtin_amdgcn_sched_group_barrier(0x400, EXPS, 0);
+        }
+    }
+#endif
+}
+
 // One range of keys for up to 16 * MT query rows, few enough that memory is what bounds it.  A wave takes 32 keys a step (K straight to registers, V
 // through a piece of LDS of its own, no barrier); the next 32 are on their way while the present ones are worked on.  `share` waves
-// have the range in turn: 4, which join at the end through LDS, or 1 where ranges are short and many.
+// have the range in turn: 4 or 2, which join at the end through LDS, or 1 where ranges are short and many.  keep: the range is one
+// (the waves of a workgroup meet in the join).
 template <class T, int DP, int MT, bool WHOLE, bool GROUPED>
 __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, bool own, const Sequence& seq, int slot,
-                           int share, unsigned char* lds) {
+                           int share, bool keep, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
     constexpr int KS = DP / 32, CH = DP / 8, PER = 64 / CH, VI = kFewKeys / PER, PITCH = few_pitch(DP);
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -212,7 +233,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
         }
     };
 
-    int kt = first_key + (share > 1 ? kFewKeys * wave : 0);
+    int kt = first_key + kFewKeys * (wave & (share - 1));
     Pages page, next_page;
     if (kt < end_key) {
         page = look_up(kt);
@@ -250,20 +271,6 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) kf[t][ks] = __builtin_bit_cast(x8, chunk_moved<WHOLE>(kr[t][ks], 4 * ks + grp, p.D));
-        // A number that is no page: not read, and whoever sees its keys gets NaN
-        const auto no_page = [&](int t) {
-            if constexpr (GROUPED) return !is_page(p, __builtin_amdgcn_readfirstlane(page.id[t]));
-            else return !is_page(p, __shfl(page.id[0], 16 * t + l16));
-        };
-        if (GROUPED ? no_page(0) || no_page(1) : __any(!is_page(p, page.id[0]))) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-                if (no_page(t)) {
-                    constexpr int N = (int)Number<T>::kNan;
-#pragma unroll
-                    for (int ks = 0; ks < KS; ++ks) kf[t][ks] = __builtin_bit_cast(x8, i32x4{N, N, N, N});
-                }
-        }
         f32x4 s[MT][2];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
@@ -273,6 +280,19 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) s[mt][t] = mfma16(kf[t][ks], q[mt][ks], s[mt][t]);
             }
+        // A number that is no page: not read, and whoever sees its keys gets NaN
+        bool no_page = !is_page(p, page.id[0]);
+        if constexpr (GROUPED) no_page = no_page || !is_page(p, page.id[1]);
+        if (__any(no_page)) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!is_page(p, GROUPED ? page.id[GROUPED ? t : 0] : __shfl(page.id[0], 16 * t + 4 * grp + i))) {
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) s[mt][t][i] = __builtin_nanf("");
+                    }
+        }
         load_k(kt + stride, next_page);
         page = next_page;
         next_page = page_after;
@@ -336,6 +356,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                 }
             __builtin_amdgcn_wave_barrier();
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int dt = 0; dt < DP / 16; ++dt) {
             const unsigned at = mine_at + (4 * grp + (l16 >> 2)) * PITCH + 32 * dt + 8 * (l16 & 3);
@@ -347,6 +368,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                 o[mt][dt] = mfma16(vf, pf_rest[mt], o[mt][dt]);
             }
         }
+        in_turn<DP / 16, 2 * MT, 2, 4, 0, 0>();
     }
 
     // A row's result from threads that have some of its features each: the part as it is, or O / l.
@@ -386,17 +408,18 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const int row = row0 + 16 * mt + l16;
-            if (row >= row_end) continue;
+            if (row >= row_end || !keep) continue;
             const Row r = begin_row(row, m[mt], l[mt], grp == 0);
 #pragma unroll
             for (int dt = 0; dt < DP / 16; ++dt) put(r, 16 * dt + 4 * grp, o[mt][dt]);
         }
         return;
     }
-    // The waves' parts: 16 rows at a time through LDS, thread t joins features of row t / 16.
+    // The waves' parts: 16 rows at a time through LDS, 16 threads for a row.
     constexpr int OP = DP + 4, F4 = DP / 64;                       // floats per row; vectors of four per thread
     float* const all_o = (float*)lds;                              // [wave][16][OP]
     float* const all_ml = all_o + 4 * 16 * OP;                     // [wave][16][2]
+    const int first_wave = wave & ~(share - 1);                    // of those that share the range
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         __syncthreads();
@@ -407,47 +430,24 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
             all_ml[(wave * 16 + l16) * 2 + 1] = l[mt];
         }
         __syncthreads();
-        const int r = (int)threadIdx.x >> 4, part = (int)threadIdx.x & 15, row = row0 + 16 * mt + r;
-        if (row < row_end) {
-            float top = -__builtin_inff(), total = 0.0f, f[4];
-#pragma unroll
-            for (int w = 0; w < 4; ++w) top = fmaxf(top, all_ml[(w * 16 + r) * 2]);
+        for (int r = ((wave - first_wave) * 64 + lane) >> 4; r < 16; r += 4 * share) {
+            const int part = lane & 15, row = row0 + 16 * mt + r;
+            if (row >= row_end || !keep) continue;
+            float top = -__builtin_inff(), total = 0.0f;
+            for (int w = first_wave; w < first_wave + share; ++w) top = fmaxf(top, all_ml[(w * 16 + r) * 2]);
             const float shift = top == -__builtin_inff() ? 0.0f : top;
+            f32x4 x[F4] = {};
+            for (int w = first_wave; w < first_wave + share; ++w) {
+                const float f = exp2_fast(all_ml[(w * 16 + r) * 2] - shift);
+                total += f * all_ml[(w * 16 + r) * 2 + 1];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                f[w] = exp2_fast(all_ml[(w * 16 + r) * 2] - shift);
-                total += f[w] * all_ml[(w * 16 + r) * 2 + 1];
+                for (int v = 0; v < F4; ++v) x[v] += *(f32x4*)(all_o + (w * 16 + r) * OP + (part + 16 * v) * 4) * f;
             }
             const Row to = begin_row(row, top, total, part == 0);
 #pragma unroll
-            for (int v = 0; v < F4; ++v) {
-                const int d = (part + 16 * v) * 4;
-                f32x4 x = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int w = 0; w < 4; ++w) x += *(f32x4*)(all_o + (w * 16 + r) * OP + d) * f[w];
-                put(to, d, x);
-            }
+            for (int v = 0; v < F4; ++v) put(to, (part + 16 * v) * 4, x[v]);
         }
     }
-}
-
-// The order of a stretch of code with MFMAS matrix instructions: AHEAD reads of LDS in front, then READS of them, VALU vector instructions and EXPS
-// exponentials behind each matrix instruction.  Left to itself the compiler reads what an instruction needs right before it and waits.
-template <int MFMAS, int READS, int AHEAD, int VALU, int EXPS>
-__device__ __forceinline__ void in_turn() {
-#if defined(__HIP_DEVICE_COMPILE__)
-    if constexpr (AHEAD > 0) __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
-    if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x402, 4 * (VALU + EXPS), 0);
-#pragma unroll
-    for (int i = 0; i < MFMAS; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-        if constexpr (VALU > 0) {
-            __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
-            __builtin_amdgcn_sched_group_barrier(0x400, EXPS, 0);
-        }
-    }
-#endif
 }
 
 // One range of the prefix for 32 * NW query rows, many enough that the matrix cores are what bounds it: K and V of 64 keys (32 where D is
@@ -555,7 +555,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int t = 0; t < KT; ++t) s[t] = mfma32(__builtin_bit_cast(x8, *(const i32x4*)(buf + (32 * t + l32) * KP + 32 * ks + 16 * half)), q[ks], s[t]);
-        in_turn<KS * KT, 1, 6, 0, 0>();
+        in_turn<KS * KT, 1, 1, 6, 0, 0>();
         if (kt + KEYS > end_key) {
             int left = end_key - kt;
             arrived_scalar(left);              // (or its comparisons are made in every step, ahead of the branch)
@@ -619,7 +619,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
                 pf = next;
                 rest = next_rest;
             }
-            in_turn<2 * KT * (DP / 32) * TERMS, 2 / TERMS, 0, 20 / (DP / 32), 8 / (DP / 32)>();
+            in_turn<2 * KT * (DP / 32) * TERMS, 1, 2 / TERMS, 0, 20 / (DP / 32), 8 / (DP / 32)>();
             __builtin_amdgcn_sched_barrier(0);
         });
         if (over) *again = 1;
@@ -667,18 +667,22 @@ __global__ void __launch_bounds__(256, few_waves(DP, MT)) attend_few_kernel(cons
         const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
         if (h >= p.Hk) return;
         const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
-        attend_few<T, DP, MT, WHOLE, GROUPED>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, 4, lds);
+        attend_few<T, DP, MT, WHOLE, GROUPED>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, 4, true, lds);
         return;
     }
-    // (sequences differ in length, so that their ranges go round; the tiles of a range stay together)
-    const int own_place = (place - p.prefix_per_xcd) * (p.own_share == 1 ? 4 : 1) + (p.own_share == 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : 0);
-    const int tile = own_place % p.own_tiles, rest = own_place / p.own_tiles * 8 + xcd, split = rest % p.own_splits, bh = rest / p.own_splits, h = bh % p.Hk, b = bh / p.Hk;
-    if (b >= p.B) return;
+    // Sequences differ in length, so that their ranges go round the XCDs; the tiles of a range stay together, and the heads of a token where they are
+    // neighbours in memory, with lines that two heads share.
+    const int at_once = 4 / p.own_share, own_place = (place - p.prefix_per_xcd) * at_once + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / p.own_share;
+    const int tile = own_place % p.own_tiles, j = own_place / p.own_tiles, together = p.own_heads_together;
+    const int rest = j / together * 8 + xcd, inner = j % together, heads = p.Hk / together;       // together: Hk or 1
+    const int h = together > 1 ? inner : rest / p.own_splits % heads, bs = together > 1 ? rest : rest / p.own_splits / heads * p.own_splits + rest % p.own_splits;
+    const int split = bs % p.own_splits, b = min(bs / p.own_splits, p.B - 1);
+    const bool keep = bs / p.own_splits < p.B;
     const Sequence seq = sequence_of(p, b);
     const int steps = (seq.len + p.own_step - 1) / p.own_step, per = (steps + p.own_splits - 1) / p.own_splits, nG = p.n * p.G;
-    const int first = min(split * per * p.own_step, seq.len), end = min(first + per * p.own_step, seq.len);
+    const int first = min(split * per * p.own_step, seq.len), end = keep ? min(first + per * p.own_step, seq.len) : first;
     attend_few<T, DP, OWN, WHOLE, GROUPED>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq,
-                                           p.prefix_splits + split, p.own_share, lds);
+                                           p.prefix_splits + split, p.own_share, keep, lds);
 }
 
 // Many rows: ranges of the prefix for 32 rows of each of NW waves, with P in TERMS terms.  XCDs as above.

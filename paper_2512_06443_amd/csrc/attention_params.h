@@ -25,6 +25,7 @@ struct AttendParams {
     int B, n, Hk, G, D, page_log, pages;
     int P, max_own;
     int prefix_splits, prefix_chunk;   // keys per split
+    int own_heads_together;            // Hk where a token's heads are worked on by one XCD, else 1
     int own_splits, own_share, own_step;   // waves to a range; its keys are a multiple of own_step but for the end
     int prefix_tiles, own_tiles;       // tiles of rows
     int prefix_per_xcd, own_per_xcd;   // workgroups
@@ -35,7 +36,7 @@ struct AttendParams {
 constexpr int kFewKeys = 32;           // keys of a wave's step where rows are few
 __host__ __device__ constexpr int few_pitch(int DP) { return DP * 2 + 32; }
 __host__ __device__ constexpr int few_lds(int DP) { return 4 * kFewKeys * few_pitch(DP); }
-__host__ __device__ constexpr int few_waves(int DP, int MT) { return DP > 128 ? 1 : (MT > 1 || DP > 64 ? 2 : 4); }   // of a SIMD
+__host__ __device__ constexpr int few_waves(int DP, int MT) { return DP > 128 ? 1 : (MT > 1 ? 2 : (DP > 64 ? 2 : 4)); }   // of a SIMD
 __host__ __device__ constexpr int many_keys(int DP) { return DP > 128 ? 32 : 64; }
 __host__ __device__ constexpr int many_k_pitch(int DP) { return DP * 2 + 16; }
 __host__ __device__ constexpr int many_v_pitch(int DP) { return DP * 2 + 64; }
@@ -43,7 +44,7 @@ __host__ __device__ constexpr int many_buffer(int DP) { return many_keys(DP) * (
 
 struct AttendPlan {
     int MT, waves, own_mt, DP;         // tile of the prefix: 16 * MT rows; MT = 0: 32 for each of the waves, by a kernel of its own
-    int own_share, own_step, grouped;
+    int own_share, own_step, own_heads_together, grouped;
     int prefix_tiles, prefix_splits, prefix_chunk, prefix_per_xcd, own_tiles, own_splits, own_per_xcd, direct;
     int64_t rows;
     size_t o_bytes, ml_bytes;

@@ -111,7 +111,7 @@ CASES = {
     # own tokens of many pages, several parts
     "long_own": dict(B=1, n=1, Hq=8, Hk=2, D=128, P=0, lens=[5000], page=16),
     "long_own_and_prefix": dict(B=2, n=2, Hq=4, Hk=2, D=64, P=3001, lens=[4097, 2], page=128, dtype=torch.float16),
-    # many query rows: tiles of 128
+    # more query rows than a tile
     "rows_128": dict(B=33, n=1, Hq=8, Hk=2, D=128, P=200, lens=[(7 * i) % 150 for i in range(33)], page=16),
     "rows_128_tail": dict(B=17, n=2, Hq=8, Hk=1, D=100, P=1001, lens=[1 + (13 * i) % 90 for i in range(17)], page=32, dtype=torch.float16, token_major=True),
     "rows_128_d64": dict(B=40, n=1, Hq=16, Hk=2, D=64, P=65, lens=[i % 5 for i in range(40)], page=8),
@@ -125,6 +125,55 @@ CASES = {
     "prompt_behind_prefix": dict(B=2, n=45, Hq=4, Hk=2, D=64, P=70, lens=[45, 60], page=16, dtype=torch.float16),
     "one_head_each": dict(B=3, n=1, Hq=5, Hk=5, D=128, P=50, lens=[9, 10, 11], page=2),
 }
+
+# Many query rows over a long prefix: a launch of its own, 32 rows for each of four waves or eight.
+MANY = {
+    "four_waves": dict(B=20, n=1, Hq=32, Hk=8, D=64, P=15701, lens=[(11 * i) % 70 for i in range(20)], page=16),
+    "four_waves_d100": dict(B=3, n=8, Hq=32, Hk=8, D=100, P=13100, lens=[8, 100, 31], page=64, dtype=torch.float16, queries=[8, 3, 5]),
+    "eight_waves": dict(B=40, n=1, Hq=32, Hk=8, D=128, P=7950, lens=[(7 * i) % 150 for i in range(40)], page=16),
+    "eight_waves_d100": dict(B=21, n=2, Hq=32, Hk=8, D=100, P=7501, lens=[2 + (13 * i) % 90 for i in range(21)], page=32, dtype=torch.float16, token_major=True),
+    "eight_waves_d64": dict(B=41, n=1, Hq=16, Hk=2, D=64, P=15999, lens=[1] * 41, page=128, dtype=torch.float16),
+    "d256": dict(B=20, n=1, Hq=32, Hk=4, D=256, P=15777, lens=[i * 9 for i in range(20)], page=16),
+    "d132": dict(B=33, n=1, Hq=16, Hk=4, D=132, P=19001, lens=[3] * 33, page=16, dtype=torch.float16),
+    "pages_of_8": dict(B=40, n=1, Hq=32, Hk=8, D=128, P=7950, lens=[5] * 40, page=8),          # (too short for that launch: tiles)
+    "no_own": dict(B=40, n=1, Hq=32, Hk=8, D=64, P=7950, lens=[0] * 40, page=16),
+}
+
+
+@pytest.mark.parametrize("dtype", ["cache", "fp32"])
+@pytest.mark.parametrize("name", list(MANY))
+def test_many_rows_against_64_bits(B, name, dtype):
+    case = Case(**MANY[name])
+    print(name, dtype, B.query_shared_prefix_attention(*case.shape, case.P, max(case.lens)), flush=True)
+    out, lse = case.run(B, dtype=torch.float32 if dtype == "fp32" else None, want_lse=True, max_own_len=max(case.lens))
+    case.check(out, lse.cpu(), only=[0, case.shape[0] - 1])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_many_rows_whose_scores_rise(B, dtype):
+    """Scores far above those of the first keys: the range is worked on again.  In one range, in the last ones, and everywhere."""
+    for where in (slice(1000, 1001), slice(7000, 7940), slice(70, None)):
+        case = Case(B=40, n=1, Hq=32, Hk=8, D=64, P=7950, lens=[4] * 40, page=16, dtype=dtype)
+        case.prefix[0][where] *= 40
+        case.write()
+        out, lse = case.run(B, dtype=torch.float32, want_lse=True)
+        case.check(out, lse.cpu(), only=[0, 39])
+
+
+def test_many_rows_with_infinities_and_pages_that_cannot_be(B):
+    case = Case(**MANY["eight_waves"])
+    want, _ = case.run(B)
+    assert want.isfinite().all()
+    case.prefix[1][5000, 3, 7] = float("inf")                             # one value of one key head: that feature of its query heads
+    case.write()
+    out, _ = case.run(B)
+    hit = torch.zeros_like(out, dtype=torch.bool)
+    hit[:, :, 12:16, 7] = True
+    assert torch.equal(out[~hit], want[~hit]) and not out[hit].isfinite().any()
+    case = Case(**MANY["eight_waves"])
+    case.prefix_pages[300] = case.k.shape[0]
+    out, _ = case.run(B)
+    assert out.isnan().all()
 
 
 @pytest.mark.parametrize("dtype", ["cache", "fp32"])
@@ -142,7 +191,7 @@ def test_against_64_bits(B, name, dtype):
 
 
 def test_every_tile_is_among_the_cases(B):
-    rows = {B.query_shared_prefix_attention(c["B"], c["n"], c["Hq"], c["Hk"], c["D"], c["P"], max(c["lens"]))[0] for c in CASES.values()}
+    rows = {B.query_shared_prefix_attention(c["B"], c["n"], c["Hq"], c["Hk"], c["D"], c["P"], max(c["lens"]))[0] for c in [*CASES.values(), *MANY.values()]}
     assert rows == {16, 32, 128, 256}
 
 
