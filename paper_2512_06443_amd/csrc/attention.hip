@@ -104,8 +104,8 @@ int heads_params(HeadsParams& p, const vlut_heads* const (&in)[3], float eps, co
 
 template <class TI, class TO>
 int launch_heads_t(const HeadsParams& p, int vec, int together, dim3 grid, hipStream_t stream) {
-    if (vec == 4) return together == 4 ? launch(heads_kernel<TI, TO, 4, 4>, grid, 256, 0, stream, p) : launch(heads_kernel<TI, TO, 4, 1>, grid, 256, 0, stream, p);
-    if (vec == 2) return together == 4 ? launch(heads_kernel<TI, TO, 2, 4>, grid, 256, 0, stream, p) : launch(heads_kernel<TI, TO, 2, 1>, grid, 256, 0, stream, p);
+    if (vec == 4) return together > 1 ? launch(heads_kernel<TI, TO, 4, 2>, grid, 256, 0, stream, p) : launch(heads_kernel<TI, TO, 4, 1>, grid, 256, 0, stream, p);
+    if (vec == 2) return together > 1 ? launch(heads_kernel<TI, TO, 2, 4>, grid, 256, 0, stream, p) : launch(heads_kernel<TI, TO, 2, 1>, grid, 256, 0, stream, p);
     return launch(heads_kernel<TI, TO, 1, 1>, grid, 256, 0, stream, p);
 }
 template <class TI>
@@ -118,8 +118,9 @@ int launch_heads(HeadsParams& p, int in, int out, int vec, hipStream_t stream) {
     // lanes of a row: enough for its units (at most 64; a lane has two where pairs are single)
     p.lanes_log = std::min(6, log2_of((p.D + 2 * vec - 1) / (2 * vec)));
     const unsigned per = 256u >> p.lanes_log;
-    // Four heads together where that leaves every unit eight workgroups (HEADS_FIGURES)
-    const int together = vec > 1 && (uint64_t)p.tokens * p.heads >= 4ull * 8 * kUnits * per ? 4 : 1;
+    // Heads together where rows are enough for two workgroups of such groups on every unit.  us for one / two / four together, 4096 tokens: 40 heads of
+    // 128 from fp32 28.2 / 27.5 / 27.8, 16 heads to a cache 12.0 / 11.5 / 12.3, 64 heads of 100 (vectors of two) 57.5 / 48.5 / 45.0.
+    const int most = vec == 4 ? 2 : (vec == 2 ? 4 : 1), together = (uint64_t)p.tokens * p.heads >= 8ull * kUnits * per ? most : 1;
     unsigned blocks = 0;
     for (HeadRows& k : p.kind) {
         k.groups_of_token = (unsigned)((k.heads + together - 1) / together);
