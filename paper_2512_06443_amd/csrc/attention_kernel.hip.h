@@ -36,13 +36,13 @@ template <>
 struct Number<__bf16> {
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     static constexpr unsigned kExponents = 0x7f807f80u, kNan = 0x7fc07fc0u;
-    static constexpr float kSlack = 24.0f;
+    static constexpr bool kWide = true;               // weights may be as large as fp32's
 };
 template <>
 struct Number<_Float16> {
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     static constexpr unsigned kExponents = 0x7c007c00u, kNan = 0x7e007e00u;
-    static constexpr float kSlack = 15.0f;             // (weights below 2^15 are inside the type)
+    static constexpr bool kWide = false;
 };
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ f32x4 mfma16(Number<__bf16>::x8 a, Number<__bf16>::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -124,15 +124,12 @@ template <int GROUPS, int MFMAS, int READS, int AHEAD, int VALU, int EXPS>
 __device__ __forceinline__ void in_turn() {
 #if defined(__HIP_DEVICE_COMPILE__)
     if constexpr (AHEAD > 0) __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
-    if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x402, 4 * (VALU + EXPS), 0);
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x8, MFMAS, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
-        if constexpr (VALU > 0) {
-            __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
-            __builtin_amdgcn_sched_group_barrier(0x400, EXPS, 0);
-        }
+        if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(0x2, VALU, 0);
+        if constexpr (EXPS > 0) __builtin_amdgcn_sched_group_barrier(0x400, EXPS, 0);
     }
 #endif
 }
@@ -455,15 +452,16 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 // worked on, and are stored behind them; one barrier per step.
 // What the vector units have to do beside the matrix instructions is kept short:
 //   - a wave's load covers GK neighbouring keys, which share their page (the host sees to it): addresses are worked out once per wave;
-//   - O is not multiplied with every new maximum: m is the maximum of the first step's scores, and weights are powers of two of the scores above it.
-//     Where a later score is kSlack or more above that, the range is begun again, with the largest of all its scores, which a sweep over K
-//     finds.  (Multiplying where it is needed, in a branch, costs as much as always: O's registers are copied where the ways meet.)
+//   - O is not multiplied with every new maximum, and maxima are not looked for: m is the largest score of the first step, and weights are powers of
+//     two of the scores above it.  Where that does not do (bf16: the sum of weights shows one of 2^60 or so; fp16, whose weights have to stay
+//     below 2^15: a maximum per step shows one) the range is begun again with the largest of all its scores, which a sweep over K finds.
+//     (Multiplying where it is needed, in a branch, costs as much as always: O's registers are copied where the ways meet.)
 template <class T, int DP, int TERMS, int NW, bool WHOLE>
 __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, int slot, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
     constexpr int KEYS = many_keys(DP), KT = KEYS / 32, KS = DP / 16, CH = DP / 8, PER = 64 * NW / CH, LI = KEYS / PER, GK = 64 / CH;
     constexpr int KP = many_k_pitch(DP), VP = many_v_pitch(DP);
-    constexpr float kSlack = Number<T>::kSlack;
+    constexpr bool WIDE = Number<T>::kWide;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int nG = p.n * p.G, row = row0 + 32 * wave + l32;
@@ -545,7 +543,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         }
     };
     f32x16 s[KT], o[DP / 32];
-    float top, m = 0.0f, l;                    // top: the largest score of a step, times scale_log2
+    float m = 0.0f, l;
     auto score = [&](int kt, const unsigned char* buf) {
 #pragma unroll
         for (int t = 0; t < KT; ++t)
@@ -566,12 +564,15 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
                 for (int i = 0; i < 16; ++i)
                     if (32 * t + (i & 3) + 8 * (i >> 2) >= seen) s[t][i] = -__builtin_inff();
         }
-        top = s[0][0];
+    };
+    // the largest score of a step, times scale_log2
+    auto largest = [&]() {
+        float top = s[0][0];
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
+        return fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
     };
     int* const again = (int*)(lds + 2 * many_buffer(DP));
     if (tid == 0) *again = 0;                  // (the sweep's first barrier is between this and what follows)
@@ -585,9 +586,9 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         sweep([&](int kt, const unsigned char* buf) {
             const unsigned v_at = lds_base_of((void*)(buf + KEYS * KP)) + (4 * half + (l16 >> 2)) * VP + 32 * ((lane >> 4) & 1) + 8 * (l16 & 3);
             score(kt, buf);
-            m = kt == first_key && !known ? top : m;
+            if (kt == first_key && !known) m = largest();
+            if constexpr (!WIDE) over |= largest() > m + 15.0f;              // (no branch here)
             const float shift = m == -__builtin_inff() ? 0.0f : m;
-            over |= top > m + kSlack;          // (no branch here)
             // Sixteen keys at a time; the weights and V of the next are made and read while the matrix cores are on these.
             x8 vf[DP / 32], pf, rest, next, next_rest;
             auto weigh = [&](int st, x8& w, x8& w_rest) {
@@ -605,8 +606,8 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
             };
 #pragma unroll
             for (int dt = 0; dt < DP / 32; ++dt) vf[dt] = read_v(0, dt);
-            __builtin_amdgcn_sched_barrier(0);
             weigh(0, pf, rest);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int st = 0; st < 2 * KT; ++st) {
                 if (st + 1 < 2 * KT) weigh(st + 1, next, next_rest);
@@ -618,18 +619,19 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
                 }
                 pf = next;
                 rest = next_rest;
+                in_turn<(DP / 32) * TERMS, 1, 2 / TERMS, 0, (TERMS > 1 ? 40 : 20) / (DP / 32) / TERMS, 8 / (DP / 32) / TERMS>();
+                __builtin_amdgcn_sched_barrier(0);
             }
-            in_turn<2 * KT * (DP / 32) * TERMS, 1, 2 / TERMS, 0, 20 / (DP / 32), 8 / (DP / 32)>();
-            __builtin_amdgcn_sched_barrier(0);
         });
+        if constexpr (WIDE) over = !(l < 0x1p60f);
         if (over) *again = 1;
         __syncthreads();
-        if (!*again) break;                    // (never twice: m is the largest score then)
+        if (!*again || known) break;
         known = true;
         m = -__builtin_inff();
         sweep([&](int kt, const unsigned char* buf) {
             score(kt, buf);
-            m = fmaxf(m, top);
+            m = fmaxf(m, largest());
         });
         __syncthreads();
         if (tid == 0) *again = 0;
