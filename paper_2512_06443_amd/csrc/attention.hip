@@ -175,9 +175,11 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     a.DP = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
     a.own_mt = own_rows <= 16 ? 1 : 2;
     // Tiles of 16 or 32 rows whose waves share the keys, or, where the prefix' products are many, a launch of its own with 32 rows a wave.  us, by tiles /
-    // that launch (8 key heads of 128 features, bf16): 128 rows a head, 1500 keys 17.2 / 22.3, 4096 22.2 / 25.9, 9000 29.3 / 31.4, 32768 63 / 47;
-    // 256 rows, 1024 keys 15.9 / 25.1, 4096 29.9 / 31.1; 1024 rows, 500 keys 24 / 31, 1000 32 / 38.
-    a.MT = P == 0 ? a.own_mt : (rows <= 16 ? 1 : (rows <= 64 || !grouped || rows * P * Hk <= 10000000 ? 2 : 0));
+    // that launch (bf16, 8 key heads, 256 rows a head): 128 features, 2048 keys 22 / 27, 4096 29 / 31, 6000 33 / 31, 8192 39 / 38 (512 rows: 2048 keys
+    // 25 / 32, 4096 34 / 35); 64 features, 4096 keys 19 / 23, 8192 26 / 28, 16384 42 / 30; 256 features, 1024 keys 30 / 37, 2048 44 / 39, 4096 69 / 43
+    // (one key head, 800 rows: 4096 keys 34 / 39, 6000 41 / 42, 8192 47 / 44).
+    const int64_t few_products = a.DP > 128 ? 4000000 : 1280000000 / a.DP;
+    a.MT = P == 0 ? a.own_mt : (rows <= 16 ? 1 : (rows <= 64 || !grouped || rows * P * Hk <= few_products ? 2 : 0));
     a.waves = a.MT == 0 && a.DP <= 128 && rows > 128 ? 8 : 4;
     a.own_tiles = (int)ceil_div(own_rows, 16 * a.own_mt);
     const int64_t own_units = B * Hk * a.own_tiles;

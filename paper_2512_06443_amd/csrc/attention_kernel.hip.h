@@ -37,12 +37,14 @@ struct Number<__bf16> {
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     static constexpr unsigned kExponents = 0x7f807f80u, kNan = 0x7fc07fc0u;
     static constexpr bool kWide = true;               // weights may be as large as fp32's
+    static constexpr float kLift = 0.0f;
 };
 template <>
 struct Number<_Float16> {
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     static constexpr unsigned kExponents = 0x7c007c00u, kNan = 0x7e007e00u;
     static constexpr bool kWide = false;
+    static constexpr float kLift = 14.0f;             // weights are up to 2^14, so that those of 2^-38 of the largest are no zeros yet
 };
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ f32x4 mfma16(Number<__bf16>::x8 a, Number<__bf16>::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -307,7 +309,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
             float top = fmaxf(fmaxf(fmaxf(s[mt][0].x, s[mt][0].y), fmaxf(s[mt][0].z, s[mt][0].w)), fmaxf(fmaxf(s[mt][1].x, s[mt][1].y), fmaxf(s[mt][1].z, s[mt][1].w)));
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(m[mt], top * p.scale_log2), shift = now == -__builtin_inff() ? 0.0f : now;
+            const float now = fmaxf(m[mt], __builtin_fmaf(top, p.scale_log2, -Number<T>::kLift)), shift = now == -__builtin_inff() ? 0.0f : now;
             const float factor = exp2_fast(m[mt] - shift);
             m[mt] = now;
             l[mt] *= factor;
@@ -453,7 +455,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 // What the vector units have to do beside the matrix instructions is kept short:
 //   - a wave's load covers GK neighbouring keys, which share their page (the host sees to it): addresses are worked out once per wave;
 //   - O is not multiplied with every new maximum, and maxima are not looked for: m is the largest score of the first step, and weights are powers of
-//     two of the scores above it.  Where that does not do (bf16: the sum of weights shows one of 2^60 or so; fp16, whose weights have to stay
+//     two of the scores above it.  Where that does not do (bf16: the sum of weights shows one of 2^40 or so; fp16, whose weights have to stay
 //     below 2^15: a maximum per step shows one) the range is begun again with the largest of all its scores, which a sweep over K finds.
 //     (Multiplying where it is needed, in a branch, costs as much as always: O's registers are copied where the ways meet.)
 template <class T, int DP, int TERMS, int NW, bool WHOLE>
@@ -462,6 +464,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
     constexpr int KEYS = many_keys(DP), KT = KEYS / 32, KS = DP / 16, CH = DP / 8, PER = 64 * NW / CH, LI = KEYS / PER, GK = 64 / CH;
     constexpr int KP = many_k_pitch(DP), VP = many_v_pitch(DP);
     constexpr bool WIDE = Number<T>::kWide;
+    constexpr float LIFT = 0.5f * Number<T>::kLift;            // (scores after the first step may be larger)
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int nG = p.n * p.G, row = row0 + 32 * wave + l32;
@@ -586,7 +589,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         sweep([&](int kt, const unsigned char* buf) {
             const unsigned v_at = lds_base_of((void*)(buf + KEYS * KP)) + (4 * half + (l16 >> 2)) * VP + 32 * ((lane >> 4) & 1) + 8 * (l16 & 3);
             score(kt, buf);
-            if (kt == first_key && !known) m = largest();
+            if (kt == first_key && !known) m = largest() - LIFT;
             if constexpr (!WIDE) over |= largest() > m + 15.0f;              // (no branch here)
             const float shift = m == -__builtin_inff() ? 0.0f : m;
             // Sixteen keys at a time; the weights and V of the next are made and read while the matrix cores are on these.
@@ -623,7 +626,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
                 __builtin_amdgcn_sched_barrier(0);
             }
         });
-        if constexpr (WIDE) over = !(l < 0x1p60f);
+        if constexpr (WIDE) over = !(l < 0x1p40f);             // (O of values up to 2^88 has room then)
         if (over) *again = 1;
         __syncthreads();
         if (!*again || known) break;
@@ -631,7 +634,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         m = -__builtin_inff();
         sweep([&](int kt, const unsigned char* buf) {
             score(kt, buf);
-            m = fmaxf(m, largest());
+            m = fmaxf(m, largest() - LIFT);
         });
         __syncthreads();
         if (tid == 0) *again = 0;

@@ -128,15 +128,15 @@ CASES = {
 
 # Many query rows over a long prefix: a launch of its own, 32 rows for each of four waves or eight.
 MANY = {
-    "four_waves": dict(B=20, n=1, Hq=32, Hk=8, D=64, P=15701, lens=[(11 * i) % 70 for i in range(20)], page=16),
+    "four_waves": dict(B=20, n=1, Hq=32, Hk=8, D=64, P=31401, lens=[(11 * i) % 70 for i in range(20)], page=16),
     "four_waves_d100": dict(B=3, n=8, Hq=32, Hk=8, D=100, P=13100, lens=[8, 100, 31], page=64, dtype=torch.float16, queries=[8, 3, 5]),
     "eight_waves": dict(B=40, n=1, Hq=32, Hk=8, D=128, P=7950, lens=[(7 * i) % 150 for i in range(40)], page=16),
     "eight_waves_d100": dict(B=21, n=2, Hq=32, Hk=8, D=100, P=7501, lens=[2 + (13 * i) % 90 for i in range(21)], page=32, dtype=torch.float16, token_major=True),
-    "eight_waves_d64": dict(B=41, n=1, Hq=16, Hk=2, D=64, P=15999, lens=[1] * 41, page=128, dtype=torch.float16),
+    "eight_waves_d64": dict(B=41, n=1, Hq=16, Hk=2, D=64, P=31999, lens=[1] * 41, page=128, dtype=torch.float16),
     "d256": dict(B=20, n=1, Hq=32, Hk=4, D=256, P=15777, lens=[i * 9 for i in range(20)], page=16),
     "d132": dict(B=33, n=1, Hq=16, Hk=4, D=132, P=19001, lens=[3] * 33, page=16, dtype=torch.float16),
     "pages_of_8": dict(B=40, n=1, Hq=32, Hk=8, D=128, P=7950, lens=[5] * 40, page=8),          # (too short for that launch: tiles)
-    "no_own": dict(B=40, n=1, Hq=32, Hk=8, D=64, P=7950, lens=[0] * 40, page=16),
+    "no_own": dict(B=40, n=1, Hq=32, Hk=8, D=64, P=15901, lens=[0] * 40, page=16),
 }
 
 
@@ -153,11 +153,40 @@ def test_many_rows_against_64_bits(B, name, dtype):
 def test_many_rows_whose_scores_rise(B, dtype):
     """Scores far above those of the first keys: the range is worked on again.  In one range, in the last ones, and everywhere."""
     for where in (slice(1000, 1001), slice(7000, 7940), slice(70, None)):
-        case = Case(B=40, n=1, Hq=32, Hk=8, D=64, P=7950, lens=[4] * 40, page=16, dtype=dtype)
+        case = Case(B=40, n=1, Hq=32, Hk=8, D=128, P=7950, lens=[4] * 40, page=16, dtype=dtype)
         case.prefix[0][where] *= 40
         case.write()
         out, lse = case.run(B, dtype=torch.float32, want_lse=True)
         case.check(out, lse.cpu(), only=[0, 39])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("Bn,P,page", [(1, 40000, 16), (1, 40000, 4), (40, 15950, 16)])
+@pytest.mark.parametrize("where", [0, 0.6])
+def test_one_key_far_above_many(B, dtype, Bn, P, page, where):
+    """Weights of 2^-26 of the largest, of which there are so many that they count: where the largest one's value is 0 they are the whole output.
+    Bound: the scores' and the sums' of Case.check(); weights in two terms of the type, for fp16 32 rows a wave: to 2^-24 of 2^7 times the largest."""
+    D = 64
+    case = Case(B=Bn, n=1, Hq=32, Hk=8, D=D, P=P, lens=[0] * Bn, page=page, dtype=dtype)
+    case.q.zero_()
+    case.q[..., 5] = 16.0
+    k, v = case.prefix
+    top = int(where * P)
+    k.zero_()
+    k[:, :, 5] = -13 * math.log(2) / 2
+    k[top, :, 5] = 13 * math.log(2) / 2
+    v.copy_(v.abs() + 1)
+    v[top] = 0
+    case.write()
+    out, lse = case.run(B, dtype=torch.float32, want_lse=True)
+    s = 2.0 * k[:, 0, 5].cpu().double()
+    w = torch.softmax(s, 0)
+    want = torch.einsum("p,phd->hd", w, v.cpu().double()).repeat_interleave(4, 0)
+    score = (D + 4) * U32 * 10 + 4 * U32 * 30
+    tiny = 2.0 ** -31 * P * 3 if dtype == torch.float16 and Bn > 1 else 0.0
+    bound = want * (U[dtype] ** 2 + 2 * score + P * U32 + 2.0 ** -20) + tiny
+    assert ((out.cpu().double()[:, 0] - want).abs() <= bound).all()
+    assert (lse.cpu().double() - torch.logsumexp(s, 0)).abs().max() <= 2 * score + P * U32 + 2.0 ** -20
 
 
 def test_many_rows_with_infinities_and_pages_that_cannot_be(B):
