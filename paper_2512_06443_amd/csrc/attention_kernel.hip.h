@@ -685,7 +685,8 @@ __global__ void __launch_bounds__(256, few_waves(DP, MT)) attend_few_kernel(cons
     const bool keep = bs / p.own_splits < p.B;
     const Sequence seq = sequence_of(p, b);
     const int steps = (seq.len + p.own_step - 1) / p.own_step, per = (steps + p.own_splits - 1) / p.own_splits, nG = p.n * p.G;
-    const int first = min(split * per * p.own_step, seq.len), end = keep ? min(first + per * p.own_step, seq.len) : first;
+    const int seen = seq.base + (min((tile + 1) * 16 * OWN, nG) - 1) / p.G + 1;          // by the tile's last query
+    const int first = min(split * per * p.own_step, seq.len), end = keep ? min(min(first + per * p.own_step, seq.len), max(first, seen)) : first;
     attend_few<T, DP, OWN, WHOLE, GROUPED>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq,
                                            p.prefix_splits + split, p.own_share, keep, lds);
 }
