@@ -244,7 +244,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) arrived(q[mt][ks]);
     }
-    for (; kt < end_key; kt += stride) {
+    auto step = [&](auto more) {
         const bool some_masked = kt + kFewKeys > all_see;
         // V to LDS, zeros for keys past the range
         unsigned odd = 0;
@@ -263,8 +263,11 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
         for (int i = 0; i < VI; ++i) *(i32x4*)(mine + (PER * i + v_key) * PITCH + 16 * v_chunk) = vr[i];
         // What comes next, in the order in which it is waited for: the page after the next, V, K.  Also behind the last step, from its last key: in a
         // branch, registers that are loaded on one way alone would be copied, and waited for, where the ways meet.
-        const Pages page_after = look_up(kt + 2 * stride);
-        load_v(kt + stride, next_page);
+        Pages page_after;
+        if constexpr (more.value) {
+            page_after = look_up(kt + 2 * stride);
+            load_v(kt + stride, next_page);
+        }
         x8 kf[2][KS];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -292,9 +295,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                         for (int mt = 0; mt < MT; ++mt) s[mt][t][i] = __builtin_nanf("");
                     }
         }
-        load_k(kt + stride, next_page);
-        page = next_page;
-        next_page = page_after;
+        if constexpr (more.value) load_k(kt + stride, next_page);
         x8 pf[MT], pf_rest[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -368,7 +369,13 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
             }
         }
         in_turn<DP / 16, 2 * MT, 2, 4, 0, 0>();
-    }
+        if constexpr (more.value) {
+            page = next_page;
+            next_page = page_after;
+        }
+    };
+    for (; kt + stride < end_key; kt += stride) step(std::true_type{});
+    if (kt < end_key) step(std::false_type{});
 
     // A row's result from threads that have some of its features each: the part as it is, or O / l.
     struct Row {
