@@ -1,7 +1,8 @@
 // The native form of norm_rope, append_kv and shared_prefix_attention.  Part of torch_calls.cpp (included there, behind its helpers); what is said
 // there holds: None for every argument that is not known to be ordinary or fails a check, before anything is launched, and the Python
 // form raises the error.
-// Host time of a call, Python / native form, us (what ctypes' structures, torch.empty and attribute reads take): see binding.py.
+// Host time of a call, Python / native form, us (what ctypes' structures, torch.empty and attribute reads take): norm_rope of one token 20 / 6, append_kv with
+// queries 21 / 5, shared_prefix_attention, two launches, 21 / 9.
 #pragma once
 
 #include <torch/csrc/Dtype.h>

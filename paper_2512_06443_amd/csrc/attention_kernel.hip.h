@@ -11,16 +11,20 @@ using namespace vlut_attention;
 //   m = max s,  l = sum exp(s - m),  O = sum exp(s - m) v,  output O / l;   nothing seen: 0
 // Parts of the keys are worked out apart and joined: with M = max m_i the sums of exp(m_i - M) l_i and exp(m_i - M) O_i are those of the whole.
 // The parts: the shared prefix, once for the rows of all sequences that read the same key head (B * n * G of them, G query heads to a key
-// head), cut into prefix_splits ranges; and each sequence's own tokens for its n * G rows, cut into own_splits.  One launch works all
-// of them out (a workgroup has one range and one tile of rows), combine_kernel joins them; a single part is stored as the result.
+// head), cut into prefix_splits ranges; and each sequence's own tokens for its n * G rows, cut into own_splits.  A workgroup has one
+// range and one tile of rows.  One launch works out all of them (attend_few_kernel); where the rows and the prefix are many, the prefix has a
+// launch of its own (attend_many_kernel), behind that of the own tokens.  combine_kernel joins the parts; a single part is stored as the result.
 //
 // Both products run transposed on the matrix cores, S^T = K Q^T and O^T = V^T P^T: a query is a column, so that its m, l and the factor
 // of its O are one number per lane.  The columns of S^T come out with four neighbouring keys in a lane; P^T is taken in with the keys in exactly that
 // order (the order of a sum's terms is free as long as V^T has the same), so that P goes from one product to the next without leaving its
 // registers.  V^T is read out of the row-major V in LDS by transposing reads (ds_read_b64_tr_b16: the 16 lanes of a group give the addresses of 4
 // rows x 16 features, and get four rows of one feature each).
-// Scores, m, l and O are fp32; P is rounded to the cache's type for the second product, with what the rounding left as a second term
-// where the output is fp32.
+// Scores, m, l and O are fp32.  P is carried to the second product in two terms of the cache's type, rounded and what that left (16 bits of bf16,
+// 22 of fp16): the matrix cores take no fp32, and next to memory the second term costs nothing where rows are few.  Where they are many and the output
+// has 16 bits P has one term: the output's own rounding is as large, and the second would be half as many matrix instructions again (256 rows a
+// head, 8192 keys, 8 heads: 46 us and 57).  l sums P before any rounding.
+// fp16: P is lifted by a power of two (Number::kLift), since weights below 2^-14 would lose bits and those below 2^-25 everything.
 // ---------------------------------------------------------------------------------------------
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -72,7 +76,7 @@ __device__ __forceinline__ i32x4 chunk_moved(i32x4 x, int chunk, int D) {
     return left <= 0 ? i32x4{0, 0, 0, 0} : i32x4{x.z, x.w, 0, 0};
 }
 
-// What a query row sees and where its result goes.  base: own position of the sequence's query 0; bad: lengths that cannot be.
+// What a query row sees.  base: own position of the sequence's query 0; bad: lengths that cannot be.
 struct Sequence {
     int len, queries, base, bad;
 };
@@ -140,6 +144,13 @@ __device__ __forceinline__ void in_turn() {
 // through a piece of LDS of its own, no barrier); the next 32 are on their way while the present ones are worked on.  `share` waves
 // have the range in turn: 4 or 2, which join at the end through LDS, or 1 where ranges are short and many.  keep: the range is one
 // (the waves of a workgroup meet in the join).
+// 16 rows a tile, since a wave's K in registers serves one matrix instruction of 16 x 16 x 32 each way; two tiles share K, V and their LDS reads
+// where there are more rows (more tiles: O does not fit the registers).  Two workgroups of four waves on a unit have 100 KB of loads on their way.
+// Measured, 8 key heads of 128 features in bf16: 8 sequences of up to 16384 own tokens behind 1000, 338 MB: 70 us, 4.8 TB/s (a large copy: 5.3); 64 of up
+// to 512, 102 MB: 24.6 us, 4.2 TB/s, of which the first loads' latency and unequal lengths take a fifth.  Short ranges are bound by latency, a chain
+// of page number, keys, scores, join and parts: one sequence of 40 tokens behind 512, 6 us; 64 rows a head over 2048 keys, 10.8 us.
+// 24 sequences, 32 heads of 100 features that are not shared, 5 queries each over 300 own tokens and 1500 shared ones, 88 MB: 37 us, 2.4 TB/s, bound by what
+// a wave issues and waits for per step (12 steps of the prefix, 5 of own tokens).
 template <class T, int DP, int MT, bool WHOLE, bool GROUPED>
 __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, bool own, const Sequence& seq, int slot,
                            int share, bool keep, unsigned char* lds) {
@@ -459,6 +470,11 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 // One range of the prefix for 32 * NW query rows, many enough that the matrix cores are what bounds it: K and V of 64 keys (32 where D is
 // over 128) in LDS for all NW waves, which have 32 rows each.  Two buffers: the next keys travel to registers while the present ones are
 // worked on, and are stored behind them; one barrier per step.
+// 32 rows a wave, the matrix instruction's 32 x 32 x 16; 64 would halve the LDS reads, but their O has to live in the accumulation registers, and the
+// copies cost more.  Two waves on a SIMD, so that one's exponentials go beside the other's matrix instructions.
+// Measured, 256 rows a head, 32768 keys, 8 heads of 128 features, bf16, 34 GFLOP: 46 us, 750 TFLOP/s, 55 % of the rate of a large product (and with P
+// in two terms, 52 GFLOP: 57 us, 900).  What bounds it is issue: per 16 keys of 32 rows a SIMD has 8 matrix instructions of 32 cycles and 8 exponentials of
+// 8 each for the two waves apart, with their subtractions, sums and conversions, the LDS reads and the barrier.
 // What the vector units have to do beside the matrix instructions is kept short:
 //   - a wave's load covers GK neighbouring keys, which share their page (the host sees to it): addresses are worked out once per wave;
 //   - O is not multiplied with every new maximum, and maxima are not looked for: m is the largest score of the first step, and weights are powers of
@@ -711,6 +727,7 @@ __global__ void __launch_bounds__(64 * NW, DP > 128 ? NW / 4 : 2) attend_many_ke
 
 // The parts of every row joined.  DP / 4 threads have four features each of a row's part, 2^lanes_log such groups share a row's parts, and
 // the rest of the workgroup has other rows.  A group takes four parts at a time, loads ahead of sums, and the groups meet in LDS.
+// One pass over the parts, bound by memory: 2048 rows of 33 parts of 128 features, 35 MB, 8.4 us, 4.1 TB/s; with few parts by its launch, 2.4 us.
 template <int DP>
 __global__ void __launch_bounds__(256) combine_kernel(const AttendParams p, const int lanes_log) {
     constexpr int PER = DP / 4, GROUPS = 256 / PER;

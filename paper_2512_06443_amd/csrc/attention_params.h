@@ -19,7 +19,7 @@ struct AttendParams {
     void* out;
     int64_t out_sequence, out_token, out_head;
     float* lse;
-    float *part_o, *part_ml;           // [slot][Hk][B n G][D], [slot][Hk][B n G][2]; slots: the prefix' splits, then the own parts'
+    float *part_o, *part_ml;           // [Hk][B n G][slot][D], [Hk][B n G][slot][2]; slots: the prefix' splits, then the own parts'
     float scale_log2;                  // scale * log2(e): exponentials are powers of two
     int out_type;                      // VLUT_TYPE_*
     int B, n, Hk, G, D, page_log, pages;

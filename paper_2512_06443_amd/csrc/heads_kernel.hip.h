@@ -12,6 +12,8 @@ namespace {
 // are only converted); each goes to a tensor or, by the token's slot, into a page.  A workgroup has rows of one kind.
 // A unit is two vectors of VEC features that rotate with each other (or, past R, two neighbouring ones), and a lane has one unit (two
 // of VEC = 1): a pair never leaves its lane, and the only exchange is the sum of squares over the row's 2^lanes_log lanes.
+// Bound by memory: every row is read once and written once, the tables once per token and kind.  4096 tokens, 40 heads of 128 features, fp32 to bf16,
+// 128 MB: 25.9 us, 4.9 TB/s (a large copy: 5.3); 16 heads to a cache, 50 MB: 10.4 us, 4.8 TB/s; one token: 2.5 us, a launch.
 // ---------------------------------------------------------------------------------------------
 struct HeadRows {              // what the rows of one kind (queries, keys, values) are read from and written to; strides in elements
     const void* in;

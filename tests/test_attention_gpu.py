@@ -373,3 +373,26 @@ def test_refusals(B):
         with pytest.raises(B.VlutError) as e:
             call()
         assert e.value.status == status
+
+
+def test_native_and_python_form_agree(B, monkeypatch):
+    """The calls without their native form: the same numbers, to the bit."""
+    if B._native is None:
+        pytest.skip("built with a torch for ROCm only")
+    case = Case(B=3, n=2, Hq=8, Hk=2, D=64, P=100, lens=[5, 40, 2], page=16, queries=[2, 1, 2])
+    x = torch.randn((6, 12, 64), device="cuda")
+    angle = torch.rand((50, 32), device="cuda")
+    rotation = dict(positions=torch.arange(6, device="cuda") * 9, cos=angle.cos(), sin=angle.sin())
+    weight = torch.rand(64, device="cuda")
+
+    def run():
+        k, v = (torch.zeros((2, 2, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        slots = torch.tensor([3, -1, 17, 0, 31, 5], device="cuda")
+        q = B.append_kv(x[:, 8:10], x[:, 10:], slots, k, v, q=x[:, :8], q_weight=weight, k_weight=weight, **rotation)
+        return [q, k, v, *B.norm_rope(x[:, :8], x[:, 8:10], q_weight=weight, dtype=torch.float16, interleaved=True, **rotation),
+                *case.run(B, dtype=torch.float32, want_lse=True, scale=0.3)]
+
+    native = run()
+    monkeypatch.setattr(B, "_native", None)
+    monkeypatch.setattr(B, "_load_native", lambda L: None)
+    assert all(torch.equal(a, b) for a, b in zip(native, run()))
