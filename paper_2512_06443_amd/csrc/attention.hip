@@ -173,13 +173,18 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     a.own_heads_together = neighbours ? (int)Hk : 1;
     a.rows = rows;
     a.DP = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
-    a.own_mt = own_rows <= 16 ? 1 : 2;
+    a.own_mt = own_rows <= 16 || a.DP > 128 ? 1 : 2;        // (of 256 features two tiles' O and queries do not fit the registers)
     // Tiles of 16 or 32 rows whose waves share the keys, or, where the prefix' products are many, a launch of its own with 32 rows a wave.  us, by tiles /
     // that launch (bf16, 8 key heads, 256 rows a head): 128 features, 2048 keys 22 / 27, 4096 29 / 31, 6000 33 / 31, 8192 39 / 38 (512 rows: 2048 keys
-    // 25 / 32, 4096 34 / 35); 64 features, 4096 keys 19 / 23, 8192 26 / 28, 16384 42 / 30; 256 features, 1024 keys 30 / 37, 2048 44 / 39, 4096 69 / 43
-    // (one key head, 800 rows: 4096 keys 34 / 39, 6000 41 / 42, 8192 47 / 44).
-    const int64_t few_products = a.DP > 128 ? 4000000 : 1280000000 / a.DP;
-    a.MT = P == 0 ? a.own_mt : (rows <= 16 ? 1 : (rows <= 64 || !grouped || rows * P * Hk <= few_products ? 2 : 0));
+    // 25 / 32, 4096 34 / 35); 64 features, 4096 keys 19 / 23, 8192 26 / 28, 16384 42 / 30; 256 features, 1024 keys 29 / 37, 2048 46 / 40, 4096 66 / 43
+    // (128 rows: 3900 keys 48 / 41; one key head, 800 rows: 4096 keys 31 / 40, 6000 39 / 43, 8192 48 / 44).
+    const int64_t few_products = a.DP > 128 ? 3500000 : 1280000000 / a.DP;
+    const bool many = P > 0 && rows > 64 && grouped && rows * P * Hk > few_products;
+    // Tiles of 16 where 32 would read less but a step per workgroup is about all there is: us, 32 / 16, 8 key heads of 128: 64 rows a head, 2048 keys, own 512
+    // 16.5 / 15.2; 256 rows, 500 keys, own 100 17.7 / 15.9; 5 key heads, 64 rows, 2048 keys, own 256 13.9 / 12.9.  (64 rows, 8192 keys 22.8 / 23.4; 128
+    // rows, 8192 keys 23.4 / 28.5.)  Of 256 features 32 rows would not fit the registers: 64 rows, 4096 keys 35.6 / 30.3.
+    const bool few_steps = own_rows <= 16 && Hk * ceil_div(rows, 16) * ceil_div(P, 128) + B * Hk * ceil_div(max_own, 128) <= 4 * kUnits;
+    a.MT = many ? 0 : (P == 0 ? a.own_mt : (rows <= 16 || few_steps || a.DP > 128 ? 1 : 2));
     a.waves = a.MT == 0 && a.DP <= 128 && rows > 128 ? 8 : 4;
     a.own_tiles = (int)ceil_div(own_rows, 16 * a.own_mt);
     const int64_t own_units = B * Hk * a.own_tiles;

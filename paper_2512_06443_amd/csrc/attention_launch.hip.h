@@ -51,11 +51,14 @@ int launch_many_terms(const AttendPlan& a, const AttendParams& p, hipStream_t st
 template <class T, int DP, bool WHOLE>
 int launch_attend_w(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
     if (a.MT == 1) return launch_few<T, DP, 1, 1, WHOLE>(a, p, stream);
-    if (a.MT == 2) return a.own_mt == 1 ? launch_few<T, DP, 2, 1, WHOLE>(a, p, stream) : launch_few<T, DP, 2, 2, WHOLE>(a, p, stream);
+    if constexpr (DP <= 128)
+        if (a.MT == 2) return a.own_mt == 1 ? launch_few<T, DP, 2, 1, WHOLE>(a, p, stream) : launch_few<T, DP, 2, 2, WHOLE>(a, p, stream);
     if (a.own_per_xcd > 0) {                   // the sequences' own tokens alone
         AttendParams own = p;
         own.prefix_per_xcd = 0;
-        const int rc = a.own_mt == 1 ? launch_few<T, DP, 1, 1, WHOLE>(a, own, stream) : launch_few<T, DP, 2, 2, WHOLE>(a, own, stream);
+        int rc;
+        if constexpr (DP > 128) rc = launch_few<T, DP, 1, 1, WHOLE>(a, own, stream);
+        else rc = a.own_mt == 1 ? launch_few<T, DP, 1, 1, WHOLE>(a, own, stream) : launch_few<T, DP, 2, 2, WHOLE>(a, own, stream);
         if (rc != VLUT_OK) return rc;
     }
     if constexpr (DP <= 128)
