@@ -20,10 +20,11 @@ using namespace vlut_attention;
 // order (the order of a sum's terms is free as long as V^T has the same), so that P goes from one product to the next without leaving its
 // registers.  V^T is read out of the row-major V in LDS by transposing reads (ds_read_b64_tr_b16: the 16 lanes of a group give the addresses of 4
 // rows x 16 features, and get four rows of one feature each).
-// Scores, m, l and O are fp32.  P is carried to the second product in two terms of the cache's type, rounded and what that left (16 bits of bf16,
-// 22 of fp16): the matrix cores take no fp32, and next to memory the second term costs nothing where rows are few.  Where they are many and the output
-// has 16 bits P has one term: the output's own rounding is as large, and the second would be half as many matrix instructions again (256 rows a
-// head, 8192 keys, 8 heads: 46 us and 57).  l sums P before any rounding.
+// Scores, m, l and O are fp32, and l sums P before any rounding.  The matrix cores take no fp32, so that P is carried to the second product in terms of
+// the cache's type, each what the rounding of those before it left.  For outputs of 16 bits: two (16 bits of bf16, 22 of fp16), and one where rows are
+// many, since the second is half as many matrix instructions again (256 rows a head, 32768 keys, 8 heads: 46 us and 57) for what the output's own
+// rounding is as large as.  For fp32: what carries 24 bits of bf16, three, where rows are few (64 sequences of 8 key heads behind 4096: 31.7 us and 34.2;
+// bound by memory or latency no difference), and two where they are many, 2e-6 of the result, of which the sums' own roundings are the larger part.
 // fp16: P is lifted by a power of two (Number::kLift), since weights below 2^-14 would lose bits and those below 2^-25 everything.
 // ---------------------------------------------------------------------------------------------
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -42,6 +43,7 @@ struct Number<__bf16> {
     static constexpr unsigned kExponents = 0x7f807f80u, kNan = 0x7fc07fc0u;
     static constexpr bool kWide = true;               // weights may be as large as fp32's
     static constexpr float kLift = 0.0f;
+    static constexpr int kTerms = 3;                  // that carry 24 bits
 };
 template <>
 struct Number<_Float16> {
@@ -49,6 +51,7 @@ struct Number<_Float16> {
     static constexpr unsigned kExponents = 0x7c007c00u, kNan = 0x7e007e00u;
     static constexpr bool kWide = false;
     static constexpr float kLift = 14.0f;             // weights are up to 2^14, so that those of 2^-38 of the largest are no zeros yet
+    static constexpr int kTerms = 2;
 };
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ f32x4 mfma16(Number<__bf16>::x8 a, Number<__bf16>::x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -151,7 +154,7 @@ __device__ __forceinline__ void in_turn() {
 // of page number, keys, scores, join and parts: one sequence of 40 tokens behind 512, 6 us; 64 rows a head over 2048 keys, 10.8 us.
 // 24 sequences, 32 heads of 100 features that are not shared, 5 queries each over 300 own tokens and 1500 shared ones, 88 MB: 37 us, 2.4 TB/s, bound by what
 // a wave issues and waits for per step (12 steps of the prefix, 5 of own tokens).
-template <class T, int DP, int MT, bool WHOLE, bool GROUPED>
+template <class T, int DP, int MT, int TERMS, bool WHOLE, bool GROUPED>
 __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, bool own, const Sequence& seq, int slot,
                            int share, bool keep, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
@@ -307,7 +310,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                     }
         }
         if constexpr (more.value) load_k(kt + stride, next_page);
-        x8 pf[MT], pf_rest[MT];
+        x8 pf[MT][TERMS];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             if (some_masked) {
@@ -331,8 +334,12 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
                 for (int i = 0; i < 4; ++i) {
                     const float e = exp2_fast(__builtin_fmaf(s[mt][t][i], p.scale_log2, -shift));
                     l[mt] += e;
-                    pf[mt][4 * t + i] = (T)e;
-                    pf_rest[mt][4 * t + i] = (T)(e - (float)(T)e);
+                    float left = e;
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) {
+                        pf[mt][k][4 * t + i] = (T)left;
+                        left -= (float)(T)left;
+                    }
                 }
 #pragma unroll
             for (int dt = 0; dt < DP / 16; ++dt) o[mt][dt] *= factor;
@@ -343,7 +350,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) *(T*)(mine + (16 * (e >> 2) + 4 * grp + (e & 3)) * PITCH + 2 * DP + 2 * l16) = pf[mt][e];
+                for (int e = 0; e < 8; ++e) *(T*)(mine + (16 * (e >> 2) + 4 * grp + (e & 3)) * PITCH + 2 * DP + 2 * l16) = pf[mt][0][e];
                 __builtin_amdgcn_wave_barrier();
                 for (int key = 0; key < kFewKeys && kt + key < end_key; ++key) {
                     const bool seen = kt + key < limit[mt];
@@ -374,12 +381,11 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
             const s16x4 v0 = lds_read_transposed(at), v1 = lds_read_transposed(at + 16 * PITCH);
             const x8 vf = __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                o[mt][dt] = mfma16(vf, pf[mt], o[mt][dt]);
-                o[mt][dt] = mfma16(vf, pf_rest[mt], o[mt][dt]);
-            }
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) o[mt][dt] = mfma16(vf, pf[mt][k], o[mt][dt]);
         }
-        in_turn<DP / 16, 2 * MT, 2, 4, 0, 0>();
+        in_turn<DP / 16, TERMS * MT, 2, 4, 0, 0>();
         if constexpr (more.value) {
             page = next_page;
             next_page = page_after;
@@ -686,7 +692,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
 
 // Few rows: ranges of the prefix for 16 * MT rows, and of the sequences' own tokens for 16 * OWN.  WHOLE: D is DP.  GROUPED: 16 keys share a page.
 // Workgroups go to the 8 XCDs in turn; those of one range, which differ in their rows alone, are given to one XCD (one L2).
-template <class T, int DP, int MT, int OWN, bool WHOLE, bool GROUPED>
+template <class T, int DP, int MT, int OWN, int TERMS, bool WHOLE, bool GROUPED>
 __global__ void __launch_bounds__(256, few_waves(DP, MT)) attend_few_kernel(const AttendParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     const int xcd = (int)blockIdx.x & 7, place = (int)blockIdx.x >> 3;
@@ -695,7 +701,7 @@ __global__ void __launch_bounds__(256, few_waves(DP, MT)) attend_few_kernel(cons
         const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
         if (h >= p.Hk) return;
         const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
-        attend_few<T, DP, MT, WHOLE, GROUPED>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, 4, true, lds);
+        attend_few<T, DP, MT, TERMS, WHOLE, GROUPED>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, 4, true, lds);
         return;
     }
     // Sequences differ in length, so that their ranges go round the XCDs; the tiles of a range stay together, and the heads of a token where they are
@@ -710,7 +716,7 @@ __global__ void __launch_bounds__(256, few_waves(DP, MT)) attend_few_kernel(cons
     const int steps = (seq.len + p.own_step - 1) / p.own_step, per = (steps + p.own_splits - 1) / p.own_splits, nG = p.n * p.G;
     const int seen = seq.base + (min((tile + 1) * 16 * OWN, nG) - 1) / p.G + 1;          // by the tile's last query
     const int first = min(split * per * p.own_step, seq.len), end = keep ? min(min(first + per * p.own_step, seq.len), max(first, seen)) : first;
-    attend_few<T, DP, OWN, WHOLE, GROUPED>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq,
+    attend_few<T, DP, OWN, TERMS, WHOLE, GROUPED>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq,
                                            p.prefix_splits + split, p.own_share, keep, lds);
 }
 

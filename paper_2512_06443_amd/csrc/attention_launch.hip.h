@@ -24,17 +24,22 @@ bool allow_lds(const void* kfn, int bytes, std::atomic<unsigned>& done_mask) {
     return true;
 }
 
-template <class T, int DP, int MT, int OWN, bool WHOLE, bool GROUPED>
+template <class T, int DP, int MT, int OWN, int TERMS, bool WHOLE, bool GROUPED>
 int launch_few_t(const AttendParams& p, hipStream_t stream) {
     static std::atomic<unsigned> done{0};
     constexpr int lds = few_lds(DP);
-    auto kfn = attend_few_kernel<T, DP, MT, OWN, WHOLE, GROUPED>;
+    auto kfn = attend_few_kernel<T, DP, MT, OWN, TERMS, WHOLE, GROUPED>;
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
     return launch(kfn, dim3(8u * (unsigned)(p.prefix_per_xcd + p.own_per_xcd)), 256, lds, stream, p);
 }
+template <class T, int DP, int MT, int OWN, int TERMS, bool WHOLE>
+int launch_few_terms(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+    return a.grouped ? launch_few_t<T, DP, MT, OWN, TERMS, WHOLE, true>(p, stream) : launch_few_t<T, DP, MT, OWN, TERMS, false, false>(p, stream);
+}
 template <class T, int DP, int MT, int OWN, bool WHOLE>
 int launch_few(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
-    return a.grouped ? launch_few_t<T, DP, MT, OWN, WHOLE, true>(p, stream) : launch_few_t<T, DP, MT, OWN, false, false>(p, stream);
+    if (p.out_type == VLUT_TYPE_F32) return launch_few_terms<T, DP, MT, OWN, Number<T>::kTerms, WHOLE>(a, p, stream);
+    return launch_few_terms<T, DP, MT, OWN, 2, WHOLE>(a, p, stream);
 }
 template <class T, int DP, int NW, int TERMS, bool WHOLE>
 int launch_many(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
