@@ -151,7 +151,7 @@ __device__ __forceinline__ void in_turn() {
 // where there are more rows (more tiles: O does not fit the registers).  Two workgroups of four waves on a unit have 100 KB of loads on their way.
 // Measured, 8 key heads of 128 features in bf16: 8 sequences of up to 16384 own tokens behind 1000, 338 MB: 70 us, 4.8 TB/s (a large copy: 5.3); 64 of up
 // to 512, 102 MB: 24.6 us, 4.2 TB/s, of which the first loads' latency and unequal lengths take a fifth.  Short ranges are bound by latency, a chain
-// of page number, keys, scores, join and parts: one sequence of 40 tokens behind 512, 6 us; 64 rows a head over 2048 keys, 10.8 us.
+// of page number, keys, scores, join and parts: one sequence of 40 tokens behind 512, 6 us; 16 of 256 behind 2048, 9.7 us.
 // 24 sequences, 32 heads of 100 features that are not shared, 5 queries each over 300 own tokens and 1500 shared ones, 88 MB: 37 us, 2.4 TB/s, bound by what
 // a wave issues and waits for per step (12 steps of the prefix, 5 of own tokens).
 template <class T, int DP, int MT, int TERMS, bool WHOLE, bool GROUPED>
