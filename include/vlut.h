@@ -473,7 +473,8 @@ int vlut_append_kv(const vlut_heads* k, const vlut_heads* v, const vlut_heads* q
  * D: a multiple of four, 8 <= D <= VLUT_MAX_HEAD_FEATURES, and q, k, v and 16-bit outputs have even strides and dword-aligned data
  * (VLUT_ERR_UNSUPPORTED otherwise).  Lengths out of range and page numbers outside the cache are found on the device: they read nothing, and
  * the queries that depend on them get NaN.
- * vlut_query_shared_prefix_attention: out4 (host) = { query rows per workgroup, parts of the prefix, parts of an own sequence, workgroups }.
+ * vlut_query_shared_prefix_attention: out4 (host) = { query rows per workgroup, parts of the prefix, parts of an own sequence, workgroups }, for a cache
+ * whose pages hold 16 tokens or more and whose heads' rows are apart in memory; vlut_shared_prefix_attention_bytes is enough for any cache.
  */
 size_t vlut_shared_prefix_attention_bytes(int64_t B, int64_t n, int64_t q_heads, int64_t k_heads, int64_t D, int64_t prefix_len, int64_t max_own_len);
 int vlut_query_shared_prefix_attention(int64_t B, int64_t n, int64_t q_heads, int64_t k_heads, int64_t D, int64_t prefix_len, int64_t max_own_len, int* out4);
