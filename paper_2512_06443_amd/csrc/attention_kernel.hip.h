@@ -21,9 +21,9 @@ using namespace vlut_attention;
 // registers.  V^T is read out of the row-major V in LDS by transposing reads (ds_read_b64_tr_b16: the 16 lanes of a group give the addresses of 4
 // rows x 16 features, and get four rows of one feature each).
 // Scores, m, l and O are fp32, and l sums P before any rounding.  The matrix cores take no fp32, so that P is carried to the second product in terms of
-// the cache's type, each what the rounding of those before it left.  For outputs of 16 bits: two (16 bits of bf16, 22 of fp16), and one where rows are
-// many, since the second is half as many matrix instructions again (256 rows a head, 32768 keys, 8 heads: 46 us and 57) for what the output's own
-// rounding is as large as.  For fp32: what carries 24 bits of bf16, three, where rows are few (64 sequences of 8 key heads behind 4096: 31.7 us and 34.2;
+// the cache's type, each what the rounding of those before it left.  For outputs of 16 bits: two (16 bits of bf16, 22 of fp16), so that the output's own
+// rounding is what is left.  One would save half as many matrix instructions again where rows are many (256 rows a head, 32768 keys, 8 heads: 46 us and 57),
+// and be 40 % further off.  For fp32: what carries 24 bits of bf16, three, where rows are few (64 sequences of 8 key heads behind 4096: 31.7 us and 34.2;
 // bound by memory or latency no difference), and two where they are many, 2e-6 of the result, of which the sums' own roundings are the larger part.
 // fp16: P is lifted by a power of two (Number::kLift), since weights below 2^-14 would lose bits and those below 2^-25 everything.
 // ---------------------------------------------------------------------------------------------

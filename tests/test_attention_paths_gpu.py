@@ -1,0 +1,120 @@
+"""shared_prefix_attention on each of its paths: what one of them could lose and another keep.
+
+A path is the kernel and the tile that a call's sizes lead to; every case says which one it is for and finds that it runs."""
+from __future__ import annotations
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from test_attention_gpu import U, U32, Case  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B(vlut_lib_path):
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2512_06443_amd import binding
+    binding.lib()
+    return binding
+
+
+BF16, F16 = torch.bfloat16, torch.float16
+
+# Rows of a workgroup (16, 32: waves that share a tile; 128, 256: a launch of its own for the prefix, four or eight waves of 32) -> sizes.
+PATHS = {
+    "16_d64": (16, dict(B=4, n=1, Hq=8, Hk=2, D=64, P=700, lens=[3, 0, 40, 9], page=16)),
+    "16_d128": (16, dict(B=1, n=1, Hq=4, Hk=1, D=128, P=900, lens=[70], page=64)),
+    "16_d200": (16, dict(B=9, n=1, Hq=8, Hk=2, D=200, P=1000, lens=[1] * 9, page=16)),
+    "16_pages_of_4": (16, dict(B=4, n=1, Hq=8, Hk=2, D=96, P=700, lens=[3, 0, 40, 9], page=4)),
+    "32_d64": (32, dict(B=16, n=1, Hq=32, Hk=8, D=64, P=4200, lens=[5 * i for i in range(16)], page=16)),
+    "32_d100": (32, dict(B=16, n=1, Hq=32, Hk=8, D=100, P=4200, lens=[5 * i for i in range(16)], page=32)),
+    "32_d128": (32, dict(B=8, n=2, Hq=32, Hk=8, D=128, P=4321, lens=[40, 2, 3, 70, 100, 31, 32, 33], page=16)),
+    "32_drafts_d128": (32, dict(B=2, n=9, Hq=8, Hk=2, D=128, P=333, lens=[9, 77], page=16)),
+    "128_d64": (128, dict(B=32, n=1, Hq=32, Hk=8, D=64, P=19600, lens=[3] * 32, page=16)),
+    "128_d100": (128, dict(B=24, n=1, Hq=32, Hk=8, D=100, P=13100, lens=[3] * 24, page=32)),
+    "128_d132": (128, dict(B=33, n=1, Hq=16, Hk=4, D=132, P=7001, lens=[3] * 33, page=16)),
+    "128_d256": (128, dict(B=40, n=1, Hq=16, Hk=4, D=256, P=5600, lens=[3] * 40, page=16)),
+    "256_d64": (256, dict(B=41, n=1, Hq=16, Hk=2, D=64, P=31999, lens=[1] * 41, page=128)),
+    "256_d100": (256, dict(B=21, n=2, Hq=32, Hk=8, D=100, P=7501, lens=[2] * 21, page=32)),
+    "256_d128": (256, dict(B=40, n=1, Hq=32, Hk=8, D=128, P=7950, lens=[4] * 40, page=16)),
+}
+
+
+def path(B, name, dtype, **more) -> Case:
+    rows, sizes = PATHS[name]
+    case = Case(**sizes, dtype=dtype, **more)
+    got = B.query_shared_prefix_attention(*case.shape, case.P, case.table.shape[1] * case.page)
+    assert got[0] == rows
+    print(name, dtype, got, flush=True)
+    return case
+
+
+def per_key_head(case, x):
+    """[B][n][Hq][...] -> [Hk][rows of it][...] in 64 bits."""
+    Bn, n, Hq, Hk, _ = case.shape
+    return x.double().unflatten(2, (Hk, Hq // Hk)).movedim(2, 0).flatten(1, 3)
+
+
+def sharp_weights(case, rest=-25.0):
+    """Queries and keys of one feature: scores are single products and exact.  Every feature of V has two keys of its own, whose weights are
+    e^-2 to 1 (and cancel in the odd features); all other keys are `rest`, too low to count, but for one of -9 in 32, ahead of the others, from which the
+    largest score of any range's first keys is no further than what 32 bits' scores tell exactly.  Own tokens: `rest`."""
+    Bn, n, Hq, Hk, D = case.shape
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    case.q.zero_()
+    case.q[..., 0] = 1 + torch.randint(0, 8, (Bn, n, Hq), generator=gen, device="cuda") / 128
+    k, v = case.prefix
+    k.zero_()
+    v.zero_()
+    k[:, :, 0] = rest
+    k[::32, :, 0] = -9.0
+    for own in case.own:
+        own[0].zero_()
+        own[0][:, :, 0] = rest
+        own[1].zero_()
+    for h in range(Hk):
+        at = torch.randperm(case.P, generator=gen, device="cuda")[:2 * D]
+        at = torch.where(at % 32 == 0, at + 1, at).clamp_(max=case.P - 1).unique()
+        at = at[:at.numel() // 2 * 2]
+        a, b = at[0::2], at[1::2]
+        k[at, h, 0] = (-2 * torch.rand(at.numel(), generator=gen, device="cuda")).to(k.dtype)
+        f = torch.arange(a.numel(), device="cuda")
+        x = (1 + torch.rand(a.numel(), generator=gen, device="cuda")).to(v.dtype)
+        v[a, h, f] = x
+        odd = f % 2 == 1
+        v[b[odd], h, f[odd]] = -x[odd]
+    case.write()
+
+
+def formula(case):
+    """Of the prefix alone, per key head in 64 bits: (output, sum of the terms' magnitudes, log of the sum of exponentials); scale 1, scores of feature 0."""
+    q = per_key_head(case, case.q)[..., 0]
+    k, v = (x.double().transpose(0, 1) for x in case.prefix)
+    outs = []
+    for h in range(case.shape[3]):
+        s = q[h][:, None] * k[h][None, :, 0]
+        w = torch.softmax(s, -1)
+        outs.append((w @ v[h], w @ v[h].abs(), torch.logsumexp(s, -1)))
+    return [torch.stack(x) for x in zip(*outs)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("name", list(PATHS))
+def test_weights_keep_their_bits_for_outputs_of_16_bits(B, name, dtype):
+    """out * exp(lse), of which the sum of weights cancels, is off by its output's rounding and by 2^-16 (two terms of bf16; fp16 less) of its terms'
+    magnitudes for the weights; by 2^-18 of those at most for all else: scores times log2(e) above a maximum within 16 (2^-20.5), an exponential (2^-23), sums of
+    two keys' terms (six additions, 2^-21), parts joined (2^-21), lse (2^-20.5).  One term of bf16 alone would be 2^-9."""
+    case = path(B, name, dtype)
+    sharp_weights(case)
+    out, lse = case.run(B, scale=1.0, want_lse=True)
+    want, size, want_lse = formula(case)
+    got, got_lse = per_key_head(case, out), per_key_head(case, lse)
+    factor = (got_lse - want_lse).exp()[..., None]
+    off = (got * factor - want).abs()
+    tiny = 2.0 ** -24 if dtype == F16 else 1e-38                          # outputs below fp16's normal range
+    bound = want.abs() * U[dtype] * 1.01 + size * (2.0 ** -16 + 2.0 ** -18) + tiny
+    assert (off / bound).max().item() <= 1.0
