@@ -460,8 +460,7 @@ int vlut_append_kv(const vlut_heads* k, const vlut_heads* v, const vlut_heads* q
  * values that a query does not see have no influence on it, NaN and infinities included.
  *   q, out            B * n tokens: token j of sequence b at b * sequence_stride + j * token_stride; q of the cache's type, out of that type or
  *                     fp32.  Scores, sums and partial results are fp32; softmax weights go to the product with V in terms of the cache's type, each
- *                     what the rounding of those before it left: for fp32 outputs three of bf16 or two of fp16 (with many query rows two of
- *                     either), for 16-bit outputs two.
+ *                     what the rounding of those before it left: for fp32 outputs three of bf16 or two of fp16, for 16-bit outputs two.
  *   prefix_pages      dev, ceil(prefix_len / page_size) pages of the prefix (may be NULL for prefix_len 0)
  *   page_table        dev [B][table_stride]: pages of each sequence's own tokens, own token 0 first in page 0 (may be NULL for max_own_len 0);
  *                     ceil(max_own_len / page_size) of each row are valid where own_lens reaches them

@@ -22,9 +22,10 @@ using namespace vlut_attention;
 // rows x 16 features, and get four rows of one feature each).
 // Scores, m, l and O are fp32, and l sums P before any rounding.  The matrix cores take no fp32, so that P is carried to the second product in terms of
 // the cache's type, each what the rounding of those before it left.  For outputs of 16 bits: two (16 bits of bf16, 22 of fp16), so that the output's own
-// rounding is what is left.  One would save half as many matrix instructions again where rows are many (256 rows a head, 32768 keys, 8 heads: 46 us and 57),
-// and be 40 % further off.  For fp32: what carries 24 bits of bf16, three, where rows are few (64 sequences of 8 key heads behind 4096: 31.7 us and 34.2;
-// bound by memory or latency no difference), and two where they are many, 2e-6 of the result, of which the sums' own roundings are the larger part.
+// rounding is what is left.  For fp32: what carries 24 bits of bf16, three, or two of fp16.  A caller gets the same bits from either kernel.  A term more is
+// half as many matrix instructions again where rows are many: 256 rows a head, 32768 keys, 8 heads 46 us with one, 57 with two (one would leave bf16 outputs 40 %
+// further off); 1024 rows a head, 8192 keys 57 with two, 71 with three (two would leave fp32 outputs 2.4e-6 of the result off instead of 4e-7).  Where rows are
+// few, bound by memory or latency: 64 sequences of 8 key heads behind 4096 31.7 us with two, 34.2 with three.
 // fp16: P is lifted by a power of two (Number::kLift), since weights below 2^-14 would lose bits and those below 2^-25 everything.
 // ---------------------------------------------------------------------------------------------
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -622,14 +623,17 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
             if constexpr (!WIDE) over |= largest() > m + 15.0f;              // (no branch here)
             const float shift = m == -__builtin_inff() ? 0.0f : m;
             // Sixteen keys at a time; the weights and V of the next are made and read while the matrix cores are on these.
-            x8 vf[DP / 32], pf, rest, next, next_rest;
-            auto weigh = [&](int st, x8& w, x8& w_rest) {
+            x8 vf[DP / 32], pf[TERMS], next[TERMS];
+            auto weigh = [&](int st, x8 (&w)[TERMS]) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float e = exp2_fast(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], p.scale_log2, -shift));
-                    l += e;
-                    w[i] = (T)e;
-                    if constexpr (TERMS > 1) w_rest[i] = (T)(e - (float)(T)e);
+                    float left = exp2_fast(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], p.scale_log2, -shift));
+                    l += left;
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) {
+                        w[k][i] = (T)left;
+                        left -= (float)(T)left;
+                    }
                 }
             };
             auto read_v = [&](int st, int dt) {
@@ -638,20 +642,21 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
             };
 #pragma unroll
             for (int dt = 0; dt < DP / 32; ++dt) vf[dt] = read_v(0, dt);
-            weigh(0, pf, rest);
+            weigh(0, pf);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int st = 0; st < 2 * KT; ++st) {
-                if (st + 1 < 2 * KT) weigh(st + 1, next, next_rest);
+                if (st + 1 < 2 * KT) weigh(st + 1, next);
 #pragma unroll
                 for (int dt = 0; dt < DP / 32; ++dt) {
-                    o[dt] = mfma32(vf[dt], pf, o[dt]);
-                    if constexpr (TERMS > 1) o[dt] = mfma32(vf[dt], rest, o[dt]);
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) o[dt] = mfma32(vf[dt], pf[k], o[dt]);
                     if (st + 1 < 2 * KT) vf[dt] = read_v(st + 1, dt);
                 }
-                pf = next;
-                rest = next_rest;
-                in_turn<(DP / 32) * TERMS, 1, 2 / TERMS, 0, (TERMS > 1 ? 40 : 20) / (DP / 32) / TERMS, 8 / (DP / 32) / TERMS>();
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) pf[k] = next[k];
+                if constexpr (TERMS == 2) in_turn<(DP / 32) * 2, 1, 1, 0, 20 / (DP / 32), 4 / (DP / 32)>();
+                else in_turn<DP / 32, TERMS, 2, 0, 20 * TERMS / (DP / 32), 8 / (DP / 32)>();
                 __builtin_amdgcn_sched_barrier(0);
             }
         });

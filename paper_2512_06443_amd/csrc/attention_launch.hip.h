@@ -49,6 +49,11 @@ int launch_many(const AttendPlan& a, const AttendParams& p, hipStream_t stream) 
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
     return launch(kfn, dim3(8u * (unsigned)a.prefix_per_xcd), 64 * NW, lds, stream, p);
 }
+template <class T, int DP, int NW, bool WHOLE>
+int launch_many_terms(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
+    if (p.out_type == VLUT_TYPE_F32) return launch_many<T, DP, NW, Number<T>::kTerms, WHOLE>(a, p, stream);
+    return launch_many<T, DP, NW, 2, WHOLE>(a, p, stream);
+}
 template <class T, int DP, bool WHOLE>
 int launch_attend_w(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
     if (a.MT == 1) return launch_few<T, DP, 1, 1, WHOLE>(a, p, stream);
@@ -63,8 +68,8 @@ int launch_attend_w(const AttendPlan& a, const AttendParams& p, hipStream_t stre
         if (rc != VLUT_OK) return rc;
     }
     if constexpr (DP <= 128)
-        if (a.waves == 8) return launch_many<T, DP, 8, 2, WHOLE>(a, p, stream);
-    return launch_many<T, DP, 4, 2, WHOLE>(a, p, stream);
+        if (a.waves == 8) return launch_many_terms<T, DP, 8, WHOLE>(a, p, stream);
+    return launch_many_terms<T, DP, 4, WHOLE>(a, p, stream);
 }
 template <class T, int DP>
 int launch_attend_d(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {

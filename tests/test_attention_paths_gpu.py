@@ -118,3 +118,18 @@ def test_weights_keep_their_bits_for_outputs_of_16_bits(B, name, dtype):
     tiny = 2.0 ** -24 if dtype == F16 else 1e-38                          # outputs below fp16's normal range
     bound = want.abs() * U[dtype] * 1.01 + size * (2.0 ** -16 + 2.0 ** -18) + tiny
     assert (off / bound).max().item() <= 1.0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("name", list(PATHS))
+def test_weights_keep_their_bits_for_outputs_of_fp32(B, name, dtype):
+    """The same for fp32 outputs: weights in three terms of bf16 (2^-24) or two of fp16 (2^-22), 1.2 * 2^-19 of the terms' magnitudes with all else.
+    Two terms of bf16 would be 2^-18 off at most, which so many weights come near."""
+    case = path(B, name, dtype)
+    sharp_weights(case)
+    out, lse = case.run(B, scale=1.0, dtype=torch.float32, want_lse=True)
+    want, size, want_lse = formula(case)
+    got, got_lse = per_key_head(case, out), per_key_head(case, lse)
+    off = (got * (got_lse - want_lse).exp()[..., None] - want).abs()
+    worst = (off / (want.abs() * U32 + size * (1.2 * 2.0 ** -19) + 1e-38)).max().item()
+    assert worst <= 1.0
