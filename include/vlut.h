@@ -456,8 +456,8 @@ int vlut_append_kv(const vlut_heads* k, const vlut_heads* v, const vlut_heads* q
  * Attention of B sequences with n query tokens each, over a paged cache whose first prefix_len tokens they share.  Query j (of the last
  * query_lens[b] of sequence b's own_lens[b] own tokens) sees the whole prefix and the own tokens 0 .. own_lens[b] - query_lens[b] + j:
  *   out[b][j][h] = sum_t softmax_t(scale * q[b][j][h] . k[t][h / G]) v[t][h / G],   G = query heads / key heads.
- * The prefix is worked on once for all sequences.  A query that sees nothing, and queries from query_lens[b] on, get 0 (and lse -inf).  Keys and
- * values that a query does not see have no influence on it, NaN and infinities included.
+ * The prefix is worked on once for all sequences.  A query that sees nothing, or nothing but keys that score -inf, and queries from query_lens[b] on,
+ * get 0 (and lse -inf).  Keys and values that a query does not see have no influence on it, NaN and infinities included.
  *   q, out            B * n tokens: token j of sequence b at b * sequence_stride + j * token_stride; q of the cache's type, out of that type or
  *                     fp32.  Scores, sums and partial results are fp32; softmax weights go to the product with V in terms of the cache's type, each
  *                     what the rounding of those before it left: for fp32 outputs three of bf16 or two of fp16, for 16-bit outputs two.

@@ -486,7 +486,8 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 //   - a wave's load covers GK neighbouring keys, which share their page (the host sees to it): addresses are worked out once per wave;
 //   - O is not multiplied with every new maximum, and maxima are not looked for: m is the largest score of the first step, and weights are powers of
 //     two of the scores above it.  Where that does not do (bf16: the sum of weights shows one of 2^40 or so; fp16, whose weights have to stay
-//     below 2^15: a maximum per step shows one) the range is begun again with the largest of all its scores, which a sweep over K finds.
+//     below 2^15: a maximum per step shows one; a first step whose scores are all -inf, which says nothing of the others) the range is begun again with the
+//     largest of all its scores, which a sweep over K finds.
 //     (Multiplying where it is needed, in a branch, costs as much as always: O's registers are copied where the ways meet.)
 template <class T, int DP, int TERMS, int NW, bool WHOLE>
 __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, int slot, unsigned char* lds) {
@@ -660,7 +661,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
                 __builtin_amdgcn_sched_barrier(0);
             }
         });
-        if constexpr (WIDE) over = !(l < 0x1p40f);             // (O of values up to 2^88 has room then)
+        if constexpr (WIDE) over = !(l < 0x1p40f) || m == -__builtin_inff();             // (O of values up to 2^88 has room then)
         if (over) *again = 1;
         __syncthreads();
         if (!*again || known) break;

@@ -3,6 +3,8 @@
 A path is the kernel and the tile that a call's sizes lead to; every case says which one it is for and finds that it runs."""
 from __future__ import annotations
 
+import copy
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -133,3 +135,44 @@ def test_weights_keep_their_bits_for_outputs_of_fp32(B, name, dtype):
     off = (got * (got_lse - want_lse).exp()[..., None] - want).abs()
     worst = (off / (want.abs() * U32 + size * (1.2 * 2.0 ** -19) + 1e-38)).max().item()
     assert worst <= 1.0
+
+
+def check_without(case, hidden, out, lse):
+    """The formula without the keys `hidden` [P] of the prefix."""
+    seen = copy.copy(case)
+    seen.prefix = tuple(x[~hidden] for x in case.prefix)
+    seen.P = seen.prefix[0].shape[0]
+    seen.check(out, lse.cpu(), only=[0, case.shape[0] - 1])
+
+
+def range_of(B, case):
+    """Keys of one part of the prefix, where the prefix has a launch of its own (a multiple of 64, or of 32 over 128 features)."""
+    keys, parts = 64 if case.shape[4] <= 128 else 32, B.query_shared_prefix_attention(*case.shape, case.P, case.table.shape[1] * case.page)[1]
+    return -(-(-(-case.P // parts)) // keys) * keys
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("name", list(PATHS))
+@pytest.mark.parametrize("where", ["one_range", "every_range", "all_but_one", "all"])
+def test_keys_of_minus_infinity_count_for_nothing(B, name, dtype, where):
+    """Keys that score -inf in front of others: of the first part alone, of every part, everywhere but at one key, everywhere.  The others as they come,
+    and so low (-375 and below) that they would be nothing above any other reference than their own."""
+    for low in (False, True):
+        case = path(B, name, dtype)
+        at, part = torch.arange(case.P, device="cuda"), range_of(B, case)
+        hidden = {"one_range": at < 70, "every_range": at % part < 70, "all_but_one": at != case.P - 9, "all": at >= 0}[where]
+        case.q[..., 0] = 1
+        if low:
+            case.prefix[0][..., 0] = -375 * case.shape[4] ** 0.5
+            for own in case.own:
+                own[0][..., 0] = -375 * case.shape[4] ** 0.5
+        # (by an infinite key, and, in bf16, by its lowest value, whose product passes 32 bits)
+        case.prefix[0][hidden, :, 0] = float("-inf")
+        if dtype == BF16 and not low:
+            case.q[..., 0] = 4
+            case.prefix[0][hidden, :, 0] = torch.finfo(BF16).min
+        case.write()
+        for kind in (torch.float32, None):
+            out, lse = case.run(B, dtype=kind, want_lse=True)
+            assert out.isfinite().all()
+            check_without(case, hidden, out, lse)
