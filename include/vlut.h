@@ -458,8 +458,10 @@ int vlut_append_kv(const vlut_heads* k, const vlut_heads* v, const vlut_heads* q
  *   out[b][j][h] = sum_t softmax_t(scale * q[b][j][h] . k[t][h / G]) v[t][h / G],   G = query heads / key heads.
  * The prefix is worked on once for all sequences.  A query that sees nothing, or nothing but keys that score -inf, and queries from query_lens[b] on,
  * get 0 (and lse -inf).  Keys and values that a query does not see have no influence on it, NaN and infinities included.
+ * An infinite value that a query sees makes that feature of its output infinite; NaN with infinities of both signs, where the key's score is -inf, and
+ * where the key's part of the sum is below 2^-126 of the largest.
  *   q, out            B * n tokens: token j of sequence b at b * sequence_stride + j * token_stride; q of the cache's type, out of that type or
- *                     fp32.  Scores, sums and partial results are fp32; softmax weights go to the product with V in terms of the cache's type, each
+ *                     fp32, apart from q.  Scores, sums and partial results are fp32; softmax weights go to the product with V in terms of the cache's type, each
  *                     what the rounding of those before it left: for fp32 outputs three of bf16 or two of fp16, for 16-bit outputs two.
  *   prefix_pages      dev, ceil(prefix_len / page_size) pages of the prefix (may be NULL for prefix_len 0)
  *   page_table        dev [B][table_stride]: pages of each sequence's own tokens, own token 0 first in page 0 (may be NULL for max_own_len 0);

@@ -144,6 +144,130 @@ __device__ __forceinline__ void in_turn() {
 #endif
 }
 
+// An infinity or NaN: a number, either of two.
+template <class T>
+__device__ __forceinline__ bool has_odd(unsigned x) {
+    constexpr unsigned high = Number<T>::kExponents & 0xffff0000u, low = Number<T>::kExponents & 0xffffu;
+    return ((x & high) == high) | ((x & low) == low);
+}
+__device__ __forceinline__ bool is_odd(float x) { return !(fabsf(x) < __builtin_inff()); }
+
+// The kernel's parameters, its first argument, read again: as the reference that the loops have they would wait in registers throughout.
+__device__ __forceinline__ const AttendParams& parameters() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    auto at = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(const AttendParams*)at;
+#else
+    static AttendParams none;
+    return none;
+#endif
+}
+// Infinite values that a row sees.  P's further terms are zero or negative, so that their products with an infinity are NaN or the other infinity, and the
+// sum is NaN where the formula has that infinity.  A part (or result) that came out as no number although its weights are numbers is therefore settled by the
+// wave that stored it: its rows (bits of `rows`, from row0 on) get, in the features concerned, the sum of the infinities and NaN among the values of the range's
+// keys that they see, with weights of 1, or 0 for a score of -inf.  (Where there are none, finite values passed 32 bits: NaN.)
+// It reads V once more, and keys and queries where it finds such values, straight from memory and after everything else, so that it takes nothing from the
+// loops: a look at their results, 0.2 us of 12.3 for 16 sequences of 256 behind 2048, nothing that shows where ranges are longer.
+template <class T, int DP>
+__device__ void settle_odd(const int32_t* pages, int h, int first_key, int end_key, int row0, unsigned rows, bool own, const Sequence& seq, int slot) {
+    constexpr int F = DP / 64, AHEAD = 8;                          // features of a lane; keys at a time
+    const AttendParams& p = parameters();
+    for (int* x : {&h, &first_key, &end_key, &row0, &slot}) {      // (or what is worked out from these waits in registers too)
+        *x = __builtin_amdgcn_readfirstlane(*x);
+        arrived_scalar(*x);
+    }
+    const int lane = (int)threadIdx.x & 63, d = F * lane, nG = p.n * p.G, mask = (1 << p.page_log) - 1;
+    const bool has = d < p.D;
+    __threadfence();                                               // (other lanes have stored the results)
+    struct Row {
+        int b, j, head;
+    };
+    auto row_at = [&](int row) {
+        const int b = row / nG, in_seq = row - b * nG, j = in_seq / p.G;
+        return Row{b, j, h * p.G + in_seq - j * p.G};
+    };
+    auto result = [&](int row) -> int64_t {
+        if (!p.direct) return (((int64_t)h * p.rows + row) * (p.prefix_splits + p.own_splits) + slot) * p.D + d;
+        const Row r = row_at(row);
+        return r.b * p.out_sequence + r.j * p.out_token + r.head * p.out_head + d;
+    };
+    auto get = [&](int64_t at) -> float {
+        if (!p.direct) return p.part_o[at];
+        if (p.out_type == VLUT_TYPE_F32) return ((const float*)p.out)[at];
+        return (float)((const T*)p.out)[at];                       // (outputs of 16 bits are of the cache's type)
+    };
+    auto set = [&](int64_t at, float x) {
+        if (!p.direct) p.part_o[at] = x;
+        else if (p.out_type == VLUT_TYPE_F32) ((float*)p.out)[at] = x;
+        else ((T*)p.out)[at] = (T)x;
+    };
+    auto token = [&](const void* of, int key, int64_t page_stride, int64_t head_stride, int64_t token_stride) {
+        const int id = pages[key >> p.page_log];
+        return (const T*)of + (is_page(p, id) ? id : 0) * page_stride + h * head_stride + (key & mask) * token_stride + d;
+    };
+    unsigned lost[F] = {};                                         // a bit for each row
+#pragma unroll 1
+    for (unsigned left = rows; left; left &= left - 1) {
+        const int r = __builtin_ctz(left);
+        const int64_t at = result(row0 + r);
+        if (p.direct && !own && sequence_of(p, row_at(row0 + r).b).bad) continue;      // (NaN for that)
+        for (int f = 0; f < F && has; ++f)
+            if (is_odd(get(at + f))) {
+                lost[f] |= 1u << r;
+                set(at + f, 0.0f);
+            }
+    }
+#pragma unroll 1
+    for (int key0 = first_key; key0 < end_key; key0 += AHEAD) {
+        unsigned x[AHEAD][F > 1 ? F / 2 : 1];                      // (rows start at a dword)
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const T* const v = token(p.v, min(key0 + i, end_key - 1), p.v_page, p.v_head, p.v_token);
+            if constexpr (F == 1) x[i][0] = has ? *(const unsigned short*)v : 0u;
+            else {
+#pragma unroll
+                for (int w = 0; w < F / 2; ++w) x[i][w] = has ? ((const unsigned*)v)[w] : 0u;
+            }
+        }
+        unsigned found = 0;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            bool odd = false;
+#pragma unroll
+            for (unsigned w : x[i]) odd |= has_odd<T>(w);
+            found |= key0 + i < end_key && __any(odd) ? 1u << i : 0u;
+        }
+#pragma unroll 1
+        for (; found; found &= found - 1) {
+            const int key = key0 + __builtin_ctz(found);
+            const T* const v = token(p.v, key, p.v_page, p.v_head, p.v_token);
+            const T* const k = token(p.k, key, p.k_page, p.k_head, p.k_token);
+#pragma unroll 1
+            for (unsigned left = rows; left; left &= left - 1) {
+                const int r = __builtin_ctz(left);
+                const Row its = row_at(row0 + r);
+                if (own && key > seq.base + its.j) continue;
+                const T* const q = (const T*)p.q + its.b * p.q_sequence + its.j * p.q_token + its.head * p.q_head + d;
+                float s = 0.0f;
+                for (int f = 0; f < F && has; ++f) s += (float)q[f] * (float)k[f];
+                for (int m = 1; m < 64; m *= 2) s += __shfl_xor(s, m);
+                const float weight = s > -__builtin_inff() ? 1.0f : 0.0f;
+                const int64_t at = result(row0 + r);
+                for (int f = 0; f < F && has; ++f)
+                    if ((lost[f] >> r & 1) && is_odd((float)v[f])) set(at + f, get(at + f) + weight * (float)v[f]);
+            }
+        }
+    }
+#pragma unroll 1
+    for (unsigned left = rows; left; left &= left - 1) {
+        const int r = __builtin_ctz(left);
+        const int64_t at = result(row0 + r);
+        for (int f = 0; f < F && has; ++f)
+            if ((lost[f] >> r & 1) && get(at + f) == 0.0f) set(at + f, __builtin_nanf(""));
+    }
+}
+
 // One range of keys for up to 16 * MT query rows, few enough that memory is what bounds it.  A wave takes 32 keys a step (K straight to registers, V
 // through a piece of LDS of its own, no barrier); the next 32 are on their way while the present ones are worked on.  `share` waves
 // have the range in turn: 4 or 2, which join at the end through LDS, or 1 where ranges are short and many.  keep: the range is one
@@ -155,8 +279,9 @@ __device__ __forceinline__ void in_turn() {
 // of page number, keys, scores, join and parts: one sequence of 40 tokens behind 512, 6 us; 16 of 256 behind 2048, 9.7 us.
 // 24 sequences, 32 heads of 100 features that are not shared, 5 queries each over 300 own tokens and 1500 shared ones, 88 MB: 37 us, 2.4 TB/s, bound by what
 // a wave issues and waits for per step (12 steps of the prefix, 5 of own tokens).
+// Returns the rows that the wave has to settle (settle_odd).
 template <class T, int DP, int MT, int TERMS, bool WHOLE, bool GROUPED>
-__device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, bool own, const Sequence& seq, int slot,
+__device__ unsigned attend_few(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, bool own, const Sequence& seq, int slot,
                            int share, bool keep, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
     constexpr int KS = DP / 32, CH = DP / 8, PER = 64 / CH, VI = kFewKeys / PER, PITCH = few_pitch(DP);
@@ -266,12 +391,11 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
         for (int i = 0; i < VI; ++i) vr[i] = chunk_moved<WHOLE>(vr[i], v_chunk, p.D);
         if (some_masked) {
-            constexpr unsigned E = Number<T>::kExponents;
 #pragma unroll
             for (int i = 0; i < VI; ++i) {
                 if (kt + PER * i + v_key >= end_key) vr[i] = i32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int w = 0; w < 4; ++w) odd |= ((vr[i][w] & (E & 0xffff0000u)) == (E & 0xffff0000u)) | ((vr[i][w] & (E & 0xffffu)) == (E & 0xffffu));
+                for (int w = 0; w < 4; ++w) odd |= has_odd<T>((unsigned)vr[i][w]);
             }
         }
 #pragma unroll
@@ -361,7 +485,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float x = (float)*(const T*)(mine + key * PITCH + 32 * dt + 8 * grp + 2 * i);
-                            if (seen && !(fabsf(x) < __builtin_inff())) o[mt][dt][i] += weight * x;
+                            if (seen && is_odd(x)) o[mt][dt][i] += weight * x;
                         }
                 }
                 __builtin_amdgcn_wave_barrier();
@@ -371,7 +495,7 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
 #pragma unroll 1
                 for (int e = 0; e < 8; ++e) {
                     T* const x = (T*)(mine + (PER * i + v_key) * PITCH + 16 * v_chunk) + e;
-                    if (!(fabsf((float)*x) < __builtin_inff())) *x = (T)0.0f;
+                    if (is_odd((float)*x)) *x = (T)0.0f;
                 }
             __builtin_amdgcn_wave_barrier();
         }
@@ -428,16 +552,25 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
         l[mt] += __shfl_xor(l[mt], 16);
         l[mt] += __shfl_xor(l[mt], 32);
     }
+    unsigned odd_rows = 0;                     // whose result is none although their weights are numbers
     if (share == 1) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const int row = row0 + 16 * mt + l16;
-            if (row >= row_end || !keep) continue;
+            const bool real = row < row_end && keep;
+            float zero = 0.0f;
+#pragma unroll
+            for (int dt = 0; dt < DP / 16; ++dt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) zero = __builtin_fmaf(o[mt][dt][i], 0.0f, zero);
+            const uint64_t odd = __ballot(real && zero != 0.0f && l[mt] == l[mt]);
+            odd_rows |= (unsigned)((odd | odd >> 16 | odd >> 32 | odd >> 48) & 0xffff) << (16 * mt);
+            if (!real) continue;
             const Row r = begin_row(row, m[mt], l[mt], grp == 0);
 #pragma unroll
             for (int dt = 0; dt < DP / 16; ++dt) put(r, 16 * dt + 4 * grp, o[mt][dt]);
         }
-        return;
+        return odd_rows;
     }
     // The waves' parts: 16 rows at a time through LDS, 16 threads for a row.
     constexpr int OP = DP + 4, F4 = DP / 64;                       // floats per row; vectors of four per thread
@@ -456,22 +589,36 @@ __device__ void attend_few(const AttendParams& p, const int32_t* pages, int h, i
         __syncthreads();
         for (int r = ((wave - first_wave) * 64 + lane) >> 4; r < 16; r += 4 * share) {
             const int part = lane & 15, row = row0 + 16 * mt + r;
-            if (row >= row_end || !keep) continue;
-            float top = -__builtin_inff(), total = 0.0f;
-            for (int w = first_wave; w < first_wave + share; ++w) top = fmaxf(top, all_ml[(w * 16 + r) * 2]);
-            const float shift = top == -__builtin_inff() ? 0.0f : top;
-            f32x4 x[F4] = {};
-            for (int w = first_wave; w < first_wave + share; ++w) {
-                const float f = exp2_fast(all_ml[(w * 16 + r) * 2] - shift);
-                total += f * all_ml[(w * 16 + r) * 2 + 1];
+            bool odd = false;
+            if (row < row_end && keep) {
+                float top = -__builtin_inff(), total = 0.0f;
+                for (int w = first_wave; w < first_wave + share; ++w) top = fmaxf(top, all_ml[(w * 16 + r) * 2]);
+                const float shift = top == -__builtin_inff() ? 0.0f : top;
+                f32x4 x[F4] = {};
+                for (int w = first_wave; w < first_wave + share; ++w) {
+                    const float f = exp2_fast(all_ml[(w * 16 + r) * 2] - shift);
+                    total += f * all_ml[(w * 16 + r) * 2 + 1];
 #pragma unroll
-                for (int v = 0; v < F4; ++v) x[v] += *(f32x4*)(all_o + (w * 16 + r) * OP + (part + 16 * v) * 4) * f;
+                    for (int v = 0; v < F4; ++v) x[v] += *(f32x4*)(all_o + (w * 16 + r) * OP + (part + 16 * v) * 4) * f;
+                }
+                const Row to = begin_row(row, top, total, part == 0);
+                float zero = 0.0f;
+#pragma unroll
+                for (int v = 0; v < F4; ++v) {
+                    put(to, (part + 16 * v) * 4, x[v]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) zero = __builtin_fmaf(x[v][i], 0.0f, zero);
+                }
+                odd = zero != 0.0f && total == total;
             }
-            const Row to = begin_row(row, top, total, part == 0);
+            const uint64_t odds = __ballot(odd);
+            if (odds) {
 #pragma unroll
-            for (int v = 0; v < F4; ++v) put(to, (part + 16 * v) * 4, x[v]);
+                for (int g = 0; g < 4; ++g) odd_rows |= odds >> (16 * g) & 0xffff ? 1u << (16 * mt + r - grp + g) : 0u;
+            }
         }
     }
+    return __builtin_amdgcn_readfirstlane(odd_rows);
 }
 
 // One range of the prefix for 32 * NW query rows, many enough that the matrix cores are what bounds it: K and V of 64 keys (32 where D is
@@ -675,6 +822,12 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         if (tid == 0) *again = 0;
     }
     l += __shfl_xor(l, 32);
+    float zero = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(o[dt][i], 0.0f, zero);
+    const uint64_t odd = __ballot(row < row_end && zero != 0.0f && l == l);
     // O turned through the wave's piece of LDS (nobody reads the buffers any more), 32 features at a time, so that a store has whole lines.
     constexpr int TP = 36;                     // floats from row to row
     float* const turned = (float*)lds + wave * 32 * TP;
@@ -694,6 +847,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         __builtin_amdgcn_wave_barrier();
     }
     if (half == 0 && row < row_end) *(f32x2*)(p.part_ml + (part0 + l32 * stride) * 2) = f32x2{m, l};
+    if (__builtin_expect(odd != 0, 0)) settle_odd<T, DP>(pages, h, first_key, end_key, row0 + 32 * wave, (unsigned)(odd | odd >> 32), false, Sequence{}, slot);
 }
 
 // Few rows: ranges of the prefix for 16 * MT rows, and of the sequences' own tokens for 16 * OWN.  WHOLE: D is DP.  GROUPED: 16 keys share a page.
@@ -707,7 +861,8 @@ __global__ void __launch_bounds__(256, few_waves(DP, MT)) attend_few_kernel(cons
         const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
         if (h >= p.Hk) return;
         const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
-        attend_few<T, DP, MT, TERMS, WHOLE, GROUPED>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, 4, true, lds);
+        const unsigned odd = attend_few<T, DP, MT, TERMS, WHOLE, GROUPED>(p, p.prefix_pages, h, first, end, tile * 16 * MT, p.rows, false, Sequence{}, split, 4, true, lds);
+        if (__builtin_expect(odd != 0, 0)) settle_odd<T, DP>(p.prefix_pages, h, first, end, tile * 16 * MT, odd, false, Sequence{}, split);
         return;
     }
     // Sequences differ in length, so that their ranges go round the XCDs; the tiles of a range stay together, and the heads of a token where they are
@@ -722,8 +877,10 @@ __global__ void __launch_bounds__(256, few_waves(DP, MT)) attend_few_kernel(cons
     const int steps = (seq.len + p.own_step - 1) / p.own_step, per = (steps + p.own_splits - 1) / p.own_splits, nG = p.n * p.G;
     const int seen = seq.base + (min((tile + 1) * 16 * OWN, nG) - 1) / p.G + 1;          // by the tile's last query
     const int first = min(split * per * p.own_step, seq.len), end = keep ? min(min(first + per * p.own_step, seq.len), max(first, seen)) : first;
-    attend_few<T, DP, OWN, TERMS, WHOLE, GROUPED>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq,
-                                           p.prefix_splits + split, p.own_share, keep, lds);
+    const unsigned odd = attend_few<T, DP, OWN, TERMS, WHOLE, GROUPED>(p, p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, (b + 1) * nG, true, seq,
+                                                                p.prefix_splits + split, p.own_share, keep, lds);
+    if (__builtin_expect(odd != 0, 0))
+        settle_odd<T, DP>(p.page_table + b * p.table_stride, h, first, end, b * nG + tile * 16 * OWN, odd, true, seq, p.prefix_splits + split);
 }
 
 // Many rows: ranges of the prefix for 32 rows of each of NW waves, with P in TERMS terms.  XCDs as above.

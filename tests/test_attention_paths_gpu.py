@@ -176,3 +176,65 @@ def test_keys_of_minus_infinity_count_for_nothing(B, name, dtype, where):
             out, lse = case.run(B, dtype=kind, want_lse=True)
             assert out.isfinite().all()
             check_without(case, hidden, out, lse)
+
+
+# Besides the paths above: one part, whose workgroups store the result.
+ONE_PART = {
+    "prefix_alone": dict(B=2, n=1, Hq=4, Hk=2, D=64, P=77, lens=[0, 0], page=16),
+    "prefix_alone_d256": dict(B=3, n=2, Hq=4, Hk=1, D=256, P=128, lens=[0, 0, 0], page=4),
+    "own_alone": dict(B=3, n=3, Hq=4, Hk=2, D=128, P=0, lens=[20, 37, 5], page=16),
+    "own_alone_of_one_wave": dict(B=300, n=1, Hq=16, Hk=8, D=100, P=0, lens=[30 - i % 20 for i in range(300)], page=16),
+    "own_alone_many_queries": dict(B=2, n=40, Hq=4, Hk=2, D=64, P=0, lens=[40, 90], page=64),
+}
+
+
+@pytest.mark.parametrize("kind", ["cache", "fp32"])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("name", [*PATHS, *ONE_PART])
+def test_infinite_values_that_are_seen(B, name, dtype, kind):
+    """The formula's infinities and NaN, wherever the key is, in the features of the queries that see them, and no other number changed."""
+    inf, nan = float("inf"), float("nan")
+    case = path(B, name, dtype) if name in PATHS else Case(**ONE_PART[name], dtype=dtype)
+    Bn, n, Hq, Hk, D = case.shape
+    h, G, P = Hk - 1, Hq // Hk, case.P
+    case.q[..., 0] = 1
+    of, length = (case.prefix, P) if P else (case.own[Bn - 1], case.lens[Bn - 1])
+    of[0][2, h, 0] = -inf                                                 # a key that weighs nothing
+    case.write()
+    run = lambda: case.run(B, dtype=torch.float32 if kind == "fp32" else None, want_lse=True, max_own_len=max(case.lens))  # noqa: E731
+    clean, clean_lse = run()
+    assert clean.isfinite().all()
+    # token (of those that several sequences see, where there is a prefix) and feature -> value
+    last, middle = length - 1, length // 2
+    given = [(1, 3, inf), (middle, 7, -inf), (middle, 11, inf), (last, 11, -inf), (1, 15, nan), (last, 19, inf), (1, 23, -inf), (last, 23, -inf), (2, 27, inf), (0, D - 1, inf)]
+    want = clean.clone()
+    for t, f, x in given:
+        of[1][t, h, f] = x
+    for b in range(Bn) if P else [Bn - 1]:
+        for j in range(n):
+            sees = P if P else length - n + j + 1
+            for f in {f for _, f, _ in given}:
+                seen = [0.0 * x if t == 2 else x for t, g, x in given if g == f and t < sees]
+                if seen:
+                    want[b, j, h * G:(h + 1) * G, f] = sum(seen)
+    # a sequence's last own token: its last query's alone
+    for b in {0, Bn // 2}:
+        if P and case.lens[b] >= n:
+            case.own[b][1][-1, 0, 30] = -inf
+            want[b, n - 1, :G, 30] = -inf if want[b, n - 1, 0, 30].isfinite() else nan
+    case.write()
+    got, lse = run()
+    assert torch.equal(lse, clean_lse)
+    same = (got == want) | (got.isnan() & want.isnan())
+    assert same.all(), (same.logical_not().nonzero()[:4].tolist(), got[~same][:4].tolist(), want[~same][:4].tolist())
+
+
+def test_infinite_values_of_sequences_that_cannot_be(B):
+    """Lengths out of range are NaN, whatever the prefix holds."""
+    case = Case(B=3, n=1, Hq=4, Hk=2, D=64, P=77, lens=[0, 0, 0], page=16)
+    case.prefix[1][3, :, 5] = float("inf")
+    case.write()
+    case.own_lens[1] = 17
+    out, lse = case.run(B, want_lse=True)
+    assert out[1].isnan().all() and lse[1].isnan().all()
+    assert (out[[0, 2]][..., 5] == float("inf")).all() and out[[0, 2]][..., :5].isfinite().all() and out[[0, 2]][..., 6:].isfinite().all()
