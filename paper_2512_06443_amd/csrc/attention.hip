@@ -203,7 +203,7 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
         const auto blocks = [&](int64_t per) { return ceil_div(Hk * a.prefix_tiles * ceil_div(steps, per), 8) * 8 + own_blocks(ceil_div(own_steps, per)); };
         int64_t per = std::max<int64_t>(1, ceil_div(Hk * a.prefix_tiles * steps + ceil_div(own_units * own_steps, 4 / a.own_share), slots));
         for (int more = 0; more < 8 && per < most && blocks(per) > slots; ++more) ++per;
-        a.prefix_chunk = (int)(128 * per);
+        a.prefix_chunk = (int)(128 * std::min(per, std::max<int64_t>(1, steps)));       // (`per` may be any number where rows are many)
         per_own = own_blocks(1) >= slots ? std::max<int64_t>(1, own_steps) : per;
     } else {
         a.prefix_tiles = (int)ceil_div(rows, 32 * a.waves);

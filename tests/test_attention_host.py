@@ -143,3 +143,41 @@ def test_native_form_declines_what_it_does_not_know(L):
     assert n.shared_prefix_attention() is None
     with pytest.raises(TypeError):
         n.bind_attention(1)
+
+
+def parts_of(L, Bn, n, Hq, Hk, D, prefix, own, page_size):
+    """Parts of a call over such a cache, prefix and own tokens together, by the workspace that it asks for (0: a single one)."""
+    rows = Bn * n * Hq
+    c = cache(page_size=page_size, strides=(Hk * page_size * D, page_size * D, D), n=Hk)
+    q = heads(token=Hq * D, head=D, n=Hq)
+    call = lambda size: attend(L, q=q, out=q, stride=n * Hq * D, c=c, prefix_len=prefix, max_own=own, Bn=Bn, n=n, D=D, ws=P if size else None, ws_bytes=size)  # noqa: E731
+    if call(0) != B.VLUT_ERR_NULL:
+        return 0
+    low, high = 0, 4096                                                   # parts; the workspace of `high` is enough, that of `low` is not
+    need = lambda parts: (rows * parts * D * 4 + 255) // 256 * 256 + rows * parts * 8  # noqa: E731
+    assert call(need(high)) == B.VLUT_ERR_DEVICE
+    while high - low > 1:
+        middle = (low + high) // 2
+        low, high = (middle, high) if call(need(middle)) == B.VLUT_ERR_SMALL_BUFFER else (low, middle)
+    return high
+
+
+# Sizes at which a part of the prefix would have more keys than 32 bits hold if it went by the work of all rows alone.
+LARGE = [(1, 2097152, 1, 1, 128, 1, 33554304), (1, 1048576, 32, 8, 128, 1, 1048576), (1, 1 << 20, 32, 8, 128, 100, 1 << 20), (16, 1 << 16, 32, 8, 128, 1, 1 << 16),
+         (1, 1, 65535, 65535, 128, 1 << 20, 1), (1, 1, 60000, 60000, 8, (1 << 30) - 1, 0), (2, 1 << 19, 8, 8, 64, 1000, (1 << 30) - 1)]
+
+
+@pytest.mark.parametrize("page_size", [1, 8, 16, 64])
+@pytest.mark.parametrize("sizes", LARGE)
+def test_plans_of_many_rows_and_long_ranges(L, sizes, page_size):
+    """Each has its prefix among its parts, for pages of any size."""
+    if torch.cuda.is_available():
+        pytest.skip("addresses of nothing")
+    Bn, n, Hq, Hk, D, prefix, own = sizes
+    need = B.shared_prefix_attention_bytes(*sizes)
+    parts = parts_of(L, *sizes, page_size)
+    assert (parts >= 2) if own else (parts == 0 or parts >= 2)
+    assert parts <= math.ceil(prefix / 128) + max(1, math.ceil(own / 32))
+    assert need >= Bn * n * Hq * parts * (D * 4 + 8)
+    rows, prefix_parts, own_parts, groups = B.query_shared_prefix_attention(*sizes)
+    assert prefix_parts >= 1 and own_parts >= (own > 0) and groups >= 1
