@@ -128,10 +128,16 @@ int launch_heads(HeadsParams& p, int in, int out, int vec, hipStream_t stream) {
         blocks += (k.groups + per - 1) / per;
         k.end_block = blocks;
     }
-    const dim3 grid(blocks);
-    if (in == VLUT_TYPE_F32) return launch_heads_out<float>(p, out, vec, together, grid, stream);
-    if (in == VLUT_TYPE_BF16) return launch_heads_out<__bf16>(p, out, vec, together, grid, stream);
-    return launch_heads_out<_Float16>(p, out, vec, together, grid, stream);
+    // A launch's threads are numbered in 32 bits: more are several launches.
+    constexpr unsigned most_blocks = 1u << 23;
+    int rc = VLUT_OK;
+    for (p.first_block = 0; rc == VLUT_OK && p.first_block < blocks; p.first_block += most_blocks) {
+        const dim3 grid(std::min(blocks - p.first_block, most_blocks));
+        if (in == VLUT_TYPE_F32) rc = launch_heads_out<float>(p, out, vec, together, grid, stream);
+        else if (in == VLUT_TYPE_BF16) rc = launch_heads_out<__bf16>(p, out, vec, together, grid, stream);
+        else rc = launch_heads_out<_Float16>(p, out, vec, together, grid, stream);
+    }
+    return rc;
 }
 
 // Rows that go to a tensor of their own.

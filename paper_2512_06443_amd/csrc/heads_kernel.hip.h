@@ -33,6 +33,7 @@ struct HeadsParams {
     int64_t table_rows, slot_end;
     float eps;
     unsigned tokens, heads;    // heads of all kinds per token
+    unsigned first_block;      // of this launch
     int D, R, interleaved, lanes_log, page_log;
 };
 
@@ -74,9 +75,10 @@ template <class TI, class TO, int VEC, int HEADS>
 __global__ void __launch_bounds__(256) heads_kernel(const HeadsParams p) {
     constexpr int UNITS = VEC == 1 ? 2 : 1;         // of a lane: D <= 256 has at most 128 units of one pair
     const int lane = (int)threadIdx.x & ((1 << p.lanes_log) - 1);
-    const int which = blockIdx.x < p.kind[0].end_block ? 0 : (blockIdx.x < p.kind[1].end_block ? 1 : 2);
+    const unsigned at_block = p.first_block + blockIdx.x;
+    const int which = at_block < p.kind[0].end_block ? 0 : (at_block < p.kind[1].end_block ? 1 : 2);
     const HeadRows& k = p.kind[which];
-    const unsigned block = blockIdx.x - (which == 0 ? 0u : p.kind[which - 1].end_block), group = block * (256u >> p.lanes_log) + (threadIdx.x >> p.lanes_log);
+    const unsigned block = at_block - (which == 0 ? 0u : p.kind[which - 1].end_block), group = block * (256u >> p.lanes_log) + (threadIdx.x >> p.lanes_log);
     const bool alive = group < k.groups;
     const unsigned r = alive ? group : k.groups - 1;        // (the exchange below wants every lane)
     const unsigned token = r / k.groups_of_token;

@@ -252,3 +252,16 @@ def test_no_norm_reads_no_more_than_its_row(B):
     same = torch.ones((3, 4), dtype=torch.bool, device="cuda")
     same[1, 2] = same[2, 0] = False
     assert torch.equal(a[same], b[same]) and b[1, 2].isnan().all() and b[2, 0, 5].isnan() and (np.delete(b[2, 0].cpu().numpy(), 5) == 0).all()
+
+
+def test_more_heads_than_a_launch_has_threads_for(B):
+    """2^24 - 1 tokens (all the same ones: a stride of 0) of five heads, four of them to a workgroup."""
+    N, H, D = (1 << 24) - 1, 5, 66
+    if torch.cuda.mem_get_info()[0] < 3 * N * H * D * 2:
+        pytest.skip("no room")
+    x = torch.randn((1, H, D), device="cuda").to(torch.bfloat16)
+    w = torch.rand(D, device="cuda")
+    want, _ = B.norm_rope(x, q_weight=w)
+    got, _ = B.norm_rope(x.expand(N, H, D), q_weight=w)
+    for part in got.split(1 << 22):
+        assert (part == want).all()
