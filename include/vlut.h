@@ -471,6 +471,7 @@ int vlut_append_kv(const vlut_heads* k, const vlut_heads* v, const vlut_heads* q
  *   lse               dev or NULL, fp32 [B][n][heads]: log of the sum of exp(scale * q . k)
  *   scale             finite and > 0
  *   workspace         dev, 16-byte aligned, workspace_bytes >= vlut_shared_prefix_attention_bytes(...); may be NULL when that is 0
+ * B and n below 2^24, B * n * heads below 2^30, lengths below 2^30, and no more workgroups than a launch has (2^24; VLUT_ERR_SHAPE otherwise).
  * D: a multiple of four, 8 <= D <= VLUT_MAX_HEAD_FEATURES, and q, k, v and 16-bit outputs have even strides and dword-aligned data
  * (VLUT_ERR_UNSUPPORTED otherwise).  Lengths out of range and page numbers outside the cache are found on the device: they read nothing, and
  * the queries that depend on them get NaN.

@@ -18,15 +18,11 @@ namespace {
 using namespace vlut_attention;
 
 constexpr int kUnits = 256;            // compute units that a launch is to fill
+constexpr int64_t kMostBlocks = 1 << 24;       // of 256 threads
 
 bool type_ok(int type) { return type == VLUT_TYPE_F32 || type == VLUT_TYPE_BF16 || type == VLUT_TYPE_F16; }
 int type_bytes(int type) { return type == VLUT_TYPE_F32 ? 4 : 2; }
 bool power_of_two(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
-int log2_of(int64_t v) {
-    int k = 0;
-    while (((int64_t)1 << k) < v) ++k;
-    return k;
-}
 
 // ---------------------------------------------------------------------------------------------
 // Heads
@@ -165,15 +161,13 @@ int check_cache(const vlut_cache* c) {
 // Attention
 // ---------------------------------------------------------------------------------------------
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 // grouped: 16 keys share their page, as the kernel for many rows wants it.  neighbours: a token's heads are neighbours in memory.
 int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int64_t P, int64_t max_own, bool grouped, bool neighbours, AttendPlan* out) {
     if (B < 1 || n < 1 || Hk < 1 || Hq < 1 || Hq >= (1 << 16) || Hq % Hk || B >= kMaxDim || n >= kMaxDim) return VLUT_ERR_SHAPE;
     if (P < 0 || max_own < 0 || P >= ((int64_t)1 << 30) || max_own >= ((int64_t)1 << 30) || D < 1) return VLUT_ERR_SHAPE;
     if (D < 8 || D > VLUT_MAX_HEAD_FEATURES || D % 4) return VLUT_ERR_UNSUPPORTED;
-    const int64_t G = Hq / Hk, own_rows = n * G, rows = B * own_rows;
-    if (rows * Hk >= ((int64_t)1 << 30)) return VLUT_ERR_SHAPE;
+    const int64_t G = Hq / Hk, own_rows = n * G, rows = own_rows < ((int64_t)1 << 30) ? B * own_rows : own_rows;       // (below 2^54)
+    if (rows >= ((int64_t)1 << 30) || rows * Hk >= ((int64_t)1 << 30)) return VLUT_ERR_SHAPE;
     AttendPlan a{};
     a.grouped = grouped;
     a.own_heads_together = neighbours ? (int)Hk : 1;
@@ -220,12 +214,18 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     a.prefix_splits = P > 0 ? (int)ceil_div(P, a.prefix_chunk) : 0;
     a.own_splits = (int)ceil_div(own_steps, per_own);
     if (a.prefix_splits + a.own_splits == 0) a.own_splits = 1;      // nothing is seen: a workgroup stores that
-    const int64_t ranges = B * Hk * a.own_splits, prefix_blocks = Hk * a.prefix_tiles * a.prefix_splits;
-    if (ranges * a.own_tiles + prefix_blocks + 64 >= ((int64_t)1 << 30)) return VLUT_ERR_SHAPE;
-    a.prefix_per_xcd = (int)ceil_div(prefix_blocks, 8);
-    a.own_per_xcd = (int)(own_blocks(a.own_splits) / 8);
+    const int64_t prefix_blocks = ceil_div(Hk * a.prefix_tiles * a.prefix_splits, 8) * 8, own_all = own_blocks(a.own_splits);
+    const int parts_log = log2_of(ceil_div(a.prefix_splits + a.own_splits, 4)), groups_log = log2_of(1024 / a.DP);      // (combine_kernel's)
+    a.combine_lanes_log = std::min(groups_log, parts_log);
+    const int64_t combine_blocks = ceil_div(rows * Hk, 1 << (groups_log - a.combine_lanes_log));
+    // A launch's threads are numbered in 32 bits.
+    if (a.MT > 0 ? prefix_blocks + own_all >= kMostBlocks : (own_all >= kMostBlocks || prefix_blocks * a.waves / 4 >= kMostBlocks)) return VLUT_ERR_SHAPE;
+    a.prefix_per_xcd = (int)(prefix_blocks / 8);
+    a.own_per_xcd = (int)(own_all / 8);
     a.direct = a.MT > 0 && a.prefix_splits + a.own_splits == 1;
     if (!a.direct) {
+        if (combine_blocks >= kMostBlocks) return VLUT_ERR_SHAPE;
+        a.combine_blocks = (int)combine_blocks;
         const size_t parts = (size_t)(a.prefix_splits + a.own_splits) * (size_t)Hk * (size_t)rows;
         a.o_bytes = (parts * (size_t)D * 4 + 255) & ~(size_t)255;
         a.ml_bytes = parts * 8;

@@ -4,13 +4,6 @@
 
 namespace {
 
-int log2_of(int64_t v) {
-    int k = 0;
-    while (((int64_t)1 << k) < v) ++k;
-    return k;
-}
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 bool allow_lds(const void* kfn, int bytes, std::atomic<unsigned>& done_mask) {
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) return false;
@@ -75,9 +68,7 @@ template <class T, int DP>
 int launch_attend_d(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {
     const int rc = p.D == DP ? launch_attend_w<T, DP, true>(a, p, stream) : launch_attend_w<T, DP, false>(a, p, stream);
     if (rc != VLUT_OK || a.direct) return rc;
-    constexpr int groups = 256 / (DP / 4);
-    const int lanes_log = std::min(log2_of(groups), log2_of(ceil_div(a.prefix_splits + a.own_splits, 4)));
-    return launch(combine_kernel<DP>, dim3((unsigned)ceil_div(a.rows * p.Hk, groups >> lanes_log)), 256, 0, stream, p, lanes_log);
+    return launch(combine_kernel<DP>, dim3((unsigned)a.combine_blocks), 256, 0, stream, p, a.combine_lanes_log);
 }
 template <class T>
 int launch_attend(const AttendPlan& a, const AttendParams& p, hipStream_t stream) {

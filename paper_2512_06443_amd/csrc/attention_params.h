@@ -33,6 +33,13 @@ struct AttendParams {
     int direct;                        // a single part: workgroups store the result
 };
 
+inline int log2_of(int64_t v) {
+    int k = 0;
+    while (((int64_t)1 << k) < v) ++k;
+    return k;
+}
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 constexpr int kFewKeys = 32;           // keys of a wave's step where rows are few
 __host__ __device__ constexpr int few_pitch(int DP) { return DP * 2 + 32; }
 __host__ __device__ constexpr int few_lds(int DP) { return 4 * kFewKeys * few_pitch(DP); }
@@ -46,6 +53,7 @@ struct AttendPlan {
     int MT, waves, own_mt, DP;         // tile of the prefix: 16 * MT rows; MT = 0: 32 for each of the waves, by a kernel of its own
     int own_share, own_step, own_heads_together, grouped;
     int prefix_tiles, prefix_splits, prefix_chunk, prefix_per_xcd, own_tiles, own_splits, own_per_xcd, direct;
+    int combine_lanes_log, combine_blocks;
     int64_t rows;
     size_t o_bytes, ml_bytes;
 };

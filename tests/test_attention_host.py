@@ -181,3 +181,20 @@ def test_plans_of_many_rows_and_long_ranges(L, sizes, page_size):
     assert need >= Bn * n * Hq * parts * (D * 4 + 8)
     rows, prefix_parts, own_parts, groups = B.query_shared_prefix_attention(*sizes)
     assert prefix_parts >= 1 and own_parts >= (own > 0) and groups >= 1
+
+
+def test_attention_refuses_more_than_a_launch_or_64_bits_hold(L):
+    """Workgroups of 256 threads past 2^32 threads, by own ranges, by the prefix' tiles and by rows whose parts are joined, and rows past 2^63."""
+    most = (1 << 24) - 1
+    for sizes in ((most, most, 65535, 1, 64, 10, 10), (most, most, 65535, 1, 64, 0, 0), (1 << 23, 1 << 23, 1 << 15, 1, 8, 5, 5),
+                  (most, 1, 8, 8, 64, 0, 16), (most, 1, 8, 8, 64, 20, 16), (most, 1, 16, 8, 128, 100000, 0)):
+        assert B.shared_prefix_attention_bytes(*sizes) == 0, sizes
+        with pytest.raises(B.VlutError) as e:
+            B.query_shared_prefix_attention(*sizes)
+        assert e.value.status == B.VLUT_ERR_SHAPE
+        Bn, n, Hq, Hk, D, prefix, own = sizes
+        q = heads(token=Hq * D, head=D, n=Hq)
+        c = cache(n=Hk, strides=(Hk * 16 * D, 16 * D, D))
+        assert attend(L, q=q, out=q, stride=n * Hq * D, c=c, prefix_len=prefix, max_own=own, Bn=Bn, n=n, D=D) == B.VLUT_ERR_SHAPE
+    for sizes in ((1 << 22, 1, 8, 8, 64, 0, 16), (1 << 20, 4, 8, 8, 64, 20, 16), (1, 1 << 22, 32, 8, 128, 0, 1 << 22), (1, most, 4, 4, 128, 0, most)):
+        assert B.query_shared_prefix_attention(*sizes)[3] < 1 << 24
