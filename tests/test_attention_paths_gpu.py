@@ -238,3 +238,93 @@ def test_infinite_values_of_sequences_that_cannot_be(B):
     out, lse = case.run(B, want_lse=True)
     assert out[1].isnan().all() and lse[1].isnan().all()
     assert (out[[0, 2]][..., 5] == float("inf")).all() and out[[0, 2]][..., :5].isfinite().all() and out[[0, 2]][..., 6:].isfinite().all()
+
+
+# Every kernel that is compiled for one type of the cache: features of the accumulators (64, 128, 256) filled or not, pages of 16 tokens and more or less, tiles of
+# 16 rows for both parts, of 32 and 16, of 32 and 32, and 128 or 256 rows for the prefix with tiles of 16 or 32 for the own tokens.
+TILES = {
+    "16_16": (16, dict(B=4, n=1, Hq=8, Hk=2, P=300, lens=[3, 0, 140, 9])),
+    "32_16": (32, dict(B=64, n=1, Hq=16, Hk=8, P=300, lens=[260 - 31 * i % 200 for i in range(64)])),
+    "32_32": (32, dict(B=3, n=9, Hq=8, Hk=2, P=333, lens=[9, 77, 200])),
+    "128_16": (128, dict(B=32, n=1, Hq=32, Hk=8, lens=[3 + 4 * i for i in range(32)])),
+    "128_32": (128, dict(B=6, n=5, Hq=32, Hk=8, lens=[3, 5, 8, 13, 21, 34])),
+    "256_16": (256, dict(B=40, n=1, Hq=32, Hk=8, lens=[3 + 4 * i for i in range(40)])),
+    "256_32": (256, dict(B=8, n=5, Hq=32, Hk=8, lens=[3, 5, 8, 13, 21, 34, 55, 89])),
+}
+
+
+def instances():
+    for D in (64, 48, 128, 100, 256, 200):
+        for page in (16, 4):
+            for tiles in ("16_16",) if D > 128 else ("16_16", "32_16", "32_32"):
+                yield D, page, tiles
+        for tiles in ("128_16", "128_32") if D > 128 else ("128_16", "128_32", "256_16", "256_32"):
+            yield D, 16, tiles
+
+
+@pytest.mark.parametrize("kind", ["cache", "fp32"])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D,page,tiles", list(instances()))
+def test_every_kernel_against_64_bits(B, D, page, tiles, dtype, kind):
+    rows, sizes = TILES[tiles]
+    sizes = dict(sizes)
+    if "P" not in sizes:                                                  # long enough for a launch of its own
+        own = sizes["B"] * sizes["n"] * sizes["Hq"] // sizes["Hk"] * sizes["Hk"]
+        sizes["P"] = (3500000 if D > 128 else 1280000000 // (64 if D <= 64 else 128)) // own + 77
+    case = Case(**sizes, D=D, page=page, dtype=dtype)
+    got = B.query_shared_prefix_attention(*case.shape, case.P, max(case.lens))
+    print(D, page, tiles, dtype, kind, got, flush=True)
+    assert got[0] == (128 if D > 128 and rows > 128 else rows)
+    out, lse = case.run(B, dtype=torch.float32 if kind == "fp32" else None, want_lse=True, max_own_len=max(case.lens))
+    case.check(out, lse.cpu(), only=[0, case.shape[0] - 1])
+
+
+@pytest.mark.parametrize("kind", ["cache", "fp32"])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("name", [name for name in PATHS if PATHS[name][0] > 32])
+def test_scores_that_rise_above_a_ranges_first(B, name, dtype, kind):
+    """Ranges that are worked on again with their largest score: one, the last ones, all of them."""
+    for where in (slice(1000, 1001), slice(-900, -10), slice(70, None)):
+        case = path(B, name, dtype)
+        case.prefix[0][where] *= 40
+        case.write()
+        out, lse = case.run(B, dtype=torch.float32 if kind == "fp32" else None, want_lse=True)
+        case.check(out, lse.cpu(), only=[0, case.shape[0] - 1])
+
+
+@pytest.mark.parametrize("what", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("name", ["32_d128", "32_drafts_d128", "256_d100"])
+def test_own_tokens_that_are_not_seen_have_no_influence(B, name, dtype, what):
+    """The last own token, seen by the last query alone, in keys and values."""
+    case = path(B, name, dtype)
+    some = torch.tensor([m >= case.shape[1] for m in case.lens])
+    clean, clean_lse = case.run(B, want_lse=True)
+    for own in case.own:
+        own[0][-1], own[1][-1] = what, what
+    case.write()
+    out, lse = case.run(B, want_lse=True)
+    assert torch.equal(out[:, :-1], clean[:, :-1]) and torch.equal(lse[:, :-1], clean_lse[:, :-1])
+    assert not out[some][:, -1].isfinite().all(-1).any()
+
+
+@pytest.mark.parametrize("name", list(PATHS))
+def test_replays_of_a_graph(B, name):
+    """The call captured once; new queries and lengths, eager work and a workspace of NaN between the replays."""
+    case = path(B, name, BF16)
+    bound = max(case.lens)
+    want, _ = case.run(B, max_own_len=bound)
+    out = torch.empty_like(want)
+    ws = torch.empty(B.shared_prefix_attention_bytes(*case.shape, case.P, bound), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        case.run(B, out=out, workspace=ws, max_own_len=bound)
+    for step in range(4):
+        case.q.mul_(0.8)
+        case.own_lens.sub_(1 if step == 1 else 0).clamp_(min=0)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        eager, _ = case.run(B, max_own_len=bound)
+        assert torch.equal(got, eager) and got.isfinite().all()

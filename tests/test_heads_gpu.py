@@ -265,3 +265,81 @@ def test_more_heads_than_a_launch_has_threads_for(B):
     got, _ = B.norm_rope(x.expand(N, H, D), q_weight=w)
     for part in got.split(1 << 22):
         assert (part == want).all()
+
+
+def sample(N):
+    """Tokens to be compared: the first, the last, and some between."""
+    return torch.tensor(sorted({0, 1, N - 1, *range(5, N, max(1, N // 61))}), device="cuda")
+
+
+# Rows enough (tokens * heads of 2048 workgroups with a head per group of lanes) for several heads of a token to go together: two of vectors of four, four of
+# vectors of two; head counts that these do not divide.
+TOGETHER = [  # N, Hq, Hk, D, R, in, out, norm, interleaved
+    (6000, 7, 5, 128, 128, torch.float32, torch.bfloat16, True, False),
+    (6000, 5, 1, 128, 64, torch.bfloat16, torch.bfloat16, True, True),
+    (40000, 1, 1, 128, 128, torch.float32, torch.float32, False, False),
+    (5000, 7, 5, 100, 100, torch.float32, torch.float16, True, False),
+    (5000, 6, 3, 100, 52, torch.float16, torch.float32, True, True),
+    (30000, 1, 2, 100, 0, torch.bfloat16, torch.float16, True, False),
+    (3000, 9, 2, 256, 256, torch.float32, torch.bfloat16, True, False),
+    (7000, 5, 7, 64, 40, torch.float16, torch.float16, False, True),
+    (12000, 5, 7, 12, 12, torch.float32, torch.float32, True, False),
+]
+
+
+@pytest.mark.parametrize("per_head", [False, True])
+@pytest.mark.parametrize("N,Hq,Hk,D,R,src,dst,norm,interleaved", TOGETHER)
+def test_several_heads_together(B, N, Hq, Hk, D, R, src, dst, norm, interleaved, per_head):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(N + D)
+    q, k = (torch.randn((N, H, D), generator=gen, device="cuda").to(src) for H in (Hq, Hk))
+    weight = lambda H: torch.randn((H, D) if per_head else (D,), generator=gen, device="cuda") if norm else None  # noqa: E731
+    qw, kw = weight(Hq), weight(Hk)
+    cos, sin = tables(gen, 50, R) if R else (None, None)
+    positions = torch.randint(0, 50, (N,), generator=gen, device="cuda") if R else None
+    more = dict(eps=1e-5, interleaved=interleaved)
+    got = B.norm_rope(q, k, positions, cos, sin, qw, kw, dtype=dst, **more)
+    at = sample(N)
+    for g, x, w in zip(got, (q, k), (qw, kw)):
+        near(g[at], *definition(x[at], w, 1e-5, None if positions is None else positions[at], cos, sin, interleaved), D)
+    few = B.norm_rope(q[:20], k[:20], None if positions is None else positions[:20], cos, sin, qw, kw, dtype=dst, **more)      # one head at a time
+    assert torch.equal(few[0], got[0][:20]) and torch.equal(few[1], got[1][:20])
+    same = B.norm_rope(q, k, positions, cos, sin, qw, kw, dtype=src, **more)
+    B.norm_rope(q, k, positions, cos, sin, qw, kw, q_out=q, k_out=k, **more)                       # in place
+    assert torch.equal(q, same[0]) and torch.equal(k, same[1])
+
+
+@pytest.mark.parametrize("page,token_major", [(16, False), (64, True)])
+@pytest.mark.parametrize("N,Hq,Hk,D,R,src,dst,norm,interleaved", [c for c in TOGETHER if c[6] != torch.float32])
+@pytest.mark.parametrize("with_q", [False, True])
+def test_append_of_several_heads_together(B, N, Hq, Hk, D, R, src, dst, norm, interleaved, page, token_major, with_q):
+    N = N if with_q else max(N, -(-33000 // Hk))
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(N + D + page)
+    pages = -(-N * 9 // 8 // page)
+    shape = (pages, page, Hk, D) if token_major else (pages, Hk, page, D)
+    caches = [torch.randn(shape, generator=gen, device="cuda").to(dst) for _ in range(2)]
+    caches = [c.transpose(1, 2) for c in caches] if token_major else caches
+    before = [c.clone() for c in caches]
+    qkv = torch.randn((N, (Hq + 2 * Hk) * D), generator=gen, device="cuda").to(src)
+    q, k, v = (t.unflatten(1, (-1, D)) for t in qkv.split([Hq * D, Hk * D, Hk * D], dim=1))
+    slots = torch.randperm(pages * page, generator=gen, device="cuda")[:N].contiguous()
+    slots[::7] = -1
+    slots[3], slots[4], slots[N - 2] = pages * page, 1 << 45, -(1 << 40)
+    cos, sin = tables(gen, 30, R) if R else (None, None)
+    positions = torch.randint(0, 30, (N,), generator=gen, device="cuda") if R else None
+    kw, qw = (torch.randn((Hk, D), generator=gen, device="cuda"), torch.randn(D, generator=gen, device="cuda")) if norm else (None, None)
+    got = B.append_kv(k, v, slots, *caches, positions, cos, sin, k_weight=kw, interleaved=interleaved, q=q if with_q else None, q_weight=qw if with_q else None)
+    at = sample(N)
+    if with_q:
+        near(got[at], *definition(q[at], qw, 1e-6, None if positions is None else positions[at], cos, sin, interleaved), D, "q")
+    kept = (slots >= 0) & (slots < pages * page)
+    flat = [c.permute(0, 2, 1, 3).reshape(pages * page, Hk, D) for c in caches]
+    at = at[kept[at]]
+    near(flat[0][slots[at]], *definition(k[at], kw, 1e-6, None if positions is None else positions[at], cos, sin, interleaved), D, "keys")
+    keys = B.norm_rope(k, None, positions, cos, sin, kw, interleaved=interleaved, dtype=dst)[0]      # all of them, by the other call
+    assert torch.equal(flat[0][slots[kept]], keys[kept]) and torch.equal(flat[1][slots[kept]], v[kept].to(dst))
+    untouched = torch.ones(pages * page, dtype=torch.bool, device="cuda")
+    untouched[slots[kept]] = False
+    for c, b in zip(flat, before):
+        assert torch.equal(c[untouched], b.permute(0, 2, 1, 3).reshape(pages * page, Hk, D)[untouched])
