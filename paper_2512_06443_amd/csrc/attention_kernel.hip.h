@@ -126,6 +126,11 @@ __device__ __forceinline__ void arrived_scalar(int& x) {
     asm volatile("" : "+s"(x));
 #endif
 }
+__device__ __forceinline__ int there(int x) {                      // (a number that all lanes have)
+    x = __builtin_amdgcn_readfirstlane(x);
+    arrived_scalar(x);
+    return x;
+}
 
 // The order of a stretch of code that ends here: AHEAD reads of LDS in front, then, GROUPS times, MFMAS matrix instructions, READS reads, VALU vector
 // instructions and EXPS exponentials.  Left to itself the compiler reads what an instruction needs right before it and waits, or all that is needed
@@ -152,7 +157,8 @@ __device__ __forceinline__ bool has_odd(unsigned x) {
 }
 __device__ __forceinline__ bool is_odd(float x) { return !(fabsf(x) < __builtin_inff()); }
 
-// The kernel's parameters, its first argument, read again: as the reference that the loops have they would wait in registers throughout.
+// The kernel's parameters, its first argument, read again: as the reference that the loops have they would wait in registers throughout.  For a kernel
+// itself alone: a function that is not part of one has no such argument.
 __device__ __forceinline__ const AttendParams& parameters() {
 #if defined(__HIP_DEVICE_COMPILE__)
     auto at = __builtin_amdgcn_kernarg_segment_ptr();
@@ -168,15 +174,13 @@ __device__ __forceinline__ const AttendParams& parameters() {
 // wave that stored it: its rows (bits of `rows`, from row0 on) get, in the features concerned, the sum of the infinities and NaN among the values of the range's
 // keys that they see, with weights of 1, or 0 for a score of -inf.  (Where there are none, finite values passed 32 bits: NaN.)
 // It reads V once more, and keys and queries where it finds such values, straight from memory and after everything else, so that it takes nothing from the
-// loops: a look at their results, 0.2 us of 12.3 for 16 sequences of 256 behind 2048, nothing that shows where ranges are longer.
+// loops: a look at their results, 0.2 us of 12.3 for 16 sequences of 256 behind 2048, 0.7 of 73 for 8 of 16384.
 template <class T, int DP>
-__device__ void settle_odd(const int32_t* pages, int h, int first_key, int end_key, int row0, unsigned rows, bool own, const Sequence& seq, int slot) {
+__device__ __forceinline__ void settle_odd(const int32_t* pages, int h, int first_key, int end_key, int row0, unsigned rows, bool own, const Sequence& seq, int slot) {
     constexpr int F = DP / 64, AHEAD = 8;                          // features of a lane; keys at a time
     const AttendParams& p = parameters();
-    for (int* x : {&h, &first_key, &end_key, &row0, &slot}) {      // (or what is worked out from these waits in registers too)
-        *x = __builtin_amdgcn_readfirstlane(*x);
-        arrived_scalar(*x);
-    }
+    // (or what is worked out from these waits in registers too)
+    h = there(h), first_key = there(first_key), end_key = there(end_key), row0 = there(row0), slot = there(slot);
     const int lane = (int)threadIdx.x & 63, d = F * lane, nG = p.n * p.G, mask = (1 << p.page_log) - 1;
     const bool has = d < p.D;
     __threadfence();                                               // (other lanes have stored the results)
@@ -636,8 +640,9 @@ __device__ unsigned attend_few(const AttendParams& p, const int32_t* pages, int 
 //     below 2^15: a maximum per step shows one; a first step whose scores are all -inf, which says nothing of the others) the range is begun again with the
 //     largest of all its scores, which a sweep over K finds.
 //     (Multiplying where it is needed, in a branch, costs as much as always: O's registers are copied where the ways meet.)
+// Returns the rows that the wave has to settle.
 template <class T, int DP, int TERMS, int NW, bool WHOLE>
-__device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, int slot, unsigned char* lds) {
+__device__ unsigned attend_many(const AttendParams& p, const int32_t* pages, int h, int first_key, int end_key, int row0, int row_end, int slot, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
     constexpr int KEYS = many_keys(DP), KT = KEYS / 32, KS = DP / 16, CH = DP / 8, PER = 64 * NW / CH, LI = KEYS / PER, GK = 64 / CH;
     constexpr int KP = many_k_pitch(DP), VP = many_v_pitch(DP);
@@ -847,7 +852,7 @@ __device__ void attend_many(const AttendParams& p, const int32_t* pages, int h, 
         __builtin_amdgcn_wave_barrier();
     }
     if (half == 0 && row < row_end) *(f32x2*)(p.part_ml + (part0 + l32 * stride) * 2) = f32x2{m, l};
-    if (__builtin_expect(odd != 0, 0)) settle_odd<T, DP>(pages, h, first_key, end_key, row0 + 32 * wave, (unsigned)(odd | odd >> 32), false, Sequence{}, slot);
+    return (unsigned)(odd | odd >> 32);
 }
 
 // Few rows: ranges of the prefix for 16 * MT rows, and of the sequences' own tokens for 16 * OWN.  WHOLE: D is DP.  GROUPED: 16 keys share a page.
@@ -891,7 +896,9 @@ __global__ void __launch_bounds__(64 * NW, DP > 128 ? NW / 4 : 2) attend_many_ke
     const int tile = i % p.prefix_tiles, rest = i / p.prefix_tiles, split = rest % p.prefix_splits, h = rest / p.prefix_splits;
     if (h >= p.Hk) return;
     const int first = split * p.prefix_chunk, end = min(p.P, first + p.prefix_chunk);
-    attend_many<T, DP, TERMS, NW, WHOLE>(p, p.prefix_pages, h, first, end, tile * 32 * NW, p.rows, split, lds);
+    const unsigned odd = attend_many<T, DP, TERMS, NW, WHOLE>(p, p.prefix_pages, h, first, end, tile * 32 * NW, p.rows, split, lds);
+    if (__builtin_expect(odd != 0, 0))
+        settle_odd<T, DP>(p.prefix_pages, h, first, end, tile * 32 * NW + 32 * ((int)threadIdx.x >> 6), odd, false, Sequence{}, split);
 }
 
 // The parts of every row joined.  DP / 4 threads have four features each of a row's part, 2^lanes_log such groups share a row's parts, and
