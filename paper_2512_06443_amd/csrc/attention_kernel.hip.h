@@ -637,8 +637,8 @@ __device__ unsigned attend_few(const AttendParams& p, const int32_t* pages, int 
 //   - a wave's load covers GK neighbouring keys, which share their page (the host sees to it): addresses are worked out once per wave;
 //   - O is not multiplied with every new maximum, and maxima are not looked for: m is the largest score of the first step, and weights are powers of
 //     two of the scores above it.  Where that does not do (bf16: the sum of weights shows one of 2^40 or so; fp16, whose weights have to stay
-//     below 2^15: a maximum per step shows one; a first step whose scores are all -inf, which says nothing of the others) the range is begun again with the
-//     largest of all its scores, which a sweep over K finds.
+//     below 2^15: a maximum per step shows one; a first step whose scores are all -inf, which says nothing of the others; an O past fp32 by weights above 1)
+//     the range is begun again with the largest of all its scores, which a sweep over K finds.
 //     (Multiplying where it is needed, in a branch, costs as much as always: O's registers are copied where the ways meet.)
 // Returns the rows that the wave has to settle.
 template <class T, int DP, int TERMS, int NW, bool WHOLE>
@@ -760,6 +760,14 @@ __device__ unsigned attend_many(const AttendParams& p, const int32_t* pages, int
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
         return fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
     };
+    auto finite = [&]() {
+        float zero = 0.0f;                     // (or NaN)
+#pragma unroll
+        for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(o[dt][i], 0.0f, zero);
+        return zero == 0.0f;
+    };
     int* const again = (int*)(lds + 2 * many_buffer(DP));
     if (tid == 0) *again = 0;                  // (the sweep's first barrier is between this and what follows)
     for (bool known = false;;) {
@@ -813,7 +821,8 @@ __device__ unsigned attend_many(const AttendParams& p, const int32_t* pages, int
                 __builtin_amdgcn_sched_barrier(0);
             }
         });
-        if constexpr (WIDE) over = !(l < 0x1p40f) || m == -__builtin_inff();             // (O of values up to 2^88 has room then)
+        // (both halves' weights: a lane's O is of the keys of both)
+        if constexpr (WIDE) over = !(l + __shfl_xor(l, 32) < (finite() ? 0x1p40f : (float)(end_key - first_key + 1))) || m == -__builtin_inff();
         if (over) *again = 1;
         __syncthreads();
         if (!*again || known) break;
@@ -827,12 +836,7 @@ __device__ unsigned attend_many(const AttendParams& p, const int32_t* pages, int
         if (tid == 0) *again = 0;
     }
     l += __shfl_xor(l, 32);
-    float zero = 0.0f;
-#pragma unroll
-    for (int dt = 0; dt < DP / 32; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(o[dt][i], 0.0f, zero);
-    const uint64_t odd = __ballot(row < row_end && zero != 0.0f && l == l);
+    const uint64_t odd = __ballot(row < row_end && !finite() && l == l);
     // O turned through the wave's piece of LDS (nobody reads the buffers any more), 32 features at a time, so that a store has whole lines.
     constexpr int TP = 36;                     // floats from row to row
     float* const turned = (float*)lds + wave * 32 * TP;

@@ -60,9 +60,9 @@ def per_key_head(case, x):
     return x.double().unflatten(2, (Hk, Hq // Hk)).movedim(2, 0).flatten(1, 3)
 
 
-def sharp_weights(case, rest=-25.0):
+def sharp_weights(case, rest=-25.0, ahead=-9.0):
     """Queries and keys of one feature: scores are single products and exact.  Every feature of V has two keys of its own, whose weights are
-    e^-2 to 1 (and cancel in the odd features); all other keys are `rest`, too low to count, but for one of -9 in 32, ahead of the others, from which the
+    e^-2 to 1 (and cancel in the odd features); all other keys are `rest`, too low to count, but for one of `ahead` in 32, ahead of the others, from which the
     largest score of any range's first keys is no further than what 32 bits' scores tell exactly.  Own tokens: `rest`."""
     Bn, n, Hq, Hk, D = case.shape
     gen = torch.Generator(device="cuda")
@@ -73,7 +73,7 @@ def sharp_weights(case, rest=-25.0):
     k.zero_()
     v.zero_()
     k[:, :, 0] = rest
-    k[::32, :, 0] = -9.0
+    k[::32, :, 0] = ahead
     for own in case.own:
         own[0].zero_()
         own[0][:, :, 0] = rest
@@ -328,3 +328,18 @@ def test_replays_of_a_graph(B, name):
         got = out.clone()
         eager, _ = case.run(B, max_own_len=bound)
         assert torch.equal(got, eager) and got.isfinite().all()
+
+
+@pytest.mark.parametrize("name", list(PATHS))
+def test_large_values_behind_low_scores(B, name):
+    """Values of 2^100 whose scores are 2^33 and more above those of their range's first keys: the product of both is past 32 bits, the result is not.
+    Bound: as for fp32 outputs above, with scores up to 36 from the maximum that a tile's waves begin with (2^-19 * log(2) more)."""
+    case = path(B, name, BF16)
+    sharp_weights(case, ahead=-25.0)
+    case.prefix[1].mul_(2.0 ** 100)
+    case.write()
+    out, lse = case.run(B, scale=1.0, dtype=torch.float32, want_lse=True)
+    want, size, want_lse = formula(case)
+    got, got_lse = per_key_head(case, out), per_key_head(case, lse)
+    off = (got * (got_lse - want_lse).exp()[..., None] - want).abs()
+    assert (off <= want.abs() * U32 + size * (1.2 + 0.7) * 2.0 ** -19 + 1e-38).all()
