@@ -175,9 +175,12 @@ int plan_attention(int64_t B, int64_t n, int64_t Hq, int64_t Hk, int64_t D, int6
     a.DP = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
     a.own_mt = own_rows <= 16 || a.DP > 128 ? 1 : 2;        // (of 256 features two tiles' O and queries do not fit the registers)
     // Tiles of 16 or 32 rows whose waves share the keys, or, where the prefix' products are many, a launch of its own with 32 rows a wave.  us, by tiles /
-    // that launch (bf16, 8 key heads, 256 rows a head): 128 features, 2048 keys 22 / 27, 4096 29 / 31, 6000 33 / 31, 8192 39 / 38 (512 rows: 2048 keys
-    // 25 / 32, 4096 34 / 35); 64 features, 4096 keys 19 / 23, 8192 26 / 28, 16384 42 / 30; 256 features, 1024 keys 29 / 37, 2048 46 / 40, 4096 66 / 43
-    // (128 rows: 3900 keys 48 / 41; one key head, 800 rows: 4096 keys 31 / 40, 6000 39 / 43, 8192 48 / 44).
+    // that launch, 8 key heads, for bf16 outputs (fp32): 128 features, 256 rows a head, 2048 keys 22 / 30 (23 / 33), 4096 28 / 34 (29 / 36), 6000 32 / 33
+    // (33 / 36), 8192 39 / 37 (40 / 40), 12000 50 / 42 (51 / 47); 512 rows, 2048 keys 24 / 34, 4096 34 / 37 (37 / 41), 6000 44 / 42 (48 / 47); 64 features, 256
+    // rows, 8192 keys 26 / 30 (29 / 32), 12000 33 / 31 (37 / 34), 16384 41 / 34 (48 / 38); 256 features, 256 rows, 1024 keys 28 / 39, 2048 45 / 41, 4096
+    // 65 / 44 (66 / 46); 128 rows, 3900 keys 34 / 39; one key head, 800 rows, 4096 keys 28 / 41, 6000 37 / 44, 8192 46 / 45.
+    // (The two meet at half as many products again as said here, where up to a tenth of the time lies between them, now that the launch's weights have a
+    // term more than when the limit was set.)
     const int64_t few_products = a.DP > 128 ? 3500000 : 1280000000 / a.DP;
     const bool many = P > 0 && rows > 64 && grouped && rows * P * Hk > few_products;
     // Tiles of 16 where 32 would read less but a step per workgroup is about all there is: us, 32 / 16, 8 key heads of 128: 64 rows a head, 2048 keys, own 512

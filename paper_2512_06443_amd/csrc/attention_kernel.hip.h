@@ -23,8 +23,8 @@ using namespace vlut_attention;
 // Scores, m, l and O are fp32, and l sums P before any rounding.  The matrix cores take no fp32, so that P is carried to the second product in terms of
 // the cache's type, each what the rounding of those before it left.  For outputs of 16 bits: two (16 bits of bf16, 22 of fp16), so that the output's own
 // rounding is what is left.  For fp32: what carries 24 bits of bf16, three, or two of fp16.  A caller gets the same bits from either kernel.  A term more is
-// half as many matrix instructions again where rows are many: 256 rows a head, 32768 keys, 8 heads 46 us with one, 57 with two (one would leave bf16 outputs 40 %
-// further off); 1024 rows a head, 8192 keys 57 with two, 71 with three (two would leave fp32 outputs 2.4e-6 of the result off instead of 4e-7).  Where rows are
+// half as many matrix instructions again where rows are many: 256 rows a head, 32768 keys, 8 heads 46 us with one, 60 with two (one would leave bf16 outputs 40 %
+// further off); 1024 rows a head, 8192 keys 58 with two, 73 with three (two would leave fp32 outputs 2.4e-6 of the result off instead of 4e-7).  Where rows are
 // few, bound by memory or latency: 64 sequences of 8 key heads behind 4096 31.7 us with two, 34.2 with three.
 // fp16: P is lifted by a power of two (Number::kLift), since weights below 2^-14 would lose bits and those below 2^-25 everything.
 // ---------------------------------------------------------------------------------------------
@@ -174,7 +174,8 @@ __device__ __forceinline__ const AttendParams& parameters() {
 // wave that stored it: its rows (bits of `rows`, from row0 on) get, in the features concerned, the sum of the infinities and NaN among the values of the range's
 // keys that they see, with weights of 1, or 0 for a score of -inf.  (Where there are none, finite values passed 32 bits: NaN.)
 // It reads V once more, and keys and queries where it finds such values, straight from memory and after everything else, so that it takes nothing from the
-// loops: a look at their results, 0.2 us of 12.3 for 16 sequences of 256 behind 2048, 0.7 of 73 for 8 of 16384.
+// loops: a look at their results, 0.2 us of 12.3 for 16 sequences of 256 behind 2048, 0.7 of 73 for 8 of 16384.  Where there is something to settle: 64
+// sequences behind 32768, 92 us, one infinite value of the prefix 480 us, one in every range and key head 600.
 template <class T, int DP>
 __device__ __forceinline__ void settle_odd(const int32_t* pages, int h, int first_key, int end_key, int row0, unsigned rows, bool own, const Sequence& seq, int slot) {
     constexpr int F = DP / 64, AHEAD = 8;                          // features of a lane; keys at a time
@@ -280,7 +281,7 @@ __device__ __forceinline__ void settle_odd(const int32_t* pages, int h, int firs
 // where there are more rows (more tiles: O does not fit the registers).  Two workgroups of four waves on a unit have 100 KB of loads on their way.
 // Measured, 8 key heads of 128 features in bf16: 8 sequences of up to 16384 own tokens behind 1000, 338 MB: 70 us, 4.8 TB/s (a large copy: 5.3); 64 of up
 // to 512, 102 MB: 24.6 us, 4.2 TB/s, of which the first loads' latency and unequal lengths take a fifth.  Short ranges are bound by latency, a chain
-// of page number, keys, scores, join and parts: one sequence of 40 tokens behind 512, 6 us; 16 of 256 behind 2048, 9.7 us.
+// of page number, keys, scores, join and parts: one sequence of 40 tokens behind 512, 6.2 us; 16 of 256 behind 2048, 9.4 us.
 // 24 sequences, 32 heads of 100 features that are not shared, 5 queries each over 300 own tokens and 1500 shared ones, 88 MB: 37 us, 2.4 TB/s, bound by what
 // a wave issues and waits for per step (12 steps of the prefix, 5 of own tokens).
 // Returns the rows that the wave has to settle (settle_odd).
@@ -630,15 +631,18 @@ __device__ unsigned attend_few(const AttendParams& p, const int32_t* pages, int 
 // worked on, and are stored behind them; one barrier per step.
 // 32 rows a wave, the matrix instruction's 32 x 32 x 16; 64 would halve the LDS reads, but their O has to live in the accumulation registers, and the
 // copies cost more.  Two waves on a SIMD, so that one's exponentials go beside the other's matrix instructions.
-// Measured, 256 rows a head, 32768 keys, 8 heads of 128 features, bf16, 34 GFLOP: 46 us, 750 TFLOP/s, 55 % of the rate of a large product (and with P
-// in two terms, 52 GFLOP: 57 us, 900).  What bounds it is issue: per 16 keys of 32 rows a SIMD has 8 matrix instructions of 32 cycles and 8 exponentials of
-// 8 each for the two waves apart, with their subtractions, sums and conversions, the LDS reads and the barrier.
+// Measured, 8 heads of 128 features, bf16: 256 rows a head, 32768 keys, P in two terms, 52 GFLOP: 60 us, 850 TFLOP/s, 62 % of the rate of a large product;
+// 1024 rows, 8192 keys, P in three terms, 69 GFLOP: 73 us, 940 TFLOP/s.  Counted there, of a SIMD's cycles (1.75 GHz): matrix cores busy 46 % and 51 %, vector units
+// 43 % and 48 %, LDS 21 % and 18 % with hardly a conflict; of a wave's, a third it issues, a third it waits for its turn or for a unit, a third (27 %) for data
+// and barriers.  So no unit is full: matrix and vector work of a SIMD's two waves, which the barrier holds in one phase, follow each other for the most
+// part instead of lying beside each other.
 // What the vector units have to do beside the matrix instructions is kept short:
 //   - a wave's load covers GK neighbouring keys, which share their page (the host sees to it): addresses are worked out once per wave;
 //   - O is not multiplied with every new maximum, and maxima are not looked for: m is the largest score of the first step, and weights are powers of
 //     two of the scores above it.  Where that does not do (bf16: the sum of weights shows one of 2^40 or so; fp16, whose weights have to stay
 //     below 2^15: a maximum per step shows one; a first step whose scores are all -inf, which says nothing of the others; an O past fp32 by weights above 1)
-//     the range is begun again with the largest of all its scores, which a sweep over K finds.
+//     the range is begun again with the largest of all its scores, which a sweep over K finds.  (64 sequences behind 32768, such scores in every range: 92 -> 162
+//     us, fp16 96 -> 169.)
 //     (Multiplying where it is needed, in a branch, costs as much as always: O's registers are copied where the ways meet.)
 // Returns the rows that the wave has to settle.
 template <class T, int DP, int TERMS, int NW, bool WHOLE>
