@@ -626,7 +626,7 @@ __device__ unsigned attend_few(const AttendParams& p, const int32_t* pages, int 
     return __builtin_amdgcn_readfirstlane(odd_rows);
 }
 
-// One range of the prefix for 32 * NW query rows, many enough that the matrix cores are what bounds it: K and V of 64 keys (32 where D is
+// One range of the prefix for 32 * NW query rows, many enough that memory is not what bounds it: K and V of 64 keys (32 where D is
 // over 128) in LDS for all NW waves, which have 32 rows each.  Two buffers: the next keys travel to registers while the present ones are
 // worked on, and are stored behind them; one barrier per step.
 // 32 rows a wave, the matrix instruction's 32 x 32 x 16; 64 would halve the LDS reads, but their O has to live in the accumulation registers, and the
