@@ -485,6 +485,62 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
                                  const int32_t* query_lens_or_null, int64_t B, int64_t n, int64_t D, float scale, const vlut_heads* out,
                                  int64_t out_sequence_stride, float* lse_or_null, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Between the products of a decoder layer, and behind the last one.  Inference only, as above.
+ */
+
+/* Rows of tokens: element (token, k) is data[token * row_stride + k], features contiguous, stride in elements. */
+typedef struct vlut_rows {
+    const void* data;           /* dev; written through where the struct describes an output */
+    int64_t row_stride;
+    int32_t type;               /* VLUT_TYPE_* */
+} vlut_rows;
+
+#define VLUT_ACTIVATION_NONE 0
+#define VLUT_ACTIVATION_SIGMOID 1  /* 1 / (1 + exp(-x))            */
+#define VLUT_ACTIVATION_SILU 2     /* x / (1 + exp(-x))            */
+#define VLUT_ACTIVATION_RELU2 3    /* max(x, 0)^2                  */
+#define VLUT_ACTIVATION_GELU 4     /* x (1 + erf(x / sqrt(2))) / 2 */
+#define VLUT_MAX_ROW_FEATURES 32768
+
+/*
+ * Behind a block, its output y: the norm after it, its gate, the residual's sum, and the norm before the next block, in one pass:
+ *   t = y / sqrt(mean(y^2) + eps) * weight     (t = y without a weight)
+ *   h = residual + scale * act(gate) * t       (scale * t without a gate)
+ *   x = h / sqrt(mean(h^2) + eps) * next_weight
+ * fp32 throughout, each output rounded once to its type; x is of the h that is not rounded.
+ *   N tokens (1 <= N < 2^24), K features (1 <= K <= VLUT_MAX_ROW_FEATURES; more: VLUT_ERR_UNSUPPORTED), any strides and alignment
+ *   weight, next_weight    dev, fp32 [K], or NULL: no such norm (x NULL with next_weight)
+ *   gate                   of y's type or fp32; row_stride 0: one for all tokens; NULL (with VLUT_ACTIVATION_NONE): none
+ *   scale                  finite
+ *   h                      of the residual's type; h or x may be y, the residual or the gate (same data, type and strides), else nothing overlaps them
+ */
+int vlut_residual_norm(const vlut_rows* y, const float* weight_or_null, const vlut_rows* gate_or_null, int activation, float scale, const vlut_rows* residual,
+                       const float* next_weight_or_null, float eps, int64_t N, int64_t K, const vlut_rows* h, const vlut_rows* x_or_null, void* stream);
+
+/*
+ * Inside a block, ahead of its last product: t = act(gate) * x (act(x) without a gate), out = t / sqrt(mean(t^2) + eps) * weight (out = t without a
+ * weight).  fp32 throughout, rounded once; sizes, types and overlaps as in vlut_residual_norm.
+ */
+int vlut_gated_norm(const vlut_rows* x, const vlut_rows* gate_or_null, int activation, const float* weight_or_null, float eps, int64_t N, int64_t K,
+                    const vlut_rows* out, void* stream);
+
+/*
+ * Of N rows of V logits (1 <= N < 2^24, 1 <= V < 2^30), with z = logits / temperature and p = softmax(z):
+ *   logprob[n]   = log p[tokens[n]]; NaN for a token outside [0, V), which is not read (both NULL where not wanted)
+ *   entropy[n]   = -sum p log p (NULL where not wanted)
+ *   top_ids, top_logprobs [N][top]: the largest logits, in order, equal ones by the lowest index, and their log p (NULL for top 0)
+ * Sums in fp32.  A logit of -inf is a token that is not allowed: log p is -inf, it adds nothing, and it comes behind all others among the largest; a row of
+ * nothing else has an entropy of 0.  A NaN or an infinity above makes the row's log p and entropy NaN (NaN comes out as -inf does among the ids).
+ *   top           0 <= top <= V, at most VLUT_MAX_TOP (VLUT_ERR_UNSUPPORTED otherwise)
+ *   temperature   finite and > 0
+ *   workspace     dev, 16-byte aligned, workspace_bytes >= vlut_token_logprobs_bytes(...); may be NULL when that is 0
+ */
+#define VLUT_MAX_TOP 64
+size_t vlut_token_logprobs_bytes(int64_t N, int64_t V, int top);
+int vlut_token_logprobs(const vlut_rows* logits, const int64_t* tokens_or_null, float temperature, int top, int64_t N, int64_t V, float* logprob_or_null,
+                        float* entropy_or_null, int64_t* top_ids_or_null, float* top_logprobs_or_null, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,6 +38,7 @@ EXPORTS = [
     "vlut_mpgemm_lean", "vlut_mpgemm_g5_lean", "vlut_mpgemm_mixed_lean",
     "vlut_norm_rope", "vlut_append_kv", "vlut_shared_prefix_attention", "vlut_shared_prefix_attention_bytes",
     "vlut_query_shared_prefix_attention",
+    "vlut_residual_norm", "vlut_gated_norm", "vlut_token_logprobs", "vlut_token_logprobs_bytes",
 ]
 
 _lib = None
@@ -58,6 +59,10 @@ class _Cache(ctypes.Structure):          # vlut_cache
                 ("k_page", ctypes.c_int64), ("k_head", ctypes.c_int64), ("k_token", ctypes.c_int64),
                 ("v_page", ctypes.c_int64), ("v_head", ctypes.c_int64), ("v_token", ctypes.c_int64),
                 ("heads", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
+class _Rows(ctypes.Structure):           # vlut_rows
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("type", ctypes.c_int32)]
 
 
 class VlutError(RuntimeError):
@@ -126,6 +131,11 @@ def lib() -> ctypes.CDLL:
         L.vlut_query_shared_prefix_attention.restype = ci
         L.vlut_shared_prefix_attention.argtypes = [heads, i64, cache, p, i64, p, i64, p, i64, p, i64, i64, i64, cf, heads, i64, p, p, sz, p]
         L.vlut_shared_prefix_attention.restype = ci
+        rows = ctypes.POINTER(_Rows)
+        L.vlut_residual_norm.argtypes, L.vlut_residual_norm.restype = [rows, p, rows, ci, cf, rows, p, cf, i64, i64, rows, rows, p], ci
+        L.vlut_gated_norm.argtypes, L.vlut_gated_norm.restype = [rows, rows, ci, p, cf, i64, i64, rows, p], ci
+        L.vlut_token_logprobs_bytes.argtypes, L.vlut_token_logprobs_bytes.restype = [i64, i64, ci], sz
+        L.vlut_token_logprobs.argtypes, L.vlut_token_logprobs.restype = [rows, p, cf, ci, i64, i64, p, p, p, p, p, sz, p], ci
         L.vlut_set_plan.argtypes, L.vlut_set_plan.restype = [ci, ci, ci, ci], ci
         L.vlut_query_plan.argtypes, L.vlut_query_plan.restype = [i64, i64, i64, ctypes.POINTER(ci)], ci
         _load_native(L)
@@ -148,6 +158,7 @@ _NATIVE_ORDER = ("vlut_quantize_act", "vlut_mpgemm_lean", "vlut_workspace_used",
                  "vlut_packed_weight_bytes_mixed")
 
 _NATIVE_ATTENTION_ORDER = ("vlut_norm_rope", "vlut_append_kv", "vlut_shared_prefix_attention", "vlut_shared_prefix_attention_bytes")
+_NATIVE_LAYER_ORDER = ("vlut_residual_norm", "vlut_gated_norm", "vlut_token_logprobs", "vlut_token_logprobs_bytes")
 
 
 def built_for() -> str:
@@ -167,7 +178,7 @@ def _load_native(L: ctypes.CDLL) -> None:
         return
     if getattr(mod, "built_for", None) != built_for():      # (whose symbols are all here)
         return
-    for bind, order in ((mod.bind, _NATIVE_ORDER), (mod.bind_attention, _NATIVE_ATTENTION_ORDER)):
+    for bind, order in ((mod.bind, _NATIVE_ORDER), (mod.bind_attention, _NATIVE_ATTENTION_ORDER), (mod.bind_layer, _NATIVE_LAYER_ORDER)):
         bind(*[ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in order])
     _native = mod
 
@@ -691,3 +702,118 @@ def shared_prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
         max_own_len, _ptr(query_lens), B, n, D, D ** -0.5 if scale is None else scale, ctypes.byref(rows[1]), out.stride(0), _ptr(lse),
         _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()), "vlut_shared_prefix_attention")
     return out, lse
+
+
+# ---- around a block: norms, gate, residual; behind the last product: log probabilities
+_ACTIVATIONS = {None: 0, "none": 0, "sigmoid": 1, "silu": 2, "relu2": 3, "gelu": 4}
+
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """The tensors are on the current device, whose current stream the call is given."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor on {t.device}: the current device is wanted")
+
+
+def _rows(t: Optional[torch.Tensor], shape, what: str) -> Optional[_Rows]:
+    """[N][K], features contiguous."""
+    if t is None:
+        return None
+    _on_gpu(t, 2, what)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: a tensor of {tuple(shape)} is wanted, not {tuple(t.shape)}")
+    return _Rows(t.data_ptr(), t.stride(0), _TYPES[t.dtype])
+
+
+def _weight(t: Optional[torch.Tensor], K: int, what: str) -> Optional[torch.Tensor]:
+    if t is not None and not (t.is_cuda and t.dtype == torch.float32 and tuple(t.shape) == (K,) and t.is_contiguous()):
+        raise ValueError(f"{what}: a contiguous fp32 GPU tensor [{K}] is wanted")
+    return t
+
+
+def _gate(gate: Optional[torch.Tensor], y: torch.Tensor) -> Optional[torch.Tensor]:
+    """One for all tokens as rows that lie on each other."""
+    return gate.expand(y.shape) if gate is not None and gate.dim() == 1 and y.dim() == 2 and gate.shape[0] == y.shape[1] else gate
+
+
+def _activation(name: Optional[str]) -> int:
+    if name not in _ACTIVATIONS:
+        raise ValueError(f"activation: one of {sorted(k for k in _ACTIVATIONS if k)} is wanted, not {name!r}")
+    return _ACTIVATIONS[name]
+
+
+def residual_norm(y: torch.Tensor, residual: torch.Tensor, weight: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                  activation: Optional[str] = None, scale: float = 1.0, next_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, next_out: Optional[torch.Tensor] = None):
+    """Runs vlut_residual_norm behind a block with output y [N][K]: h = residual + scale * act(gate) * norm(y), and the next block's input
+    x = norm(h) where `next_weight` is given, in one pass.  weight, next_weight: fp32 [K] of RMS norms (weight None: no norm after the block).  gate: [N][K], or
+    [K] for all tokens, of y's type or fp32; activation: None, "sigmoid", "silu", "relu2" or "gelu" of it.  Returns (h of the residual's type, x or
+    None of type `dtype`, default y's); `out` and `next_out` may be an input itself (the residual, say)."""
+    if _native is not None:
+        r = _native.residual_norm(y, residual, weight, gate, activation, scale, next_weight, eps, dtype, out, next_out)
+        if r is not None:
+            return _outputs(r, "vlut_residual_norm")
+    _on_gpu(y, 2, "y")
+    N, K = y.shape
+    code, gate = _activation(activation), _gate(gate, y)
+    if residual.dtype not in _TYPES or (next_out is not None and next_weight is None):
+        raise ValueError("next_out: a next_weight is wanted" if residual.dtype in _TYPES else f"residual: fp32, bf16 or fp16 is wanted, not {residual.dtype}")
+    if out is None:
+        out = torch.empty((N, K), dtype=residual.dtype, device=y.device)
+    if next_out is None and next_weight is not None:
+        next_out = torch.empty((N, K), dtype=y.dtype if dtype is None else dtype, device=y.device)
+    _here(y, residual, weight, gate, next_weight, out, next_out)
+    rows = [_rows(t, (N, K), what) for t, what in ((y, "y"), (gate, "gate"), (residual, "residual"), (out, "out"), (next_out, "next_out"))]
+    _check(lib().vlut_residual_norm(_ref(rows[0]), _ptr(_weight(weight, K, "weight")), _ref(rows[1]), code, scale, _ref(rows[2]),
+                                    _ptr(_weight(next_weight, K, "next_weight")), eps, N, K, _ref(rows[3]), _ref(rows[4]), _stream()), "vlut_residual_norm")
+    return out, next_out
+
+
+def gated_norm(x: torch.Tensor, gate: Optional[torch.Tensor] = None, activation: Optional[str] = "silu", weight: Optional[torch.Tensor] = None,
+               eps: float = 1e-6, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Runs vlut_gated_norm inside a block: act(gate) * x (act(x) without a gate), x [N][K], and its RMS norm where `weight` (fp32 [K]) is given.  x and gate may be
+    views of a stacked gate|up projection's rows.  Returns out of type `dtype` (default: x's)."""
+    if _native is not None:
+        r = _native.gated_norm(x, gate, activation, weight, eps, dtype, out)
+        if r is not None:
+            return _outputs(r, "vlut_gated_norm")[0]
+    _on_gpu(x, 2, "x")
+    N, K = x.shape
+    code, gate = _activation(activation), _gate(gate, x)
+    if out is None:
+        out = torch.empty((N, K), dtype=x.dtype if dtype is None else dtype, device=x.device)
+    _here(x, gate, weight, out)
+    rows = [_rows(t, (N, K), what) for t, what in ((x, "x"), (gate, "gate"), (out, "out"))]
+    _check(lib().vlut_gated_norm(_ref(rows[0]), _ref(rows[1]), code, _ptr(_weight(weight, K, "weight")), eps, N, K, _ref(rows[2]), _stream()), "vlut_gated_norm")
+    return out
+
+
+def token_logprobs_bytes(N: int, V: int, top: int = 0) -> int:
+    return lib().vlut_token_logprobs_bytes(N, V, top)
+
+
+def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0, want_entropy: bool = True,
+                   workspace: Optional[torch.Tensor] = None):
+    """Runs vlut_token_logprobs on logits [N][V] (fp32, bf16 or fp16; -inf: not allowed): (log probabilities of the int64 `tokens` [N] or None, entropies or
+    None, int64 ids [N][top] of the largest logits or None, their log probabilities or None); fp32, of softmax(logits / temperature)."""
+    if _native is not None:
+        r = _native.token_logprobs(logits, tokens, top, temperature, want_entropy, workspace)
+        if r is not None:
+            return _outputs(r, "vlut_token_logprobs")
+    _on_gpu(logits, 2, "logits")
+    N, V = logits.shape
+    if tokens is not None:
+        _indices(tokens, torch.int64, N, "tokens")
+    new = lambda dtype, *shape: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
+    _here(logits, tokens, workspace)
+    logprob = None if tokens is None else new(torch.float32, N)
+    entropy = new(torch.float32, N) if want_entropy else None
+    ids, logprobs = (new(torch.int64, N, top), new(torch.float32, N, top)) if top > 0 else (None, None)
+    if workspace is None:
+        nbytes = token_logprobs_bytes(N, V, top)
+        if nbytes:
+            workspace = new(torch.uint8, nbytes)
+    _check(lib().vlut_token_logprobs(_ref(_rows(logits, (N, V), "logits")), _ptr(tokens), temperature, top, N, V, _ptr(logprob), _ptr(entropy), _ptr(ids),
+                                     _ptr(logprobs), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()),
+           "vlut_token_logprobs")
+    return logprob, entropy, ids, logprobs

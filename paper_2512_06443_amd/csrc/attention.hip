@@ -10,6 +10,7 @@
 
 #include "attention_params.h"
 #include "common.hip.h"
+#include "host_checks.h"
 #include "launch.hip.h"
 #include "heads_kernel.hip.h"
 
@@ -20,24 +21,9 @@ using namespace vlut_attention;
 constexpr int kUnits = 256;            // compute units that a launch is to fill
 constexpr int64_t kMostBlocks = 1 << 24;       // of 256 threads
 
-bool type_ok(int type) { return type == VLUT_TYPE_F32 || type == VLUT_TYPE_BF16 || type == VLUT_TYPE_F16; }
-int type_bytes(int type) { return type == VLUT_TYPE_F32 ? 4 : 2; }
-bool power_of_two(int64_t v) { return v > 0 && (v & (v - 1)) == 0; }
-
 // ---------------------------------------------------------------------------------------------
 // Heads
 // ---------------------------------------------------------------------------------------------
-// Vectors of 4, 2 or 1: the widest that divides the pairs and whose loads and stores are aligned everywhere.
-struct Alignment {
-    int vec = 4;
-    void pointer(const void* p, int bytes) {
-        while (vec > 1 && (uintptr_t)p % (uintptr_t)(vec * bytes)) vec /= 2;
-    }
-    void stride(int64_t s) {
-        while (vec > 1 && s % vec) vec /= 2;
-    }
-};
-
 // The checks that norm_rope and append_kv share; fills in p but for where rows go.
 int heads_params(HeadsParams& p, const vlut_heads* const (&in)[3], float eps, const vlut_rotation* rot, int64_t N, int64_t D, Alignment& a) {
     if (N < 1 || N >= kMaxDim || D < 2 || D > VLUT_MAX_HEAD_FEATURES || D % 2) return VLUT_ERR_SHAPE;

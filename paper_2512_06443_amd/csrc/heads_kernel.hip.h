@@ -2,6 +2,8 @@
 // Part of the translation unit attention.hip (included there, in this order).
 #pragma once
 
+#include "vectors.hip.h"
+
 namespace {
 
 // ---------------------------------------------------------------------------------------------
@@ -36,39 +38,6 @@ struct HeadsParams {
     unsigned first_block;      // of this launch
     int D, R, interleaved, lanes_log, page_log;
 };
-
-template <class T, int N>
-using Vec = T __attribute__((ext_vector_type(N)));
-template <class T, int N>
-struct LoadVec {
-    typedef Vec<T, N> type;
-};
-template <class T>
-struct LoadVec<T, 1> {
-    typedef T type;
-};
-
-template <class T, int N>
-__device__ __forceinline__ void load_floats(float (&v)[N], const T* p) {
-    typedef typename LoadVec<T, N>::type L;
-    const L x = *(const L*)p;
-    if constexpr (N == 1) v[0] = (float)x;
-    else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = (float)x[i];
-    }
-}
-template <class T, int N>
-__device__ __forceinline__ void store_floats(T* p, const float (&v)[N]) {
-    typedef typename LoadVec<T, N>::type L;
-    L x;
-    if constexpr (N == 1) x = (T)v[0];
-    else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = (T)v[i];
-    }
-    *(L*)p = x;
-}
 
 // HEADS neighbouring heads of a token per group of lanes, whose loads are on their way together and whose rotation is loaded once.
 template <class TI, class TO, int VEC, int HEADS>

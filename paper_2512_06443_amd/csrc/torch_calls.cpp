@@ -276,6 +276,7 @@ PyObject* py_bind(PyObject*, PyObject* const* o, Py_ssize_t n) {
 }  // namespace
 
 #include "attention_calls.h"
+#include "layer_calls.h"
 
 namespace {
 
@@ -293,6 +294,10 @@ PyMethodDef kMethods[] = {
     {"norm_rope", (PyCFunction)(void (*)(void))py_norm_rope, METH_FASTCALL, nullptr},
     {"append_kv", (PyCFunction)(void (*)(void))py_append_kv, METH_FASTCALL, nullptr},
     {"shared_prefix_attention", (PyCFunction)(void (*)(void))py_shared_prefix_attention, METH_FASTCALL, nullptr},
+    {"bind_layer", (PyCFunction)(void (*)(void))py_bind_layer, METH_FASTCALL, nullptr},
+    {"residual_norm", (PyCFunction)(void (*)(void))py_residual_norm, METH_FASTCALL, nullptr},
+    {"gated_norm", (PyCFunction)(void (*)(void))py_gated_norm, METH_FASTCALL, nullptr},
+    {"token_logprobs", (PyCFunction)(void (*)(void))py_token_logprobs, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_vlut_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
