@@ -486,6 +486,35 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
                                  int64_t out_sequence_stride, float* lse_or_null, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention of B sequences with new tokens, packed one sequence behind the other, over a paged cache that holds their keys and values already: prompts,
+ * chunks of them, drafts and single tokens in one call.  Sequence b has the rows query_starts[b] .. query_starts[b + 1] - 1 of q and out, n of them, and
+ * lens[b] tokens in all, of which the n are the last: query j has position p = lens[b] - n + j and sees the tokens max(0, p - window + 1) .. p (0 .. p with a window of 0):
+ *   out[row][h] = sum_t softmax_t(scale * q[row][h] . k[t][h / G]) v[t][h / G],   G = query heads / key heads.
+ * A query that sees nothing, or nothing but keys that score -inf, gets 0 (and lse -inf).  Rows of no sequence are left as they are.  Keys and values that a query does
+ * not see have no influence on it, NaN and infinities included.  An infinite value that a query sees makes that feature of its output infinite; NaN with
+ * infinities of both signs, and where the key's score is -inf.
+ *   q, out            N tokens; q of the cache's type, out of that type or fp32, apart from q.  Scores and sums are fp32; softmax weights go to the product with V in the
+ *                     cache's type, for fp32 outputs in as many terms of it as carry 24 bits.
+ *   page_table        dev [B][table_stride]: pages of each sequence, token 0 first in page 0; ceil(lens[b] / page_size) of a row are read.  NULL for max_len 0
+ *   query_starts      dev [B + 1], ascending, within 0 .. N (a sequence whose two are not has no rows)
+ *   lens              dev [B], 0 <= lens[b] <= max_len
+ *   max_queries, max_len   host: upper bounds of what is on the device, which size the launch and the workspace
+ *   lse               dev or NULL, fp32 [N][heads]: log of the sum of exp(scale * q . k)
+ *   scale             finite and > 0
+ *   workspace         dev, 16-byte aligned, workspace_bytes >= vlut_chunk_attention_bytes(...); may be NULL when that is 0
+ * N and B below 2^24, N * heads, lengths and window below 2^30, and no more workgroups than a launch has (2^22; VLUT_ERR_SHAPE otherwise).  D and alignment as in
+ * vlut_shared_prefix_attention.  Lengths past max_len, more queries than max_queries and page numbers outside the cache are found on the device: they read
+ * nothing, and the queries that depend on them get NaN (more queries than max_queries: or their result).
+ * vlut_query_chunk_attention: out6 (host) = { rows of a key head up to which a sequence is worked on as one of few (0: none), parts of its keys at most, keys of a
+ * part; rows of a tile of the others (0: none), parts of its keys at most, keys of a part }.
+ */
+size_t vlut_chunk_attention_bytes(int64_t N, int64_t B, int64_t q_heads, int64_t k_heads, int64_t D, int64_t max_queries, int64_t max_len, int64_t window);
+int vlut_query_chunk_attention(int64_t N, int64_t B, int64_t q_heads, int64_t k_heads, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, int* out6);
+int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int32_t* page_table, int64_t table_stride, const int32_t* query_starts, const int32_t* lens,
+                         int64_t N, int64_t B, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, float scale, const vlut_heads* out, float* lse_or_null,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Between the products of a decoder layer, and behind the last one.  Inference only, as above.
  */
 

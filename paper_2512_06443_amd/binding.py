@@ -38,6 +38,7 @@ EXPORTS = [
     "vlut_mpgemm_lean", "vlut_mpgemm_g5_lean", "vlut_mpgemm_mixed_lean",
     "vlut_norm_rope", "vlut_append_kv", "vlut_shared_prefix_attention", "vlut_shared_prefix_attention_bytes",
     "vlut_query_shared_prefix_attention",
+    "vlut_chunk_attention", "vlut_chunk_attention_bytes", "vlut_query_chunk_attention",
     "vlut_residual_norm", "vlut_gated_norm", "vlut_token_logprobs", "vlut_token_logprobs_bytes",
 ]
 
@@ -131,6 +132,10 @@ def lib() -> ctypes.CDLL:
         L.vlut_query_shared_prefix_attention.restype = ci
         L.vlut_shared_prefix_attention.argtypes = [heads, i64, cache, p, i64, p, i64, p, i64, p, i64, i64, i64, cf, heads, i64, p, p, sz, p]
         L.vlut_shared_prefix_attention.restype = ci
+        L.vlut_chunk_attention_bytes.argtypes, L.vlut_chunk_attention_bytes.restype = [i64] * 8, sz
+        L.vlut_query_chunk_attention.argtypes, L.vlut_query_chunk_attention.restype = [i64] * 8 + [ctypes.POINTER(ci)], ci
+        L.vlut_chunk_attention.argtypes = [heads, cache, p, i64, p, p, i64, i64, i64, i64, i64, i64, cf, heads, p, p, sz, p]
+        L.vlut_chunk_attention.restype = ci
         rows = ctypes.POINTER(_Rows)
         L.vlut_residual_norm.argtypes, L.vlut_residual_norm.restype = [rows, p, rows, ci, cf, rows, p, cf, i64, i64, rows, rows, p], ci
         L.vlut_gated_norm.argtypes, L.vlut_gated_norm.restype = [rows, rows, ci, p, cf, i64, i64, rows, p], ci
@@ -158,7 +163,7 @@ _NATIVE_ORDER = ("vlut_quantize_act", "vlut_mpgemm_lean", "vlut_workspace_used",
                  "vlut_packed_weight_bytes_mixed")
 
 _NATIVE_ATTENTION_ORDER = ("vlut_norm_rope", "vlut_append_kv", "vlut_shared_prefix_attention", "vlut_shared_prefix_attention_bytes")
-_NATIVE_LAYER_ORDER = ("vlut_residual_norm", "vlut_gated_norm", "vlut_token_logprobs", "vlut_token_logprobs_bytes")
+_NATIVE_LAYER_ORDER = ("vlut_chunk_attention", "vlut_chunk_attention_bytes", "vlut_residual_norm", "vlut_gated_norm", "vlut_token_logprobs", "vlut_token_logprobs_bytes")
 
 
 def built_for() -> str:
@@ -704,15 +709,71 @@ def shared_prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     return out, lse
 
 
-# ---- around a block: norms, gate, residual; behind the last product: log probabilities
-_ACTIVATIONS = {None: 0, "none": 0, "sigmoid": 1, "silu": 2, "relu2": 3, "gelu": 4}
-
-
+# ---- chunks of new tokens over a paged cache
 def _here(*tensors: Optional[torch.Tensor]) -> None:
     """The tensors are on the current device, whose current stream the call is given."""
     for t in tensors:
         if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
             raise ValueError(f"a tensor on {t.device}: the current device is wanted")
+
+
+def chunk_attention_bytes(N: int, B: int, q_heads: int, k_heads: int, D: int, max_queries: int, max_len: int, window: int = 0) -> int:
+    return lib().vlut_chunk_attention_bytes(N, B, q_heads, k_heads, D, max_queries, max_len, window)
+
+
+def query_chunk_attention(N: int, B: int, q_heads: int, k_heads: int, D: int, max_queries: int, max_len: int, window: int = 0) -> Tuple[int, int, int, int, int, int]:
+    """(rows of a key head up to which a sequence is worked on as one of few, parts of its keys at most, keys of a part; rows of a tile of the others, parts,
+    keys) of such a call."""
+    out = (ctypes.c_int * 6)()
+    _check(lib().vlut_query_chunk_attention(N, B, q_heads, k_heads, D, max_queries, max_len, window, out), "vlut_query_chunk_attention")
+    return tuple(out)
+
+
+def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tensor, query_starts: torch.Tensor, lens: torch.Tensor,
+                    max_queries: Optional[int] = None, max_len: Optional[int] = None, window: int = 0, scale: Optional[float] = None,
+                    dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, want_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """Runs vlut_chunk_attention: q [N][heads][D] (the cache's type) holds the new tokens of B sequences one behind the other, sequence b's from row
+    query_starts[b] to query_starts[b + 1] (int32 [B + 1]); they are the last of its lens[b] tokens (int32 [B]), whose keys and values the pages of
+    its row of `page_table` (int32 [B][pages]) hold.  Each sees the tokens up to itself, the last `window` of them where that is not 0.
+    max_queries, max_len: upper bounds (default: N, and what the table's rows hold).  scale: default D ** -0.5.  dtype: fp32 or the cache's
+    (default).  Returns (out [N][heads][D], lse fp32 [N][heads] or None); rows of no sequence are left as they are."""
+    if _native is not None:
+        r = _native.chunk_attention(q, k_cache, v_cache, page_table, query_starts, lens, max_queries, max_len, window, scale, dtype, out, want_lse, workspace)
+        if r is not None:
+            return _outputs(r, "vlut_chunk_attention")
+    _on_gpu(q, 3, "q")
+    N, Hq, D = q.shape
+    cache = _cache(k_cache, v_cache, D)
+    page_size, Hk = k_cache.shape[2], k_cache.shape[1]
+    if not page_table.is_cuda or page_table.dtype != torch.int32 or page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table: an int32 GPU tensor [B][pages] is wanted")
+    B, room = page_table.shape[0], page_table.shape[1] * page_size
+    if not (query_starts.is_cuda and query_starts.dtype == torch.int32 and query_starts.is_contiguous() and tuple(query_starts.shape) == (B + 1,)):
+        raise ValueError(f"query_starts: a contiguous int32 GPU tensor [{B + 1}] is wanted")
+    _indices(lens, torch.int32, B, "lens")
+    max_len = room if max_len is None else max_len
+    max_queries = N if max_queries is None else max_queries
+    if max_len > room:
+        raise ValueError("max_len: more tokens than the rows of page_table hold")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype if dtype is None else dtype, device=q.device)
+    _on_gpu(out, 3, "out")
+    if out.shape != q.shape:
+        raise ValueError("out: a tensor of q's shape is wanted")
+    _here(q, k_cache, v_cache, page_table, query_starts, lens, out, workspace)
+    lse = torch.empty((N, Hq), dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        nbytes = chunk_attention_bytes(N, B, Hq, Hk, D, max_queries, max_len, window)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    _check(lib().vlut_chunk_attention(_ref(_heads(q, what="q")), _ref(cache), _ptr(page_table), page_table.stride(0), query_starts.data_ptr(), lens.data_ptr(), N, B, D,
+                                      max_queries, max_len, window, D ** -0.5 if scale is None else scale, _ref(_heads(out, what="out")), _ptr(lse), _ptr(workspace),
+                                      0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()), "vlut_chunk_attention")
+    return out, lse
+
+
+# ---- around a block: norms, gate, residual; behind the last product: log probabilities
+_ACTIVATIONS = {None: 0, "none": 0, "sigmoid": 1, "silu": 2, "relu2": 3, "gelu": 4}
 
 
 def _rows(t: Optional[torch.Tensor], shape, what: str) -> Optional[_Rows]:

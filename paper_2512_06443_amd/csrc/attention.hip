@@ -135,14 +135,6 @@ int rows_out(HeadRows& k, const vlut_heads* out, int type, Alignment& a) {
     return VLUT_OK;
 }
 
-int check_cache(const vlut_cache* c) {
-    if (!c || !c->k || !c->v) return VLUT_ERR_NULL;
-    if (c->type != VLUT_TYPE_BF16 && c->type != VLUT_TYPE_F16) return VLUT_ERR_UNSUPPORTED;
-    if (c->heads < 1 || c->heads >= (1 << 16) || c->pages < 1 || c->page_size < 1) return VLUT_ERR_SHAPE;
-    if (!power_of_two(c->page_size) || c->page_size > 65536) return VLUT_ERR_UNSUPPORTED;
-    return VLUT_OK;
-}
-
 // ---------------------------------------------------------------------------------------------
 // Attention
 // ---------------------------------------------------------------------------------------------
@@ -229,11 +221,6 @@ bool grouped_keys(const vlut_cache& c) {
     for (int64_t s : {c.k_page_stride, c.v_page_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30);
     for (int64_t s : {c.k_token_stride, c.v_token_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) / std::max<int64_t>(c.page_size, 16);
     return ok;
-}
-
-// Rows that start at a dword.
-bool at_dwords(const void* p, int64_t s0, int64_t s1, int64_t s2, int bytes) {
-    return (uintptr_t)p % 4 == 0 && (bytes == 4 || (s0 % 2 == 0 && s1 % 2 == 0 && s2 % 2 == 0));
 }
 
 }  // namespace

@@ -4,19 +4,6 @@
 
 namespace {
 
-bool allow_lds(const void* kfn, int bytes, std::atomic<unsigned>& done_mask) {
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return false;
-    const unsigned bit = (dev >= 0 && dev < 32) ? (1u << dev) : 0u;
-    if (bit && (done_mask.load(std::memory_order_relaxed) & bit)) return true;
-    if (hipFuncSetAttribute(kfn, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) {
-        (void)hipGetLastError();
-        return false;
-    }
-    done_mask.fetch_or(bit, std::memory_order_relaxed);
-    return true;
-}
-
 template <class T, int DP, int MT, int OWN, int TERMS, bool WHOLE, bool GROUPED>
 int launch_few_t(const AttendParams& p, hipStream_t stream) {
     static std::atomic<unsigned> done{0};

@@ -1,0 +1,185 @@
+// Attention of chunks of new tokens over a paged cache, for MI355X (gfx950): its host side and part of the C ABI; the kernels are in two more units.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "vlut.h"
+
+#include "chunk_params.h"
+#include "host_checks.h"
+
+namespace {
+
+using namespace vlut_chunk;
+
+constexpr int kUnits = 256;            // compute units that a launch is to fill
+constexpr int64_t kMost = (int64_t)1 << 30, kMostBlocks = (int64_t)1 << 22;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t whole_lines(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+int log2_of(int64_t v) {
+    int k = 0;
+    while (((int64_t)1 << k) < v) ++k;
+    return k;
+}
+
+// fast: see ChunkPlan.  The workspace does not depend on it.
+int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, ChunkPlan* out) {
+    if (N < 1 || N >= ((int64_t)1 << 24) || B < 1 || B >= ((int64_t)1 << 24) || Hk < 1 || Hq < 1 || Hq >= (1 << 16) || Hq % Hk) return VLUT_ERR_SHAPE;
+    if (max_len < 0 || max_len >= kMost || max_queries < 0 || window < 0 || window >= kMost || D < 1 || N * Hq >= kMost) return VLUT_ERR_SHAPE;
+    if (D < 8 || D > VLUT_MAX_HEAD_FEATURES || D % 4) return VLUT_ERR_UNSUPPORTED;
+    ChunkPlan a{};
+    const int64_t G = Hq / Hk, most_rows = std::min(max_queries, N) * G;
+    // Keys that a tile of `tokens` neighbouring tokens sees, at most (it begins at a multiple of 32, up to 31 keys earlier).
+    const auto seen = [&](int64_t tokens) { return std::max<int64_t>(1, window ? std::min(max_len, window + tokens) : max_len) + 31; };
+    a.DP = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
+    a.many = most_rows > kFewRows;
+    // With one sequence that may have many rows there is nothing for a launch for few.
+    a.few = !a.many || (B > 1 && G <= kFewRows);
+    if (a.few) {
+        a.few_row_places = (int)std::min<int64_t>(kFewRows, std::max<int64_t>(1, most_rows / G) * G);
+        const int64_t keys = seen(kFewRows), steps = ceil_div(keys, 128);
+        const int64_t slots = (a.DP > 128 ? 1 : 2) * kUnits;
+        // Parts so that the workgroups are four rounds of those that run at once, of four steps at least; where that many are not there, of one.
+        int64_t per = std::max<int64_t>(4, ceil_div(B * Hk * steps, 4 * slots));
+        if (B * Hk * ceil_div(steps, per) < slots) per = std::max<int64_t>(1, std::min(per, B * Hk * steps / slots));
+        a.few_chunk = (int)(128 * per);
+        a.few_splits = (int)ceil_div(keys, a.few_chunk);
+        const int64_t blocks = ceil_div(B * Hk * a.few_splits, 8);
+        if (8 * blocks >= kMostBlocks) return VLUT_ERR_SHAPE;
+        a.few_per_xcd = (int)blocks;
+        if (a.few_splits > 1) {
+            const size_t parts = (size_t)a.few_splits * (size_t)B * (size_t)Hk * (size_t)a.few_row_places;
+            a.few_o_bytes = whole_lines(parts * (size_t)D * 4);
+            a.few_ml_bytes = whole_lines(parts * 8);
+        }
+    }
+    if (a.many) {
+        const int64_t rows = N * G;
+        a.many_waves = a.DP <= 128 && rows * Hk >= 256 * kUnits ? 8 : 4;
+        a.many_rows = 32 * a.many_waves;
+        a.many_tiles = (int)std::min(rows / a.many_rows + B, (rows + B * (a.many_rows - 1)) / a.many_rows);
+        const int64_t keys = seen(a.many_rows / G + 1), step = a.DP > 128 ? 32 : 64;
+        const int64_t slots = (a.many_waves == 4 && a.DP <= 128 ? 2 : 1) * kUnits, tiles = a.many_tiles * Hk;
+        int64_t splits = std::min(std::max<int64_t>(1, slots / tiles), ceil_div(keys, 256));
+        a.many_chunk = (int)(ceil_div(ceil_div(keys, splits), step) * step);
+        a.many_splits = (int)ceil_div(keys, a.many_chunk);
+        const int64_t blocks = ceil_div(tiles * a.many_splits, 8);
+        if (8 * blocks * a.many_waves / 4 >= kMostBlocks) return VLUT_ERR_SHAPE;
+        a.many_per_xcd = (int)blocks;
+        if (a.many_splits > 1) {
+            const size_t parts = (size_t)a.many_splits * (size_t)N * (size_t)Hq;
+            a.many_o_bytes = whole_lines(parts * (size_t)D * 4);
+            a.many_ml_bytes = whole_lines(parts * 8);
+        }
+    }
+    *out = a;
+    return VLUT_OK;
+}
+
+// Eight keys share their page, and strides and the offsets inside a page fit 31 bits, in bytes.
+bool grouped_by_eight(const vlut_cache& c) {
+    bool ok = c.page_size >= 8;
+    for (int64_t s : {c.k_page_stride, c.v_page_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30);
+    for (int64_t s : {c.k_token_stride, c.v_token_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) / std::max<int64_t>(c.page_size, 8);
+    return ok;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t vlut_chunk_attention_bytes(int64_t N, int64_t B, int64_t q_heads, int64_t k_heads, int64_t D, int64_t max_queries, int64_t max_len, int64_t window) {
+    ChunkPlan a;
+    return plan_chunks(N, B, q_heads, k_heads, D, max_queries, max_len, window, &a) == VLUT_OK ? a.bytes() : 0;
+}
+
+int vlut_query_chunk_attention(int64_t N, int64_t B, int64_t q_heads, int64_t k_heads, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, int* out6) {
+    if (!out6) return VLUT_ERR_NULL;
+    ChunkPlan a;
+    const int rc = plan_chunks(N, B, q_heads, k_heads, D, max_queries, max_len, window, &a);
+    if (rc != VLUT_OK) return rc;
+    out6[0] = a.few ? a.few_row_places : 0;
+    out6[1] = a.few_splits;
+    out6[2] = a.few_chunk;
+    out6[3] = a.many_rows;
+    out6[4] = a.many_splits;
+    out6[5] = a.many_chunk;
+    return VLUT_OK;
+}
+
+int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int32_t* page_table, int64_t table_stride, const int32_t* query_starts, const int32_t* lens,
+                         int64_t N, int64_t B, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, float scale, const vlut_heads* out, float* lse_or_null,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+    if (!q || !out) return VLUT_ERR_NULL;
+    int rc = check_cache(cache);
+    if (rc != VLUT_OK) return rc;
+    ChunkPlan a;
+    rc = plan_chunks(N, B, q->heads, cache->heads, D, max_queries, max_len, window, &a);
+    if (rc != VLUT_OK) return rc;
+    if (!q->data || !out->data || !query_starts || !lens || (max_len > 0 && !page_table)) return VLUT_ERR_NULL;
+    if (out->heads != q->heads || q->type != cache->type || (out->type != cache->type && out->type != VLUT_TYPE_F32)) return VLUT_ERR_SHAPE;
+    if (cache->pages >= ((int64_t)1 << 31)) return VLUT_ERR_SHAPE;
+    if (!(scale > 0.0f) || !std::isfinite(scale)) return VLUT_ERR_UNSUPPORTED;
+    if (!at_dwords(q->data, 0, q->token_stride, q->head_stride, 2) ||
+        !at_dwords(cache->k, cache->k_page_stride, cache->k_head_stride, cache->k_token_stride, 2) ||
+        !at_dwords(cache->v, cache->v_page_stride, cache->v_head_stride, cache->v_token_stride, 2) ||
+        !at_dwords(out->data, 0, out->token_stride, out->head_stride, type_bytes(out->type)))
+        return VLUT_ERR_UNSUPPORTED;
+    if (a.bytes()) {
+        if (!workspace) return VLUT_ERR_NULL;
+        if (workspace_bytes < a.bytes()) return VLUT_ERR_SMALL_BUFFER;
+        if ((uintptr_t)workspace % 16) return VLUT_ERR_UNSUPPORTED;
+    }
+    a.fast = D == a.DP && grouped_by_eight(*cache);
+    ChunkParams p{};
+    p.q = q->data;
+    p.k = cache->k;
+    p.v = cache->v;
+    p.q_token = q->token_stride;
+    p.q_head = q->head_stride;
+    p.k_page = cache->k_page_stride;
+    p.k_head = cache->k_head_stride;
+    p.k_token = cache->k_token_stride;
+    p.v_page = cache->v_page_stride;
+    p.v_head = cache->v_head_stride;
+    p.v_token = cache->v_token_stride;
+    p.page_table = page_table;
+    p.starts = query_starts;
+    p.lens = lens;
+    p.table_stride = table_stride;
+    p.out = (void*)out->data;
+    p.out_token = out->token_stride;
+    p.out_head = out->head_stride;
+    p.lse = lse_or_null;
+    unsigned char* at = (unsigned char*)workspace;
+    p.few_o = (float*)at;
+    p.few_ml = (float*)(at += a.few_o_bytes);
+    p.many_o = (float*)(at += a.few_ml_bytes);
+    p.many_ml = (float*)(at += a.many_o_bytes);
+    p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    p.out_type = out->type;
+    p.N = (int)N;
+    p.B = (int)B;
+    p.Hk = cache->heads;
+    p.G = q->heads / cache->heads;
+    p.D = (int)D;
+    p.page_log = log2_of(cache->page_size);
+    p.pages = (int)cache->pages;
+    p.max_len = (int)max_len;
+    p.window = (int)(window ? window : kMost);
+    p.few_rows = a.few ? a.few_row_places : 0;
+    p.few_splits = a.few_splits;
+    p.few_chunk = a.few_chunk;
+    p.few_per_xcd = a.few_per_xcd;
+    p.many_splits = a.many_splits;
+    p.many_chunk = a.many_chunk;
+    p.many_tiles = a.many_tiles;
+    p.many_per_xcd = a.many_per_xcd;
+    p.many_rows = a.many_rows;
+    return cache->type == VLUT_TYPE_BF16 ? launch_bf16(a, p, (hipStream_t)stream) : launch_f16(a, p, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,9 +1,11 @@
-// The native form of residual_norm, gated_norm and token_logprobs.  Part of torch_calls.cpp (included there, behind attention_calls.h); what is said there holds.
+// The native form of chunk_attention, residual_norm, gated_norm and token_logprobs.  Part of torch_calls.cpp (included there, behind attention_calls.h); what is said there holds.
 #pragma once
 
 namespace {
 
 struct LayerApi {                              // in the order of binding._NATIVE_LAYER_ORDER
+    decltype(&vlut_chunk_attention) chunk_attention;
+    decltype(&vlut_chunk_attention_bytes) chunk_attention_bytes;
     decltype(&vlut_residual_norm) residual_norm;
     decltype(&vlut_gated_norm) gated_norm;
     decltype(&vlut_token_logprobs) token_logprobs;
@@ -21,6 +23,54 @@ bool here(const T*... t) {
     const c10::DeviceIndex current = c10::hip::current_device();
     return (... && (!t || t->device().index() == current));
 }
+
+// chunk_attention(q, k_cache, v_cache, page_table, query_starts, lens, max_queries, max_len, window, scale, dtype, out, want_lse, workspace)
+PyObject* py_chunk_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        const at::Tensor *q, *gout, *gws;
+        vlut_cache cache;
+        int64_t max_queries, max_len, window;
+        float scale;
+        if (!layer_call(n, 14) || !features(q = plain(o[0]), 3)) Py_RETURN_NONE;
+        const int64_t N = q->size(0), Hq = q->size(1), D = q->size(2);
+        const at::Tensor *kc = plain(o[1]), *vc = plain(o[2]), *table = plain(o[3]), *starts = plain(o[4]), *lens = plain(o[5]);
+        if (D < 1 || !cache_of(kc, vc, D, cache) || cache.page_size < 1 || !table || table->scalar_type() != at::kInt || table->dim() != 2 ||
+            (table->size(1) > 1 && table->stride(1) != 1))
+            Py_RETURN_NONE;
+        const int64_t B = table->size(0), room = table->size(1) * cache.page_size;
+        if (!starts || starts->scalar_type() != at::kInt || starts->dim() != 1 || starts->size(0) != B + 1 || !starts->is_contiguous() || !indices(lens, at::kInt, B)) Py_RETURN_NONE;
+        if (o[6] == Py_None) max_queries = N;
+        else if (!whole(o[6], max_queries)) Py_RETURN_NONE;
+        if (o[7] == Py_None) max_len = room;
+        else if (!whole(o[7], max_len)) Py_RETURN_NONE;
+        if (max_len > room || !whole(o[8], window)) Py_RETURN_NONE;
+        if (o[9] == Py_None) scale = (float)std::pow((double)D, -0.5);
+        else if (!real(o[9], scale)) Py_RETURN_NONE;
+        c10::ScalarType type = q->scalar_type();
+        const int want_lse = PyObject_IsTrue(o[12]);
+        if (want_lse < 0) { PyErr_Clear(); Py_RETURN_NONE; }
+        if (!type_of(o[10], type) || !optional_features(o[11], gout, 3) || (gout && !same_sizes(*gout, *q)) || !optional(o[13], gws) || (gws && !gws->data_ptr()) ||
+            !here(q, kc, vc, table, starts, lens, gout, gws))
+            Py_RETURN_NONE;
+        at::Tensor out, lse, ws;
+        if (gout) out = *gout;
+        if (gws) ws = *gws;
+        int rc;
+        without_gil([&] {
+            if (!gout) out = make(q->sizes(), type, q->device());
+            if (want_lse) lse = make({N, Hq}, at::kFloat, q->device());
+            if (!gws) {
+                const size_t need = g_layer.chunk_attention_bytes(N, B, Hq, cache.heads, D, max_queries, max_len, window);
+                if (need) ws = make({(int64_t)need}, at::kByte, q->device());
+            }
+            const vlut_heads qi = heads_of(*q), oi = heads_of(out);
+            rc = g_layer.chunk_attention(&qi, &cache, (const int32_t*)table->data_ptr(), table->stride(0), (const int32_t*)starts->data_ptr(), (const int32_t*)lens->data_ptr(),
+                                         N, B, D, max_queries, max_len, window, scale, &oi, ptr<float>(lse), ptr<void>(ws), ws.defined() ? bytes_of(ws) : 0, stream());
+        });
+        return result(rc, out, lse);
+    });
+}
+
 bool rows_like(const at::Tensor* t, int64_t N, int64_t K) { return features(t, 2) && t->size(0) == N && t->size(1) == K; }
 bool row_weight(const at::Tensor* w, int64_t K) { return !w || (w->scalar_type() == at::kFloat && w->dim() == 1 && w->size(0) == K && w->is_contiguous()); }
 vlut_rows rows_of(const at::Tensor& t) { return {t.data_ptr(), t.stride(0), number_type(t.scalar_type())}; }

@@ -295,6 +295,7 @@ PyMethodDef kMethods[] = {
     {"append_kv", (PyCFunction)(void (*)(void))py_append_kv, METH_FASTCALL, nullptr},
     {"shared_prefix_attention", (PyCFunction)(void (*)(void))py_shared_prefix_attention, METH_FASTCALL, nullptr},
     {"bind_layer", (PyCFunction)(void (*)(void))py_bind_layer, METH_FASTCALL, nullptr},
+    {"chunk_attention", (PyCFunction)(void (*)(void))py_chunk_attention, METH_FASTCALL, nullptr},
     {"residual_norm", (PyCFunction)(void (*)(void))py_residual_norm, METH_FASTCALL, nullptr},
     {"gated_norm", (PyCFunction)(void (*)(void))py_gated_norm, METH_FASTCALL, nullptr},
     {"token_logprobs", (PyCFunction)(void (*)(void))py_token_logprobs, METH_FASTCALL, nullptr},
