@@ -79,11 +79,12 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
     return VLUT_OK;
 }
 
-// Eight keys share their page, and strides and the offsets inside a page fit 31 bits, in bytes.
+// Eight keys share their page, rows start at 16 bytes, and strides and the offsets inside a page fit 31 bits, in bytes.
 bool grouped_by_eight(const vlut_cache& c) {
-    bool ok = c.page_size >= 8;
-    for (int64_t s : {c.k_page_stride, c.v_page_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30);
-    for (int64_t s : {c.k_token_stride, c.v_token_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) / std::max<int64_t>(c.page_size, 8);
+    bool ok = c.page_size >= 8 && (uintptr_t)c.k % 16 == 0 && (uintptr_t)c.v % 16 == 0;
+    for (int64_t s : {c.k_page_stride, c.v_page_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) && s % 8 == 0;
+    for (int64_t s : {c.k_head_stride, c.v_head_stride}) ok = ok && s % 8 == 0;
+    for (int64_t s : {c.k_token_stride, c.v_token_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) / std::max<int64_t>(c.page_size, 8) && s % 8 == 0;
     return ok;
 }
 
@@ -133,7 +134,7 @@ int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int
         if (workspace_bytes < a.bytes()) return VLUT_ERR_SMALL_BUFFER;
         if ((uintptr_t)workspace % 16) return VLUT_ERR_UNSUPPORTED;
     }
-    a.fast = D == a.DP && grouped_by_eight(*cache);
+    a.fast = D % 8 == 0 && grouped_by_eight(*cache);
     ChunkParams p{};
     p.q = q->data;
     p.k = cache->k;

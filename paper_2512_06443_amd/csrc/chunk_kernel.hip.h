@@ -132,24 +132,98 @@ __device__ __forceinline__ void settle_chunk(const ChunkParams& p, const Tile& t
     }
 }
 
-// A tile's part.  FAST: heads of DP features, and 8 neighbouring keys share their page, so that addresses are worked out once per wave.
+// The kernel's parameters, its first argument, read again: what is wanted behind the loops only would wait in registers throughout.
+__device__ __forceinline__ const ChunkParams& parameters() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    auto at = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(const ChunkParams*)at;
+#else
+    static ChunkParams none;
+    return none;
+#endif
+}
+// The compiler knows nothing of x from here on.
+__device__ __forceinline__ void stay(int& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+v"(x));
+#endif
+}
+
+__device__ __forceinline__ void pinned(float& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+v"(x));
+#endif
+}
+
+// 16 bytes per lane from `base` + `at` on to LDS, lane after lane from `to` on.  Written out: the compiler, when it issues such a load itself, waits for all of them
+// ahead of every LDS read that follows.  No result register; the LDS address is in M0.
+#if defined(__HIP_DEVICE_COMPILE__)
+__device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned at, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+#else
+inline __device__ void load_to_lds(const unsigned char*, unsigned, unsigned) {}
+template <int N>
+inline __device__ void wait_loads() {}
+inline __device__ void wait_lds() {}
+#endif
+template <class V>
+__device__ __forceinline__ V& at_lds(unsigned at) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return *(V*)(__attribute__((address_space(3))) V*)at;
+#else
+    static V none;
+    return none;
+#endif
+}
+
+// Without what is no number: zeros for it, and whether there was any.
+template <class T>
+__device__ __forceinline__ i32x4 without_odd(i32x4 v, unsigned& odd) {
+    constexpr unsigned high = Number<T>::kExponents & 0xffff0000u, low = Number<T>::kExponents & 0xffffu;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const unsigned x = (unsigned)v[w];
+        const unsigned drop = ((x & high) == high ? 0xffff0000u : 0u) | ((x & low) == low ? 0xffffu : 0u);
+        v[w] = (int)(x & ~drop);
+        odd |= drop;
+    }
+    return v;
+}
+
+// A tile's part.  FAST: keys and values are loaded straight to LDS, DEPTH steps ahead, addresses worked out once per wave and 8 keys.  Each stage is exactly
+// LOADS loads per wave, also past the end of the part, where its last keys are loaded again, so that vmcnt((DEPTH - 1) * LOADS) stands for "the
+// stage that was asked for first is there"; what else a wave loads meanwhile only makes that wait longer.  Where waves share the keys each has its own pieces
+// of the stages, and no wave waits for another.
+// Rows of LDS are DP features one behind the other, 16-byte chunks c at c ^ f(row): of keys, so that 16 rows' chunks lie in 64 banks; of values, so that the four
+// rows of a transposing read do.  Chunks behind D are not loaded: zeros from before the first stage.
 template <class T, int DP, int RW, int KW, int TERMS, bool FAST>
 __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
     constexpr bool FEW = KW > 1, WIDE = Number<T>::kWide;
-    constexpr int NW = RW * KW, WK = wave_keys(DP, KW), KT = WK / 32, KEYS = step_keys(DP, KW), KS = DP / 16, CH = DP / 8, PER = 64 * NW / CH, LI = KEYS / PER, GK = 64 / CH;
-    constexpr int KP = k_pitch(DP), VP = v_pitch(DP), BYTES = buffer_bytes_of(DP, KW), DT = DP / 32;
+    constexpr int NW = RW * KW, WK = wave_keys(DP, KW), KT = WK / 32, KEYS = step_keys(DP, KW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
     constexpr float LIFT = 0.5f * Number<T>::kLift;            // (scores after the first step may be larger)
-    static_assert(PER * LI == KEYS, "whole loads");
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int wave_row0 = t.row0 + 32 * rw, row = wave_row0 + l32;
     const int first_key = t.first, end_key = t.end;
 
-    float* const row_m = (float*)(lds + tile_bytes(DP, RW, KW));       // [KW][32 RW], then l
+    // behind the buffers: the waves' m and l where they share rows, where the rows' results go and their factors, two flags (the part is to be
+    // begun again; there is something to settle), pages' numbers
+    float* const row_m = (float*)(lds + tile_bytes(DP, RW, KW, FAST));
     float* const row_l = row_m + 32 * NW;
-    int* const again = (int*)(row_l + 32 * NW);                        // then: whether there is something to settle
+    int64_t* const row_to = (int64_t*)(row_l + 32 * NW);
+    float* const row_factor = (float*)(row_to + 32 * RW);
+    int* const again = (int*)(row_factor + 32 * RW);
+    int* const page_ids = again + 4;
     if (tid == 0) again[0] = again[1] = 0;
+    if (FAST && p.D < DP) {
+        for (int x = 16 * tid; x < tile_bytes(DP, RW, KW, FAST); x += 16 * 64 * NW) *(i32x4*)(lds + x) = i32x4{0, 0, 0, 0};
+    }
     wg_barrier_lds();                                                  // (they are set ahead of the first step's barrier)
 
     // rows past the tile's end do as its last one
@@ -160,123 +234,223 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const int chunk = 2 * ks + half;
-            q[ks] = __builtin_bit_cast(x8, chunk_moved<FAST>(*(const dword_aligned_i32x4*)(src + chunk_at<FAST>(chunk, p.D)), chunk, p.D));
+            q[ks] = __builtin_bit_cast(x8, chunk_moved<false>(*(const dword_aligned_i32x4*)(src + chunk_at<false>(chunk, p.D)), chunk, p.D));
         }
     }
     const int sees_from = max(0, pos - p.window + 1), sees_to = min(end_key, pos + 1);
     const bool blind = sees_to <= max(sees_from, first_key);           // nothing of this part
-    // of the wave's rows, and of the workgroup's: from where to where all of them see, and any
+    // of the wave's rows, and of the workgroup's: from where to where all of them see
     auto position = [&](int of) { return t.seq.base + min(of, t.row_end - 1) / p.G; };
     const int low = position(min(wave_row0, t.row_end - 1)), high = position(wave_row0 + 31);
-    const int all_from = max(0, high - p.window + 1), all_to = low + 1, any_from = max(0, low - p.window + 1), any_to = wave_row0 < t.row_end ? high + 1 : 0;
-    const int tile_low = position(t.row0), tile_high = position(t.row_end - 1), tile_from = max(0, tile_high - p.window + 1), tile_to = tile_low + 1;
+    const int all_from = max(0, high - p.window + 1), all_to = min(end_key, low + 1);
+    const int tile_from = max(0, position(t.row_end - 1) - p.window + 1), tile_to = min(end_key, position(t.row0) + 1);
 
     const int32_t* const pages = p.page_table + t.b * p.table_stride;
     const T* const kh = (const T*)p.k + t.h * p.k_head;
     const T* const vh = (const T*)p.v + t.h * p.v_head;
-    const int mask = (1 << p.page_log) - 1, last = end_key - 1, last_group = last & ~(GK - 1);
-    const int chunk = lane % CH, to_key = GK * wave + lane / CH;
-    const unsigned at = 2u * (unsigned)chunk_at<FAST>(chunk, p.D), k_lane = (unsigned)(lane / CH) * 2u * (unsigned)p.k_token + at, v_lane = (unsigned)(lane / CH) * 2u * (unsigned)p.v_token + at;
-    const unsigned to_k = (unsigned)(to_key * KP + 16 * chunk), to_v = (unsigned)(KEYS * KP + to_key * VP + 16 * chunk);
-    i32x4 kr[LI], vr[LI];
-    int ids[LI];
-    unsigned bad = 0;                          // ids: the next keys' pages; bad: a bit for each loaded key (group) that is in none
-    // (keys past the part read its last one, or another of that one's group: scores are masked, V is zeroed)
-    auto key_of_load = [&](int kt, int i) { return FAST ? min(kt + PER * i + GK * wave, last_group) : min(kt + PER * i + to_key, last); };
-    auto look_up = [&](int kt) {
-#pragma unroll
-        for (int i = 0; i < LI; ++i) ids[i] = pages[key_of_load(kt, i) >> p.page_log];
-    };
-    auto load = [&](int kt) {
-        bad = 0;
-#pragma unroll
-        for (int i = 0; i < LI; ++i) {
-            const int in_page = key_of_load(kt, i) & mask;
-            const unsigned named = FAST ? (unsigned)__builtin_amdgcn_readfirstlane(ids[i]) : (unsigned)ids[i];
-            const bool page = named < (unsigned)p.pages;
-            bad |= page ? 0u : 1u << i;
-            const uint64_t id = page ? named : 0u;
-            if constexpr (FAST) {              // (strides are below 2^31 bytes here, and so are offsets inside a page)
-                kr[i] = *(const dword_aligned_i32x4*)((const unsigned char*)kh + (id * (unsigned)p.k_page * 2u + (unsigned)in_page * 2u * (unsigned)p.k_token) + k_lane);
-                vr[i] = *(const dword_aligned_i32x4*)((const unsigned char*)vh + (id * (unsigned)p.v_page * 2u + (unsigned)in_page * 2u * (unsigned)p.v_token) + v_lane);
-            } else {
-                kr[i] = *(const dword_aligned_i32x4*)(kh + (int64_t)id * p.k_page + in_page * p.k_token + chunk_at<FAST>(chunk, p.D));
-                vr[i] = *(const dword_aligned_i32x4*)(vh + (int64_t)id * p.v_page + in_page * p.v_token + chunk_at<FAST>(chunk, p.D));
-            }
-        }
-    };
-    auto store = [&](int kt, unsigned char* to) {
-        if (bad) {                             // a number that is no page: whoever sees its keys gets NaN
-#pragma unroll
-            for (int i = 0; i < LI; ++i)
-                if (bad >> i & 1) {
-                    constexpr int N = (int)Number<T>::kNan;
-                    kr[i] = i32x4{N, N, N, N};
-                }
-        }
-        if (kt + KEYS > min(end_key, tile_to) || kt < tile_from) {     // not every row sees every key
-            unsigned odd = 0;
-#pragma unroll
-            for (int i = 0; i < LI; ++i) {
-                if (kt + PER * i + to_key >= end_key) vr[i] = i32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const unsigned x = (unsigned)vr[i][w];
-                    constexpr unsigned high_bits = Number<T>::kExponents & 0xffff0000u, low_bits = Number<T>::kExponents & 0xffffu;
-                    const unsigned drop = ((x & high_bits) == high_bits ? 0xffff0000u : 0u) | ((x & low_bits) == low_bits ? 0xffffu : 0u);
-                    vr[i][w] = (int)(x & ~drop);
-                    odd |= drop;
-                }
-            }
-            if (odd) again[1] = 1;
-        }
-#pragma unroll
-        for (int i = 0; i < LI; ++i) {
-            *(i32x4*)(to + to_k + PER * i * KP) = chunk_moved<FAST>(kr[i], chunk, p.D);
-            *(i32x4*)(to + to_v + PER * i * VP) = chunk_moved<FAST>(vr[i], chunk, p.D);
-        }
-    };
+    const int page_log = p.page_log, mask = (1 << page_log) - 1, last = end_key - 1;
+    const float scale_log2 = p.scale_log2;
 
-    // All keys of the part, in steps: use(kt, K and V in LDS) between two barriers each.
+    // sweep(use): all keys of the part, in steps: use(first key, keys' place in LDS, values')
+    // Where a lane reads: of keys, 8 features of row l32 (and 32 rows further); of values, a corner of a transposing read.
+    constexpr int ROW_K = FAST ? DP * 2 : k_pitch(DP), ROW_V = FAST ? DP * 2 : v_pitch(DP);
+    auto turn_k = [](int r) { return DP == 64 ? (r >> 1) & 7 : r & 15; };
+    auto turn_v = [](int r) { return DP == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3); };
+    const unsigned k_lane = (unsigned)(l32 * ROW_K + 16 * (FAST ? half ^ turn_k(l32) : half));
+    const int v_row = 4 * half + (l16 >> 2), v_chunk = 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1);
+    const unsigned v_lane = (unsigned)(v_row * ROW_V + 16 * (FAST ? v_chunk ^ turn_v(v_row) : v_chunk) + 8 * (l16 & 1));
+    auto k_at = [&](unsigned base, int ks) { return FAST ? (base + k_lane) ^ (unsigned)(32 * ks) : base + k_lane + (unsigned)(32 * ks); };
+    auto v_at = [&](unsigned base, int dt) { return FAST ? (base + v_lane) ^ (unsigned)(64 * dt) : base + v_lane + (unsigned)(64 * dt); };
+    const unsigned lds0 = lds_base_of(lds);
+
     auto sweep = [&](auto use) {
         if (first_key >= end_key) return;
-        look_up(first_key);
-        load(first_key);
-        look_up(first_key + KEYS);
+        if constexpr (FAST) {
+            constexpr int S = stages(DP, RW, KW), DEPTH = FEW ? S : S - 1, OWN = FEW ? WK : KEYS / NW, LOADS = 2 * OWN / GK, PERIOD = 16 / GK > 0 ? 16 / GK : 1;
+            constexpr int PART = FEW ? WK * DP * 4 : stage_bytes(DP, KW), V_OFF = PART / 2;         // bytes of a stage (of the wave), and where its values begin
+            static_assert(OWN % 8 == 0 && 8 % GK == 0, "whole groups of 8 keys");
+            const unsigned base0 = lds0 + (FEW ? kw * S * PART : 0);
+            const int own0 = OWN * wave, in_stage = FEW ? 0 : own0;    // the wave's keys in a step, and where they are in a stage
+            const unsigned char *const kb = (const unsigned char*)kh, *const vb = (const unsigned char*)vh;
+            const unsigned k_page = 2u * (unsigned)p.k_page, v_page = 2u * (unsigned)p.v_page, k_token = 2u * (unsigned)p.k_token, v_token = 2u * (unsigned)p.v_token;
+            const bool has = 8 * (lane % CH) < p.D;                    // (a chunk that there is)
+            unsigned k_from[PERIOD], v_from[PERIOD];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) arrived(q[ks]);
-        store(first_key, lds);
-        int turn = 0;
-        for (int kt = first_key; kt < end_key; kt += KEYS, turn ^= 1) {
-            wg_barrier_lds();
-            load(kt + KEYS);                   // (behind the last step too, from the last keys)
-            look_up(kt + 2 * KEYS);
-            if constexpr (buffers(KW) == 2) {
-                use(kt, lds + turn * BYTES);
-                if (kt + KEYS < end_key) store(kt + KEYS, lds + (turn ^ 1) * BYTES);
-            } else {
-                use(kt, lds);
-                if (kt + KEYS < end_key) {
-                    wg_barrier_lds();
-                    store(kt + KEYS, lds);
+            for (int x = 0; x < PERIOD; ++x) {
+                const int r = in_stage + GK * x + lane / CH;
+                k_from[x] = (unsigned)(lane / CH) * k_token + 16u * (unsigned)((lane % CH) ^ turn_k(r));
+                v_from[x] = (unsigned)(lane / CH) * v_token + 16u * (unsigned)((lane % CH) ^ turn_v(r));
+            }
+            bool has_k[PERIOD], has_v[PERIOD];
+#pragma unroll
+            for (int x = 0; x < PERIOD; ++x) {
+                const int r = in_stage + GK * x + lane / CH;
+                has_k[x] = 8 * ((lane % CH) ^ turn_k(r)) < p.D;
+                has_v[x] = 8 * ((lane % CH) ^ turn_v(r)) < p.D;
+            }
+            (void)has;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) arrived(q[ks]);
+            for (int s0 = first_key; s0 < end_key; s0 += kStretch) {
+                const int s1 = s0 + min(end_key - s0, kStretch), id0 = s0 >> page_log, ids = ((s1 - 1) >> page_log) - id0 + 1;
+                wait_loads<0>();
+                __syncthreads();               // (nobody reads the stretch before any more)
+                for (int x = tid; x < ids; x += 64 * NW) {
+                    const int id = pages[id0 + x];
+                    page_ids[x] = (unsigned)id < (unsigned)p.pages ? id : -1;
+                }
+                __syncthreads();
+                const int last_group = (s1 - 1) & ~7;
+                unsigned bad = 0;              // a bit for every 8 keys of the wave in every stage, the newest lowest, that are in no page
+                auto issue = [&](int kt, unsigned stage) {
+#pragma unroll
+                    for (int g = 0; g < OWN / 8; ++g) {
+                        const int key = min(kt + own0 + 8 * g, last_group);
+                        const int named = __builtin_amdgcn_readfirstlane(page_ids[(key >> page_log) - id0]);
+                        bad = bad << 1 | (unsigned)(named < 0);
+                        const unsigned id = (unsigned)max(named, 0), in_page = (unsigned)(key & mask);
+                        const unsigned char* const k = kb + ((uint64_t)id * k_page + in_page * k_token);
+                        const unsigned char* const v = vb + ((uint64_t)id * v_page + in_page * v_token);
+#pragma unroll
+                        for (int i = 0; i < 8 / GK; ++i) {
+                            const int r = 8 * g + GK * i, x = r / GK % PERIOD;
+                            const unsigned to = stage + (unsigned)((in_stage + r) * ROW_K);
+                            if (has_k[x]) load_to_lds(k + (unsigned)(GK * i) * k_token, k_from[x], to);
+                            if (has_v[x]) load_to_lds(v + (unsigned)(GK * i) * v_token, v_from[x], to + V_OFF);
+                        }
+                    }
+                };
+                unsigned now = base0, next = base0;                    // stages: the one that is worked on, and the one that is asked for
+                auto step_on = [&](unsigned& stage) { stage = stage + PART == base0 + S * PART ? base0 : stage + PART; };
+#pragma unroll
+                for (int x = 0; x < DEPTH; ++x) {
+                    issue(s0 + x * KEYS, next);
+                    step_on(next);
+                }
+                for (int kt = s0; kt < s1; kt += KEYS) {
+                    wait_loads<(DEPTH - 1) * LOADS>();
+                    const bool odd_pages = (bad >> ((DEPTH - 1) * (OWN / 8)) & ((1u << (OWN / 8)) - 1)) != 0;
+                    if (kt + KEYS > tile_to || kt < tile_from || odd_pages) {          // not every row sees every key
+                        unsigned odd = 0;
+#pragma unroll
+                        for (int x = 0; x < OWN / GK; ++x) {
+                            const unsigned to = now + (unsigned)((in_stage + GK * x) * ROW_K + 16 * lane);
+                            i32x4 v = without_odd<T>(at_lds<i32x4>(to + V_OFF), odd);
+                            if (kt + own0 + GK * x + lane / CH >= end_key) v = i32x4{0, 0, 0, 0};
+                            at_lds<i32x4>(to + V_OFF) = v;
+                            if (bad >> ((DEPTH - 1) * (OWN / 8) + OWN / 8 - 1 - GK * x / 8) & 1) {     // a number that is no page: whoever sees its keys gets NaN
+                                constexpr int N = (int)Number<T>::kNan;
+                                at_lds<i32x4>(to) = i32x4{N, N, N, N};
+                            }
+                        }
+                        if (odd) again[1] = 1;
+                    }
+                    if constexpr (!FEW) {
+                        wg_barrier_lds();
+                        issue(kt + DEPTH * KEYS, next);                // (behind the last step too, from the last keys)
+                        use(kt, now, now + V_OFF);
+                    } else {
+                        use(kt, now, now + V_OFF);
+                        wait_lds();
+                        issue(kt + DEPTH * KEYS, next);
+                    }
+                    step_on(now);
+                    step_on(next);
+                }
+            }
+            wait_loads<0>();
+        } else {
+            constexpr int PER = 64 * NW / CH, LI = KEYS / PER, BYTES = buffer_bytes_of(DP, KW);
+            static_assert(PER * LI == KEYS, "whole loads");
+            const int chunk = lane % CH, to_key = GK * wave + lane / CH;
+            const unsigned to_k = (unsigned)(to_key * ROW_K + 16 * chunk), to_v = (unsigned)(KEYS * ROW_K + to_key * ROW_V + 16 * chunk);
+            i32x4 kr[LI], vr[LI];
+            int ids[LI];
+            unsigned bad = 0;                  // ids: the next keys' pages; bad: a bit for each loaded key that is in none
+            // (keys past the part read its last one: scores are masked, V is zeroed)
+            auto look_up = [&](int kt) {
+#pragma unroll
+                for (int i = 0; i < LI; ++i) ids[i] = pages[min(kt + PER * i + to_key, last) >> page_log];
+            };
+            auto load = [&](int kt) {
+                bad = 0;
+#pragma unroll
+                for (int i = 0; i < LI; ++i) {
+                    const int in_page = min(kt + PER * i + to_key, last) & mask;
+                    const bool page = (unsigned)ids[i] < (unsigned)p.pages;
+                    bad |= page ? 0u : 1u << i;
+                    const int64_t id = page ? ids[i] : 0;
+                    kr[i] = *(const dword_aligned_i32x4*)(kh + id * p.k_page + in_page * p.k_token + chunk_at<false>(chunk, p.D));
+                    vr[i] = *(const dword_aligned_i32x4*)(vh + id * p.v_page + in_page * p.v_token + chunk_at<false>(chunk, p.D));
+                }
+            };
+            auto store = [&](int kt, unsigned char* to) {
+                if (bad) {
+#pragma unroll
+                    for (int i = 0; i < LI; ++i)
+                        if (bad >> i & 1) {
+                            constexpr int N = (int)Number<T>::kNan;
+                            kr[i] = i32x4{N, N, N, N};
+                        }
+                }
+                if (kt + KEYS > tile_to || kt < tile_from) {
+                    unsigned odd = 0;
+#pragma unroll
+                    for (int i = 0; i < LI; ++i) {
+                        if (kt + PER * i + to_key >= end_key) vr[i] = i32x4{0, 0, 0, 0};
+                        vr[i] = without_odd<T>(vr[i], odd);
+                    }
+                    if (odd) again[1] = 1;
+                }
+#pragma unroll
+                for (int i = 0; i < LI; ++i) {
+                    *(i32x4*)(to + to_k + PER * i * ROW_K) = chunk_moved<false>(kr[i], chunk, p.D);
+                    *(i32x4*)(to + to_v + PER * i * ROW_V) = chunk_moved<false>(vr[i], chunk, p.D);
+                }
+            };
+            const unsigned own_k = (unsigned)(WK * kw * ROW_K), own_v = (unsigned)(KEYS * ROW_K + WK * kw * ROW_V);
+            look_up(first_key);
+            load(first_key);
+            look_up(first_key + KEYS);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) arrived(q[ks]);
+            store(first_key, lds);
+            int turn = 0;
+            for (int kt = first_key; kt < end_key; kt += KEYS, turn ^= 1) {
+                wg_barrier_lds();
+                load(kt + KEYS);               // (behind the last step too, from the last keys)
+                look_up(kt + 2 * KEYS);
+                if constexpr (buffers(KW) == 2) {
+                    use(kt, lds0 + turn * BYTES + own_k, lds0 + turn * BYTES + own_v);
+                    if (kt + KEYS < end_key) store(kt + KEYS, lds + (turn ^ 1) * BYTES);
+                } else {
+                    use(kt, lds0 + own_k, lds0 + own_v);
+                    if (kt + KEYS < end_key) {
+                        wg_barrier_lds();
+                        store(kt + KEYS, lds);
+                    }
                 }
             }
         }
     };
     f32x16 s[KT], o[DT];
     float m = 0.0f, l;
-    auto score = [&](int k0, const unsigned char* buf) {
+    auto score = [&](int k0, unsigned base) {
 #pragma unroll
         for (int i = 0; i < KT; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[i][e] = 0.0f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
+        for (int ks = 0; ks < KS; ++ks) {
+            const unsigned at = k_at(base, ks);
 #pragma unroll
-            for (int i = 0; i < KT; ++i) s[i] = mfma32(__builtin_bit_cast(x8, *(const i32x4*)(buf + (32 * i + l32) * KP + 32 * ks + 16 * half)), q[ks], s[i]);
+            for (int i = 0; i < KT; ++i) s[i] = mfma32(__builtin_bit_cast(x8, at_lds<i32x4>(at + 32 * i * ROW_K)), q[ks], s[i]);
+        }
         in_turn<KS * KT, 1, 1, 6, 0, 0>();
-        if (k0 + WK > min(all_to, end_key) || k0 < all_from) {
-            const int to = sees_to - k0 - 4 * half, from = sees_from - k0 - 4 * half;
+        if (k0 + WK > all_to || k0 < all_from) {
+            int to = sees_to - k0 - 4 * half, from = sees_from - k0 - 4 * half;
+            stay(to);                          // (or the comparisons are made in every step, ahead of the branch)
+            stay(from);
 #pragma unroll
             for (int i = 0; i < KT; ++i)
 #pragma unroll
@@ -293,7 +467,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         for (int i = 0; i < KT; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[i][e]);
-        return fmaxf(top, __shfl_xor(top, 32)) * p.scale_log2;
+        return fmaxf(top, __shfl_xor(top, 32)) * scale_log2;
     };
     auto finite = [&]() {
         float zero = 0.0f;                     // (or NaN)
@@ -311,12 +485,8 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
-        sweep([&](int kt, const unsigned char* buf) {
-            const int k0 = kt + WK * kw;
-            if (k0 >= min(any_to, end_key) || k0 + WK <= any_from) return;             // (the wave's rows see nothing of it)
-            const unsigned char* const kb = buf + WK * kw * KP;
-            const unsigned v_at = lds_base_of((void*)(buf + KEYS * KP + WK * kw * VP)) + (4 * half + (l16 >> 2)) * VP + 32 * ((lane >> 4) & 1) + 8 * (l16 & 3);
-            score(k0, kb);
+        sweep([&](int kt, unsigned k_base, unsigned v_base) {
+            score(kt + WK * kw, k_base);
             if (!known && __any(m == none)) {
                 const float top = largest() - LIFT;
                 m = m == none ? top : m;
@@ -324,10 +494,13 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             const float shift = m == none ? 0.0f : m;
             // Sixteen keys at a time; the weights and V of the next are made and read while the matrix cores are on these.
             x8 vf[DT], pf[TERMS], next[TERMS];
+            unsigned v_from[DT];
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) v_from[dt] = v_at(v_base, dt);
             auto weigh = [&](int st, x8 (&w)[TERMS]) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    float left = exp2_fast(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], p.scale_log2, -shift));
+                    float left = exp2_fast(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], scale_log2, -shift));
                     l += left;
 #pragma unroll
                     for (int k = 0; k < TERMS; ++k) {
@@ -337,7 +510,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 }
             };
             auto read_v = [&](int st, int dt) {
-                const s16x4 v0 = lds_read_transposed(v_at + 16 * st * VP + 64 * dt), v1 = lds_read_transposed(v_at + (16 * st + 8) * VP + 64 * dt);
+                const s16x4 v0 = lds_read_transposed(v_from[dt] + 16 * st * ROW_V), v1 = lds_read_transposed(v_from[dt] + (16 * st + 8) * ROW_V);
                 return __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
             };
 #pragma unroll
@@ -358,6 +531,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 in_turn<DT, TERMS, 2, 0, 20 * TERMS / DT, 8 / DT>();
                 __builtin_amdgcn_sched_barrier(0);
             }
+            pinned(l);                         // (or the sums are made behind the loop, from registers that wait for that)
         });
         // (a lane's O is of the keys of both halves)
         const float both = l + __shfl_xor(l, 32);
@@ -366,10 +540,8 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         if (!again[0] || known) break;
         known = true;
         m = none;
-        sweep([&](int kt, const unsigned char* buf) {
-            const int k0 = kt + WK * kw;
-            if (k0 >= min(any_to, end_key) || k0 + WK <= any_from) return;
-            score(k0, buf + WK * kw * KP);
+        sweep([&](int kt, unsigned k_base, unsigned) {
+            score(kt + WK * kw, k_base);
             m = fmaxf(m, largest() - LIFT);
         });
         __syncthreads();
@@ -379,32 +551,31 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     if (l == 0.0f) m = none;                   // (nothing is of any weight: m may be anything)
 
     // The results leave through LDS (nobody reads the buffers any more), so that a store has whole lines.
-    auto put = [&](int r, int d, const f32x4& x, float total) {        // row r of the tile, its O from feature d on and its l
-        if (t.row0 + r >= t.row_end || d >= p.D) return;
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) odd |= is_odd(x[i]);
-        if (odd && total == total) again[1] = 1;
-        const int at_row = t.row0 + r;
-        if (t.direct) {
-            const int its = at_row / p.G;
-            store_four(p, (t.seq.start + its) * p.out_token + (int64_t)(t.h * p.G + at_row - its * p.G) * p.out_head + d,
-                       total == 0.0f ? f32x4{0, 0, 0, 0} : x * (1.0f / total));
-        } else *(f32x4*)((FEW ? p.few_o : p.many_o) + part_at<FEW>(p, t.seq, t.b, t.h, at_row, t.split, p.few_rows) * p.D + d) = x;
-    };
-    auto put_sums = [&](int r, float top, float total) {
-        const int at_row = t.row0 + r;
+    const ChunkParams& z = parameters();
+    // where a row's result goes and what it is multiplied with: its 1 / l, or 1 where it is a part
+    auto place = [&](int r, float top, float total) {
+        const int at_row = t.row0 + r, its = at_row / z.G, head = t.h * z.G + at_row - its * z.G;
+        const int64_t part = part_at<FEW>(z, t.seq, t.b, t.h, at_row, t.split, z.few_rows);
+        row_to[r] = t.direct ? (t.seq.start + its) * z.out_token + head * z.out_head : part * z.D;
+        row_factor[r] = total != total ? total : (total == 0.0f ? 0.0f : (t.direct ? 1.0f / total : 1.0f));
         if (at_row >= t.row_end) return;
-        if (!t.direct) *(f32x2*)((FEW ? p.few_ml : p.many_ml) + part_at<FEW>(p, t.seq, t.b, t.h, at_row, t.split, p.few_rows) * 2) = f32x2{top, total};
-        else if (p.lse) {
-            const int its = at_row / p.G;
-            p.lse[(int64_t)(t.seq.start + its) * (p.Hk * p.G) + t.h * p.G + at_row - its * p.G] = lse_of(top, total);
-        }
+        if (!t.direct) *(f32x2*)((FEW ? z.few_ml : z.many_ml) + part * 2) = f32x2{top, total};
+        else if (z.lse) z.lse[(int64_t)(t.seq.start + its) * (z.Hk * z.G) + head] = lse_of(top, total);
+    };
+    float* const parts = FEW ? z.few_o : z.many_o;
+    auto put = [&](int r, int d, const f32x4& x) {                     // row r of the tile, its O from feature d on
+        if (t.row0 + r >= t.row_end || d >= z.D) return;
+        const float factor = row_factor[r];
+        const int64_t to = row_to[r] + d;
+        const f32x4 y = factor == 0.0f ? f32x4{0, 0, 0, 0} : x * factor;
+        if (__builtin_fmaf(y.x, 0.0f, __builtin_fmaf(y.y, 0.0f, __builtin_fmaf(y.z, 0.0f, y.w * 0.0f))) != 0.0f && factor == factor) again[1] = 1;
+        if (t.direct) store_four(z, to, y);
+        else *(f32x4*)(parts + to) = y;
     };
     if constexpr (!FEW) {
         constexpr int TF = turn_features(DP), TP = TF + 4;             // floats from row to row
         float* const turned = (float*)lds + wave * 32 * TP;
-        if (half == 0) row_l[32 * wave + l32] = l;
+        if (half == 0) place(32 * wave + l32, m, l);
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int d0 = 0; d0 < DP; d0 += TF) {
@@ -418,11 +589,10 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
 #pragma unroll
             for (int i = 0; i < 32 * LANES / 64; ++i) {
                 const int r = i * (64 / LANES) + lane / LANES, d = 4 * (lane % LANES);
-                put(32 * wave + r, d0 + d, *(const f32x4*)(turned + r * TP + d), row_l[32 * wave + r]);
+                put(32 * wave + r, d0 + d, *(const f32x4*)(turned + r * TP + d));
             }
             __builtin_amdgcn_wave_barrier();
         }
-        if (half == 0) put_sums(32 * wave + l32, m, l);
     } else {
         constexpr int TP = DP + 4;
         float* const turned = (float*)lds + wave * 32 * TP;
@@ -443,8 +613,15 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             f32x4 x = f32x4{o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3]} * factor;
             *(f32x4*)(turned + l32 * TP + 8 * i + 4 * half) = counts ? x : f32x4{0, 0, 0, 0};
         }
-        __syncthreads();
-        if (half == 0) row_l[32 * wave + l32] = counts ? l * factor : 0.0f;
+        if (wave == 0 && half == 0) {
+            float total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < KW; ++w) {
+                const float part = row_l[32 * w + l32], its = row_m[32 * w + l32];
+                total += part == 0.0f ? 0.0f : part * (its == none ? 0.0f : exp2_fast(its - top));
+            }
+            place(l32, total == 0.0f ? none : top, total);
+        }
         __syncthreads();
         constexpr int LANES = DP / 4, ROWS = 64 * NW / LANES;
         const int d = 4 * (tid % LANES);
@@ -452,19 +629,9 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         for (int i = 0; i < 32 / ROWS; ++i) {
             const int r = i * ROWS + tid / LANES;
             f32x4 x = f32x4{0, 0, 0, 0};
-            float total = 0.0f;
 #pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                x += *(const f32x4*)((const float*)lds + (32 * w + r) * TP + d);
-                total += row_l[32 * w + r];
-            }
-            put(r, d, x, total);
-        }
-        if (wave == 0 && half == 0) {
-            float total = 0.0f;
-#pragma unroll
-            for (int w = 0; w < KW; ++w) total += row_l[32 * w + l32];
-            put_sums(l32, total == 0.0f ? none : top, total);
+            for (int w = 0; w < KW; ++w) x += *(const f32x4*)((const float*)lds + (32 * w + r) * TP + d);
+            put(r, d, x);
         }
     }
     __syncthreads();
@@ -472,21 +639,15 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         // every wave settles its own rows, or its share of them
         __threadfence();
         unsigned rows = 0;
-        for (int r = 0; r < 32; ++r) {
-            float total = 0.0f;
-            if constexpr (FEW) {
-                if (r % KW != kw) continue;
-                for (int w = 0; w < KW; ++w) total += row_l[32 * w + r];
-            } else total = row_l[32 * wave + r];
-            if (wave_row0 + r < t.row_end && total == total) rows |= 1u << r;
-        }
-        settle_chunk<T, DP, FEW>(p, t, wave_row0, rows);
+        for (int r = FEW ? kw : 0; r < 32; r += FEW ? KW : 1)
+            if (wave_row0 + r < t.row_end && row_factor[32 * rw + r] == row_factor[32 * rw + r]) rows |= 1u << r;
+        settle_chunk<T, DP, FEW>(z, t, wave_row0, rows);
     }
 }
 
 // Few rows: workgroups are numbered sequence by sequence, key head by key head, part by part.
 template <class T, int DP, int TERMS, bool FAST>
-__global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) few_rows_kernel(const ChunkParams p) {
+__global__ void __launch_bounds__(64 * few_waves(DP, FAST), DP > 128 || FAST ? 1 : 2) few_rows_kernel(const ChunkParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     const int i = ((int)blockIdx.x & 7) * p.few_per_xcd + ((int)blockIdx.x >> 3);
     Tile t;
@@ -501,7 +662,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) few_rows_kernel(const C
     if (t.row_end > p.few_rows) {
         // another launch's; where there is none, more queries than the caller said that there are: NaN
         if (p.many_per_xcd == 0 && t.split == 0)
-            for (int64_t x = threadIdx.x; x < (int64_t)t.row_end * (p.D / 4); x += 256) {
+            for (int64_t x = threadIdx.x; x < (int64_t)t.row_end * (p.D / 4); x += 64 * few_waves(DP, FAST)) {
                 const int row = (int)(x / (p.D / 4)), j = row / p.G, d = 4 * (int)(x % (p.D / 4));
                 const float nan = __builtin_nanf("");
                 store_four(p, (t.seq.start + j) * p.out_token + (int64_t)(t.h * p.G + row - j * p.G) * p.out_head + d, f32x4{nan, nan, nan, nan});
@@ -514,7 +675,7 @@ __global__ void __launch_bounds__(256, DP > 128 ? 1 : 2) few_rows_kernel(const C
     t.direct = r.parts == 1;
     t.first = r.first + t.split * p.few_chunk;
     t.end = t.first + min(r.end - t.first, p.few_chunk);
-    attend_chunk<T, DP, 1, 4, TERMS, FAST>(p, t, lds);
+    attend_chunk<T, DP, 1, few_waves(DP, FAST), TERMS, FAST>(p, t, lds);
 }
 
 // Many rows: tile `at` of the sequences' tiles, one sequence behind the other and the last tile of each, which sees the most, first.

@@ -7,15 +7,15 @@ namespace {
 template <class T, int DP, int TERMS, bool FAST>
 int launch_few_rows(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
     static std::atomic<unsigned> done{0};
-    constexpr int lds = lds_bytes(DP, 1, 4);
+    constexpr int waves = few_waves(DP, FAST), lds = lds_bytes(DP, 1, waves, FAST);
     auto kfn = few_rows_kernel<T, DP, TERMS, FAST>;
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
-    return launch(kfn, dim3(8u * (unsigned)a.few_per_xcd), 256, lds, stream, p);
+    return launch(kfn, dim3(8u * (unsigned)a.few_per_xcd), 64 * waves, lds, stream, p);
 }
 template <class T, int DP, int RW, int TERMS, bool FAST>
 int launch_many_rows(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
     static std::atomic<unsigned> done{0};
-    constexpr int lds = lds_bytes(DP, RW, 1);
+    constexpr int lds = lds_bytes(DP, RW, 1, FAST);
     auto kfn = many_rows_kernel<T, DP, RW, TERMS, FAST>;
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
     return launch(kfn, dim3(8u * (unsigned)a.many_per_xcd), 64 * RW, lds, stream, p);
