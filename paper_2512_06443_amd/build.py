@@ -11,7 +11,7 @@ from concurrent.futures import ThreadPoolExecutor
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SRC = os.path.join(_HERE, "csrc", "vlut.hip")
-SOURCES = (SRC, *(os.path.join(_HERE, "csrc", f"{part}.hip") for part in ("attention", "attention_bf16", "attention_f16", "chunk", "chunk_bf16", "chunk_f16", "layer")))       # the library's translation units
+SOURCES = (SRC, *(os.path.join(_HERE, "csrc", f"{part}.hip") for part in ("attention", "attention_bf16", "attention_f16", "chunk", "chunk_bf16", "chunk_bf16_f32", "chunk_f16", "chunk_f16_f32", "layer")))       # the library's translation units
 LIB = os.path.join(_HERE, "libvlut.so")
 TORCH_SRC = os.path.join(_HERE, "csrc", "torch_calls.cpp")
 TORCH_LIB = os.path.join(_HERE, "_vlut_torch.so")

@@ -25,8 +25,8 @@ int log2_of(int64_t v) {
     return k;
 }
 
-// fast: see ChunkPlan.  The workspace does not depend on it.
-int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, ChunkPlan* out) {
+// registers: keys go through registers to LDS (which changes nothing of the workspace: where the largest tiles are, every tile is one part).
+int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, bool registers, ChunkPlan* out) {
     if (N < 1 || N >= ((int64_t)1 << 24) || B < 1 || B >= ((int64_t)1 << 24) || Hk < 1 || Hq < 1 || Hq >= (1 << 16) || Hq % Hk) return VLUT_ERR_SHAPE;
     if (max_len < 0 || max_len >= kMost || max_queries < 0 || window < 0 || window >= kMost || D < 1 || N * Hq >= kMost) return VLUT_ERR_SHAPE;
     if (D < 8 || D > VLUT_MAX_HEAD_FEATURES || D % 4) return VLUT_ERR_UNSUPPORTED;
@@ -40,12 +40,12 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
     a.few = !a.many || (B > 1 && G <= kFewRows);
     if (a.few) {
         a.few_row_places = (int)std::min<int64_t>(kFewRows, std::max<int64_t>(1, most_rows / G) * G);
-        const int64_t keys = seen(kFewRows), steps = ceil_div(keys, 128);
-        const int64_t slots = (a.DP > 128 ? 1 : 2) * kUnits;
-        // Parts so that the workgroups are four rounds of those that run at once, of four steps at least; where that many are not there, of one.
-        int64_t per = std::max<int64_t>(4, ceil_div(B * Hk * steps, 4 * slots));
-        if (B * Hk * ceil_div(steps, per) < slots) per = std::max<int64_t>(1, std::min(per, B * Hk * steps / slots));
-        a.few_chunk = (int)(128 * per);
+        // Keys that one tile sees, in steps.  Parts so that the workgroups are six rounds of those that run at once, of two steps at least; where that many are not
+        // there, of one.
+        const int64_t step = step_keys(a.DP, 1), keys = seen(kFewRows), steps = ceil_div(keys, step);
+        int64_t per = std::max<int64_t>(2, ceil_div(B * Hk * steps, 6 * kUnits));
+        if (B * Hk * ceil_div(steps, per) < kUnits) per = 1;
+        a.few_chunk = (int)(step * per);
         a.few_splits = (int)ceil_div(keys, a.few_chunk);
         const int64_t blocks = ceil_div(B * Hk * a.few_splits, 8);
         if (8 * blocks >= kMostBlocks) return VLUT_ERR_SHAPE;
@@ -57,17 +57,16 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
         }
     }
     if (a.many) {
-        const int64_t rows = N * G;
-        a.many_waves = a.DP <= 128 && rows * Hk >= 256 * kUnits ? 8 : 4;
-        a.many_rows = 32 * a.many_waves;
+        const int64_t rows = N * G, waves = waves_of(a.DP);
+        a.row_waves = !registers && a.DP <= 128 && rows * Hk >= 4 * 256 * kUnits ? 8 : 4;
+        a.many_rows = 32 * a.row_waves;
         a.many_tiles = (int)std::min(rows / a.many_rows + B, (rows + B * (a.many_rows - 1)) / a.many_rows);
-        const int64_t keys = seen(a.many_rows / G + 1), step = a.DP > 128 ? 32 : 64;
-        const int64_t slots = (a.many_waves == 4 && a.DP <= 128 ? 2 : 1) * kUnits, tiles = a.many_tiles * Hk;
-        int64_t splits = std::min(std::max<int64_t>(1, slots / tiles), ceil_div(keys, 256));
+        const int64_t keys = seen(a.many_rows / G + 1), step = wave_keys(a.DP, a.row_waves) * (waves / a.row_waves), tiles = a.many_tiles * Hk;
+        const int64_t splits = std::min(std::max<int64_t>(1, kUnits / tiles), ceil_div(keys, 512));
         a.many_chunk = (int)(ceil_div(ceil_div(keys, splits), step) * step);
         a.many_splits = (int)ceil_div(keys, a.many_chunk);
         const int64_t blocks = ceil_div(tiles * a.many_splits, 8);
-        if (8 * blocks * a.many_waves / 4 >= kMostBlocks) return VLUT_ERR_SHAPE;
+        if (8 * blocks >= kMostBlocks) return VLUT_ERR_SHAPE;
         a.many_per_xcd = (int)blocks;
         if (a.many_splits > 1) {
             const size_t parts = (size_t)a.many_splits * (size_t)N * (size_t)Hq;
@@ -79,12 +78,12 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
     return VLUT_OK;
 }
 
-// Eight keys share their page, rows start at 16 bytes, and strides and the offsets inside a page fit 31 bits, in bytes.
-bool grouped_by_eight(const vlut_cache& c) {
-    bool ok = c.page_size >= 8 && (uintptr_t)c.k % 16 == 0 && (uintptr_t)c.v % 16 == 0;
-    for (int64_t s : {c.k_page_stride, c.v_page_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) && s % 8 == 0;
-    for (int64_t s : {c.k_head_stride, c.v_head_stride}) ok = ok && s % 8 == 0;
-    for (int64_t s : {c.k_token_stride, c.v_token_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) / std::max<int64_t>(c.page_size, 8) && s % 8 == 0;
+// Eight keys share their page, rows start at a multiple of `unit` elements, and strides and the offsets inside a page fit 31 bits, in bytes.
+bool grouped_by_eight(const vlut_cache& c, int unit) {
+    bool ok = c.page_size >= 8 && (uintptr_t)c.k % (2 * unit) == 0 && (uintptr_t)c.v % (2 * unit) == 0;
+    for (int64_t s : {c.k_page_stride, c.v_page_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) && s % unit == 0;
+    for (int64_t s : {c.k_head_stride, c.v_head_stride}) ok = ok && s % unit == 0;
+    for (int64_t s : {c.k_token_stride, c.v_token_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) / std::max<int64_t>(c.page_size, 8) && s % unit == 0;
     return ok;
 }
 
@@ -94,13 +93,13 @@ extern "C" {
 
 size_t vlut_chunk_attention_bytes(int64_t N, int64_t B, int64_t q_heads, int64_t k_heads, int64_t D, int64_t max_queries, int64_t max_len, int64_t window) {
     ChunkPlan a;
-    return plan_chunks(N, B, q_heads, k_heads, D, max_queries, max_len, window, &a) == VLUT_OK ? a.bytes() : 0;
+    return plan_chunks(N, B, q_heads, k_heads, D, max_queries, max_len, window, false, &a) == VLUT_OK ? a.bytes() : 0;
 }
 
 int vlut_query_chunk_attention(int64_t N, int64_t B, int64_t q_heads, int64_t k_heads, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, int* out6) {
     if (!out6) return VLUT_ERR_NULL;
     ChunkPlan a;
-    const int rc = plan_chunks(N, B, q_heads, k_heads, D, max_queries, max_len, window, &a);
+    const int rc = plan_chunks(N, B, q_heads, k_heads, D, max_queries, max_len, window, false, &a);
     if (rc != VLUT_OK) return rc;
     out6[0] = a.few ? a.few_row_places : 0;
     out6[1] = a.few_splits;
@@ -118,7 +117,8 @@ int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int
     int rc = check_cache(cache);
     if (rc != VLUT_OK) return rc;
     ChunkPlan a;
-    rc = plan_chunks(N, B, q->heads, cache->heads, D, max_queries, max_len, window, &a);
+    const bool registers = !grouped_by_eight(*cache, 2);
+    rc = plan_chunks(N, B, q->heads, cache->heads, D, max_queries, max_len, window, registers, &a);
     if (rc != VLUT_OK) return rc;
     if (!q->data || !out->data || !query_starts || !lens || (max_len > 0 && !page_table)) return VLUT_ERR_NULL;
     if (out->heads != q->heads || q->type != cache->type || (out->type != cache->type && out->type != VLUT_TYPE_F32)) return VLUT_ERR_SHAPE;
@@ -134,7 +134,7 @@ int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int
         if (workspace_bytes < a.bytes()) return VLUT_ERR_SMALL_BUFFER;
         if ((uintptr_t)workspace % 16) return VLUT_ERR_UNSUPPORTED;
     }
-    a.fast = D % 8 == 0 && grouped_by_eight(*cache);
+    a.load = registers ? kThroughRegisters : (D % 8 || !grouped_by_eight(*cache, 8) ? kDwords : (D < a.DP ? kVectors : kWholeVectors));
     ChunkParams p{};
     p.q = q->data;
     p.k = cache->k;
@@ -161,7 +161,7 @@ int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int
     p.many_o = (float*)(at += a.few_ml_bytes);
     p.many_ml = (float*)(at += a.many_o_bytes);
     p.scale_log2 = (float)((double)scale * 1.4426950408889634);
-    p.out_type = out->type;
+    p.inverse_g = 1.0f / (float)(q->heads / cache->heads);
     p.N = (int)N;
     p.B = (int)B;
     p.Hk = cache->heads;
@@ -180,6 +180,7 @@ int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int
     p.many_tiles = a.many_tiles;
     p.many_per_xcd = a.many_per_xcd;
     p.many_rows = a.many_rows;
+    if (out->type == VLUT_TYPE_F32) return cache->type == VLUT_TYPE_BF16 ? launch_bf16_f32(a, p, (hipStream_t)stream) : launch_f16_f32(a, p, (hipStream_t)stream);
     return cache->type == VLUT_TYPE_BF16 ? launch_bf16(a, p, (hipStream_t)stream) : launch_f16(a, p, (hipStream_t)stream);
 }
 

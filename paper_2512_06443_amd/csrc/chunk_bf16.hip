@@ -1,4 +1,4 @@
-// The kernels of the attention of chunks over a cache of type bf16: a translation unit of its own for the time it takes to compile.
+// The kernels of the attention of chunks over a cache of type bf16, outputs of that type: a translation unit of its own for the time it takes to compile.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -13,4 +13,4 @@
 #include "chunk_kernel.hip.h"
 #include "chunk_launch.hip.h"
 
-int vlut_chunk::launch_bf16(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) { return launch_chunks<__bf16>(a, p, stream); }
+int vlut_chunk::launch_bf16(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) { return launch_chunks<__bf16, 1>(a, p, stream); }

@@ -1,0 +1,16 @@
+// The kernels of the attention of chunks over a cache of type f16, outputs of fp32: a translation unit of its own for the time it takes to compile.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cstdint>
+
+#include "vlut.h"
+
+#include "chunk_params.h"
+#include "common.hip.h"
+#include "launch.hip.h"
+#include "chunk_kernel.hip.h"
+#include "chunk_launch.hip.h"
+
+int vlut_chunk::launch_f16_f32(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) { return launch_chunks<_Float16, Number<_Float16>::kTerms>(a, p, stream); }

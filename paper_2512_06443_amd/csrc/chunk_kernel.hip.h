@@ -55,14 +55,17 @@ __device__ __forceinline__ Range range_of(const ChunkParams& p, const Chunk& c, 
     return r;
 }
 
-__device__ __forceinline__ void store_four(const ChunkParams& p, int64_t at, const f32x4& o) {
-    if (p.out_type == VLUT_TYPE_F32) *(dword_aligned_f32x4*)((float*)p.out + at) = o;
-    else if (p.out_type == VLUT_TYPE_BF16) {
-        typedef __bf16 x4 __attribute__((ext_vector_type(4), aligned(4)));
-        *(x4*)((__bf16*)p.out + at) = x4{(__bf16)o.x, (__bf16)o.y, (__bf16)o.z, (__bf16)o.w};
-    } else {
-        typedef _Float16 x4 __attribute__((ext_vector_type(4), aligned(4)));
-        *(x4*)((_Float16*)p.out + at) = x4{(_Float16)o.x, (_Float16)o.y, (_Float16)o.z, (_Float16)o.w};
+// Outputs: of the cache's type where weights are carried in one term, else fp32.
+template <class T, int TERMS>
+struct Output { typedef float type; };
+template <class T>
+struct Output<T, 1> { typedef T type; };
+template <class O>
+__device__ __forceinline__ void store_four(void* out, int64_t at, const f32x4& o) {
+    if constexpr (sizeof(O) == 4) *(dword_aligned_f32x4*)((float*)out + at) = o;
+    else {
+        typedef O x4 __attribute__((ext_vector_type(4), aligned(4)));
+        *(x4*)((O*)out + at) = x4{(O)o.x, (O)o.y, (O)o.z, (O)o.w};
     }
 }
 
@@ -70,22 +73,24 @@ __device__ __forceinline__ void store_four(const ChunkParams& p, int64_t at, con
 struct Tile {
     Chunk seq;
     int b, h, row0, row_end;           // rows of the sequence and key head: query * G + head
+    int j0, g0;                        // row0's
     int first, end;                    // keys
     int split, direct;
 };
-// Where row `row` of a tile's part is among the parts.
+// The query of row row0 + r, r < 256: exact, as (x + 1/2) / G is 1 / (2 G) away from a whole number at least, and x far below 2^21.
+__device__ __forceinline__ int query_of(const ChunkParams& p, const Tile& t, int r) { return t.j0 + (int)(((float)(t.g0 + r) + 0.5f) * p.inverse_g); }
+// Where a row of a tile's part is among the parts: `row` where rows are few, else the query and its head.
 template <bool FEW>
-__device__ __forceinline__ int64_t part_at(const ChunkParams& p, const Chunk& c, int b, int h, int row, int split, int places) {
-    if constexpr (FEW) return (((int64_t)split * p.B + b) * p.Hk + h) * places + row;
-    const int j = row / p.G;
-    return ((int64_t)split * p.N + c.start + j) * (p.Hk * p.G) + h * p.G + row - j * p.G;
+__device__ __forceinline__ int64_t part_at(const ChunkParams& p, const Chunk& c, int b, int h, int row, int j, int head, int split) {
+    if constexpr (FEW) return (((int64_t)split * p.B + b) * p.Hk + h) * p.few_rows + row;
+    return ((int64_t)split * p.N + c.start + j) * (p.Hk * p.G) + head;
 }
 
 // Values that are no numbers.  Zeros stand for them in the products' steps of which some row does not see every key (0 times them would reach every row); they, and
 // infinities that rows see, which weights of 0 or in several terms make NaN of, are settled here, once the results are stored, by a look at the part's values: a row's
 // feature with such values among the keys that it sees is their sum, with weights of 1, or 0 for a score of -inf.  NaN with infinities of both signs.
 // Rows: those of `rows` (bits, from row0 on).  Not part of the loops: a flag and a look at the results; where there is something to settle, a read of V per wave.
-template <class T, int DP, bool FEW>
+template <class T, class O, int DP, bool FEW>
 __device__ __forceinline__ void settle_chunk(const ChunkParams& p, const Tile& t, int row0, unsigned rows) {
     constexpr int F = DP / 64;
     const int lane = (int)threadIdx.x & 63, d = F * lane, mask = (1 << p.page_log) - 1;
@@ -107,26 +112,23 @@ __device__ __forceinline__ void settle_chunk(const ChunkParams& p, const Tile& t
         if (!__any(odd)) continue;
         const T* const k = token(p.k, key, p.k_page, p.k_head, p.k_token);
         for (unsigned left = rows; left; left &= left - 1) {
-            const int r = __builtin_ctz(left), row = row0 + r, j = row / p.G, g = row - j * p.G, pos = t.seq.base + j;
+            const int r = __builtin_ctz(left), row = row0 + r, j = query_of(p, t, row - t.row0), head = t.h * p.G + row - j * p.G, pos = t.seq.base + j;
             if (key > pos || key <= pos - p.window) continue;
-            const T* const q = (const T*)p.q + (t.seq.start + j) * p.q_token + (int64_t)(t.h * p.G + g) * p.q_head + d;
+            const T* const q = (const T*)p.q + (t.seq.start + j) * p.q_token + head * p.q_head + d;
             float s = 0.0f;
             for (int f = 0; f < F && has; ++f)
                 if (d + f < p.D) s += (float)q[f] * (float)k[f];
             for (int m = 1; m < 64; m *= 2) s += __shfl_xor(s, m);
             const float weight = s > -__builtin_inff() ? 1.0f : 0.0f;
-            const int64_t out = (t.seq.start + j) * p.out_token + (int64_t)(t.h * p.G + g) * p.out_head + d;
-            const int64_t part = part_at<FEW>(p, t.seq, t.b, t.h, row, t.split, p.few_rows) * p.D + d;
+            O* const out = (O*)p.out + (t.seq.start + j) * p.out_token + head * p.out_head + d;
+            float* const part = (FEW ? p.few_o : p.many_o) + part_at<FEW>(p, t.seq, t.b, t.h, row, j, head, t.split) * p.D + d;
             for (int f = 0; f < F && has; ++f)
                 if (is_odd(x[f])) {
-                    float was = 0.0f;
-                    float* const o = (FEW ? p.few_o : p.many_o) + part + f;
-                    if (touched[f] >> r & 1) was = !t.direct ? *o : (p.out_type == VLUT_TYPE_F32 ? ((const float*)p.out)[out + f] : (float)((const T*)p.out)[out + f]);
+                    float sum = weight * x[f];
+                    if (touched[f] >> r & 1) sum += t.direct ? (float)out[f] : part[f];
                     touched[f] |= 1u << r;
-                    was += weight * x[f];
-                    if (!t.direct) *o = was;
-                    else if (p.out_type == VLUT_TYPE_F32) ((float*)p.out)[out + f] = was;
-                    else ((T*)p.out)[out + f] = (T)was;
+                    if (t.direct) out[f] = (O)sum;
+                    else part[f] = sum;
                 }
         }
     }
@@ -156,17 +158,21 @@ __device__ __forceinline__ void pinned(float& x) {
 #endif
 }
 
-// 16 bytes per lane from `base` + `at` on to LDS, lane after lane from `to` on.  Written out: the compiler, when it issues such a load itself, waits for all of them
+// 16 bytes (or a dword) per lane from `base` + `at` on to LDS, lane after lane from `to` on.  Written out: the compiler, when it issues such a load itself, waits for all of them
 // ahead of every LDS read that follows.  No result register; the LDS address is in M0.
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned at, unsigned to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory", "m0");
 }
+__device__ __forceinline__ void load_dword_to_lds(const unsigned char* base, unsigned at, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory", "m0");
+}
 template <int N>
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N < 63 ? N : 63) : "memory"); }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 #else
 inline __device__ void load_to_lds(const unsigned char*, unsigned, unsigned) {}
+inline __device__ void load_dword_to_lds(const unsigned char*, unsigned, unsigned) {}
 template <int N>
 inline __device__ void wait_loads() {}
 inline __device__ void wait_lds() {}
@@ -195,17 +201,24 @@ __device__ __forceinline__ i32x4 without_odd(i32x4 v, unsigned& odd) {
     return v;
 }
 
-// A tile's part.  FAST: keys and values are loaded straight to LDS, DEPTH steps ahead, addresses worked out once per wave and 8 keys.  Each stage is exactly
-// LOADS loads per wave, also past the end of the part, where its last keys are loaded again, so that vmcnt((DEPTH - 1) * LOADS) stands for "the
-// stage that was asked for first is there"; what else a wave loads meanwhile only makes that wait longer.  Where waves share the keys each has its own pieces
-// of the stages, and no wave waits for another.
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+template <int N>
+struct Count { static constexpr int value = N; };
+
+// A tile's part.  Where keys and values are loaded straight to LDS they are asked for AHEAD steps ahead, addresses worked out once per wave and 8 keys.  Each stage is
+// exactly LOADS loads per wave, also past the end of the part, where its last keys are loaded again, so that vmcnt((AHEAD - 1) * LOADS) stands for "the
+// stage that was asked for first is there"; what else a wave loads meanwhile only makes that wait longer.
 // Rows of LDS are DP features one behind the other, 16-byte chunks c at c ^ f(row): of keys, so that 16 rows' chunks lie in 64 banks; of values, so that the four
 // rows of a transposing read do.  Chunks behind D are not loaded: zeros from before the first stage.
-template <class T, int DP, int RW, int KW, int TERMS, bool FAST>
+// Where rows are few each wave has its keys for itself, and none waits for another; a step's keys are asked for as soon as the first product is done with
+// the ones before, its values behind the second.
+template <class T, int DP, int RW, int TERMS, int LOAD>
 __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
-    constexpr bool FEW = KW > 1, WIDE = Number<T>::kWide;
-    constexpr int NW = RW * KW, WK = wave_keys(DP, KW), KT = WK / 32, KEYS = step_keys(DP, KW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
+    typedef typename Output<T, TERMS>::type O;
+    constexpr bool FEW = RW == 1, WIDE = Number<T>::kWide, DIRECT = LOAD != kThroughRegisters, OWN_KEYS = own_keys(RW, LOAD), TURNS = turns(DP, RW, LOAD);
+    constexpr int NW = waves_of(DP), KW = NW / RW, WK = wave_keys(DP, RW), KT = WK / 32, KEYS = step_keys(DP, RW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
     constexpr float LIFT = 0.5f * Number<T>::kLift;            // (scores after the first step may be larger)
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
@@ -214,34 +227,34 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
 
     // behind the buffers: the waves' m and l where they share rows, where the rows' results go and their factors, two flags (the part is to be
     // begun again; there is something to settle), pages' numbers
-    float* const row_m = (float*)(lds + tile_bytes(DP, RW, KW, FAST));
+    float* const row_m = (float*)(lds + tile_bytes(DP, RW, LOAD));
     float* const row_l = row_m + 32 * NW;
     int64_t* const row_to = (int64_t*)(row_l + 32 * NW);
-    float* const row_factor = (float*)(row_to + 32 * RW);
-    int* const again = (int*)(row_factor + 32 * RW);
+    float* const row_factor = (float*)(row_to + 32 * NW);
+    int* const again = (int*)(row_factor + 32 * NW);
     int* const page_ids = again + 4;
     if (tid == 0) again[0] = again[1] = 0;
-    if (FAST && p.D < DP) {
-        for (int x = 16 * tid; x < tile_bytes(DP, RW, KW, FAST); x += 16 * 64 * NW) *(i32x4*)(lds + x) = i32x4{0, 0, 0, 0};
+    if constexpr (LOAD == kDwords || LOAD == kVectors) {
+        for (int x = 16 * tid; x < tile_bytes(DP, RW, LOAD); x += 16 * 64 * NW) *(i32x4*)(lds + x) = i32x4{0, 0, 0, 0};
     }
     wg_barrier_lds();                                                  // (they are set ahead of the first step's barrier)
 
     // rows past the tile's end do as its last one
-    const int real = min(row, t.row_end - 1), j = real / p.G, pos = t.seq.base + j;
+    const int real = min(row, t.row_end - 1), j = query_of(p, t, real - t.row0), pos = t.seq.base + j;
     x8 q[KS];
     {
         const T* const src = (const T*)p.q + (t.seq.start + j) * p.q_token + (int64_t)(t.h * p.G + real - j * p.G) * p.q_head;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const int chunk = 2 * ks + half;
-            q[ks] = __builtin_bit_cast(x8, chunk_moved<false>(*(const dword_aligned_i32x4*)(src + chunk_at<false>(chunk, p.D)), chunk, p.D));
+            q[ks] = __builtin_bit_cast(x8, chunk_moved<LOAD == kWholeVectors>(*(const dword_aligned_i32x4*)(src + chunk_at<LOAD == kWholeVectors>(chunk, p.D)), chunk, p.D));
         }
     }
     const int sees_from = max(0, pos - p.window + 1), sees_to = min(end_key, pos + 1);
     const bool blind = sees_to <= max(sees_from, first_key);           // nothing of this part
     // of the wave's rows, and of the workgroup's: from where to where all of them see
-    auto position = [&](int of) { return t.seq.base + min(of, t.row_end - 1) / p.G; };
-    const int low = position(min(wave_row0, t.row_end - 1)), high = position(wave_row0 + 31);
+    auto position = [&](int of) { return t.seq.base + __builtin_amdgcn_readfirstlane(query_of(p, t, min(of, t.row_end - 1) - t.row0)); };
+    const int low = position(wave_row0), high = position(wave_row0 + 31);
     const int all_from = max(0, high - p.window + 1), all_to = min(end_key, low + 1);
     const int tile_from = max(0, position(t.row_end - 1) - p.window + 1), tile_to = min(end_key, position(t.row0) + 1);
 
@@ -251,116 +264,183 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     const int page_log = p.page_log, mask = (1 << page_log) - 1, last = end_key - 1;
     const float scale_log2 = p.scale_log2;
 
-    // sweep(use): all keys of the part, in steps: use(first key, keys' place in LDS, values')
     // Where a lane reads: of keys, 8 features of row l32 (and 32 rows further); of values, a corner of a transposing read.
-    constexpr int ROW_K = FAST ? DP * 2 : k_pitch(DP), ROW_V = FAST ? DP * 2 : v_pitch(DP);
+    constexpr int ROW_K = k_pitch(DP, LOAD), ROW_V = v_pitch(DP, LOAD);
     auto turn_k = [](int r) { return DP == 64 ? (r >> 1) & 7 : r & 15; };
     auto turn_v = [](int r) { return DP == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3); };
-    const unsigned k_lane = (unsigned)(l32 * ROW_K + 16 * (FAST ? half ^ turn_k(l32) : half));
+    const unsigned k_lane = (unsigned)(l32 * ROW_K + 16 * (DIRECT ? half ^ turn_k(l32) : half));
     const int v_row = 4 * half + (l16 >> 2), v_chunk = 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1);
-    const unsigned v_lane = (unsigned)(v_row * ROW_V + 16 * (FAST ? v_chunk ^ turn_v(v_row) : v_chunk) + 8 * (l16 & 1));
-    auto k_at = [&](unsigned base, int ks) { return FAST ? (base + k_lane) ^ (unsigned)(32 * ks) : base + k_lane + (unsigned)(32 * ks); };
-    auto v_at = [&](unsigned base, int dt) { return FAST ? (base + v_lane) ^ (unsigned)(64 * dt) : base + v_lane + (unsigned)(64 * dt); };
+    const unsigned v_lane = (unsigned)(v_row * ROW_V + 16 * (DIRECT ? v_chunk ^ turn_v(v_row) : v_chunk) + 8 * (l16 & 1));
+    auto k_at = [&](unsigned base, int ks) { return DIRECT ? (base + k_lane) ^ (unsigned)(32 * ks) : base + k_lane + (unsigned)(32 * ks); };
+    auto v_at = [&](unsigned base, int dt) { return DIRECT ? (base + v_lane) ^ (unsigned)(64 * dt) : base + v_lane + (unsigned)(64 * dt); };
     const unsigned lds0 = lds_base_of(lds);
 
-    auto sweep = [&](auto use) {
+    // All keys of the part, in steps: multiply(first key of the step, where the wave's keys are), weigh_up(first key, where its values are).
+    auto sweep = [&](auto multiply, auto weigh_up, auto in_turns) {
         if (first_key >= end_key) return;
-        if constexpr (FAST) {
-            constexpr int S = stages(DP, RW, KW), DEPTH = FEW ? S : S - 1, OWN = FEW ? WK : KEYS / NW, LOADS = 2 * OWN / GK, PERIOD = 16 / GK > 0 ? 16 / GK : 1;
-            constexpr int PART = FEW ? WK * DP * 4 : stage_bytes(DP, KW), V_OFF = PART / 2;         // bytes of a stage (of the wave), and where its values begin
-            static_assert(OWN % 8 == 0 && 8 % GK == 0, "whole groups of 8 keys");
-            const unsigned base0 = lds0 + (FEW ? kw * S * PART : 0);
-            const int own0 = OWN * wave, in_stage = FEW ? 0 : own0;    // the wave's keys in a step, and where they are in a stage
+        if constexpr (DIRECT) {
+            // Of a load: its bytes, rows or the parts of one, loads of a wave and step.  OWN: keys that a wave loads.
+            constexpr int UNIT = LOAD == kDwords ? 4 : 16, BYTES = 64 * UNIT, ROW = 2 * DP, RPI = BYTES > ROW ? BYTES / ROW : 1, SPLIT = ROW > BYTES ? ROW / BYTES : 1;
+            constexpr int OWN = OWN_KEYS ? WK : WK / RW, LOADS = OWN / RPI * SPLIT, PERIOD = UNIT == 16 ? 16 / RPI : 1;
+            constexpr int AHEAD = OWN_KEYS ? 1 : ahead(DP, RW), PART = WK * ROW;       // bytes of a stage
+            static_assert(OWN % 8 == 0 && 8 % RPI == 0, "whole groups of 8 keys");
+            // the rings of the wave's group (or of the wave alone), the wave's keys in a step and where they are in a stage
+            const bool later = TURNS && wave >= NW / 2;
+            const unsigned k_ring = lds0 + (OWN_KEYS ? wave * ring_bytes(DP, RW, false) : kw * ring_bytes(DP, RW, false)), v_ring = k_ring + key_ring(DP, RW) * PART;
+            const unsigned k_ring_end = v_ring, v_ring_end = v_ring + (unsigned)((KW > 1 ? value_ring(DP, RW, later) : value_ring(DP, RW, TURNS)) * PART);
+            const int in_stage = OWN_KEYS ? 0 : OWN * rw, own0 = WK * kw + in_stage;
             const unsigned char *const kb = (const unsigned char*)kh, *const vb = (const unsigned char*)vh;
             const unsigned k_page = 2u * (unsigned)p.k_page, v_page = 2u * (unsigned)p.v_page, k_token = 2u * (unsigned)p.k_token, v_token = 2u * (unsigned)p.v_token;
-            const bool has = 8 * (lane % CH) < p.D;                    // (a chunk that there is)
+            const int row_in = lane * UNIT / ROW, row_bytes = 2 * p.D;
+            // vectors: a lane's offsets, which repeat every 16 rows, and whether there is such a chunk
             unsigned k_from[PERIOD], v_from[PERIOD];
-#pragma unroll
-            for (int x = 0; x < PERIOD; ++x) {
-                const int r = in_stage + GK * x + lane / CH;
-                k_from[x] = (unsigned)(lane / CH) * k_token + 16u * (unsigned)((lane % CH) ^ turn_k(r));
-                v_from[x] = (unsigned)(lane / CH) * v_token + 16u * (unsigned)((lane % CH) ^ turn_v(r));
-            }
             bool has_k[PERIOD], has_v[PERIOD];
+            if constexpr (UNIT == 16) {
 #pragma unroll
-            for (int x = 0; x < PERIOD; ++x) {
-                const int r = in_stage + GK * x + lane / CH;
-                has_k[x] = 8 * ((lane % CH) ^ turn_k(r)) < p.D;
-                has_v[x] = 8 * ((lane % CH) ^ turn_v(r)) < p.D;
+                for (int x = 0; x < PERIOD; ++x) {
+                    const int r = in_stage + RPI * x + row_in, ck = (lane % CH) ^ turn_k(r), cv = (lane % CH) ^ turn_v(r);
+                    k_from[x] = (unsigned)row_in * k_token + 16u * (unsigned)ck;
+                    v_from[x] = (unsigned)row_in * v_token + 16u * (unsigned)cv;
+                    has_k[x] = LOAD == kWholeVectors || 16 * ck < row_bytes;
+                    has_v[x] = LOAD == kWholeVectors || 16 * cv < row_bytes;
+                }
             }
-            (void)has;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) arrived(q[ks]);
+            // dwords: a lane's place in its row
+            const unsigned in_row = (unsigned)(lane * UNIT % ROW), k_in = (unsigned)row_in * k_token, v_in = (unsigned)row_in * v_token;
             for (int s0 = first_key; s0 < end_key; s0 += kStretch) {
                 const int s1 = s0 + min(end_key - s0, kStretch), id0 = s0 >> page_log, ids = ((s1 - 1) >> page_log) - id0 + 1;
-                wait_loads<0>();
-                __syncthreads();               // (nobody reads the stretch before any more)
+                if (s0 > first_key) {
+                    wait_loads<0>();
+                    __syncthreads();           // (nobody reads the stretch before any more)
+                }
                 for (int x = tid; x < ids; x += 64 * NW) {
                     const int id = pages[id0 + x];
                     page_ids[x] = (unsigned)id < (unsigned)p.pages ? id : -1;
                 }
                 __syncthreads();
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) arrived(q[ks]);
                 const int last_group = (s1 - 1) & ~7;
                 unsigned bad = 0;              // a bit for every 8 keys of the wave in every stage, the newest lowest, that are in no page
-                auto issue = [&](int kt, unsigned stage) {
+                // a stage's keys (Yes, No), values (No, Yes) or both
+                auto issue = [&](int kt, unsigned k_stage, unsigned v_stage, auto keys, auto values) {
 #pragma unroll
                     for (int g = 0; g < OWN / 8; ++g) {
                         const int key = min(kt + own0 + 8 * g, last_group);
                         const int named = __builtin_amdgcn_readfirstlane(page_ids[(key >> page_log) - id0]);
-                        bad = bad << 1 | (unsigned)(named < 0);
+                        if constexpr (keys.value) bad = bad << 1 | (unsigned)(named < 0);
                         const unsigned id = (unsigned)max(named, 0), in_page = (unsigned)(key & mask);
                         const unsigned char* const k = kb + ((uint64_t)id * k_page + in_page * k_token);
                         const unsigned char* const v = vb + ((uint64_t)id * v_page + in_page * v_token);
 #pragma unroll
-                        for (int i = 0; i < 8 / GK; ++i) {
-                            const int r = 8 * g + GK * i, x = r / GK % PERIOD;
-                            const unsigned to = stage + (unsigned)((in_stage + r) * ROW_K);
-                            if (has_k[x]) load_to_lds(k + (unsigned)(GK * i) * k_token, k_from[x], to);
-                            if (has_v[x]) load_to_lds(v + (unsigned)(GK * i) * v_token, v_from[x], to + V_OFF);
+                        for (int i = 0; i < 8 / RPI; ++i) {
+                            const int r = 8 * g + RPI * i;
+                            const unsigned to_k = k_stage + (unsigned)((in_stage + r) * ROW), to_v = v_stage + (unsigned)((in_stage + r) * ROW);
+                            if constexpr (UNIT == 16) {
+                                const int x = r / RPI % PERIOD;
+                                if constexpr (keys.value)
+                                    if (has_k[x]) load_to_lds(k + (unsigned)(RPI * i) * k_token, k_from[x], to_k);
+                                if constexpr (values.value)
+                                    if (has_v[x]) load_to_lds(v + (unsigned)(RPI * i) * v_token, v_from[x], to_v);
+                            } else {
+                                const unsigned fk = 16u * (unsigned)turn_k(in_stage + r), fv = 16u * (unsigned)turn_v(in_stage + r);
+#pragma unroll
+                                for (int part = 0; part < SPLIT; ++part) {
+                                    const unsigned ck = (in_row + (unsigned)(part * BYTES)) ^ fk, cv = (in_row + (unsigned)(part * BYTES)) ^ fv;
+                                    if constexpr (keys.value)
+                                        if ((int)ck < row_bytes) load_dword_to_lds(k + (unsigned)(RPI * i) * k_token, RPI > 1 ? k_in + ck : ck, to_k + part * BYTES);
+                                    if constexpr (values.value)
+                                        if ((int)cv < row_bytes) load_dword_to_lds(v + (unsigned)(RPI * i) * v_token, RPI > 1 ? v_in + cv : cv, to_v + part * BYTES);
+                                }
+                            }
                         }
                     }
                 };
-                unsigned now = base0, next = base0;                    // stages: the one that is worked on, and the one that is asked for
-                auto step_on = [&](unsigned& stage) { stage = stage + PART == base0 + S * PART ? base0 : stage + PART; };
+                // What the wave has loaded of the step kt, once it is there: a number that is no page (whoever sees its keys gets NaN), values of keys that not
+                // every row sees.  newer: stages asked for since.
+                auto mend_keys = [&](unsigned stage, int newer) {
+                    const unsigned its = bad >> (newer * (OWN / 8)) & ((1u << (OWN / 8)) - 1);
+                    if (its != 0) {
 #pragma unroll
-                for (int x = 0; x < DEPTH; ++x) {
-                    issue(s0 + x * KEYS, next);
-                    step_on(next);
-                }
-                for (int kt = s0; kt < s1; kt += KEYS) {
-                    wait_loads<(DEPTH - 1) * LOADS>();
-                    const bool odd_pages = (bad >> ((DEPTH - 1) * (OWN / 8)) & ((1u << (OWN / 8)) - 1)) != 0;
-                    if (kt + KEYS > tile_to || kt < tile_from || odd_pages) {          // not every row sees every key
+                        for (int x = 0; x < OWN / GK; ++x) {
+                            constexpr int N = (int)Number<T>::kNan;
+                            if (its >> (OWN / 8 - 1 - GK * x / 8) & 1) at_lds<i32x4>(stage + (unsigned)((in_stage + GK * x) * ROW + 16 * lane)) = i32x4{N, N, N, N};
+                        }
+                    }
+                };
+                auto mend_values = [&](int kt, unsigned stage) {
+                    if (kt + KEYS > tile_to || kt < tile_from) {
                         unsigned odd = 0;
 #pragma unroll
                         for (int x = 0; x < OWN / GK; ++x) {
-                            const unsigned to = now + (unsigned)((in_stage + GK * x) * ROW_K + 16 * lane);
-                            i32x4 v = without_odd<T>(at_lds<i32x4>(to + V_OFF), odd);
+                            const unsigned at = stage + (unsigned)((in_stage + GK * x) * ROW + 16 * lane);
+                            i32x4 v = without_odd<T>(at_lds<i32x4>(at), odd);
                             if (kt + own0 + GK * x + lane / CH >= end_key) v = i32x4{0, 0, 0, 0};
-                            at_lds<i32x4>(to + V_OFF) = v;
-                            if (bad >> ((DEPTH - 1) * (OWN / 8) + OWN / 8 - 1 - GK * x / 8) & 1) {     // a number that is no page: whoever sees its keys gets NaN
-                                constexpr int N = (int)Number<T>::kNan;
-                                at_lds<i32x4>(to) = i32x4{N, N, N, N};
-                            }
+                            at_lds<i32x4>(at) = v;
                         }
                         if (odd) again[1] = 1;
                     }
-                    if constexpr (!FEW) {
-                        wg_barrier_lds();
-                        issue(kt + DEPTH * KEYS, next);                // (behind the last step too, from the last keys)
-                        use(kt, now, now + V_OFF);
-                    } else {
-                        use(kt, now, now + V_OFF);
+                };
+                if constexpr (OWN_KEYS) {
+                    issue(s0, k_ring, v_ring, Yes{}, No{});
+                    issue(s0, k_ring, v_ring, No{}, Yes{});
+                    for (int kt = s0; kt < s1; kt += KEYS) {
+                        wait_loads<LOADS>();
+                        mend_keys(k_ring, 0);
+                        multiply(kt, k_ring);
+                        wait_lds();            // (the reads are done: LDS may be written)
+                        issue(kt + KEYS, k_ring, v_ring, Yes{}, No{});         // (behind the last step too, from the last keys)
+                        wait_loads<LOADS>();
+                        mend_values(kt, v_ring);
+                        weigh_up(kt, v_ring);
                         wait_lds();
-                        issue(kt + DEPTH * KEYS, next);
+                        issue(kt + KEYS, k_ring, v_ring, No{}, Yes{});
                     }
-                    step_on(now);
-                    step_on(next);
+                } else {
+                    // stages: the ones that are worked on, and the ones that are asked for
+                    unsigned k_now = k_ring, v_now = v_ring, k_next = k_ring, v_next = v_ring;
+                    auto on = [](unsigned& stage, unsigned ring, unsigned end) { stage = stage + PART == end ? ring : stage + PART; };
+                    auto next_stage = [&](int kt) {
+                        issue(kt, k_next, v_next, Yes{}, Yes{});
+                        on(k_next, k_ring, k_ring_end);
+                        on(v_next, v_ring, v_ring_end);
+                    };
+#pragma unroll
+                    for (int x = 0; x < AHEAD; ++x) next_stage(s0 + x * KEYS);
+                    // the stage of step kt is there, for all waves
+                    auto begin = [&](int kt) {
+                        wait_loads<2 * (AHEAD - 1) * LOADS>();
+                        mend_keys(k_now, AHEAD - 1);
+                        mend_values(kt, v_now);
+                        wg_barrier_lds();
+                        next_stage(kt + AHEAD * KEYS);                 // (behind the last step too, from the last keys)
+                    };
+                    if constexpr (in_turns.value) {
+                        begin(s0);
+                        multiply(s0, k_now);
+                        for (int kt = s0 + KEYS; kt < s1; kt += KEYS) {
+                            const unsigned before = v_now;
+                            on(k_now, k_ring, k_ring_end);
+                            on(v_now, v_ring, v_ring_end);
+                            begin(kt);
+                            weigh_up(kt - KEYS, before);
+                            multiply(kt, k_now);
+                        }
+                        weigh_up(s0 + (s1 - 1 - s0) / KEYS * KEYS, v_now);
+                    } else {
+                        for (int kt = s0; kt < s1; kt += KEYS) {
+                            begin(kt);
+                            multiply(kt, k_now);
+                            weigh_up(kt, v_now);
+                            on(k_now, k_ring, k_ring_end);
+                            on(v_now, v_ring, v_ring_end);
+                        }
+                    }
                 }
             }
             wait_loads<0>();
         } else {
-            constexpr int PER = 64 * NW / CH, LI = KEYS / PER, BYTES = buffer_bytes_of(DP, KW);
+            constexpr int PER = 64 * NW / CH, LI = KEYS / PER, BYTES = stage_bytes(DP, RW, LOAD);
             static_assert(PER * LI == KEYS, "whole loads");
             const int chunk = lane % CH, to_key = GK * wave + lane / CH;
             const unsigned to_k = (unsigned)(to_key * ROW_K + 16 * chunk), to_v = (unsigned)(KEYS * ROW_K + to_key * ROW_V + 16 * chunk);
@@ -420,11 +500,13 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 wg_barrier_lds();
                 load(kt + KEYS);               // (behind the last step too, from the last keys)
                 look_up(kt + 2 * KEYS);
-                if constexpr (buffers(KW) == 2) {
-                    use(kt, lds0 + turn * BYTES + own_k, lds0 + turn * BYTES + own_v);
+                if constexpr (stages(RW) == 2) {
+                    multiply(kt, lds0 + turn * BYTES + own_k);
+                    weigh_up(kt, lds0 + turn * BYTES + own_v);
                     if (kt + KEYS < end_key) store(kt + KEYS, lds + (turn ^ 1) * BYTES);
                 } else {
-                    use(kt, lds0 + own_k, lds0 + own_v);
+                    multiply(kt, lds0 + own_k);
+                    weigh_up(kt, lds0 + own_v);
                     if (kt + KEYS < end_key) {
                         wg_barrier_lds();
                         store(kt + KEYS, lds);
@@ -435,7 +517,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     };
     f32x16 s[KT], o[DT];
     float m = 0.0f, l;
-    auto score = [&](int k0, unsigned base) {
+    auto multiply = [&](int, unsigned base) {
 #pragma unroll
         for (int i = 0; i < KT; ++i)
 #pragma unroll
@@ -447,6 +529,8 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             for (int i = 0; i < KT; ++i) s[i] = mfma32(__builtin_bit_cast(x8, at_lds<i32x4>(at + 32 * i * ROW_K)), q[ks], s[i]);
         }
         in_turn<KS * KT, 1, 1, 6, 0, 0>();
+    };
+    auto hide = [&](int k0) {
         if (k0 + WK > all_to || k0 < all_from) {
             int to = sees_to - k0 - 4 * half, from = sees_from - k0 - 4 * half;
             stay(to);                          // (or the comparisons are made in every step, ahead of the branch)
@@ -470,12 +554,12 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         return fmaxf(top, __shfl_xor(top, 32)) * scale_log2;
     };
     auto finite = [&]() {
-        float zero = 0.0f;                     // (or NaN)
+        float zero[4] = {};                    // (or NaN)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) zero = __builtin_fmaf(o[dt][e], 0.0f, zero);
-        return zero == 0.0f;
+            for (int e = 0; e < 16; ++e) zero[e & 3] = __builtin_fmaf(o[dt][e], 0.0f, zero[e & 3]);
+        return zero[0] + zero[1] + zero[2] + zero[3] == 0.0f;
     };
     const float none = -__builtin_inff();
     for (bool known = false;;) {
@@ -485,10 +569,12 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
-        sweep([&](int kt, unsigned k_base, unsigned v_base) {
-            score(kt + WK * kw, k_base);
+        auto weigh_up = [&](int kt, unsigned v_base) {
+            hide(kt + WK * kw);
             if (!known && __any(m == none)) {
-                const float top = largest() - LIFT;
+                // fp16: of a few keys the largest says little, and later ones may leave it further behind
+                const int k0 = kt + WK * kw, seen = min(sees_to, k0 + WK) - max(sees_from, k0);
+                const float top = largest() - (seen < 16 ? 0.0f : LIFT);
                 m = m == none ? top : m;
             }
             const float shift = m == none ? 0.0f : m;
@@ -532,7 +618,10 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 __builtin_amdgcn_sched_barrier(0);
             }
             pinned(l);                         // (or the sums are made behind the loop, from registers that wait for that)
-        });
+        };
+        // The matrix cores and the vector units of a SIMD work on two waves: half of the waves are on the second product of a step while the others are on the first of the next
+        if (TURNS && wave >= NW / 2) sweep(multiply, weigh_up, Yes{});
+        else sweep(multiply, weigh_up, No{});
         // (a lane's O is of the keys of both halves)
         const float both = l + __shfl_xor(l, 32);
         if (!finite() || (WIDE && !(both < 0x1p40f))) again[0] = 1;
@@ -540,10 +629,10 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         if (!again[0] || known) break;
         known = true;
         m = none;
-        sweep([&](int kt, unsigned k_base, unsigned) {
-            score(kt + WK * kw, k_base);
+        sweep(multiply, [&](int kt, unsigned) {
+            hide(kt + WK * kw);
             m = fmaxf(m, largest() - LIFT);
-        });
+        }, No{});
         __syncthreads();
     }
     l += __shfl_xor(l, 32);
@@ -552,50 +641,45 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
 
     // The results leave through LDS (nobody reads the buffers any more), so that a store has whole lines.
     const ChunkParams& z = parameters();
-    // where a row's result goes and what it is multiplied with: its 1 / l, or 1 where it is a part
-    auto place = [&](int r, float top, float total) {
-        const int at_row = t.row0 + r, its = at_row / z.G, head = t.h * z.G + at_row - its * z.G;
-        const int64_t part = part_at<FEW>(z, t.seq, t.b, t.h, at_row, t.split, z.few_rows);
-        row_to[r] = t.direct ? (t.seq.start + its) * z.out_token + head * z.out_head : part * z.D;
-        row_factor[r] = total != total ? total : (total == 0.0f ? 0.0f : (t.direct ? 1.0f / total : 1.0f));
-        if (at_row >= t.row_end) return;
+    float* const parts = FEW ? z.few_o : z.many_o;
+    // Row r of the tile: where its result goes (to `slot`) and what it is multiplied with, 1 / l, or 1 where it is a part; its sums, by one of those who place it.
+    auto place = [&](int r, int slot, float top, float total, bool sums) {
+        const int at_row = t.row0 + r, its = query_of(z, t, r), head = t.h * z.G + at_row - its * z.G;
+        const int64_t part = part_at<FEW>(z, t.seq, t.b, t.h, at_row, its, head, t.split);
+        row_to[slot] = t.direct ? (t.seq.start + its) * z.out_token + head * z.out_head : part * z.D;
+        row_factor[slot] = total != total ? total : (total == 0.0f ? 0.0f : (t.direct ? 1.0f / total : 1.0f));
+        if (!sums || at_row >= t.row_end) return;
         if (!t.direct) *(f32x2*)((FEW ? z.few_ml : z.many_ml) + part * 2) = f32x2{top, total};
         else if (z.lse) z.lse[(int64_t)(t.seq.start + its) * (z.Hk * z.G) + head] = lse_of(top, total);
     };
-    float* const parts = FEW ? z.few_o : z.many_o;
-    auto put = [&](int r, int d, const f32x4& x) {                     // row r of the tile, its O from feature d on
-        if (t.row0 + r >= t.row_end || d >= z.D) return;
-        const float factor = row_factor[r];
-        const int64_t to = row_to[r] + d;
-        const f32x4 y = factor == 0.0f ? f32x4{0, 0, 0, 0} : x * factor;
-        if (__builtin_fmaf(y.x, 0.0f, __builtin_fmaf(y.y, 0.0f, __builtin_fmaf(y.z, 0.0f, y.w * 0.0f))) != 0.0f && factor == factor) again[1] = 1;
-        if (t.direct) store_four(z, to, y);
-        else *(f32x4*)(parts + to) = y;
-    };
-    if constexpr (!FEW) {
-        constexpr int TF = turn_features(DP), TP = TF + 4;             // floats from row to row
-        float* const turned = (float*)lds + wave * 32 * TP;
-        if (half == 0) place(32 * wave + l32, m, l);
-        __builtin_amdgcn_wave_barrier();
+    // COUNT rows at once: r0, r0 + step, ..., each the lane's four features from d on, read at from + i * pitch
+    float odd = 0.0f;                          // (NaN where there is something to settle)
+    auto put = [&](auto count, int r0, int step, int slot0, int d, auto read) {
+        constexpr int COUNT = decltype(count)::value;
+        f32x4 x[COUNT];
+        float factor[COUNT];
+        int64_t to[COUNT];
 #pragma unroll
-        for (int d0 = 0; d0 < DP; d0 += TF) {
-#pragma unroll
-            for (int i = 0; i < TF / 8; ++i) {
-                const int dt = d0 / 32 + i / 4, e = 4 * (i & 3);
-                *(f32x4*)(turned + l32 * TP + 8 * i + 4 * half) = f32x4{o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3]};
-            }
-            __builtin_amdgcn_wave_barrier();
-            constexpr int LANES = TF / 4;      // of a row
-#pragma unroll
-            for (int i = 0; i < 32 * LANES / 64; ++i) {
-                const int r = i * (64 / LANES) + lane / LANES, d = 4 * (lane % LANES);
-                put(32 * wave + r, d0 + d, *(const f32x4*)(turned + r * TP + d));
-            }
-            __builtin_amdgcn_wave_barrier();
+        for (int i = 0; i < COUNT; ++i) {
+            x[i] = read(i);
+            factor[i] = row_factor[slot0 + i * step];
+            to[i] = row_to[slot0 + i * step] + d;
         }
-    } else {
-        constexpr int TP = DP + 4;
-        float* const turned = (float*)lds + wave * 32 * TP;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            const f32x4 y = factor[i] == 0.0f ? f32x4{0, 0, 0, 0} : x[i] * factor[i];
+            if (t.row0 + r0 + i * step < t.row_end && d < z.D) {
+                const float nothing = __builtin_fmaf(y.x, 0.0f, __builtin_fmaf(y.y, 0.0f, __builtin_fmaf(y.z, 0.0f, y.w * 0.0f)));
+                odd += factor[i] == factor[i] ? nothing : 0.0f;
+                if (t.direct) store_four<O>(z.out, to[i], y);
+                else *(f32x4*)(parts + to[i]) = y;
+            }
+        }
+    };
+    constexpr int LP = leave_pitch(DP, RW);
+    float* const own = (float*)lds + wave * 32 * LP;
+    if constexpr (FEW) {
+        constexpr int HALF = DP / 2, LANES = HALF / 4, ROWS = 64 * NW / LANES < 32 ? 64 * NW / LANES : 32;
         if (half == 0) {
             row_m[32 * wave + l32] = m;
             row_l[32 * wave + l32] = l;
@@ -605,14 +689,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
 #pragma unroll
         for (int w = 0; w < KW; ++w) top = fmaxf(top, row_m[32 * w + l32]);
         const float factor = m == none ? 0.0f : exp2_fast(m - top);
-        // (a part without weight says nothing, whatever 0 times its values is)
-        const bool counts = l != 0.0f;
-#pragma unroll
-        for (int i = 0; i < DP / 8; ++i) {
-            const int dt = i / 4, e = 4 * (i & 3);
-            f32x4 x = f32x4{o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3]} * factor;
-            *(f32x4*)(turned + l32 * TP + 8 * i + 4 * half) = counts ? x : f32x4{0, 0, 0, 0};
-        }
+        const bool counts = l != 0.0f;         // (a part without weight says nothing, whatever 0 times its values is)
         if (wave == 0 && half == 0) {
             float total = 0.0f;
 #pragma unroll
@@ -620,52 +697,106 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 const float part = row_l[32 * w + l32], its = row_m[32 * w + l32];
                 total += part == 0.0f ? 0.0f : part * (its == none ? 0.0f : exp2_fast(its - top));
             }
-            place(l32, total == 0.0f ? none : top, total);
+            place(l32, l32, total == 0.0f ? none : top, total, true);
         }
-        __syncthreads();
-        constexpr int LANES = DP / 4, ROWS = 64 * NW / LANES;
-        const int d = 4 * (tid % LANES);
 #pragma unroll
-        for (int i = 0; i < 32 / ROWS; ++i) {
-            const int r = i * ROWS + tid / LANES;
-            f32x4 x = f32x4{0, 0, 0, 0};
+        for (int d0 = 0; d0 < DP; d0 += HALF) {
 #pragma unroll
-            for (int w = 0; w < KW; ++w) x += *(const f32x4*)((const float*)lds + (32 * w + r) * TP + d);
-            put(r, d, x);
+            for (int i = 0; i < HALF / 8; ++i) {
+                const int dt = (d0 + 8 * i) / 32, e = 4 * (i & 3);
+                const f32x4 x = f32x4{o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3]} * factor;
+                *(f32x4*)(own + l32 * LP + 8 * i + 4 * half) = counts ? x : f32x4{0, 0, 0, 0};
+            }
+            __syncthreads();
+            const int r0 = tid / LANES, d = 4 * (tid % LANES);
+            if (r0 < ROWS)
+                put(Count<32 / ROWS>{}, r0, ROWS, r0, d0 + d, [&](int i) {
+                    f32x4 x = f32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int w = 0; w < KW; ++w) x += *(const f32x4*)((const float*)lds + (32 * w + r0 + i * ROWS) * LP + d);
+                    return x;
+                });
+            if (d0 == 0) __syncthreads();
+        }
+    } else {
+        constexpr int TF = turn_features(DP), LANES = TF / 4, ROWS = 64 / LANES;       // features that leave together, lanes of a row, rows of a store
+        float* turned = own;
+        int d_first = 0;
+        if constexpr (KW > 1) {                // the two waves of a row have half of the features each from here on: each hands the other's over
+            const int other = wave ^ RW;
+            auto four = [&](int i) { return f32x4{o[i / 4][4 * (i & 3)], o[i / 4][4 * (i & 3) + 1], o[i / 4][4 * (i & 3) + 2], o[i / 4][4 * (i & 3) + 3]}; };
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) *(f32x4*)(own + l32 * LP + 8 * i + 4 * half) = kw == 0 ? four(i + DP / 16) : four(i);
+            if (half == 0) {
+                row_m[32 * wave + l32] = m;
+                row_l[32 * wave + l32] = l;
+            }
+            __syncthreads();
+            const float om = row_m[32 * other + l32], ol = row_l[32 * other + l32], top = fmaxf(m, om);
+            const float f = m == none ? 0.0f : exp2_fast(m - top), of = om == none ? 0.0f : exp2_fast(om - top);
+            const bool counts = l != 0.0f, other_counts = ol != 0.0f;
+            turned = (float*)lds + other * 32 * LP;    // (which nobody else reads)
+            f32x4 y[DP / 16];
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) y[i] = *(const f32x4*)(turned + l32 * LP + 8 * i + 4 * half);
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+                const f32x4 x = kw == 0 ? four(i) : four(i + DP / 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i / 4][4 * (i & 3) + e] = (counts ? x[e] * f : 0.0f) + (other_counts ? y[i][e] * of : 0.0f);
+            }
+            l = (counts ? l * f : 0.0f) + (other_counts ? ol * of : 0.0f);
+            m = l == 0.0f ? none : top;
+            d_first = kw * (DP / 2);
+        }
+        if (half == 0) place(32 * rw + l32, 32 * wave + l32, m, l, kw == 0);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int d0 = 0; d0 < (KW > 1 ? DP / 2 : DP); d0 += TF) {
+#pragma unroll
+            for (int i = 0; i < TF / 8; ++i) {
+                const int dt = d0 / 32 + i / 4, e = 4 * (i & 3);
+                *(f32x4*)(turned + l32 * LP + 8 * i + 4 * half) = f32x4{o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3]};
+            }
+            __builtin_amdgcn_wave_barrier();
+            const int r = lane / LANES, d = 4 * (lane % LANES);
+            put(Count<32 / ROWS>{}, 32 * rw + r, ROWS, 32 * wave + r, d_first + d0 + d, [&](int i) { return *(const f32x4*)(turned + (r + i * ROWS) * LP + d); });
+            __builtin_amdgcn_wave_barrier();
         }
     }
+    if (odd != 0.0f) again[1] = 1;
     __syncthreads();
     if (__builtin_expect(again[1] != 0, 0)) {
         // every wave settles its own rows, or its share of them
         __threadfence();
         unsigned rows = 0;
-        for (int r = FEW ? kw : 0; r < 32; r += FEW ? KW : 1)
-            if (wave_row0 + r < t.row_end && row_factor[32 * rw + r] == row_factor[32 * rw + r]) rows |= 1u << r;
-        settle_chunk<T, DP, FEW>(z, t, wave_row0, rows);
+        for (int r = kw; r < 32; r += KW) {
+            const float factor = row_factor[FEW ? r : 32 * wave + r];
+            if (wave_row0 + r < t.row_end && factor == factor) rows |= 1u << r;
+        }
+        settle_chunk<T, O, DP, FEW>(z, t, wave_row0, rows);
     }
 }
 
-// Few rows: workgroups are numbered sequence by sequence, key head by key head, part by part.
-template <class T, int DP, int TERMS, bool FAST>
-__global__ void __launch_bounds__(64 * few_waves(DP, FAST), DP > 128 || FAST ? 1 : 2) few_rows_kernel(const ChunkParams p) {
-    extern __shared__ __align__(16) unsigned char lds[];
-    const int i = ((int)blockIdx.x & 7) * p.few_per_xcd + ((int)blockIdx.x >> 3);
+// Workgroup `i` of those for few rows, sequence by sequence, key head by key head, part by part.
+template <class T, int DP, int TERMS, int LOAD>
+__device__ __forceinline__ void few_rows(const ChunkParams& p, int i, unsigned char* lds) {
     Tile t;
     t.split = i % p.few_splits;
     t.h = i / p.few_splits % p.Hk;
     t.b = i / p.few_splits / p.Hk;
     if (t.b >= p.B) return;
     t.seq = chunk_of(p, t.b);
-    t.row0 = 0;
+    t.row0 = t.j0 = t.g0 = 0;
     t.row_end = t.seq.queries * p.G;
     if (t.row_end == 0) return;
     if (t.row_end > p.few_rows) {
-        // another launch's; where there is none, more queries than the caller said that there are: NaN
+        // worked on as many rows; where nobody does, more queries than the caller said that there are: NaN
         if (p.many_per_xcd == 0 && t.split == 0)
-            for (int64_t x = threadIdx.x; x < (int64_t)t.row_end * (p.D / 4); x += 64 * few_waves(DP, FAST)) {
+            for (int64_t x = threadIdx.x; x < (int64_t)t.row_end * (p.D / 4); x += 64 * waves_of(DP)) {
                 const int row = (int)(x / (p.D / 4)), j = row / p.G, d = 4 * (int)(x % (p.D / 4));
                 const float nan = __builtin_nanf("");
-                store_four(p, (t.seq.start + j) * p.out_token + (int64_t)(t.h * p.G + row - j * p.G) * p.out_head + d, f32x4{nan, nan, nan, nan});
+                store_four<typename Output<T, TERMS>::type>(p.out, (t.seq.start + j) * p.out_token + (int64_t)(t.h * p.G + row - j * p.G) * p.out_head + d, f32x4{nan, nan, nan, nan});
                 if (p.lse && d == 0) p.lse[(int64_t)(t.seq.start + j) * (p.Hk * p.G) + t.h * p.G + row - j * p.G] = nan;
             }
         return;
@@ -675,29 +806,31 @@ __global__ void __launch_bounds__(64 * few_waves(DP, FAST), DP > 128 || FAST ? 1
     t.direct = r.parts == 1;
     t.first = r.first + t.split * p.few_chunk;
     t.end = t.first + min(r.end - t.first, p.few_chunk);
-    attend_chunk<T, DP, 1, few_waves(DP, FAST), TERMS, FAST>(p, t, lds);
+    attend_chunk<T, DP, 1, TERMS, LOAD>(p, t, lds);
 }
 
-// Many rows: tile `at` of the sequences' tiles, one sequence behind the other and the last tile of each, which sees the most, first.
-template <class T, int DP, int RW, int TERMS, bool FAST>
-__global__ void __launch_bounds__(64 * RW, DP > 128 ? 1 : 2) many_rows_kernel(const ChunkParams p) {
-    extern __shared__ __align__(16) unsigned char lds[];
+// Workgroup `i` of those for many rows: tile `at` of the sequences' tiles, one sequence behind the other.  Of a sequence's tiles those that see the most and the least take turns,
+// so that any stretch of them is about the same work.
+template <class T, int DP, int RW, int TERMS, int LOAD>
+__device__ __forceinline__ void many_rows(const ChunkParams& p, int i, unsigned char* lds) {
     constexpr int ROWS = 32 * RW;
-    const int i = ((int)blockIdx.x & 7) * p.many_per_xcd + ((int)blockIdx.x >> 3), lane = (int)threadIdx.x & 63;
+    const int lane = (int)threadIdx.x & 63;
     int at = i % p.many_tiles;
     Tile t;
     t.split = i / p.many_tiles % p.many_splits;
     t.h = i / p.many_tiles / p.many_splits;
     if (t.h >= p.Hk) return;
     t.b = -1;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-        const int b = b0 + lane;
-        int rows = 0;
-        if (b < p.B) {
-            const int start = p.starts[b], next = p.starts[b + 1];
-            rows = start >= 0 && next >= start && next <= p.N ? (next - start) * p.G : 0;
+    if (p.B == 1) {
+        t.seq = chunk_of(p, 0);
+        const int rows = t.seq.queries * p.G, tiles = rows > p.few_rows ? (rows + ROWS - 1) / ROWS : 0;
+        if (at < tiles) {
+            t.b = 0;
+            at = at & 1 ? at >> 1 : tiles - 1 - (at >> 1);
         }
-        const int tiles = rows > p.few_rows ? (rows + ROWS - 1) / ROWS : 0;
+    } else for (int b0 = 0; b0 < p.B; b0 += 64) {
+        const Chunk c = b0 + lane < p.B ? chunk_of(p, b0 + lane) : Chunk{};
+        const int rows = c.queries * p.G, tiles = rows > p.few_rows ? (rows + ROWS - 1) / ROWS : 0;
         int sum = tiles;
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) {
@@ -706,9 +839,11 @@ __global__ void __launch_bounds__(64 * RW, DP > 128 ? 1 : 2) many_rows_kernel(co
         }
         const uint64_t past = __ballot(sum > at);
         if (past) {
-            const int f = __builtin_ctzll(past);
+            const int f = __builtin_ctzll(past), its = __shfl(tiles, f), in = at - (__shfl(sum, f) - its);
             t.b = b0 + f;
-            at = __shfl(sum, f) - 1 - at;
+            at = in & 1 ? in >> 1 : its - 1 - (in >> 1);
+            auto its_own = [&](int x) { return __builtin_amdgcn_readlane(x, __builtin_amdgcn_readfirstlane(f)); };
+            t.seq = Chunk{its_own(c.start), its_own(c.queries), its_own(c.len), its_own(c.base), its_own(c.bad)};
             break;
         }
         at -= __shfl(sum, 63);
@@ -716,19 +851,32 @@ __global__ void __launch_bounds__(64 * RW, DP > 128 ? 1 : 2) many_rows_kernel(co
     t.b = __builtin_amdgcn_readfirstlane(t.b);
     at = __builtin_amdgcn_readfirstlane(at);
     if (t.b < 0) return;
-    t.seq = chunk_of(p, t.b);
     t.row0 = at * ROWS;
     t.row_end = min(t.row0 + ROWS, t.seq.queries * p.G);
-    const Range r = range_of(p, t.seq, t.row0 / p.G, (t.row_end - 1) / p.G, p.many_chunk);
+    t.j0 = t.row0 / p.G;
+    t.g0 = t.row0 - t.j0 * p.G;
+    const Range r = range_of(p, t.seq, t.j0, __builtin_amdgcn_readfirstlane(query_of(p, t, t.row_end - 1 - t.row0)), p.many_chunk);
     if (t.split >= r.parts) return;
     t.direct = r.parts == 1;
     t.first = r.first + t.split * p.many_chunk;
     t.end = t.first + min(r.end - t.first, p.many_chunk);
-    attend_chunk<T, DP, RW, 1, TERMS, FAST>(p, t, lds);
+    attend_chunk<T, DP, RW, TERMS, LOAD>(p, t, lds);
+}
+
+// Workgroups go to the 8 XCDs in turn, and tiles of one key head, which read the same keys, to one XCD (one L2) as far as that goes.  An XCD begins with its tiles that
+// see much (every other one) and ends with those that see little; the few rows are behind them.
+template <class T, int DP, int RW, int TERMS, int LOAD>
+__global__ void __launch_bounds__(64 * waves_of(DP), DP > 128 ? 1 : 2) chunk_kernel(const ChunkParams p) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int xcd = (int)blockIdx.x & 7, place = (int)blockIdx.x >> 3, n = p.many_per_xcd;
+    if (place < n) {
+        const int heavy = (n + 1) / 2;
+        many_rows<T, DP, RW, TERMS, LOAD>(p, xcd * n + (place < heavy ? 2 * place : 2 * (n - 1 - place) + 1), lds);
+    } else few_rows<T, DP, TERMS, LOAD>(p, xcd * p.few_per_xcd + place - n, lds);
 }
 
 // The parts of every row joined, where there are several: DP / 4 threads have four features each.
-template <class T, int DP>
+template <class O, int DP>
 __global__ void __launch_bounds__(256) combine_chunks(const ChunkParams p) {
     constexpr int PER = DP / 4, ROWS = 256 / PER;
     const int Hq = p.Hk * p.G, d = (int)(threadIdx.x % PER) * 4, lane = (int)threadIdx.x & 63;
@@ -762,7 +910,7 @@ __global__ void __launch_bounds__(256) combine_chunks(const ChunkParams p) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int s = min(s0 + i, r.parts - 1);
-            const int64_t at = few ? part_at<true>(p, c, b, h, in_head, s, p.few_rows) : part_at<false>(p, c, b, h, in_head, s, 0);
+            const int64_t at = few ? part_at<true>(p, c, b, h, in_head, j, head, s) : part_at<false>(p, c, b, h, in_head, j, head, s);
             const f32x2 ml = *(const f32x2*)((few ? p.few_ml : p.many_ml) + at * 2);
             m[i] = ml.x;
             l[i] = ml.y;
@@ -785,7 +933,7 @@ __global__ void __launch_bounds__(256) combine_chunks(const ChunkParams p) {
         }
         top = now;
     }
-    store_four(p, token * p.out_token + head * p.out_head + d, total == 0.0f ? f32x4{0, 0, 0, 0} : x * (1.0f / total));
+    store_four<O>(p.out, token * p.out_token + head * p.out_head + d, total == 0.0f ? f32x4{0, 0, 0, 0} : x * (1.0f / total));
     if (p.lse && d == 0) p.lse[row] = lse_of(top, total);
 }
 

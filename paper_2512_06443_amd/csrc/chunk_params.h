@@ -22,7 +22,7 @@ struct ChunkParams {
     float *few_o, *few_ml;             // parts of sequences with few rows: [split][B][Hk][few_rows][D], [..][2]
     float *many_o, *many_ml;           // of the others: [split][N][heads][D], [..][2]
     float scale_log2;                  // scale * log2(e): exponentials are powers of two
-    int out_type;                      // VLUT_TYPE_*
+    float inverse_g;                   // 1 / G
     int N, B, Hk, G, D, page_log, pages, max_len;
     int window;                        // keys that a query sees at most
     int few_rows;                      // a sequence of up to so many rows per key head is a few-row one (0: none is)
@@ -32,42 +32,55 @@ struct ChunkParams {
 
 constexpr int kFewRows = 32;
 
-// Of a workgroup with RW x KW waves: RW groups of 32 rows, the keys of a step shared by KW.
-// Where memory is loaded straight to LDS (FAST) rows of keys lie one behind the other in several stages, a wave's own ones where waves share the keys; else
-// they go through registers, to rows that are padded.
-__host__ __device__ constexpr int few_waves(int DP, bool FAST) { return FAST && DP > 128 ? 2 : 4; }          // KW where rows are few
-__host__ __device__ constexpr int wave_keys(int DP, int KW) { return KW > 1 || DP > 128 ? 32 : 64; }
-__host__ __device__ constexpr int step_keys(int DP, int KW) { return wave_keys(DP, KW) * KW; }
-__host__ __device__ constexpr int k_pitch(int DP) { return DP * 2 + 16; }
-__host__ __device__ constexpr int v_pitch(int DP) { return DP * 2 + 64; }
-__host__ __device__ constexpr int buffer_bytes_of(int DP, int KW) { return step_keys(DP, KW) * (k_pitch(DP) + v_pitch(DP)); }
-__host__ __device__ constexpr int buffers(int KW) { return KW > 1 ? 1 : 2; }
-__host__ __device__ constexpr int stages(int DP, int RW, int KW) { return KW > 1 ? 2 : (RW > 4 || DP > 128 ? 3 : 2); }
-__host__ __device__ constexpr int stage_bytes(int DP, int KW) { return step_keys(DP, KW) * DP * 4; }
+// How keys and values come to LDS: through registers; straight, a dword or 16 bytes a lane; of rows that are as long as LDS has them.
+constexpr int kThroughRegisters = 0, kDwords = 1, kVectors = 2, kWholeVectors = 3;
+
+// A workgroup's waves: RW groups of 32 rows, the keys of a step shared by KW.  Where rows are few 1 x all; where they are many all x 1, or half x 2.
+__host__ __device__ constexpr int waves_of(int DP) { return DP > 128 ? 4 : 8; }
+__host__ __device__ constexpr bool own_keys(int RW, int LOAD) { return RW == 1 && LOAD != kThroughRegisters; }      // waves have their keys for themselves
+__host__ __device__ constexpr bool turns(int DP, int RW, int LOAD) { return RW == 8 && LOAD != kThroughRegisters; }  // a SIMD's two waves take the products in turns
+__host__ __device__ constexpr int wave_keys(int DP, int RW) { return RW == 1 || DP > 128 ? 32 : 64; }
+__host__ __device__ constexpr int step_keys(int DP, int RW) { return wave_keys(DP, RW) * (waves_of(DP) / RW); }
+__host__ __device__ constexpr int k_pitch(int DP, int LOAD) { return DP * 2 + (LOAD == kThroughRegisters ? 16 : 0); }
+__host__ __device__ constexpr int v_pitch(int DP, int LOAD) { return DP * 2 + (LOAD == kThroughRegisters ? 64 : 0); }
+// Through registers: a stage is a step's keys and values.  Straight: the KW groups of waves have rings of stages of their keys and of their values each, AHEAD of which
+// are on their way; where waves take turns the later ones read values of the step before.
+__host__ __device__ constexpr int stage_bytes(int DP, int RW, int LOAD) { return step_keys(DP, RW) * (k_pitch(DP, LOAD) + v_pitch(DP, LOAD)); }
+__host__ __device__ constexpr int stages(int RW) { return RW == 1 ? 1 : 2; }
+__host__ __device__ constexpr int ahead(int DP, int RW) { return RW == waves_of(DP) ? 2 : 1; }
+__host__ __device__ constexpr int key_ring(int DP, int RW) { return RW == 1 ? 1 : ahead(DP, RW) + 1; }
+__host__ __device__ constexpr int value_ring(int DP, int RW, bool later) { return RW == 1 ? 1 : ahead(DP, RW) + 1 + (later ? 1 : 0); }
+__host__ __device__ constexpr int ring_bytes(int DP, int RW, bool later) { return (key_ring(DP, RW) + value_ring(DP, RW, later)) * wave_keys(DP, RW) * DP * 2; }
+__host__ __device__ constexpr int buffers_bytes(int DP, int RW, int LOAD) {
+    if (LOAD == kThroughRegisters) return stages(RW) * stage_bytes(DP, RW, LOAD);
+    if (RW == 1) return waves_of(DP) * ring_bytes(DP, RW, false);
+    if (RW == waves_of(DP)) return ring_bytes(DP, RW, turns(DP, RW, LOAD));
+    return 2 * ring_bytes(DP, RW, false);
+}
 __host__ __device__ constexpr int turn_features(int DP) { return DP > 64 ? 64 : 32; }       // that leave through LDS together
 __host__ __device__ constexpr int most_of(int a, int b) { return a > b ? a : b; }
-// Keys and values, or what results leave through: rows of a wave, or the parts of KW waves.
-__host__ __device__ constexpr int tile_bytes(int DP, int RW, int KW, bool FAST) {
-    return most_of(FAST ? stages(DP, RW, KW) * stage_bytes(DP, KW) : buffers(KW) * buffer_bytes_of(DP, KW),
-                   KW > 1 ? KW * 32 * (DP + 4) * 4 : RW * 32 * (turn_features(DP) + 4) * 4);
-}
-constexpr int kStretch = 16384;        // keys whose pages' numbers are in LDS (FAST, 8 keys a page at least)
+// Keys and values, or what results leave through: for each wave 32 rows, of the features that leave together, or of half of them all.
+__host__ __device__ constexpr int leave_pitch(int DP, int RW) { return (RW == waves_of(DP) ? turn_features(DP) : DP / 2) + 4; }
+__host__ __device__ constexpr int tile_bytes(int DP, int RW, int LOAD) { return most_of(buffers_bytes(DP, RW, LOAD), waves_of(DP) * 32 * leave_pitch(DP, RW) * 4); }
+constexpr int kStretch = 16384;        // keys whose pages' numbers are in LDS (8 keys a page at least)
 constexpr int kStretchPages = kStretch / 8 + 2;
-__host__ __device__ constexpr int lds_bytes(int DP, int RW, int KW, bool FAST) {
-    return tile_bytes(DP, RW, KW, FAST) + RW * KW * 32 * 8 + RW * 32 * 12 + 16 + (FAST ? kStretchPages * 4 : 0);
+__host__ __device__ constexpr int lds_bytes(int DP, int RW, int LOAD) {
+    return tile_bytes(DP, RW, LOAD) + waves_of(DP) * 32 * 20 + 16 + (LOAD == kThroughRegisters ? 0 : kStretchPages * 4);
 }
 
 struct ChunkPlan {
-    int DP, many_waves;                // waves of a workgroup where rows are many
-    int few, many;                     // whether there is such a launch
+    int DP, row_waves, load;           // RW where rows are many; how keys come to LDS
+    int few, many;                     // whether there are such workgroups
     int few_splits, few_chunk, few_row_places, many_splits, many_chunk, many_tiles, many_rows;
     int few_per_xcd, many_per_xcd;
-    int fast;                          // heads of a multiple of 8 features in rows of 16 bytes' alignment, 8 keys share their page, strides of 31 bits
     size_t few_o_bytes, few_ml_bytes, many_o_bytes, many_ml_bytes;
     size_t bytes() const { return few_o_bytes + few_ml_bytes + many_o_bytes + many_ml_bytes; }
 };
 
+// For outputs of the cache's type, and of fp32.
 __attribute__((visibility("hidden"))) int launch_bf16(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream);
+__attribute__((visibility("hidden"))) int launch_bf16_f32(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream);
 __attribute__((visibility("hidden"))) int launch_f16(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream);
+__attribute__((visibility("hidden"))) int launch_f16_f32(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream);
 
 }  // namespace vlut_chunk

@@ -138,16 +138,15 @@ def test_longer_ones(Hq, Hk, D, news, lens, window, dtype, out):
     assert torch.equal(got, again) and torch.equal(lse, again_lse)
 
 
-def test_eight_waves():
-    """Enough rows for the largest tiles, every type and feature count that has them."""
-    for Hq, Hk, D, dtype, out in ((16, 16, 128, BF16, BF16), (32, 8, 64, F16, F16), (16, 16, 100, F16, F32), (16, 8, 128, BF16, F32)):
-        n = 256 * 256 // Hq + 77
+def test_the_largest_tiles():
+    """Enough rows for tiles of 256, every type and way of loading that has them."""
+    for Hq, Hk, D, dtype, out in ((64, 64, 128, BF16, BF16), (64, 16, 64, F16, F16), (64, 64, 100, F16, F32), (64, 32, 128, BF16, F32), (64, 8, 96, BF16, BF16)):
+        n = 4096 + 77
         assert B.query_chunk_attention(n, 1, Hq, Hk, D, n, n)[3] == 256
         c = case([n], [n + 20], Hq, Hk, D, dtype, 64, seed=1)
-        got, lse = run(c, 0, out)
-        check(c, got, lse)
-        got, lse = run(c, 100, out)
-        check(c, got, lse, 100)
+        for window in (0, 100):
+            got, lse = run(c, window, out)
+            check(c, got, lse, window)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
@@ -294,18 +293,18 @@ def test_lengths_pages_and_starts_that_cannot_be():
 
 def test_views_and_a_workspace_of_the_callers():
     N, Hq, Hk, D = 90, 8, 2, 64
-    c = case([90], [400], Hq, Hk, D, BF16, 16, seed=6, rows_behind=0)
+    c = case([90], [1400], Hq, Hk, D, BF16, 16, seed=6, rows_behind=0)
     wide = torch.randn(N, Hq + 3, D + 2, device="cuda", generator=generator(7)).to(BF16)
     q = wide[:, 2:2 + Hq, 2:]
     q.copy_(c["q"])
-    first = B.chunk_attention(**c)[0]
-    d = dict(c, q=q)
+    first = B.chunk_attention(**c, max_len=1416)[0]
+    d = dict(c, q=q, max_len=1416)
     into = torch.zeros(N, 2 * Hq, D, dtype=BF16, device="cuda")
     assert torch.equal(B.chunk_attention(**d, out=into[:, ::2])[0], first) and bool((into[:, 1::2] == 0).all())
-    need = B.chunk_attention_bytes(N, 1, Hq, Hk, D, N, 416)
+    need = B.chunk_attention_bytes(N, 1, Hq, Hk, D, N, 1416)
     assert need > 0
     ws = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
-    assert torch.equal(B.chunk_attention(**c, max_len=416, workspace=ws[:need])[0], first) and bool((ws[need:] == 255).all())
+    assert torch.equal(B.chunk_attention(**c, max_len=1416, workspace=ws[:need])[0], first) and bool((ws[need:] == 255).all())
 
 
 def test_a_cache_past_32_bits():
