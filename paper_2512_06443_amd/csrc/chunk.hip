@@ -40,11 +40,11 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
     a.few = !a.many || (B > 1 && G <= kFewRows);
     if (a.few) {
         a.few_row_places = (int)std::min<int64_t>(kFewRows, std::max<int64_t>(1, most_rows / G) * G);
-        // Keys that one tile sees, in steps.  Parts so that the workgroups are six rounds of those that run at once, of two steps at least; where that many are not
+        // Keys that one tile sees, in steps.  Parts so that the workgroups are four rounds of those that run at once, of four steps at least; where that many are not
         // there, of one.
-        const int64_t step = step_keys(a.DP, 1), keys = seen(kFewRows), steps = ceil_div(keys, step);
-        int64_t per = std::max<int64_t>(2, ceil_div(B * Hk * steps, 6 * kUnits));
-        if (B * Hk * ceil_div(steps, per) < kUnits) per = 1;
+        const int64_t step = step_keys(a.DP, 1), keys = seen(kFewRows), steps = ceil_div(keys, step), slots = 2 * kUnits;
+        int64_t per = std::max<int64_t>(4, ceil_div(B * Hk * steps, 4 * slots));
+        while (per > 1 && B * Hk * ceil_div(steps, per) < slots) per /= 2;
         a.few_chunk = (int)(step * per);
         a.few_splits = (int)ceil_div(keys, a.few_chunk);
         const int64_t blocks = ceil_div(B * Hk * a.few_splits, 8);
@@ -57,11 +57,11 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
         }
     }
     if (a.many) {
-        const int64_t rows = N * G, waves = waves_of(a.DP);
+        const int64_t rows = N * G;
         a.row_waves = !registers && a.DP <= 128 && rows * Hk >= 4 * 256 * kUnits ? 8 : 4;
         a.many_rows = 32 * a.row_waves;
         a.many_tiles = (int)std::min(rows / a.many_rows + B, (rows + B * (a.many_rows - 1)) / a.many_rows);
-        const int64_t keys = seen(a.many_rows / G + 1), step = wave_keys(a.DP, a.row_waves) * (waves / a.row_waves), tiles = a.many_tiles * Hk;
+        const int64_t keys = seen(a.many_rows / G + 1), step = step_keys(a.DP, a.row_waves), tiles = a.many_tiles * Hk;
         const int64_t splits = std::min(std::max<int64_t>(1, kUnits / tiles), ceil_div(keys, 512));
         a.many_chunk = (int)(ceil_div(ceil_div(keys, splits), step) * step);
         a.many_splits = (int)ceil_div(keys, a.many_chunk);

@@ -152,6 +152,11 @@ __device__ __forceinline__ void stay(int& x) {
 #endif
 }
 
+__device__ __forceinline__ void stay_scalar(unsigned& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("" : "+s"(x));
+#endif
+}
 __device__ __forceinline__ void pinned(float& x) {
 #if defined(__HIP_DEVICE_COMPILE__)
     asm volatile("" : "+v"(x));
@@ -164,15 +169,16 @@ __device__ __forceinline__ void pinned(float& x) {
 __device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned at, unsigned to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory", "m0");
 }
-__device__ __forceinline__ void load_dword_to_lds(const unsigned char* base, unsigned at, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory", "m0");
+// A dword of the lanes whose `at` is below `end`; all lanes of the wave have to be active.
+__device__ __forceinline__ void load_dword_to_lds(const unsigned char* base, unsigned at, unsigned from, unsigned end, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\tv_cmpx_gt_u32_e32 vcc, %3, %2\n\tglobal_load_lds_dword %1, %4\n\ts_mov_b64 exec, -1" ::"s"(to), "v"(from), "v"(at), "s"(end), "s"(base) : "memory", "m0", "vcc");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N < 63 ? N : 63) : "memory"); }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 #else
 inline __device__ void load_to_lds(const unsigned char*, unsigned, unsigned) {}
-inline __device__ void load_dword_to_lds(const unsigned char*, unsigned, unsigned) {}
+inline __device__ void load_dword_to_lds(const unsigned char*, unsigned, unsigned, unsigned, unsigned) {}
 template <int N>
 inline __device__ void wait_loads() {}
 inline __device__ void wait_lds() {}
@@ -218,7 +224,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     typedef typename Number<T>::x8 x8;
     typedef typename Output<T, TERMS>::type O;
     constexpr bool FEW = RW == 1, WIDE = Number<T>::kWide, DIRECT = LOAD != kThroughRegisters, OWN_KEYS = own_keys(RW, LOAD), TURNS = turns(DP, RW, LOAD);
-    constexpr int NW = waves_of(DP), KW = NW / RW, WK = wave_keys(DP, RW), KT = WK / 32, KEYS = step_keys(DP, RW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
+    constexpr int NW = waves_of(DP, RW), KW = NW / RW, WK = wave_keys(DP, RW), KT = WK / 32, KEYS = step_keys(DP, RW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
     constexpr float LIFT = 0.5f * Number<T>::kLift;            // (scores after the first step may be larger)
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
@@ -291,7 +297,8 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             const int in_stage = OWN_KEYS ? 0 : OWN * rw, own0 = WK * kw + in_stage;
             const unsigned char *const kb = (const unsigned char*)kh, *const vb = (const unsigned char*)vh;
             const unsigned k_page = 2u * (unsigned)p.k_page, v_page = 2u * (unsigned)p.v_page, k_token = 2u * (unsigned)p.k_token, v_token = 2u * (unsigned)p.v_token;
-            const int row_in = lane * UNIT / ROW, row_bytes = 2 * p.D;
+            const int row_in = lane * UNIT / ROW;
+            const unsigned row_bytes = 2u * (unsigned)p.D;
             // vectors: a lane's offsets, which repeat every 16 rows, and whether there is such a chunk
             unsigned k_from[PERIOD], v_from[PERIOD];
             bool has_k[PERIOD], has_v[PERIOD];
@@ -301,14 +308,14 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                     const int r = in_stage + RPI * x + row_in, ck = (lane % CH) ^ turn_k(r), cv = (lane % CH) ^ turn_v(r);
                     k_from[x] = (unsigned)row_in * k_token + 16u * (unsigned)ck;
                     v_from[x] = (unsigned)row_in * v_token + 16u * (unsigned)cv;
-                    has_k[x] = LOAD == kWholeVectors || 16 * ck < row_bytes;
-                    has_v[x] = LOAD == kWholeVectors || 16 * cv < row_bytes;
+                    has_k[x] = LOAD == kWholeVectors || 16u * (unsigned)ck < row_bytes;
+                    has_v[x] = LOAD == kWholeVectors || 16u * (unsigned)cv < row_bytes;
                 }
             }
             // dwords: a lane's place in its row
             const unsigned in_row = (unsigned)(lane * UNIT % ROW), k_in = (unsigned)row_in * k_token, v_in = (unsigned)row_in * v_token;
-            for (int s0 = first_key; s0 < end_key; s0 += kStretch) {
-                const int s1 = s0 + min(end_key - s0, kStretch), id0 = s0 >> page_log, ids = ((s1 - 1) >> page_log) - id0 + 1;
+            for (int s0 = first_key; s0 < end_key; s0 += stretch(RW)) {
+                const int s1 = s0 + min(end_key - s0, stretch(RW)), id0 = s0 >> page_log, ids = ((s1 - 1) >> page_log) - id0 + 1;
                 if (s0 > first_key) {
                     wait_loads<0>();
                     __syncthreads();           // (nobody reads the stretch before any more)
@@ -324,6 +331,10 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 unsigned bad = 0;              // a bit for every 8 keys of the wave in every stage, the newest lowest, that are in no page
                 // a stage's keys (Yes, No), values (No, Yes) or both
                 auto issue = [&](int kt, unsigned k_stage, unsigned v_stage, auto keys, auto values) {
+                    // (or multiples of these wait in registers, more than there are)
+                    unsigned k_step = k_token, v_step = v_token;
+                    stay_scalar(k_step);
+                    stay_scalar(v_step);
 #pragma unroll
                     for (int g = 0; g < OWN / 8; ++g) {
                         const int key = min(kt + own0 + 8 * g, last_group);
@@ -339,18 +350,18 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                             if constexpr (UNIT == 16) {
                                 const int x = r / RPI % PERIOD;
                                 if constexpr (keys.value)
-                                    if (has_k[x]) load_to_lds(k + (unsigned)(RPI * i) * k_token, k_from[x], to_k);
+                                    if (has_k[x]) load_to_lds(k + (unsigned)(RPI * i) * k_step, k_from[x], to_k);
                                 if constexpr (values.value)
-                                    if (has_v[x]) load_to_lds(v + (unsigned)(RPI * i) * v_token, v_from[x], to_v);
+                                    if (has_v[x]) load_to_lds(v + (unsigned)(RPI * i) * v_step, v_from[x], to_v);
                             } else {
                                 const unsigned fk = 16u * (unsigned)turn_k(in_stage + r), fv = 16u * (unsigned)turn_v(in_stage + r);
 #pragma unroll
                                 for (int part = 0; part < SPLIT; ++part) {
                                     const unsigned ck = (in_row + (unsigned)(part * BYTES)) ^ fk, cv = (in_row + (unsigned)(part * BYTES)) ^ fv;
                                     if constexpr (keys.value)
-                                        if ((int)ck < row_bytes) load_dword_to_lds(k + (unsigned)(RPI * i) * k_token, RPI > 1 ? k_in + ck : ck, to_k + part * BYTES);
+                                        load_dword_to_lds(k + (unsigned)(RPI * i) * k_step, ck, RPI > 1 ? k_in + ck : ck, row_bytes, to_k + part * BYTES);
                                     if constexpr (values.value)
-                                        if ((int)cv < row_bytes) load_dword_to_lds(v + (unsigned)(RPI * i) * v_token, RPI > 1 ? v_in + cv : cv, to_v + part * BYTES);
+                                        load_dword_to_lds(v + (unsigned)(RPI * i) * v_step, cv, RPI > 1 ? v_in + cv : cv, row_bytes, to_v + part * BYTES);
                                 }
                             }
                         }
@@ -793,7 +804,7 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int i, unsigned c
     if (t.row_end > p.few_rows) {
         // worked on as many rows; where nobody does, more queries than the caller said that there are: NaN
         if (p.many_per_xcd == 0 && t.split == 0)
-            for (int64_t x = threadIdx.x; x < (int64_t)t.row_end * (p.D / 4); x += 64 * waves_of(DP)) {
+            for (int64_t x = threadIdx.x; x < (int64_t)t.row_end * (p.D / 4); x += 64 * waves_of(DP, 1)) {
                 const int row = (int)(x / (p.D / 4)), j = row / p.G, d = 4 * (int)(x % (p.D / 4));
                 const float nan = __builtin_nanf("");
                 store_four<typename Output<T, TERMS>::type>(p.out, (t.seq.start + j) * p.out_token + (int64_t)(t.h * p.G + row - j * p.G) * p.out_head + d, f32x4{nan, nan, nan, nan});
@@ -864,15 +875,17 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int i, unsigned 
 }
 
 // Workgroups go to the 8 XCDs in turn, and tiles of one key head, which read the same keys, to one XCD (one L2) as far as that goes.  An XCD begins with its tiles that
-// see much (every other one) and ends with those that see little; the few rows are behind them.
+// see much (every other one) and ends with those that see little.
 template <class T, int DP, int RW, int TERMS, int LOAD>
-__global__ void __launch_bounds__(64 * waves_of(DP), DP > 128 ? 1 : 2) chunk_kernel(const ChunkParams p) {
+__global__ void __launch_bounds__(64 * waves_of(DP, RW), DP > 128 ? 1 : 2) many_rows_kernel(const ChunkParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
-    const int xcd = (int)blockIdx.x & 7, place = (int)blockIdx.x >> 3, n = p.many_per_xcd;
-    if (place < n) {
-        const int heavy = (n + 1) / 2;
-        many_rows<T, DP, RW, TERMS, LOAD>(p, xcd * n + (place < heavy ? 2 * place : 2 * (n - 1 - place) + 1), lds);
-    } else few_rows<T, DP, TERMS, LOAD>(p, xcd * p.few_per_xcd + place - n, lds);
+    const int xcd = (int)blockIdx.x & 7, place = (int)blockIdx.x >> 3, n = p.many_per_xcd, heavy = (n + 1) / 2;
+    many_rows<T, DP, RW, TERMS, LOAD>(p, xcd * n + (place < heavy ? 2 * place : 2 * (n - 1 - place) + 1), lds);
+}
+template <class T, int DP, int TERMS, int LOAD>
+__global__ void __launch_bounds__(64 * waves_of(DP, 1), DP > 128 ? 1 : 2) few_rows_kernel(const ChunkParams p) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    few_rows<T, DP, TERMS, LOAD>(p, ((int)blockIdx.x & 7) * p.few_per_xcd + ((int)blockIdx.x >> 3), lds);
 }
 
 // The parts of every row joined, where there are several: DP / 4 threads have four features each.

@@ -4,30 +4,42 @@
 
 namespace {
 
-template <class T, int DP, int RW, int TERMS, int LOAD>
-int launch_chunk(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
+template <class T, int DP, int TERMS, int LOAD>
+int launch_few(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
     static std::atomic<unsigned> done{0};
-    constexpr int lds = most_of(lds_bytes(DP, RW, LOAD), lds_bytes(DP, 1, LOAD));
-    static_assert(lds <= 160 * 1024, "what a unit has");
-    auto kfn = chunk_kernel<T, DP, RW, TERMS, LOAD>;
+    constexpr int lds = lds_bytes(DP, 1, LOAD);
+    static_assert(lds <= 80 * 1024, "two workgroups a unit");
+    auto kfn = few_rows_kernel<T, DP, TERMS, LOAD>;
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
-    int rc = launch(kfn, dim3(8u * (unsigned)(a.many_per_xcd + a.few_per_xcd)), 64 * waves_of(DP), lds, stream, p);
+    return launch(kfn, dim3(8u * (unsigned)a.few_per_xcd), 64 * waves_of(DP, 1), lds, stream, p);
+}
+template <class T, int DP, int RW, int TERMS, int LOAD>
+int launch_many(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
+    static std::atomic<unsigned> done{0};
+    constexpr int lds = lds_bytes(DP, RW, LOAD);
+    static_assert(lds <= 160 * 1024, "what a unit has");
+    auto kfn = many_rows_kernel<T, DP, RW, TERMS, LOAD>;
+    if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
+    return launch(kfn, dim3(8u * (unsigned)a.many_per_xcd), 64 * waves_of(DP, RW), lds, stream, p);
+}
+template <class T, int DP, int TERMS, int LOAD>
+int launch_parts(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
+    int rc = VLUT_OK;
+    if (a.many) {
+        if constexpr (DP <= 128 && LOAD != kThroughRegisters) rc = a.row_waves == 8 ? launch_many<T, DP, 8, TERMS, LOAD>(a, p, stream) : launch_many<T, DP, 4, TERMS, LOAD>(a, p, stream);
+        else rc = launch_many<T, DP, 4, TERMS, LOAD>(a, p, stream);
+    }
+    if (rc == VLUT_OK && a.few) rc = launch_few<T, DP, TERMS, LOAD>(a, p, stream);
     if (rc != VLUT_OK || a.bytes() == 0) return rc;
     constexpr int rows = 256 / (DP / 4);
     return launch(combine_chunks<typename Output<T, TERMS>::type, DP>, dim3((unsigned)(((int64_t)p.N * p.Hk * p.G + rows - 1) / rows)), 256, 0, stream, p);
 }
-template <class T, int DP, int TERMS, int LOAD>
-int launch_waves(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
-    if constexpr (DP <= 128)
-        if (a.row_waves == 8) return launch_chunk<T, DP, 8, TERMS, LOAD>(a, p, stream);
-    return launch_chunk<T, DP, 4, TERMS, LOAD>(a, p, stream);
-}
 template <class T, int DP, int TERMS>
 int launch_loads(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
-    if (a.load == kWholeVectors) return launch_waves<T, DP, TERMS, kWholeVectors>(a, p, stream);
-    if (a.load == kVectors) return launch_waves<T, DP, TERMS, kVectors>(a, p, stream);
-    if (a.load == kDwords) return launch_waves<T, DP, TERMS, kDwords>(a, p, stream);
-    return launch_chunk<T, DP, 4, TERMS, kThroughRegisters>(a, p, stream);
+    if (a.load == kWholeVectors) return launch_parts<T, DP, TERMS, kWholeVectors>(a, p, stream);
+    if (a.load == kVectors) return launch_parts<T, DP, TERMS, kVectors>(a, p, stream);
+    if (a.load == kDwords) return launch_parts<T, DP, TERMS, kDwords>(a, p, stream);
+    return launch_parts<T, DP, TERMS, kThroughRegisters>(a, p, stream);
 }
 template <class T, int TERMS>
 int launch_chunks(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {

@@ -35,37 +35,37 @@ constexpr int kFewRows = 32;
 // How keys and values come to LDS: through registers; straight, a dword or 16 bytes a lane; of rows that are as long as LDS has them.
 constexpr int kThroughRegisters = 0, kDwords = 1, kVectors = 2, kWholeVectors = 3;
 
-// A workgroup's waves: RW groups of 32 rows, the keys of a step shared by KW.  Where rows are few 1 x all; where they are many all x 1, or half x 2.
-__host__ __device__ constexpr int waves_of(int DP) { return DP > 128 ? 4 : 8; }
+// A workgroup's waves: RW groups of 32 rows, the keys of a step shared by KW.  Where rows are few 1 x 4 (features past 128: 2), two workgroups of which a unit has
+// room for; where they are many 8 x 1 or 4 x 2 (4 x 1).
+__host__ __device__ constexpr int waves_of(int DP, int RW) { return RW == 1 ? (DP > 128 ? 2 : 4) : (DP > 128 ? 4 : 8); }
 __host__ __device__ constexpr bool own_keys(int RW, int LOAD) { return RW == 1 && LOAD != kThroughRegisters; }      // waves have their keys for themselves
 __host__ __device__ constexpr bool turns(int DP, int RW, int LOAD) { return RW == 8 && LOAD != kThroughRegisters; }  // a SIMD's two waves take the products in turns
 __host__ __device__ constexpr int wave_keys(int DP, int RW) { return RW == 1 || DP > 128 ? 32 : 64; }
-__host__ __device__ constexpr int step_keys(int DP, int RW) { return wave_keys(DP, RW) * (waves_of(DP) / RW); }
+__host__ __device__ constexpr int step_keys(int DP, int RW) { return wave_keys(DP, RW) * (waves_of(DP, RW) / RW); }
 __host__ __device__ constexpr int k_pitch(int DP, int LOAD) { return DP * 2 + (LOAD == kThroughRegisters ? 16 : 0); }
 __host__ __device__ constexpr int v_pitch(int DP, int LOAD) { return DP * 2 + (LOAD == kThroughRegisters ? 64 : 0); }
 // Through registers: a stage is a step's keys and values.  Straight: the KW groups of waves have rings of stages of their keys and of their values each, AHEAD of which
 // are on their way; where waves take turns the later ones read values of the step before.
 __host__ __device__ constexpr int stage_bytes(int DP, int RW, int LOAD) { return step_keys(DP, RW) * (k_pitch(DP, LOAD) + v_pitch(DP, LOAD)); }
 __host__ __device__ constexpr int stages(int RW) { return RW == 1 ? 1 : 2; }
-__host__ __device__ constexpr int ahead(int DP, int RW) { return RW == waves_of(DP) ? 2 : 1; }
+__host__ __device__ constexpr int ahead(int DP, int RW) { return RW == waves_of(DP, RW) ? 2 : 1; }
 __host__ __device__ constexpr int key_ring(int DP, int RW) { return RW == 1 ? 1 : ahead(DP, RW) + 1; }
 __host__ __device__ constexpr int value_ring(int DP, int RW, bool later) { return RW == 1 ? 1 : ahead(DP, RW) + 1 + (later ? 1 : 0); }
 __host__ __device__ constexpr int ring_bytes(int DP, int RW, bool later) { return (key_ring(DP, RW) + value_ring(DP, RW, later)) * wave_keys(DP, RW) * DP * 2; }
 __host__ __device__ constexpr int buffers_bytes(int DP, int RW, int LOAD) {
     if (LOAD == kThroughRegisters) return stages(RW) * stage_bytes(DP, RW, LOAD);
-    if (RW == 1) return waves_of(DP) * ring_bytes(DP, RW, false);
-    if (RW == waves_of(DP)) return ring_bytes(DP, RW, turns(DP, RW, LOAD));
+    if (RW == 1) return waves_of(DP, RW) * ring_bytes(DP, RW, false);
+    if (RW == waves_of(DP, RW)) return ring_bytes(DP, RW, turns(DP, RW, LOAD));
     return 2 * ring_bytes(DP, RW, false);
 }
 __host__ __device__ constexpr int turn_features(int DP) { return DP > 64 ? 64 : 32; }       // that leave through LDS together
 __host__ __device__ constexpr int most_of(int a, int b) { return a > b ? a : b; }
 // Keys and values, or what results leave through: for each wave 32 rows, of the features that leave together, or of half of them all.
-__host__ __device__ constexpr int leave_pitch(int DP, int RW) { return (RW == waves_of(DP) ? turn_features(DP) : DP / 2) + 4; }
-__host__ __device__ constexpr int tile_bytes(int DP, int RW, int LOAD) { return most_of(buffers_bytes(DP, RW, LOAD), waves_of(DP) * 32 * leave_pitch(DP, RW) * 4); }
-constexpr int kStretch = 16384;        // keys whose pages' numbers are in LDS (8 keys a page at least)
-constexpr int kStretchPages = kStretch / 8 + 2;
+__host__ __device__ constexpr int leave_pitch(int DP, int RW) { return (RW == waves_of(DP, RW) ? turn_features(DP) : DP / 2) + 4; }
+__host__ __device__ constexpr int tile_bytes(int DP, int RW, int LOAD) { return most_of(buffers_bytes(DP, RW, LOAD), waves_of(DP, RW) * 32 * leave_pitch(DP, RW) * 4); }
+__host__ __device__ constexpr int stretch(int RW) { return RW == 1 ? 4096 : 16384; }        // keys whose pages' numbers are in LDS (8 keys a page at least)
 __host__ __device__ constexpr int lds_bytes(int DP, int RW, int LOAD) {
-    return tile_bytes(DP, RW, LOAD) + waves_of(DP) * 32 * 20 + 16 + (LOAD == kThroughRegisters ? 0 : kStretchPages * 4);
+    return tile_bytes(DP, RW, LOAD) + waves_of(DP, RW) * 32 * 20 + 16 + (LOAD == kThroughRegisters ? 0 : (stretch(RW) / 8 + 2) * 4);
 }
 
 struct ChunkPlan {
