@@ -8,6 +8,7 @@
 
 #include "vlut.h"
 
+#include "common.hip.h"
 #include "host_checks.h"
 #include "launch.hip.h"
 #include "rows_kernel.hip.h"
@@ -105,7 +106,7 @@ int plan_logits(int64_t N, int64_t V, int top, LogitsPlan* out) {
     // Parts so that there are four workgroups for each unit, of 2048 logits at least.
     const int64_t wanted = std::min<int64_t>({kMostParts, (4 * kUnits + N - 1) / N, (V + 2047) / 2048});
     const int64_t part = (V + wanted - 1) / wanted;
-    a.per = part <= 4096 ? 8 : 32;
+    a.per = part <= 4096 ? 8 : 16;
     const int64_t chunk = kLogitThreads * a.per;
     a.part = (int)((part + chunk - 1) / chunk * chunk);
     a.parts = (int)((V + a.part - 1) / a.part);
@@ -118,7 +119,7 @@ int plan_logits(int64_t N, int64_t V, int top, LogitsPlan* out) {
 }
 template <class T, int VEC>
 int launch_logits_v(const LogitsParams& p, int per, unsigned blocks, hipStream_t stream) {
-    return per == 8 ? launch(logits_kernel<T, VEC, 8>, dim3(blocks), kLogitThreads, 0, stream, p) : launch(logits_kernel<T, VEC, 32>, dim3(blocks), kLogitThreads, 0, stream, p);
+    return per == 8 ? launch(logits_kernel<T, VEC, 8>, dim3(blocks), kLogitThreads, 0, stream, p) : launch(logits_kernel<T, VEC, 16>, dim3(blocks), kLogitThreads, 0, stream, p);
 }
 template <class T>
 int launch_logits(LogitsParams& p, const LogitsPlan& a, int vec, int64_t N, hipStream_t stream) {

@@ -16,9 +16,9 @@ namespace {
 // A thread keeps its own m, l and d over its logits; they meet at the end of the part, and those of a row's parts in join_kernel:
 //   m = max m_i,  l = sum exp(m_i - m) l_i,  d = sum exp(m_i - m) (d_i + (m - m_i) l_i).
 // The largest: a key of 64 bits, the logit's bits in the order of its value ahead of ~index, orders tokens as they are to come out, ties by the lowest
-// index, and no two are alike.  Of a chunk of 256 threads' logits: the k-th largest of the threads' own largest ones is a bound that k of the chunk's logits
-// reach, and few more do; later chunks have the k-th largest so far.  What passes the bound goes to a list in LDS, in any order, and every key's rank is
-// the number of larger ones.
+// index, and no two are alike.  Of a chunk of 256 threads' logits: the k-th largest of a wave's threads' own largest ones is a bound that k of the chunk's logits
+// reach, and few more do (found bit by bit, by how many lanes reach it; its upper half will do); later chunks have the k-th largest so far, which only larger ones
+// pass.  What passes goes to a list in LDS, in any order, and every key's rank is the number of larger ones.
 // ---------------------------------------------------------------------------------------------
 constexpr int kTopKeys = 1024;                 // of the list in LDS
 constexpr int kLogitThreads = 256;
@@ -41,6 +41,15 @@ __device__ __forceinline__ unsigned ordered_bits(float x) {
 }
 __device__ __forceinline__ float from_ordered(unsigned u) { return __builtin_bit_cast(float, u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 __device__ __forceinline__ uint64_t key_of(float x, int index) { return (uint64_t)ordered_bits(x) << 32 | (unsigned)~index; }
+
+// The larger one, NaN where x is.
+__device__ __forceinline__ float at_least(float x, float least) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_elementwise_maximum(x, least);
+#else
+    return x;
+#endif
+}
 
 // m, l, d of logits that are added one after the other.
 struct LogSum {                                // (m: a logit; d in powers of two)
@@ -68,8 +77,9 @@ struct TopList {                               // of a workgroup, in LDS
     uint64_t keys[kTopKeys];
     uint64_t best[64];                         // the largest so far, in order
     uint64_t maxima[kLogitThreads];
-    int count;
     uint64_t found;
+    int count;
+    unsigned bounds[kLogitThreads / 64];
 };
 
 // keys[0 .. count) of the list, ranked: the `top` largest go to best[], behind them the rest is 0 (no key).  All threads call it, behind a barrier; it ends with one.
@@ -137,33 +147,39 @@ __device__ __forceinline__ int extract_keys(TopList& s, Key key, int had, int to
     return n;
 }
 
-// A chunk's keys into best[], which has `had` keys (0 where empty).  key(e): the thread's e-th key, 0 for none.  Returns the new count.
-template <int E, class Key>
-__device__ __forceinline__ int take_keys(TopList& s, Key key, int had, int top) {
+// A bound that at least `top` of the wave's lanes' numbers reach, by their upper 16 bits; 0 where there are not as many that are not 0.
+__device__ __forceinline__ unsigned bound_of_wave(unsigned mine, int top) {
+    unsigned bound = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+        const unsigned tried = bound | 1u << bit;
+        if (__popcll(__ballot(mine >= tried)) >= top) bound = tried;
+    }
+    return bound;
+}
+
+// A chunk's keys into best[], which has `had` keys (0 where empty).  value(e): the bits of the thread's e-th one in order, 0 for none; key(e): its key; most: the largest
+// value.  Returns the new count.
+template <int E, class Value, class Key>
+__device__ __forceinline__ int take_keys(TopList& s, unsigned most, Value value, Key key, int had, int top) {
     const int tid = (int)threadIdx.x;
-    uint64_t bound;                            // keys from here on are wanted
+    unsigned bound = 1;                        // values from here on are wanted
     if (had < top) {
-        uint64_t most = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) most = max(most, key(e));
-        s.maxima[tid] = most;
-        if (tid == 0) s.found = 0;
+        const unsigned of_wave = bound_of_wave(most, top);
+        if ((tid & 63) == 0) s.bounds[tid >> 6] = of_wave;
         __syncthreads();
-        int rank = 0;
-        for (int j = 0; j < kLogitThreads; ++j) rank += s.maxima[j] > most;
-        // (maxima of 0 are alike: none of them has a rank below top where top other ones are there)
-        if (rank == top - 1 && most != 0) s.found = most;
-        __syncthreads();
-        bound = max(s.found, (uint64_t)1);
-    } else bound = s.best[top - 1] + 1;
-    unsigned wanted = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) wanted |= key(e) >= bound ? 1u << e : 0u;
-    if (!__syncthreads_or(wanted != 0)) return had;
+        for (int w = 0; w < kLogitThreads / 64; ++w) bound = max(bound, s.bounds[w]);
+    } else bound = (unsigned)(s.best[top - 1] >> 32) + 1;      // (equal ones behind it come later)
+    const bool any = most >= bound;
+    if (!__syncthreads_or(any)) return had;
     if (tid == 0) s.count = had;
     if (tid < had) s.keys[tid] = s.best[tid];
     __syncthreads();
-    if (wanted) {
+    if (any) {
+        unsigned wanted = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) wanted |= value(e) >= bound ? 1u << e : 0u;
         int at = atomicAdd(&s.count, __popc(wanted));
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -179,35 +195,45 @@ __device__ __forceinline__ int take_keys(TopList& s, Key key, int had, int top) 
     return min(count, top);
 }
 
-// The sums of all threads, in every thread (an order that does not change).
-__device__ __forceinline__ LogSum workgroup_log_sum(LogSum s, float (&of)[kLogitThreads / 64][3], float c) {
+// The sum over the 64 lanes of a wave, in every lane and in an order that does not change.
+__device__ __forceinline__ float wave_sum_f32(float v) {
+    auto add = [&](int other) { v += __builtin_bit_cast(float, other); };
+    add(lane_xor16<1>(__builtin_bit_cast(int, v)));
+    add(lane_xor16<2>(__builtin_bit_cast(int, v)));
+    add(lane_xor7(__builtin_bit_cast(int, v)));                        // (quads are uniform by now)
+    add(lane_xor16<8>(__builtin_bit_cast(int, v)));
+    float r[4];
 #pragma unroll
-    for (int m = 32; m; m >>= 1) {
-        const float om = __shfl_xor(s.m, m), ol = __shfl_xor(s.l, m), od = __shfl_xor(s.d, m);
-        // (either lane of a pair has to get the same bits)
-        LogSum a = s, b;
-        b.m = om, b.l = ol, b.d = od;
-        if ((int)threadIdx.x & m) {
-            const LogSum t = a;
-            a = b;
-            b = t;
-        }
-        a.join(b.m, b.l, b.d, c);
-        s = a;
-    }
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 16 * i));
+    return (r[0] + r[1]) + (r[2] + r[3]);
+}
+// The sums of all threads, in every thread.
+__device__ __forceinline__ LogSum workgroup_log_sum(LogSum s, float (&of)[kLogitThreads / 64][3], float c) {
+    s.raise(wave_max_f32(s.m), c);             // (no m is NaN)
+    s.l = wave_sum_f32(s.l);
+    s.d = wave_sum_f32(s.d);
     if (((int)threadIdx.x & 63) == 0) {
         float* const at = of[threadIdx.x >> 6];
         at[0] = s.m, at[1] = s.l, at[2] = s.d;
     }
     __syncthreads();
     s.m = of[0][0], s.l = of[0][1], s.d = of[0][2];
+#pragma unroll
     for (int w = 1; w < kLogitThreads / 64; ++w) s.join(of[w][0], of[w][1], of[w][2], c);
     return s;
 }
 
+// The logit of the token that is asked for, or NaN.  Asked for first of all: two trips to memory, one behind the other.
+template <class T>
+__device__ __forceinline__ float asked(const LogitsParams& p, int64_t row) {
+    if (!p.logprob || threadIdx.x != 0) return 0.0f;
+    const int64_t token = p.tokens[row];
+    return token >= 0 && token < p.V ? (float)((const T*)p.logits)[row * p.row_stride + token] : __builtin_nanf("");
+}
+
 // What a row comes out as, from its sums and its largest keys (count of them; the row's other logits are -inf or no numbers).
 template <class T>
-__device__ __forceinline__ void store_row(const LogitsParams& p, int64_t row, const LogSum& sum, const TopList& s, int count) {
+__device__ __forceinline__ void store_row(const LogitsParams& p, int64_t row, const LogSum& sum, float its, const TopList& s, int count) {
     const int tid = (int)threadIdx.x;
     const T* const x = (const T*)p.logits + row * p.row_stride;
     const float nan = __builtin_nanf(""), ln2 = 0.69314718055994531f;
@@ -215,10 +241,7 @@ __device__ __forceinline__ void store_row(const LogitsParams& p, int64_t row, co
     const float log_l = logf(sum.l);
     auto logprob = [&](float of) { return none ? (of != of ? nan : -__builtin_inff()) : (of - sum.m) * p.inverse_temperature - log_l; };
     if (tid == 0) {
-        if (p.logprob) {
-            const int64_t token = p.tokens[row];
-            p.logprob[row] = token >= 0 && token < p.V ? logprob((float)x[token]) : nan;
-        }
+        if (p.logprob) p.logprob[row] = its != its ? nan : logprob(its);
         if (p.entropy) p.entropy[row] = none ? 0.0f : log_l + sum.d / sum.l * ln2;
     }
     if (tid >= 64 || p.top == 0) return;
@@ -254,38 +277,47 @@ __global__ void __launch_bounds__(kLogitThreads) logits_kernel(const LogitsParam
     const T* const x = (const T*)p.logits + row * p.row_stride;
     LogSum sum;
     int count = 0;
-    for (int at = first; at < end; at += CHUNK) {
-        RawVec<T, VEC> raw[E / VEC];
-        auto index = [&](int e) { return at + ((e / VEC) * kLogitThreads + tid) * VEC + e % VEC; };
+    const float its = p.parts == 1 ? asked<T>(p, row) : 0.0f;
+    auto index = [&](int at, int e) { return at + ((e / VEC) * kLogitThreads + tid) * VEC + e % VEC; };
+    RawVec<T, VEC> raw[E / VEC];
+    auto load = [&](int at) {                  // (VEC divides V; past the part others' logits, or the last ones)
 #pragma unroll
-        for (int i = 0; i < E / VEC; ++i) raw[i].load(x, min(index(i * VEC), p.V - VEC));        // (VEC divides V)
+        for (int i = 0; i < E / VEC; ++i) raw[i].load(x, min(index(at, i * VEC), p.V - VEC));
+    };
+    load(first);
+    for (int at = first; at < end; at += CHUNK) {
         float v[E];
         float top = -__builtin_inff();
 #pragma unroll
         for (int i = 0; i < E / VEC; ++i) {
             float f[VEC];
             raw[i].floats(f);
-            const bool in = index(i * VEC) < end;
+            const bool in = index(at, i * VEC) < end;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 v[i * VEC + e] = in ? f[e] : -__builtin_inff();
                 top = fmaxf(top, v[i * VEC + e]);
             }
         }
+        if (at + CHUNK < end) load(at + CHUNK);                        // (on their way meanwhile)
         sum.raise(fmaxf(sum.m, top), p.c);
-        const float m = sum.m == -__builtin_inff() ? 0.0f : sum.m;     // (-inf where all are, or are no numbers, which make l none)
+        const float m = sum.m == -__builtin_inff() ? 0.0f : sum.m;     // (-inf where all are, or are no numbers)
+        float l[2] = {}, d[2] = {};
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float u = (v[e] - m) * p.c, w = __builtin_amdgcn_exp2f(u);
-            sum.l += w;
-            sum.d = __builtin_fmaf(w, w > 0.0f ? -u : 0.0f, sum.d);
+            const float u = at_least((v[e] - m) * p.c, -200.0f), w = __builtin_amdgcn_exp2f(u);        // (2^-200 is 0 in 32 bits, and so is 0 times 200)
+            l[e & 1] += w;
+            d[e & 1] = __builtin_fmaf(w, u, d[e & 1]);
         }
+        sum.l += l[0] + l[1];
+        sum.d -= d[0] + d[1];
         if (p.top > 0)
-            count = take_keys<E>(s, [&](int e) { return v[e] > -__builtin_inff() ? key_of(v[e], index(e)) : 0; }, count, p.top);
+            count = take_keys<E>(s, top > -__builtin_inff() ? ordered_bits(top) : 0u, [&](int e) { return v[e] > -__builtin_inff() ? ordered_bits(v[e]) : 0u; },
+                                 [&](int e) { return v[e] > -__builtin_inff() ? key_of(v[e], index(at, e)) : 0; }, count, p.top);
     }
     sum = workgroup_log_sum(sum, sums, p.c);
     if (p.parts == 1) {
-        store_row<T>(p, row, sum, s, count);
+        store_row<T>(p, row, sum, its, s, count);
         return;
     }
     const int64_t at = in_call * p.parts + part;
@@ -301,6 +333,14 @@ __global__ void __launch_bounds__(kLogitThreads) logits_join_kernel(const Logits
     __shared__ float sums[kLogitThreads / 64][3];
     const int tid = (int)threadIdx.x;
     const int64_t in_call = blockIdx.x, row = p.first_row + in_call;
+    const float its = asked<T>(p, row);
+    const int all = p.parts * p.top;
+    uint64_t keys[kJoinKeys];
+#pragma unroll
+    for (int e = 0; e < kJoinKeys; ++e) {
+        const int at = tid + e * kLogitThreads;
+        keys[e] = at < all ? p.part_keys[in_call * all + at] : 0;
+    }
     LogSum sum;
     if (tid < p.parts) {
         const float4 part = *(const float4*)(p.part_sums + (in_call * p.parts + tid) * 4);
@@ -309,16 +349,12 @@ __global__ void __launch_bounds__(kLogitThreads) logits_join_kernel(const Logits
     sum = workgroup_log_sum(sum, sums, p.c);
     int count = 0;
     if (p.top > 0) {
-        const int all = p.parts * p.top;
-        uint64_t keys[kJoinKeys];
+        unsigned most = 0;
 #pragma unroll
-        for (int e = 0; e < kJoinKeys; ++e) {
-            const int at = tid + e * kLogitThreads;
-            keys[e] = at < all ? p.part_keys[in_call * all + at] : 0;
-        }
-        count = take_keys<kJoinKeys>(s, [&](int e) { return keys[e]; }, 0, p.top);
+        for (int e = 0; e < kJoinKeys; ++e) most = max(most, (unsigned)(keys[e] >> 32));
+        count = take_keys<kJoinKeys>(s, most, [&](int e) { return (unsigned)(keys[e] >> 32); }, [&](int e) { return keys[e]; }, 0, p.top);
     }
-    store_row<T>(p, row, sum, s, count);
+    store_row<T>(p, row, sum, its, s, count);
 }
 
 }  // namespace
