@@ -264,6 +264,15 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     const int all_from = max(0, high - p.window + 1), all_to = min(end_key, low + 1);
     const int tile_from = max(0, position(t.row_end - 1) - p.window + 1), tile_to = min(end_key, position(t.row0) + 1);
 
+    // Where the row's result and its sums go, worked out while the first keys are on their way; the waves that share a row have it both.
+    int64_t row_sums;
+    {
+        const int its = query_of(p, t, row - t.row0), head = t.h * p.G + row - its * p.G;
+        const int64_t part = part_at<FEW>(p, t.seq, t.b, t.h, row, its, head, t.split);
+        row_sums = t.direct ? (int64_t)(t.seq.start + its) * (p.Hk * p.G) + head : part;
+        if (half == 0) row_to[FEW ? l32 : 32 * wave + l32] = t.direct ? (t.seq.start + its) * p.out_token + head * p.out_head : part * p.D;
+    }
+
     const int32_t* const pages = p.page_table + t.b * p.table_stride;
     const T* const kh = (const T*)p.k + t.h * p.k_head;
     const T* const vh = (const T*)p.v + t.h * p.v_head;
@@ -653,15 +662,12 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     // The results leave through LDS (nobody reads the buffers any more), so that a store has whole lines.
     const ChunkParams& z = parameters();
     float* const parts = FEW ? z.few_o : z.many_o;
-    // Row r of the tile: where its result goes (to `slot`) and what it is multiplied with, 1 / l, or 1 where it is a part; its sums, by one of those who place it.
+    // Row r of the tile: what its result is multiplied with (to `slot`), 1 / l, or 1 where it is a part; its sums, by one of those who place it.
     auto place = [&](int r, int slot, float top, float total, bool sums) {
-        const int at_row = t.row0 + r, its = query_of(z, t, r), head = t.h * z.G + at_row - its * z.G;
-        const int64_t part = part_at<FEW>(z, t.seq, t.b, t.h, at_row, its, head, t.split);
-        row_to[slot] = t.direct ? (t.seq.start + its) * z.out_token + head * z.out_head : part * z.D;
         row_factor[slot] = total != total ? total : (total == 0.0f ? 0.0f : (t.direct ? 1.0f / total : 1.0f));
-        if (!sums || at_row >= t.row_end) return;
-        if (!t.direct) *(f32x2*)((FEW ? z.few_ml : z.many_ml) + part * 2) = f32x2{top, total};
-        else if (z.lse) z.lse[(int64_t)(t.seq.start + its) * (z.Hk * z.G) + head] = lse_of(top, total);
+        if (!sums || t.row0 + r >= t.row_end) return;
+        if (!t.direct) *(f32x2*)((FEW ? z.few_ml : z.many_ml) + row_sums * 2) = f32x2{top, total};
+        else if (z.lse) z.lse[row_sums] = lse_of(top, total);
     };
     // COUNT rows at once: r0, r0 + step, ..., each the lane's four features from d on, read at from + i * pitch
     float odd = 0.0f;                          // (NaN where there is something to settle)
