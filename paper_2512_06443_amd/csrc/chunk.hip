@@ -25,8 +25,7 @@ int log2_of(int64_t v) {
     return k;
 }
 
-// registers: keys go through registers to LDS (which changes nothing of the workspace: where the largest tiles are, every tile is one part).
-int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, bool registers, ChunkPlan* out) {
+int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, ChunkPlan* out) {
     if (N < 1 || N >= ((int64_t)1 << 24) || B < 1 || B >= ((int64_t)1 << 24) || Hk < 1 || Hq < 1 || Hq >= (1 << 16) || Hq % Hk) return VLUT_ERR_SHAPE;
     if (max_len < 0 || max_len >= kMost || max_queries < 0 || window < 0 || window >= kMost || D < 1 || N * Hq >= kMost) return VLUT_ERR_SHAPE;
     if (D < 8 || D > VLUT_MAX_HEAD_FEATURES || D % 4) return VLUT_ERR_UNSUPPORTED;
@@ -42,7 +41,7 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
         a.few_row_places = (int)std::min<int64_t>(kFewRows, std::max<int64_t>(1, most_rows / G) * G);
         // Keys that one tile sees, in steps.  Parts so that the workgroups are four rounds of those that run at once, of four steps at least; where that many are not
         // there, of one.
-        const int64_t step = step_keys(a.DP, 1), keys = seen(kFewRows), steps = ceil_div(keys, step), slots = 2 * kUnits;
+        const int64_t step = step_keys(a.DP, 1, few_waves(a.DP)), keys = seen(kFewRows), steps = ceil_div(keys, step), slots = 2 * kUnits;
         int64_t per = std::max<int64_t>(4, ceil_div(B * Hk * steps, 4 * slots));
         while (per > 1 && B * Hk * ceil_div(steps, per) < slots) per /= 2;
         a.few_chunk = (int)(step * per);
@@ -57,12 +56,17 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
         }
     }
     if (a.many) {
-        const int64_t rows = N * G;
-        a.row_waves = !registers && a.DP <= 128 && rows * Hk >= 4 * 256 * kUnits ? 8 : 4;
-        a.many_rows = 32 * a.row_waves;
-        a.many_tiles = (int)std::min(rows / a.many_rows + B, (rows + B * (a.many_rows - 1)) / a.many_rows);
-        const int64_t keys = seen(a.many_rows / G + 1), step = step_keys(a.DP, a.row_waves), tiles = a.many_tiles * Hk;
-        const int64_t splits = std::min(std::max<int64_t>(1, kUnits / tiles), ceil_div(keys, 512));
+        const int64_t rows = N * G, keys = seen(kManyRows / G + 1);
+        a.many_tiles = (int)std::min(rows / kManyRows + B, (rows + B * (kManyRows - 1)) / kManyRows);
+        const int64_t tiles = a.many_tiles * Hk;
+        // Two workgroups of four waves on a unit, one's waits beside the other's work, where there are tiles for that; else one whose eight waves share the keys, unless
+        // those are so many that parts of them are as good.  us, 4 x 1 / 4 x 2, parts joined included, 32 query and 8 key heads of 128 in bf16 (20 and 5 where it says
+        // so): 4096 tokens (20, 5) 125 / 131, in windows of 16 24 / 37, of 1024 77 / 89; 16384 tokens 2192 / 2446; 4096 of 64 features 91 / 123; 1024 tokens 40 / 27, behind
+        // 4096 108 / 97, 8192 177 / 168, 16384 320 / 350; 256 behind 1024 29 / 28, 4096 40 / 40, 16384 89 / 89; 32 heads of 100 that are not shared, 909 tokens in windows
+        // of 1024, 67 / 46.
+        a.key_waves = a.DP <= 128 && tiles < 2 * kUnits && keys < 12288 ? 2 : 1;
+        const int64_t slots = (a.DP <= 128 && a.key_waves == 1 ? 2 : 1) * kUnits, step = step_keys(a.DP, 4, a.key_waves);
+        const int64_t splits = std::min(std::max<int64_t>(1, slots / tiles), ceil_div(keys, 512));
         a.many_chunk = (int)(ceil_div(ceil_div(keys, splits), step) * step);
         a.many_splits = (int)ceil_div(keys, a.many_chunk);
         const int64_t blocks = ceil_div(tiles * a.many_splits, 8);
@@ -93,18 +97,18 @@ extern "C" {
 
 size_t vlut_chunk_attention_bytes(int64_t N, int64_t B, int64_t q_heads, int64_t k_heads, int64_t D, int64_t max_queries, int64_t max_len, int64_t window) {
     ChunkPlan a;
-    return plan_chunks(N, B, q_heads, k_heads, D, max_queries, max_len, window, false, &a) == VLUT_OK ? a.bytes() : 0;
+    return plan_chunks(N, B, q_heads, k_heads, D, max_queries, max_len, window, &a) == VLUT_OK ? a.bytes() : 0;
 }
 
 int vlut_query_chunk_attention(int64_t N, int64_t B, int64_t q_heads, int64_t k_heads, int64_t D, int64_t max_queries, int64_t max_len, int64_t window, int* out6) {
     if (!out6) return VLUT_ERR_NULL;
     ChunkPlan a;
-    const int rc = plan_chunks(N, B, q_heads, k_heads, D, max_queries, max_len, window, false, &a);
+    const int rc = plan_chunks(N, B, q_heads, k_heads, D, max_queries, max_len, window, &a);
     if (rc != VLUT_OK) return rc;
     out6[0] = a.few ? a.few_row_places : 0;
     out6[1] = a.few_splits;
     out6[2] = a.few_chunk;
-    out6[3] = a.many_rows;
+    out6[3] = a.many ? kManyRows : 0;
     out6[4] = a.many_splits;
     out6[5] = a.many_chunk;
     return VLUT_OK;
@@ -117,8 +121,7 @@ int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int
     int rc = check_cache(cache);
     if (rc != VLUT_OK) return rc;
     ChunkPlan a;
-    const bool registers = !grouped_by_eight(*cache, 2);
-    rc = plan_chunks(N, B, q->heads, cache->heads, D, max_queries, max_len, window, registers, &a);
+    rc = plan_chunks(N, B, q->heads, cache->heads, D, max_queries, max_len, window, &a);
     if (rc != VLUT_OK) return rc;
     if (!q->data || !out->data || !query_starts || !lens || (max_len > 0 && !page_table)) return VLUT_ERR_NULL;
     if (out->heads != q->heads || q->type != cache->type || (out->type != cache->type && out->type != VLUT_TYPE_F32)) return VLUT_ERR_SHAPE;
@@ -134,7 +137,7 @@ int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int
         if (workspace_bytes < a.bytes()) return VLUT_ERR_SMALL_BUFFER;
         if ((uintptr_t)workspace % 16) return VLUT_ERR_UNSUPPORTED;
     }
-    a.load = registers ? kThroughRegisters : (D % 8 || !grouped_by_eight(*cache, 8) ? kDwords : (D < a.DP ? kVectors : kWholeVectors));
+    a.load = !grouped_by_eight(*cache, 2) ? kThroughRegisters : (D % 8 || !grouped_by_eight(*cache, 8) ? kDwords : (D < a.DP ? kVectors : kWholeVectors));
     ChunkParams p{};
     p.q = q->data;
     p.k = cache->k;
@@ -179,7 +182,6 @@ int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int
     p.many_chunk = a.many_chunk;
     p.many_tiles = a.many_tiles;
     p.many_per_xcd = a.many_per_xcd;
-    p.many_rows = a.many_rows;
     if (out->type == VLUT_TYPE_F32) return cache->type == VLUT_TYPE_BF16 ? launch_bf16_f32(a, p, (hipStream_t)stream) : launch_f16_f32(a, p, (hipStream_t)stream);
     return cache->type == VLUT_TYPE_BF16 ? launch_bf16(a, p, (hipStream_t)stream) : launch_f16(a, p, (hipStream_t)stream);
 }

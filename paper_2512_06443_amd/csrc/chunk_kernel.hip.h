@@ -219,12 +219,12 @@ struct Count { static constexpr int value = N; };
 // rows of a transposing read do.  Chunks behind D are not loaded: zeros from before the first stage.
 // Where rows are few each wave has its keys for itself, and none waits for another; a step's keys are asked for as soon as the first product is done with
 // the ones before, its values behind the second.
-template <class T, int DP, int RW, int TERMS, int LOAD>
+template <class T, int DP, int RW, int KW, int TERMS, int LOAD>
 __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
     typedef typename Output<T, TERMS>::type O;
-    constexpr bool FEW = RW == 1, WIDE = Number<T>::kWide, DIRECT = LOAD != kThroughRegisters, OWN_KEYS = own_keys(RW, LOAD), TURNS = turns(DP, RW, LOAD);
-    constexpr int NW = waves_of(DP, RW), KW = NW / RW, WK = wave_keys(DP, RW), KT = WK / 32, KEYS = step_keys(DP, RW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
+    constexpr bool FEW = RW == 1, WIDE = Number<T>::kWide, DIRECT = LOAD != kThroughRegisters, OWN_KEYS = own_keys(RW, LOAD);
+    constexpr int NW = RW * KW, WK = wave_keys(DP, RW), KT = WK / 32, KEYS = step_keys(DP, RW, KW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
     constexpr float LIFT = 0.5f * Number<T>::kLift;            // (scores after the first step may be larger)
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
@@ -233,7 +233,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
 
     // behind the buffers: the waves' m and l where they share rows, where the rows' results go and their factors, two flags (the part is to be
     // begun again; there is something to settle), pages' numbers
-    float* const row_m = (float*)(lds + tile_bytes(DP, RW, LOAD));
+    float* const row_m = (float*)(lds + tile_bytes(DP, RW, KW, LOAD));
     float* const row_l = row_m + 32 * NW;
     int64_t* const row_to = (int64_t*)(row_l + 32 * NW);
     float* const row_factor = (float*)(row_to + 32 * NW);
@@ -241,7 +241,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     int* const page_ids = again + 4;
     if (tid == 0) again[0] = again[1] = 0;
     if constexpr (LOAD == kDwords || LOAD == kVectors) {
-        for (int x = 16 * tid; x < tile_bytes(DP, RW, LOAD); x += 16 * 64 * NW) *(i32x4*)(lds + x) = i32x4{0, 0, 0, 0};
+        for (int x = 16 * tid; x < tile_bytes(DP, RW, KW, LOAD); x += 16 * 64 * NW) *(i32x4*)(lds + x) = i32x4{0, 0, 0, 0};
     }
     wg_barrier_lds();                                                  // (they are set ahead of the first step's barrier)
 
@@ -291,18 +291,16 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     const unsigned lds0 = lds_base_of(lds);
 
     // All keys of the part, in steps: multiply(first key of the step, where the wave's keys are), weigh_up(first key, where its values are).
-    auto sweep = [&](auto multiply, auto weigh_up, auto in_turns) {
+    auto sweep = [&](auto multiply, auto weigh_up) {
         if (first_key >= end_key) return;
         if constexpr (DIRECT) {
             // Of a load: its bytes, rows or the parts of one, loads of a wave and step.  OWN: keys that a wave loads.
             constexpr int UNIT = LOAD == kDwords ? 4 : 16, BYTES = 64 * UNIT, ROW = 2 * DP, RPI = BYTES > ROW ? BYTES / ROW : 1, SPLIT = ROW > BYTES ? ROW / BYTES : 1;
             constexpr int OWN = OWN_KEYS ? WK : WK / RW, LOADS = OWN / RPI * SPLIT, PERIOD = UNIT == 16 ? 16 / RPI : 1;
-            constexpr int AHEAD = OWN_KEYS ? 1 : ahead(DP, RW), PART = WK * ROW;       // bytes of a stage
+            constexpr int AHEAD = OWN_KEYS ? 1 : ahead(DP), PART = WK * ROW;           // bytes of a stage's keys, or values
             static_assert(OWN % 8 == 0 && 8 % RPI == 0, "whole groups of 8 keys");
             // the rings of the wave's group (or of the wave alone), the wave's keys in a step and where they are in a stage
-            const bool later = TURNS && wave >= NW / 2;
-            const unsigned k_ring = lds0 + (OWN_KEYS ? wave * ring_bytes(DP, RW, false) : kw * ring_bytes(DP, RW, false)), v_ring = k_ring + key_ring(DP, RW) * PART;
-            const unsigned k_ring_end = v_ring, v_ring_end = v_ring + (unsigned)((KW > 1 ? value_ring(DP, RW, later) : value_ring(DP, RW, TURNS)) * PART);
+            const unsigned k_ring = lds0 + kw * ring_bytes(DP, RW), v_ring = k_ring + ring(DP, RW) * PART, v_ring_end = v_ring + ring(DP, RW) * PART;
             const int in_stage = OWN_KEYS ? 0 : OWN * rw, own0 = WK * kw + in_stage;
             const unsigned char *const kb = (const unsigned char*)kh, *const vb = (const unsigned char*)vh;
             const unsigned k_page = 2u * (unsigned)p.k_page, v_page = 2u * (unsigned)p.v_page, k_token = 2u * (unsigned)p.k_token, v_token = 2u * (unsigned)p.v_token;
@@ -323,8 +321,8 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             }
             // dwords: a lane's place in its row
             const unsigned in_row = (unsigned)(lane * UNIT % ROW), k_in = (unsigned)row_in * k_token, v_in = (unsigned)row_in * v_token;
-            for (int s0 = first_key; s0 < end_key; s0 += stretch(RW)) {
-                const int s1 = s0 + min(end_key - s0, stretch(RW)), id0 = s0 >> page_log, ids = ((s1 - 1) >> page_log) - id0 + 1;
+            for (int s0 = first_key; s0 < end_key; s0 += stretch(RW, KW)) {
+                const int s1 = s0 + min(end_key - s0, stretch(RW, KW)), id0 = s0 >> page_log, ids = ((s1 - 1) >> page_log) - id0 + 1;
                 if (s0 > first_key) {
                     wait_loads<0>();
                     __syncthreads();           // (nobody reads the stretch before any more)
@@ -417,50 +415,30 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                         issue(kt + KEYS, k_ring, v_ring, No{}, Yes{});
                     }
                 } else {
-                    // stages: the ones that are worked on, and the ones that are asked for
-                    unsigned k_now = k_ring, v_now = v_ring, k_next = k_ring, v_next = v_ring;
-                    auto on = [](unsigned& stage, unsigned ring, unsigned end) { stage = stage + PART == end ? ring : stage + PART; };
+                    // stages: the one that is worked on, and the one that is asked for
+                    unsigned now = 0, next = 0;
+                    auto on = [&](unsigned& stage) { stage = v_ring + stage + PART == v_ring_end ? 0 : stage + PART; };
                     auto next_stage = [&](int kt) {
-                        issue(kt, k_next, v_next, Yes{}, Yes{});
-                        on(k_next, k_ring, k_ring_end);
-                        on(v_next, v_ring, v_ring_end);
+                        issue(kt, k_ring + next, v_ring + next, Yes{}, Yes{});
+                        on(next);
                     };
 #pragma unroll
                     for (int x = 0; x < AHEAD; ++x) next_stage(s0 + x * KEYS);
-                    // the stage of step kt is there, for all waves
-                    auto begin = [&](int kt) {
+                    for (int kt = s0; kt < s1; kt += KEYS) {
                         wait_loads<2 * (AHEAD - 1) * LOADS>();
-                        mend_keys(k_now, AHEAD - 1);
-                        mend_values(kt, v_now);
-                        wg_barrier_lds();
+                        mend_keys(k_ring + now, AHEAD - 1);
+                        mend_values(kt, v_ring + now);
+                        wg_barrier_lds();      // the stage of step kt is there, for all waves, and nobody reads the one before any more
                         next_stage(kt + AHEAD * KEYS);                 // (behind the last step too, from the last keys)
-                    };
-                    if constexpr (in_turns.value) {
-                        begin(s0);
-                        multiply(s0, k_now);
-                        for (int kt = s0 + KEYS; kt < s1; kt += KEYS) {
-                            const unsigned before = v_now;
-                            on(k_now, k_ring, k_ring_end);
-                            on(v_now, v_ring, v_ring_end);
-                            begin(kt);
-                            weigh_up(kt - KEYS, before);
-                            multiply(kt, k_now);
-                        }
-                        weigh_up(s0 + (s1 - 1 - s0) / KEYS * KEYS, v_now);
-                    } else {
-                        for (int kt = s0; kt < s1; kt += KEYS) {
-                            begin(kt);
-                            multiply(kt, k_now);
-                            weigh_up(kt, v_now);
-                            on(k_now, k_ring, k_ring_end);
-                            on(v_now, v_ring, v_ring_end);
-                        }
+                        multiply(kt, k_ring + now);
+                        weigh_up(kt, v_ring + now);
+                        on(now);
                     }
                 }
             }
             wait_loads<0>();
         } else {
-            constexpr int PER = 64 * NW / CH, LI = KEYS / PER, BYTES = stage_bytes(DP, RW, LOAD);
+            constexpr int PER = 64 * NW / CH, LI = KEYS / PER, BYTES = stage_bytes(DP, RW, KW, LOAD);
             static_assert(PER * LI == KEYS, "whole loads");
             const int chunk = lane % CH, to_key = GK * wave + lane / CH;
             const unsigned to_k = (unsigned)(to_key * ROW_K + 16 * chunk), to_v = (unsigned)(KEYS * ROW_K + to_key * ROW_V + 16 * chunk);
@@ -639,9 +617,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             }
             pinned(l);                         // (or the sums are made behind the loop, from registers that wait for that)
         };
-        // The matrix cores and the vector units of a SIMD work on two waves: half of the waves are on the second product of a step while the others are on the first of the next
-        if (TURNS && wave >= NW / 2) sweep(multiply, weigh_up, Yes{});
-        else sweep(multiply, weigh_up, No{});
+        sweep(multiply, weigh_up);
         // (a lane's O is of the keys of both halves)
         const float both = l + __shfl_xor(l, 32);
         if (!finite() || (WIDE && !(both < 0x1p40f))) again[0] = 1;
@@ -652,7 +628,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         sweep(multiply, [&](int kt, unsigned) {
             hide(kt + WK * kw);
             m = fmaxf(m, largest() - LIFT);
-        }, No{});
+        });
         __syncthreads();
     }
     l += __shfl_xor(l, 32);
@@ -693,7 +669,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             }
         }
     };
-    constexpr int LP = leave_pitch(DP, RW);
+    constexpr int LP = leave_pitch(DP, KW);
     float* const own = (float*)lds + wave * 32 * LP;
     if constexpr (FEW) {
         constexpr int HALF = DP / 2, LANES = HALF / 4, ROWS = 64 * NW / LANES < 32 ? 64 * NW / LANES : 32;
@@ -810,7 +786,7 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int i, unsigned c
     if (t.row_end > p.few_rows) {
         // worked on as many rows; where nobody does, more queries than the caller said that there are: NaN
         if (p.many_per_xcd == 0 && t.split == 0)
-            for (int64_t x = threadIdx.x; x < (int64_t)t.row_end * (p.D / 4); x += 64 * waves_of(DP, 1)) {
+            for (int64_t x = threadIdx.x; x < (int64_t)t.row_end * (p.D / 4); x += 64 * few_waves(DP)) {
                 const int row = (int)(x / (p.D / 4)), j = row / p.G, d = 4 * (int)(x % (p.D / 4));
                 const float nan = __builtin_nanf("");
                 store_four<typename Output<T, TERMS>::type>(p.out, (t.seq.start + j) * p.out_token + (int64_t)(t.h * p.G + row - j * p.G) * p.out_head + d, f32x4{nan, nan, nan, nan});
@@ -823,14 +799,15 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int i, unsigned c
     t.direct = r.parts == 1;
     t.first = r.first + t.split * p.few_chunk;
     t.end = t.first + min(r.end - t.first, p.few_chunk);
-    attend_chunk<T, DP, 1, TERMS, LOAD>(p, t, lds);
+    attend_chunk<T, DP, 1, few_waves(DP), TERMS, LOAD>(p, t, lds);
 }
 
 // Workgroup `i` of those for many rows: tile `at` of the sequences' tiles, one sequence behind the other.  Of a sequence's tiles those that see the most and the least take turns,
 // so that any stretch of them is about the same work.
-template <class T, int DP, int RW, int TERMS, int LOAD>
+template <class T, int DP, int KW, int TERMS, int LOAD>
 __device__ __forceinline__ void many_rows(const ChunkParams& p, int i, unsigned char* lds) {
-    constexpr int ROWS = 32 * RW;
+    constexpr int RW = 4, ROWS = kManyRows;
+    static_assert(ROWS == 32 * RW, "32 rows a wave");
     const int lane = (int)threadIdx.x & 63;
     int at = i % p.many_tiles;
     Tile t;
@@ -877,19 +854,22 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int i, unsigned 
     t.direct = r.parts == 1;
     t.first = r.first + t.split * p.many_chunk;
     t.end = t.first + min(r.end - t.first, p.many_chunk);
-    attend_chunk<T, DP, RW, TERMS, LOAD>(p, t, lds);
+    attend_chunk<T, DP, RW, KW, TERMS, LOAD>(p, t, lds);
 }
 
 // Workgroups go to the 8 XCDs in turn, and tiles of one key head, which read the same keys, to one XCD (one L2) as far as that goes.  An XCD begins with its tiles that
-// see much (every other one) and ends with those that see little.
-template <class T, int DP, int RW, int TERMS, int LOAD>
-__global__ void __launch_bounds__(64 * waves_of(DP, RW), DP > 128 ? 1 : 2) many_rows_kernel(const ChunkParams p) {
+// see much (every other one) and ends with those that see little; where its 32 units have room for two, the second ones go the other way, so that who has the most has the
+// least beside it.
+template <class T, int DP, int KW, int TERMS, int LOAD>
+__global__ void __launch_bounds__(256 * KW, DP > 128 ? 1 : 2) many_rows_kernel(const ChunkParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
-    const int xcd = (int)blockIdx.x & 7, place = (int)blockIdx.x >> 3, n = p.many_per_xcd, heavy = (n + 1) / 2;
-    many_rows<T, DP, RW, TERMS, LOAD>(p, xcd * n + (place < heavy ? 2 * place : 2 * (n - 1 - place) + 1), lds);
+    const int xcd = (int)blockIdx.x & 7, n = p.many_per_xcd, heavy = (n + 1) / 2, both = min(n, 64);
+    int place = (int)blockIdx.x >> 3;
+    if (KW == 1 && DP <= 128 && place >= 32 && place < both) place = both - 1 - (place - 32);
+    many_rows<T, DP, KW, TERMS, LOAD>(p, xcd * n + (place < heavy ? 2 * place : 2 * (n - 1 - place) + 1), lds);
 }
 template <class T, int DP, int TERMS, int LOAD>
-__global__ void __launch_bounds__(64 * waves_of(DP, 1), DP > 128 ? 1 : 2) few_rows_kernel(const ChunkParams p) {
+__global__ void __launch_bounds__(64 * few_waves(DP), DP > 128 ? 1 : 2) few_rows_kernel(const ChunkParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     few_rows<T, DP, TERMS, LOAD>(p, ((int)blockIdx.x & 7) * p.few_per_xcd + ((int)blockIdx.x >> 3), lds);
 }
@@ -918,7 +898,7 @@ __global__ void __launch_bounds__(256) combine_chunks(const ChunkParams p) {
     const int h = head / p.G, in_head = j * p.G + head - h * p.G;
     const bool few = c.queries * p.G <= p.few_rows;
     if (!few && p.many_per_xcd == 0) return;   // (more queries than the caller said: NaN already, and there are no such parts)
-    const int row0 = few ? 0 : in_head / p.many_rows * p.many_rows, row_end = few ? c.queries * p.G : min(row0 + p.many_rows, c.queries * p.G);
+    const int row0 = few ? 0 : in_head / kManyRows * kManyRows, row_end = few ? c.queries * p.G : min(row0 + kManyRows, c.queries * p.G);
     const Range r = range_of(p, c, row0 / p.G, (row_end - 1) / p.G, few ? p.few_chunk : p.many_chunk);
     if (r.parts == 1) return;
     float top = -__builtin_inff(), total = 0.0f;

@@ -7,27 +7,27 @@ namespace {
 template <class T, int DP, int TERMS, int LOAD>
 int launch_few(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
     static std::atomic<unsigned> done{0};
-    constexpr int lds = lds_bytes(DP, 1, LOAD);
+    constexpr int lds = lds_bytes(DP, 1, few_waves(DP), LOAD);
     static_assert(lds <= 80 * 1024, "two workgroups a unit");
     auto kfn = few_rows_kernel<T, DP, TERMS, LOAD>;
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
-    return launch(kfn, dim3(8u * (unsigned)a.few_per_xcd), 64 * waves_of(DP, 1), lds, stream, p);
+    return launch(kfn, dim3(8u * (unsigned)a.few_per_xcd), 64 * few_waves(DP), lds, stream, p);
 }
-template <class T, int DP, int RW, int TERMS, int LOAD>
+template <class T, int DP, int KW, int TERMS, int LOAD>
 int launch_many(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
     static std::atomic<unsigned> done{0};
-    constexpr int lds = lds_bytes(DP, RW, LOAD);
-    static_assert(lds <= 160 * 1024, "what a unit has");
-    auto kfn = many_rows_kernel<T, DP, RW, TERMS, LOAD>;
+    constexpr int lds = lds_bytes(DP, 4, KW, LOAD);
+    static_assert(lds <= (KW == 1 && DP <= 128 ? 80 : 160) * 1024, "one or two workgroups a unit");
+    auto kfn = many_rows_kernel<T, DP, KW, TERMS, LOAD>;
     if (lds > 64 * 1024 && !allow_lds((const void*)kfn, lds, done)) return VLUT_ERR_DEVICE;
-    return launch(kfn, dim3(8u * (unsigned)a.many_per_xcd), 64 * waves_of(DP, RW), lds, stream, p);
+    return launch(kfn, dim3(8u * (unsigned)a.many_per_xcd), 256 * KW, lds, stream, p);
 }
 template <class T, int DP, int TERMS, int LOAD>
 int launch_parts(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
     int rc = VLUT_OK;
     if (a.many) {
-        if constexpr (DP <= 128 && LOAD != kThroughRegisters) rc = a.row_waves == 8 ? launch_many<T, DP, 8, TERMS, LOAD>(a, p, stream) : launch_many<T, DP, 4, TERMS, LOAD>(a, p, stream);
-        else rc = launch_many<T, DP, 4, TERMS, LOAD>(a, p, stream);
+        if constexpr (DP <= 128 && LOAD != kThroughRegisters) rc = a.key_waves == 2 ? launch_many<T, DP, 2, TERMS, LOAD>(a, p, stream) : launch_many<T, DP, 1, TERMS, LOAD>(a, p, stream);
+        else rc = launch_many<T, DP, 1, TERMS, LOAD>(a, p, stream);
     }
     if (rc == VLUT_OK && a.few) rc = launch_few<T, DP, TERMS, LOAD>(a, p, stream);
     if (rc != VLUT_OK || a.bytes() == 0) return rc;

@@ -27,51 +27,46 @@ struct ChunkParams {
     int window;                        // keys that a query sees at most
     int few_rows;                      // a sequence of up to so many rows per key head is a few-row one (0: none is)
     int few_splits, few_chunk, few_per_xcd;                            // parts at most, keys of a part, workgroups of an XCD
-    int many_splits, many_chunk, many_tiles, many_per_xcd, many_rows;  // many_tiles: at most; many_rows: of a tile
+    int many_splits, many_chunk, many_tiles, many_per_xcd;     // many_tiles: at most
 };
 
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 32, kManyRows = 128;        // of a tile
 
 // How keys and values come to LDS: through registers; straight, a dword or 16 bytes a lane; of rows that are as long as LDS has them.
 constexpr int kThroughRegisters = 0, kDwords = 1, kVectors = 2, kWholeVectors = 3;
 
-// A workgroup's waves: RW groups of 32 rows, the keys of a step shared by KW.  Where rows are few 1 x 4 (features past 128: 2), two workgroups of which a unit has
-// room for; where they are many 8 x 1 or 4 x 2 (4 x 1).
-__host__ __device__ constexpr int waves_of(int DP, int RW) { return RW == 1 ? (DP > 128 ? 2 : 4) : (DP > 128 ? 4 : 8); }
+// A workgroup's waves: RW groups of 32 rows, the keys of a step shared by KW.  Where rows are few 1 x 4 (features past 128: 1 x 2); where they are many 4 x 1 or 4 x 2
+// (features past 128: 4 x 1).  Of the workgroups of four waves a unit has room for two, of 4 x 1 with features past 128 for one.
+__host__ __device__ constexpr int few_waves(int DP) { return DP > 128 ? 2 : 4; }
 __host__ __device__ constexpr bool own_keys(int RW, int LOAD) { return RW == 1 && LOAD != kThroughRegisters; }      // waves have their keys for themselves
-__host__ __device__ constexpr bool turns(int DP, int RW, int LOAD) { return RW == 8 && LOAD != kThroughRegisters; }  // a SIMD's two waves take the products in turns
 __host__ __device__ constexpr int wave_keys(int DP, int RW) { return RW == 1 || DP > 128 ? 32 : 64; }
-__host__ __device__ constexpr int step_keys(int DP, int RW) { return wave_keys(DP, RW) * (waves_of(DP, RW) / RW); }
+__host__ __device__ constexpr int step_keys(int DP, int RW, int KW) { return wave_keys(DP, RW) * KW; }
 __host__ __device__ constexpr int k_pitch(int DP, int LOAD) { return DP * 2 + (LOAD == kThroughRegisters ? 16 : 0); }
 __host__ __device__ constexpr int v_pitch(int DP, int LOAD) { return DP * 2 + (LOAD == kThroughRegisters ? 64 : 0); }
-// Through registers: a stage is a step's keys and values.  Straight: the KW groups of waves have rings of stages of their keys and of their values each, AHEAD of which
-// are on their way; where waves take turns the later ones read values of the step before.
-__host__ __device__ constexpr int stage_bytes(int DP, int RW, int LOAD) { return step_keys(DP, RW) * (k_pitch(DP, LOAD) + v_pitch(DP, LOAD)); }
+// Through registers: a stage is a step's keys and values.  Straight: the KW groups of waves have rings of stages of their keys and values each, AHEAD of which are on
+// their way.
+__host__ __device__ constexpr int stage_bytes(int DP, int RW, int KW, int LOAD) { return step_keys(DP, RW, KW) * (k_pitch(DP, LOAD) + v_pitch(DP, LOAD)); }
 __host__ __device__ constexpr int stages(int RW) { return RW == 1 ? 1 : 2; }
-__host__ __device__ constexpr int ahead(int DP, int RW) { return RW == waves_of(DP, RW) ? 2 : 1; }
-__host__ __device__ constexpr int key_ring(int DP, int RW) { return RW == 1 ? 1 : ahead(DP, RW) + 1; }
-__host__ __device__ constexpr int value_ring(int DP, int RW, bool later) { return RW == 1 ? 1 : ahead(DP, RW) + 1 + (later ? 1 : 0); }
-__host__ __device__ constexpr int ring_bytes(int DP, int RW, bool later) { return (key_ring(DP, RW) + value_ring(DP, RW, later)) * wave_keys(DP, RW) * DP * 2; }
-__host__ __device__ constexpr int buffers_bytes(int DP, int RW, int LOAD) {
-    if (LOAD == kThroughRegisters) return stages(RW) * stage_bytes(DP, RW, LOAD);
-    if (RW == 1) return waves_of(DP, RW) * ring_bytes(DP, RW, false);
-    if (RW == waves_of(DP, RW)) return ring_bytes(DP, RW, turns(DP, RW, LOAD));
-    return 2 * ring_bytes(DP, RW, false);
+__host__ __device__ constexpr int ahead(int DP) { return DP > 128 ? 2 : 1; }
+__host__ __device__ constexpr int ring(int DP, int RW) { return RW == 1 ? 1 : ahead(DP) + 1; }
+__host__ __device__ constexpr int ring_bytes(int DP, int RW) { return ring(DP, RW) * wave_keys(DP, RW) * DP * 4; }
+__host__ __device__ constexpr int buffers_bytes(int DP, int RW, int KW, int LOAD) {
+    return LOAD == kThroughRegisters ? stages(RW) * stage_bytes(DP, RW, KW, LOAD) : KW * ring_bytes(DP, RW);
 }
 __host__ __device__ constexpr int turn_features(int DP) { return DP > 64 ? 64 : 32; }       // that leave through LDS together
 __host__ __device__ constexpr int most_of(int a, int b) { return a > b ? a : b; }
 // Keys and values, or what results leave through: for each wave 32 rows, of the features that leave together, or of half of them all.
-__host__ __device__ constexpr int leave_pitch(int DP, int RW) { return (RW == waves_of(DP, RW) ? turn_features(DP) : DP / 2) + 4; }
-__host__ __device__ constexpr int tile_bytes(int DP, int RW, int LOAD) { return most_of(buffers_bytes(DP, RW, LOAD), waves_of(DP, RW) * 32 * leave_pitch(DP, RW) * 4); }
-__host__ __device__ constexpr int stretch(int RW) { return RW == 1 ? 4096 : 16384; }        // keys whose pages' numbers are in LDS (8 keys a page at least)
-__host__ __device__ constexpr int lds_bytes(int DP, int RW, int LOAD) {
-    return tile_bytes(DP, RW, LOAD) + waves_of(DP, RW) * 32 * 20 + 16 + (LOAD == kThroughRegisters ? 0 : (stretch(RW) / 8 + 2) * 4);
+__host__ __device__ constexpr int leave_pitch(int DP, int KW) { return (KW == 1 ? turn_features(DP) : DP / 2) + 4; }
+__host__ __device__ constexpr int tile_bytes(int DP, int RW, int KW, int LOAD) { return most_of(buffers_bytes(DP, RW, KW, LOAD), RW * KW * 32 * leave_pitch(DP, KW) * 4); }
+__host__ __device__ constexpr int stretch(int RW, int KW) { return RW == 1 ? 4096 : (RW * KW == 4 ? 8192 : 16384); }        // keys whose pages' numbers are in LDS (8 keys a page at least)
+__host__ __device__ constexpr int lds_bytes(int DP, int RW, int KW, int LOAD) {
+    return tile_bytes(DP, RW, KW, LOAD) + RW * KW * 32 * 20 + 16 + (LOAD == kThroughRegisters ? 0 : (stretch(RW, KW) / 8 + 2) * 4);
 }
 
 struct ChunkPlan {
-    int DP, row_waves, load;           // RW where rows are many; how keys come to LDS
+    int DP, key_waves, load;           // KW where rows are many; how keys come to LDS
     int few, many;                     // whether there are such workgroups
-    int few_splits, few_chunk, few_row_places, many_splits, many_chunk, many_tiles, many_rows;
+    int few_splits, few_chunk, few_row_places, many_splits, many_chunk, many_tiles;
     int few_per_xcd, many_per_xcd;
     size_t few_o_bytes, few_ml_bytes, many_o_bytes, many_ml_bytes;
     size_t bytes() const { return few_o_bytes + few_ml_bytes + many_o_bytes + many_ml_bytes; }
