@@ -78,6 +78,8 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
             a.many_ml_bytes = whole_lines(parts * 8);
         }
     }
+    // (workgroups that join the parts, of 1024 / DP rows each)
+    if (a.bytes() && ceil_div(N * Hq, 1024 / a.DP) >= 4 * kMostBlocks) return VLUT_ERR_SHAPE;
     *out = a;
     return VLUT_OK;
 }
