@@ -111,7 +111,7 @@ def run(c, window=0, dtype=None, **more):
     return out, lse
 
 
-HEADS = [(20, 5, 128), (4, 4, 100), (16, 2, 64), (8, 1, 256), (6, 2, 96), (3, 3, 8), (5, 1, 60), (2, 1, 132)]
+HEADS = [(20, 5, 128), (4, 4, 100), (16, 2, 64), (8, 1, 256), (6, 2, 96), (3, 3, 8), (5, 1, 60), (2, 1, 132), (64, 1, 64), (90, 2, 36)]
 LENGTHS = [([1], [1]), ([1], [40]), ([1, 1, 1], [700, 1, 129]), ([5, 1, 8], [5, 33, 400]), ([40], [40]), ([130], [515]), ([3, 0, 200, 1, 17], [3, 9, 200, 1000, 64]),
            ([257, 64], [300, 900]), ([9], [6])]
 
