@@ -31,19 +31,22 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
     if (D < 8 || D > VLUT_MAX_HEAD_FEATURES || D % 4) return VLUT_ERR_UNSUPPORTED;
     ChunkPlan a{};
     const int64_t G = Hq / Hk, most_rows = std::min(max_queries, N) * G;
-    // Keys that a tile of `tokens` neighbouring tokens sees, at most (it begins at a multiple of 32, up to 31 keys earlier).
-    const auto seen = [&](int64_t tokens) { return std::max<int64_t>(1, window ? std::min(max_len, window + tokens) : max_len) + 31; };
+    // Keys that a tile of `tokens` neighbouring tokens sees, at most (those of a window begin at a multiple of 32, up to 31 keys earlier).
+    const auto seen = [&](int64_t tokens) { return std::max<int64_t>(1, window ? std::min(max_len, window + tokens) + 31 : max_len); };
     a.DP = D <= 64 ? 64 : (D <= 128 ? 128 : 256);
     a.many = most_rows > kFewRows;
     // With one sequence that may have many rows there is nothing for a launch for few.
     a.few = !a.many || (B > 1 && G <= kFewRows);
     if (a.few) {
         a.few_row_places = (int)std::min<int64_t>(kFewRows, std::max<int64_t>(1, most_rows / G) * G);
-        // Keys that one tile sees, in steps.  Parts so that the workgroups are four rounds of those that run at once, of four steps at least; where that many are not
-        // there, of one.
-        const int64_t step = step_keys(a.DP, 1, few_waves(a.DP)), keys = seen(kFewRows), steps = ceil_div(keys, step), slots = 2 * kUnits;
-        int64_t per = std::max<int64_t>(4, ceil_div(B * Hk * steps, 4 * slots));
-        while (per > 1 && B * Hk * ceil_div(steps, per) < slots) per /= 2;
+        // Parts only so that 640 waves are at work, each of four steps at least, and for more than eight of them: a wave's way to its first keys and its results' way out take as
+        // long as seven steps, and those that join parts 5 us.  32 steps at most, so that one long sequence among short ones does not keep the others' units waiting.
+        // us with parts of 1, 2, 4, 8, 16 steps / in one, joining included, 32 query and 8 key heads of 128 in bf16: a sequence of 1000 keys 14.1, 14.9, 16.6 / 16.5; of 8000
+        // 29.1, 21.6, 20.0, 21.6, 29.9 / 77.3; 8 of 4000 48, 36, 31, 31, 32 / 44; 16 of up to 4000 84, 63, 52, 48, 47 / 53; 48 of up to 4095 144, 109, 95, 92, 95 / 92;
+        // 64 of 2048 to 4095 230, 176, 152, 151, 151 / 143; 13 of up to 1990 in windows of 1024, 32 heads of 100 that are not shared, 77, 57, 49 / 36.
+        const int64_t step = step_keys(a.DP, 1, few_waves(a.DP)), keys = seen(kFewRows), steps = ceil_div(keys, step);
+        const int64_t wanted = ceil_div(640, few_waves(a.DP) * B * Hk);
+        const int64_t per = steps <= 8 ? steps : std::min(std::max<int64_t>(32, ceil_div(B * Hk * steps, 8192)), std::max<int64_t>(4, ceil_div(steps, wanted)));
         a.few_chunk = (int)(step * per);
         a.few_splits = (int)ceil_div(keys, a.few_chunk);
         const int64_t blocks = ceil_div(B * Hk * a.few_splits, 8);
@@ -58,7 +61,8 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
     if (a.many) {
         const int64_t rows = N * G, keys = seen(kManyRows / G + 1);
         a.many_tiles = (int)std::min(rows / kManyRows + B, (rows + B * (kManyRows - 1)) / kManyRows);
-        const int64_t tiles = a.many_tiles * Hk;
+        // As many as there are if all sequences with many rows have as many as they may have.
+        const int64_t tiles = std::min<int64_t>(a.many_tiles, ceil_div(rows, most_rows) * ceil_div(most_rows, kManyRows)) * Hk;
         // Two workgroups of four waves on a unit, one's waits beside the other's work, where there are tiles for that; else one whose eight waves share the keys, unless
         // those are so many that parts of them are as good.  us, 4 x 1 / 4 x 2, parts joined included, 32 query and 8 key heads of 128 in bf16 (20 and 5 where it says
         // so): 4096 tokens (20, 5) 125 / 131, in windows of 16 24 / 37, of 1024 77 / 89; 16384 tokens 2192 / 2446; 4096 of 64 features 91 / 123; 1024 tokens 40 / 27, behind
@@ -69,7 +73,7 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
         const int64_t splits = std::min(std::max<int64_t>(1, slots / tiles), ceil_div(keys, 512));
         a.many_chunk = (int)(ceil_div(ceil_div(keys, splits), step) * step);
         a.many_splits = (int)ceil_div(keys, a.many_chunk);
-        const int64_t blocks = ceil_div(tiles * a.many_splits, 8);
+        const int64_t blocks = ceil_div(a.many_tiles * Hk * a.many_splits, 8);
         if (8 * blocks >= kMostBlocks) return VLUT_ERR_SHAPE;
         a.many_per_xcd = (int)blocks;
         if (a.many_splits > 1) {
@@ -90,6 +94,13 @@ bool grouped_by_eight(const vlut_cache& c, int unit) {
     for (int64_t s : {c.k_page_stride, c.v_page_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) && s % unit == 0;
     for (int64_t s : {c.k_head_stride, c.v_head_stride}) ok = ok && s % unit == 0;
     for (int64_t s : {c.k_token_stride, c.v_token_stride}) ok = ok && s >= 0 && s < ((int64_t)1 << 30) / std::max<int64_t>(c.page_size, 8) && s % unit == 0;
+    return ok;
+}
+
+// Rows of D features, an odd number of fours, one behind the other: 8 of them begin and end at whole 16 bytes.
+bool in_runs(const vlut_cache& c, int64_t D) {
+    bool ok = c.k_token_stride == D && c.v_token_stride == D && (uintptr_t)c.k % 16 == 0 && (uintptr_t)c.v % 16 == 0;
+    for (int64_t s : {c.k_page_stride, c.v_page_stride, c.k_head_stride, c.v_head_stride}) ok = ok && s % 8 == 0;
     return ok;
 }
 
@@ -139,7 +150,10 @@ int vlut_chunk_attention(const vlut_heads* q, const vlut_cache* cache, const int
         if (workspace_bytes < a.bytes()) return VLUT_ERR_SMALL_BUFFER;
         if ((uintptr_t)workspace % 16) return VLUT_ERR_UNSUPPORTED;
     }
-    a.load = !grouped_by_eight(*cache, 2) ? kThroughRegisters : (D % 8 || !grouped_by_eight(*cache, 8) ? kDwords : (D < a.DP ? kVectors : kWholeVectors));
+    if (!grouped_by_eight(*cache, 2)) a.load = kThroughRegisters;
+    else if (D % 8) a.load = a.DP <= 128 && in_runs(*cache, D) ? kRuns : kDwords;
+    else if (!grouped_by_eight(*cache, 8)) a.load = kDwords;
+    else a.load = D < a.DP ? kVectors : kWholeVectors;
     ChunkParams p{};
     p.q = q->data;
     p.k = cache->k;

@@ -223,7 +223,7 @@ template <class T, int DP, int RW, int KW, int TERMS, int LOAD>
 __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
     typedef typename Output<T, TERMS>::type O;
-    constexpr bool FEW = RW == 1, WIDE = Number<T>::kWide, DIRECT = LOAD != kThroughRegisters, OWN_KEYS = own_keys(RW, LOAD);
+    constexpr bool FEW = RW == 1, WIDE = Number<T>::kWide, DIRECT = LOAD != kThroughRegisters, RUNS = LOAD == kRuns, OWN_KEYS = own_keys(RW, LOAD);
     constexpr int NW = RW * KW, WK = wave_keys(DP, RW), KT = WK / 32, KEYS = step_keys(DP, RW, KW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
     constexpr float LIFT = 0.5f * Number<T>::kLift;            // (scores after the first step may be larger)
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
@@ -280,14 +280,16 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     const float scale_log2 = p.scale_log2;
 
     // Where a lane reads: of keys, 8 features of row l32 (and 32 rows further); of values, a corner of a transposing read.
-    constexpr int ROW_K = k_pitch(DP, LOAD), ROW_V = v_pitch(DP, LOAD);
+    constexpr bool TURNED = DIRECT && !RUNS;
+    // (bytes of a row)
+    const int row_k = RUNS ? 2 * p.D : k_pitch(DP, LOAD), row_v = RUNS ? 2 * p.D : v_pitch(DP, LOAD);
     auto turn_k = [](int r) { return DP == 64 ? (r >> 1) & 7 : r & 15; };
     auto turn_v = [](int r) { return DP == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3); };
-    const unsigned k_lane = (unsigned)(l32 * ROW_K + 16 * (DIRECT ? half ^ turn_k(l32) : half));
+    const unsigned k_lane = (unsigned)(l32 * row_k + 16 * (TURNED ? half ^ turn_k(l32) : half));
     const int v_row = 4 * half + (l16 >> 2), v_chunk = 2 * ((lane >> 4) & 1) + ((l16 & 3) >> 1);
-    const unsigned v_lane = (unsigned)(v_row * ROW_V + 16 * (DIRECT ? v_chunk ^ turn_v(v_row) : v_chunk) + 8 * (l16 & 1));
-    auto k_at = [&](unsigned base, int ks) { return DIRECT ? (base + k_lane) ^ (unsigned)(32 * ks) : base + k_lane + (unsigned)(32 * ks); };
-    auto v_at = [&](unsigned base, int dt) { return DIRECT ? (base + v_lane) ^ (unsigned)(64 * dt) : base + v_lane + (unsigned)(64 * dt); };
+    const unsigned v_lane = (unsigned)(v_row * row_v + 16 * (TURNED ? v_chunk ^ turn_v(v_row) : v_chunk) + 8 * (l16 & 1));
+    auto k_at = [&](unsigned base, int ks) { return TURNED ? (base + k_lane) ^ (unsigned)(32 * ks) : base + k_lane + (unsigned)(32 * ks); };
+    auto v_at = [&](unsigned base, int dt) { return TURNED ? (base + v_lane) ^ (unsigned)(64 * dt) : base + v_lane + (unsigned)(64 * dt); };
     const unsigned lds0 = lds_base_of(lds);
 
     // All keys of the part, in steps: multiply(first key of the step, where the wave's keys are), weigh_up(first key, where its values are).
@@ -296,8 +298,10 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         if constexpr (DIRECT) {
             // Of a load: its bytes, rows or the parts of one, loads of a wave and step.  OWN: keys that a wave loads.
             constexpr int UNIT = LOAD == kDwords ? 4 : 16, BYTES = 64 * UNIT, ROW = 2 * DP, RPI = BYTES > ROW ? BYTES / ROW : 1, SPLIT = ROW > BYTES ? ROW / BYTES : 1;
-            constexpr int OWN = OWN_KEYS ? WK : WK / RW, LOADS = OWN / RPI * SPLIT, PERIOD = UNIT == 16 ? 16 / RPI : 1;
-            constexpr int AHEAD = OWN_KEYS ? 1 : ahead(DP), PART = WK * ROW;           // bytes of a stage's keys, or values
+            // (runs: 8 keys are D vectors)
+            constexpr int RUN_LOADS = DP / 64;
+            constexpr int OWN = OWN_KEYS ? WK : WK / RW, LOADS = RUNS ? OWN / 8 * RUN_LOADS : OWN / RPI * SPLIT, PERIOD = UNIT == 16 ? 16 / RPI : 1;
+            constexpr int AHEAD = OWN_KEYS ? 1 : ahead(DP), PART = WK * 2 * DP;           // bytes of a stage's keys, or values
             static_assert(OWN % 8 == 0 && 8 % RPI == 0, "whole groups of 8 keys");
             // the rings of the wave's group (or of the wave alone), the wave's keys in a step and where they are in a stage
             const unsigned k_ring = lds0 + kw * ring_bytes(DP, RW), v_ring = k_ring + ring(DP, RW) * PART, v_ring_end = v_ring + ring(DP, RW) * PART;
@@ -305,11 +309,11 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             const unsigned char *const kb = (const unsigned char*)kh, *const vb = (const unsigned char*)vh;
             const unsigned k_page = 2u * (unsigned)p.k_page, v_page = 2u * (unsigned)p.v_page, k_token = 2u * (unsigned)p.k_token, v_token = 2u * (unsigned)p.v_token;
             const int row_in = lane * UNIT / ROW;
-            const unsigned row_bytes = 2u * (unsigned)p.D;
+            const unsigned row_bytes = 2u * (unsigned)p.D, run_bytes = 8 * row_bytes;
             // vectors: a lane's offsets, which repeat every 16 rows, and whether there is such a chunk
             unsigned k_from[PERIOD], v_from[PERIOD];
             bool has_k[PERIOD], has_v[PERIOD];
-            if constexpr (UNIT == 16) {
+            if constexpr (UNIT == 16 && !RUNS) {
 #pragma unroll
                 for (int x = 0; x < PERIOD; ++x) {
                     const int r = in_stage + RPI * x + row_in, ck = (lane % CH) ^ turn_k(r), cv = (lane % CH) ^ turn_v(r);
@@ -350,6 +354,15 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                         const unsigned id = (unsigned)max(named, 0), in_page = (unsigned)(key & mask);
                         const unsigned char* const k = kb + ((uint64_t)id * k_page + in_page * k_token);
                         const unsigned char* const v = vb + ((uint64_t)id * v_page + in_page * v_token);
+                        if constexpr (RUNS) {
+#pragma unroll
+                            for (int part = 0; part < RUN_LOADS; ++part) {
+                                const unsigned of = (unsigned)(16 * lane + BYTES * part), to = (unsigned)((in_stage + 8 * g) * row_k + BYTES * part);
+                                if (of >= run_bytes) continue;
+                                if constexpr (keys.value) load_to_lds(k, of, k_stage + to);
+                                if constexpr (values.value) load_to_lds(v, of, v_stage + to);
+                            }
+                        } else
 #pragma unroll
                         for (int i = 0; i < 8 / RPI; ++i) {
                             const int r = 8 * g + RPI * i;
@@ -378,10 +391,15 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 // every row sees.  newer: stages asked for since.
                 auto mend_keys = [&](unsigned stage, int newer) {
                     const unsigned its = bad >> (newer * (OWN / 8)) & ((1u << (OWN / 8)) - 1);
-                    if (its != 0) {
+                    constexpr int N = (int)Number<T>::kNan;
+                    if (RUNS) {
+                        if (its != 0)
+                            for (int g = 0; g < OWN / 8; ++g)
+                                for (unsigned of = 16u * (unsigned)lane; of < run_bytes && (its >> (OWN / 8 - 1 - g) & 1); of += BYTES)
+                                    at_lds<i32x4>(stage + (unsigned)((in_stage + 8 * g) * row_k) + of) = i32x4{N, N, N, N};
+                    } else if (its != 0) {
 #pragma unroll
                         for (int x = 0; x < OWN / GK; ++x) {
-                            constexpr int N = (int)Number<T>::kNan;
                             if (its >> (OWN / 8 - 1 - GK * x / 8) & 1) at_lds<i32x4>(stage + (unsigned)((in_stage + GK * x) * ROW + 16 * lane)) = i32x4{N, N, N, N};
                         }
                     }
@@ -389,6 +407,22 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 auto mend_values = [&](int kt, unsigned stage) {
                     if (kt + KEYS > tile_to || kt < tile_from) {
                         unsigned odd = 0;
+                        if (RUNS) {
+#pragma unroll
+                            for (int g = 0; g < OWN / 8; ++g) {
+                                // bytes of the keys that there are
+                                const int there = min(max(end_key - (kt + own0 + 8 * g), 0), 8) * row_v;
+#pragma unroll
+                                for (int part = 0; part < RUN_LOADS; ++part) {
+                                    const unsigned of = (unsigned)(16 * lane + BYTES * part), at = stage + (unsigned)((in_stage + 8 * g) * row_v) + of;
+                                    if (of >= run_bytes) continue;
+                                    i32x4 v = without_odd<T>(at_lds<i32x4>(at), odd);
+                                    if ((int)of >= there) v.x = v.y = 0;
+                                    if ((int)of + 8 >= there) v.z = v.w = 0;
+                                    at_lds<i32x4>(at) = v;
+                                }
+                            }
+                        } else
 #pragma unroll
                         for (int x = 0; x < OWN / GK; ++x) {
                             const unsigned at = stage + (unsigned)((in_stage + GK * x) * ROW + 16 * lane);
@@ -441,7 +475,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             constexpr int PER = 64 * NW / CH, LI = KEYS / PER, BYTES = stage_bytes(DP, RW, KW, LOAD);
             static_assert(PER * LI == KEYS, "whole loads");
             const int chunk = lane % CH, to_key = GK * wave + lane / CH;
-            const unsigned to_k = (unsigned)(to_key * ROW_K + 16 * chunk), to_v = (unsigned)(KEYS * ROW_K + to_key * ROW_V + 16 * chunk);
+            const unsigned to_k = (unsigned)(to_key * row_k + 16 * chunk), to_v = (unsigned)(KEYS * row_k + to_key * row_v + 16 * chunk);
             i32x4 kr[LI], vr[LI];
             int ids[LI];
             unsigned bad = 0;                  // ids: the next keys' pages; bad: a bit for each loaded key that is in none
@@ -482,11 +516,11 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 }
 #pragma unroll
                 for (int i = 0; i < LI; ++i) {
-                    *(i32x4*)(to + to_k + PER * i * ROW_K) = chunk_moved<false>(kr[i], chunk, p.D);
-                    *(i32x4*)(to + to_v + PER * i * ROW_V) = chunk_moved<false>(vr[i], chunk, p.D);
+                    *(i32x4*)(to + to_k + PER * i * row_k) = chunk_moved<false>(kr[i], chunk, p.D);
+                    *(i32x4*)(to + to_v + PER * i * row_v) = chunk_moved<false>(vr[i], chunk, p.D);
                 }
             };
-            const unsigned own_k = (unsigned)(WK * kw * ROW_K), own_v = (unsigned)(KEYS * ROW_K + WK * kw * ROW_V);
+            const unsigned own_k = (unsigned)(WK * kw * row_k), own_v = (unsigned)(KEYS * row_k + WK * kw * row_v);
             look_up(first_key);
             load(first_key);
             look_up(first_key + KEYS);
@@ -524,7 +558,17 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         for (int ks = 0; ks < KS; ++ks) {
             const unsigned at = k_at(base, ks);
 #pragma unroll
-            for (int i = 0; i < KT; ++i) s[i] = mfma32(__builtin_bit_cast(x8, at_lds<i32x4>(at + 32 * i * ROW_K)), q[ks], s[i]);
+            for (int i = 0; i < KT; ++i) {
+                i32x4 k;
+                if constexpr (RUNS) {
+                    // (behind a row is the next one, whatever it holds)
+                    const int left = p.D - 8 * half - 16 * ks;
+                    const i32x2 a = at_lds<i32x2>(at + 32 * i * row_k), b = at_lds<i32x2>(at + 32 * i * row_k + 8);
+                    if (DP == 64 || 2 * ks >= KS) k = i32x4{left > 0 ? a.x : 0, left > 0 ? a.y : 0, left > 4 ? b.x : 0, left > 4 ? b.y : 0};
+                    else k = i32x4{a.x, a.y, b.x, b.y};
+                } else k = at_lds<i32x4>(at + 32 * i * row_k);
+                s[i] = mfma32(__builtin_bit_cast(x8, k), q[ks], s[i]);
+            }
         }
         in_turn<KS * KT, 1, 1, 6, 0, 0>();
     };
@@ -556,7 +600,10 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) zero[e & 3] = __builtin_fmaf(o[dt][e], 0.0f, zero[e & 3]);
+            for (int e = 0; e < 16; ++e) {
+                if (RUNS && 32 * dt + 8 * (e >> 2) + 4 * half >= p.D) continue;
+                zero[e & 3] = __builtin_fmaf(o[dt][e], 0.0f, zero[e & 3]);
+            }
         return zero[0] + zero[1] + zero[2] + zero[3] == 0.0f;
     };
     const float none = -__builtin_inff();
@@ -594,7 +641,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 }
             };
             auto read_v = [&](int st, int dt) {
-                const s16x4 v0 = lds_read_transposed(v_from[dt] + 16 * st * ROW_V), v1 = lds_read_transposed(v_from[dt] + (16 * st + 8) * ROW_V);
+                const s16x4 v0 = lds_read_transposed(v_from[dt] + 16 * st * row_v), v1 = lds_read_transposed(v_from[dt] + (16 * st + 8) * row_v);
                 return __builtin_bit_cast(x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
             };
 #pragma unroll
@@ -758,10 +805,11 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         }
     }
     if (odd != 0.0f) again[1] = 1;
-    __syncthreads();
+    wg_barrier_lds();                          // (no wait for the stores)
     if (__builtin_expect(again[1] != 0, 0)) {
         // every wave settles its own rows, or its share of them
         __threadfence();
+        __syncthreads();
         unsigned rows = 0;
         for (int r = kw; r < 32; r += KW) {
             const float factor = row_factor[FEW ? r : 32 * wave + r];

@@ -38,6 +38,8 @@ template <class T, int DP, int TERMS>
 int launch_loads(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) {
     if (a.load == kWholeVectors) return launch_parts<T, DP, TERMS, kWholeVectors>(a, p, stream);
     if (a.load == kVectors) return launch_parts<T, DP, TERMS, kVectors>(a, p, stream);
+    if constexpr (DP <= 128)
+        if (a.load == kRuns) return launch_parts<T, DP, TERMS, kRuns>(a, p, stream);
     if (a.load == kDwords) return launch_parts<T, DP, TERMS, kDwords>(a, p, stream);
     return launch_parts<T, DP, TERMS, kThroughRegisters>(a, p, stream);
 }

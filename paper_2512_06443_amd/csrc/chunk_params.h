@@ -32,8 +32,9 @@ struct ChunkParams {
 
 constexpr int kFewRows = 32, kManyRows = 128;        // of a tile
 
-// How keys and values come to LDS: through registers; straight, a dword or 16 bytes a lane; of rows that are as long as LDS has them.
-constexpr int kThroughRegisters = 0, kDwords = 1, kVectors = 2, kWholeVectors = 3;
+// How keys and values come to LDS: through registers; straight, a dword or 16 bytes a lane; of rows that are as long as LDS has them; rows of 4, 12, 20, ... features that
+// lie one behind the other in memory, 8 of them (16 D bytes) at a time and one behind the other in LDS too.
+constexpr int kThroughRegisters = 0, kDwords = 1, kVectors = 2, kWholeVectors = 3, kRuns = 4;
 
 // A workgroup's waves: RW groups of 32 rows, the keys of a step shared by KW.  Where rows are few 1 x 4 (features past 128: 1 x 2); where they are many 4 x 1 or 4 x 2
 // (features past 128: 4 x 1).  Of the workgroups of four waves a unit has room for two, of 4 x 1 with features past 128 for one.

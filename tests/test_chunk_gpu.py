@@ -173,11 +173,12 @@ def page_of(c, b, t):
 
 
 @pytest.mark.parametrize("dtype,out", [(BF16, BF16), (F16, F32), (F16, F16)])
-@pytest.mark.parametrize("news,lens", [([6], [500]), ([150], [400]), ([1, 100], [77, 300])])
-def test_values_and_keys_that_are_no_numbers(news, lens, dtype, out):
+@pytest.mark.parametrize("news,lens", [([6], [500]), ([150], [400]), ([1, 100], [77, 300]), ([5], [2500])])
+@pytest.mark.parametrize("D", [128, 100, 36])
+def test_values_and_keys_that_are_no_numbers(D, news, lens, dtype, out):
     """Behind a query's position, outside its window or behind the sequence's end they have no influence; seen, an infinity makes its feature infinite."""
     window = 60
-    Hq, Hk, D = 6, 3, 128
+    Hq, Hk = 6, 3
     c = case(news, lens, Hq, Hk, D, dtype, 16, seed=9)
     clean = {w: run(c, w, out) for w in (0, window)}
     b = len(news) - 1
@@ -251,9 +252,10 @@ def test_keys_that_score_minus_infinity():
     assert bool((lse[3:3 + 20, 0] == -INF).all() and (got[3:23, 0] == 0).all())
 
 
-def test_lengths_pages_and_starts_that_cannot_be():
+@pytest.mark.parametrize("D", [64, 60])
+def test_lengths_pages_and_starts_that_cannot_be(D):
     """Found on the device: nothing is read, and who depends on it gets NaN."""
-    c = case([2, 80, 1, 3], [100, 200, 150, 60], 4, 2, 64, BF16, 16, seed=4)
+    c = case([2, 80, 1, 3], [100, 200, 150, 60], 4, 2, D, BF16, 16, seed=4)
     clean, clean_lse = run(c, max_len=200)
     rows = [slice(0, 2), slice(2, 82), slice(82, 83), slice(83, 86)]
     for b, length in ((0, 201), (1, -1), (1, 2 ** 30), (2, -2 ** 31)):
@@ -289,6 +291,27 @@ def test_lengths_pages_and_starts_that_cannot_be():
     # more queries than said: NaN where few rows are all there is
     got, lse = run(c, max_len=200, max_queries=3)
     assert torch.equal(got[:2], clean[:2]) and torch.equal(got[82:86], clean[82:86]) and bool(got[2:82].isnan().all() and lse[2:82].isnan().all())
+
+
+@pytest.mark.parametrize("D", [128, 60])
+def test_pages_that_cannot_be_in_parts(D):
+    """Of few rows and of many: whoever sees the keys of such a page gets NaN, whatever part they are in."""
+    c = case([2, 1, 3], [4000, 2500, 100], 4, 2, D, BF16, 16, seed=14)
+    assert B.query_chunk_attention(6, 3, 4, 2, D, 3, 4000)[1] > 2
+    clean, clean_lse = run(c, max_len=4000, max_queries=3)
+    check(c, clean, clean_lse)
+    d = case([1, 80], [300, 3000], 4, 2, D, BF16, 16, seed=15)
+    assert B.query_chunk_attention(81, 2, 4, 2, D, 80, 3000)[4] > 2
+    clean_many, _ = run(d, max_len=3000, max_queries=80)
+    for place in (0, 40, 130):
+        bad = dict(c, page_table=c["page_table"].clone())
+        bad["page_table"][0, place] = -1
+        got, lse = run(bad, max_len=4000, max_queries=3)
+        assert bool(got[:2].isnan().all() and lse[:2].isnan().all()) and torch.equal(got[2:6], clean[2:6])
+        bad = dict(d, page_table=d["page_table"].clone())
+        bad["page_table"][1, place] = 2 ** 30
+        got, _ = run(bad, max_len=3000, max_queries=80)
+        assert bool(got[1:81].isnan().all()) and torch.equal(got[:1], clean_many[:1])
 
 
 def test_views_and_a_workspace_of_the_callers():
