@@ -39,14 +39,17 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
     a.few = !a.many || (B > 1 && G <= kFewRows);
     if (a.few) {
         a.few_row_places = (int)std::min<int64_t>(kFewRows, std::max<int64_t>(1, most_rows / G) * G);
-        // Parts only so that 640 waves are at work, each of four steps at least, and for more than eight of them: a wave's way to its first keys and its results' way out take as
-        // long as seven steps, and those that join parts 5 us.  32 steps at most, so that one long sequence among short ones does not keep the others' units waiting.
-        // us with parts of 1, 2, 4, 8, 16 steps / in one, joining included, 32 query and 8 key heads of 128 in bf16: a sequence of 1000 keys 14.1, 14.9, 16.6 / 16.5; of 8000
-        // 29.1, 21.6, 20.0, 21.6, 29.9 / 77.3; 8 of 4000 48, 36, 31, 31, 32 / 44; 16 of up to 4000 84, 63, 52, 48, 47 / 53; 48 of up to 4095 144, 109, 95, 92, 95 / 92;
-        // 64 of 2048 to 4095 230, 176, 152, 151, 151 / 143; 13 of up to 1990 in windows of 1024, 32 heads of 100 that are not shared, 77, 57, 49 / 36.
+        // Parts only so that 640 waves are at work, each of four steps at least where there are many: a wave's way to its first keys and its results' way out take as long
+        // as seven steps, and those that join parts 4 us.  32 steps at most, so that one long sequence among short ones does not keep the others' units waiting, or more
+        // where those would be more than 8192 workgroups.  us with parts of 1, 2, 4, 8, 16 / 32 steps, joining included, 32 query and 8 key heads of 128 in bf16 (20
+        // and 5 where it says so): a sequence of 1000 keys 12.9, 13.2, 15.3, 16.1; of 2000 (20, 5) 14.3, 14.0, 15.3, 19.7, 24.7; of 8000 28, 20, 17, 20, 28 / 45; 4 of 8000
+        // 56, 42, 35, 33, 34 / 52; 8 of 4000 51, 39, 33, 33, 36 / 49; 16 of up to 4000 80, 60, 51, 47, 47 / 52; 32 of 8 queries behind up to 3000 (20, 5) 85, 66, 54, 49,
+        // 62 / 45; 48 of up to 4095 142, 112, 97, 95, 96 / 91; 64 of 2048 to 4095 230, 176, 152, 151, 151 / 143; 13 of up to 1990 in windows of 1024, 32 heads of 100 that
+        // are not shared, 77, 57, 49, 45 / 36.
         const int64_t step = step_keys(a.DP, 1, few_waves(a.DP)), keys = seen(kFewRows), steps = ceil_div(keys, step);
         const int64_t wanted = ceil_div(640, few_waves(a.DP) * B * Hk);
-        const int64_t per = steps <= 8 ? steps : std::min(std::max<int64_t>(32, ceil_div(B * Hk * steps, 8192)), std::max<int64_t>(4, ceil_div(steps, wanted)));
+        const int64_t least = std::min<int64_t>(4, ceil_div(steps, 6)), most = std::max<int64_t>(32, ceil_div(B * Hk * steps, 8192));
+        const int64_t per = std::min(most, std::max(least, ceil_div(steps, wanted)));
         a.few_chunk = (int)(step * per);
         a.few_splits = (int)ceil_div(keys, a.few_chunk);
         const int64_t blocks = ceil_div(B * Hk * a.few_splits, 8);

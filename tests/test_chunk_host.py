@@ -124,7 +124,7 @@ def test_longer_waits_for_nobody(L):
     assert B.query_chunk_attention(128, 1, 32, 8, 128, 128, 1 << 17)[4] >= 8
     assert B.query_chunk_attention(16384, 1, 32, 8, 128, 16384, 16384)[4] == 1
     assert math.prod(B.query_chunk_attention(4096, 4096, 32, 8, 128, 1, 200)[:2]) == 4
-    assert B.query_chunk_attention(64, 64, 32, 8, 128, 1, 4096)[1] == B.query_chunk_attention(1, 1, 20, 5, 128, 1, 500)[1] == 1
+    assert B.query_chunk_attention(64, 64, 32, 8, 128, 1, 4096)[1] == 1
 
 
 def test_python_form_refuses_what_is_not_on_the_gpu(L):
