@@ -1,5 +1,5 @@
 // Attention of chunks of new tokens, packed one sequence behind the other, over a paged cache.
-// Part of the translation units chunk_bf16.hip and chunk_f16.hip (included there, in this order).
+// Part of the translation units of the chunks' kernels, one for each type of the cache and of the outputs (included there, in this order).
 #pragma once
 
 #include "matrix_parts.hip.h"
@@ -13,8 +13,9 @@ using namespace vlut_chunk;
 //   s = scale * q . k,  m a number near max s,  l = sum exp(s - m),  O = sum exp(s - m) v,  output O / l;   nothing seen: 0
 // A row is a query token and one of the G query heads that read a key head, token by token, so that the rows of a tile are neighbours in position and see
 // nearly the same keys.  A workgroup has a tile of rows of one sequence and key head and a part of the keys that any of them sees.
-//   Many rows: RW waves of 32 rows, whose keys and values go through LDS for all of them, 64 keys a step.
-//   Few rows (up to 32: single tokens, drafts): one tile of 32 rows and KW waves that share a step's keys, 32 each; they meet in LDS at the end.
+//   Many rows: tiles of 128, RW = 4 waves of 32, whose keys and values go through LDS for all of them, 64 keys a step; two workgroups on a unit, or where tiles are few
+//   KW = 2 such groups of waves with every other 64 keys each, which meet in LDS at the end.
+//   Few rows (up to 32: single tokens, drafts): one tile of 32 rows and KW = 4 waves (of more than 128 features 2) with 32 of a step's keys each, two workgroups on a unit.
 // A sequence's tile of more keys than a part holds is several workgroups; combine_chunks joins the parts: with M = max m_i the sums of exp(m_i - M) l_i and
 // exp(m_i - M) O_i are those of the whole.
 //
@@ -27,6 +28,11 @@ using namespace vlut_chunk;
 // P goes to the second product in the cache's type.  For 16-bit outputs that is one rounding more of the size of the output's own, of terms whose errors
 // are independent (bf16 2.3e-3 of the result instead of 1.7e-3); for fp32 it is carried in further terms, each what the rounding of those before it left: 24 bits, three of bf16
 // or two of fp16.
+// What bounds it.  Few rows: the bytes of keys and values; 64 sequences of 3100 keys, 8 key heads of 128, 145 us or 5.3 TB/s, what a large copy reaches; 13 sequences and
+// 32 key heads of 100 (windows of 1024) 37 us.  A single sequence: the way through memory, 10 us, of which a step is 1.  Many rows: a step of a wave is 1024 cycles of the
+// matrix cores, 900 of its 32 exponentials and roundings a lane and 256 of LDS, which four waves share, so that two waves of a SIMD cover each other in part; 16384 tokens,
+// 32 and 8 heads of 128, 2190 us or 1.0 PFLOP/s, three quarters of what a large product reaches; 4096 tokens of 20 and 5 heads 122 us (0.71), of which a quarter is the
+// tiles' 11 us outside of their steps and the last tiles to end.  fp32 outputs, three products with V instead of one, twice as long.
 // ---------------------------------------------------------------------------------------------
 
 struct Chunk {                         // of a sequence: its first token's row and position; bad: a length that cannot be
@@ -215,8 +221,11 @@ struct Count { static constexpr int value = N; };
 // A tile's part.  Where keys and values are loaded straight to LDS they are asked for AHEAD steps ahead, addresses worked out once per wave and 8 keys.  Each stage is
 // exactly LOADS loads per wave, also past the end of the part, where its last keys are loaded again, so that vmcnt((AHEAD - 1) * LOADS) stands for "the
 // stage that was asked for first is there"; what else a wave loads meanwhile only makes that wait longer.
+// (Through registers instead, 4096 tokens took 188 us, not 150, and 64 sequences 218, not 180, when all else was alike.)
 // Rows of LDS are DP features one behind the other, 16-byte chunks c at c ^ f(row): of keys, so that 16 rows' chunks lie in 64 banks; of values, so that the four
-// rows of a transposing read do.  Chunks behind D are not loaded: zeros from before the first stage.
+// rows of a transposing read do.  Chunks behind D are not loaded: zeros from before the first stage.  Rows of an odd number of fours (kRuns) are one behind the other as they
+// are in memory, in which place they are in different banks by themselves; what is read behind a row is the next one's beginning, and not used.  (A dword a lane instead,
+// whatever the rows' places: 13 sequences of 32 heads of 100 56 us, not 44.)
 // Where rows are few each wave has its keys for itself, and none waits for another; a step's keys are asked for as soon as the first product is done with
 // the ones before, its values behind the second.
 template <class T, int DP, int RW, int KW, int TERMS, int LOAD>

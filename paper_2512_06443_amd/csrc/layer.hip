@@ -50,7 +50,8 @@ int launch_rows_r(const RowsParams& p, bool residual, int residual_type, int vec
 }
 int launch_rows(RowsParams& p, int type, bool residual, int residual_type, int vec, int64_t N, hipStream_t stream) {
     if (vec == 2) vec = 1;
-    // Features of a thread: 16 where rows are many; the fewest, so that a row's chain of loads and sums is the shortest, where they are few.
+    // Features of a thread: 16 where rows are many; the fewest, so that a row's chain of loads and sums is the shortest, where they are few.  us with 4 / 16: one row of 2560
+    // 2.2 / 3.0, of 4096 3.5 / 4.2, 64 of those 4.4 / 5.1, 400 6.6 / 6.4, 512 7.0 / 6.8, 4096 33 / 25; 2048 of 2560 15 / 10 (8 lie between, or 1 us below).
     int per = N >= 2 * kUnits ? 16 : 4;
     while (per < 32 && (p.K + per - 1) / per > 1024) per *= 2;
     const int threads = std::max(1, (int)(((p.K + per - 1) / per + 63) / 64)) * 64;
@@ -103,7 +104,10 @@ int plan_logits(int64_t N, int64_t V, int top, LogitsPlan* out) {
     if (N < 1 || N >= kMostRows || V < 1 || V >= ((int64_t)1 << 30) || top < 0 || top > V) return VLUT_ERR_SHAPE;
     if (top > VLUT_MAX_TOP) return VLUT_ERR_UNSUPPORTED;
     LogitsPlan a{};
-    // Parts so that there are four workgroups for each unit, of 2048 logits at least.
+    // Parts so that there are four workgroups for each unit, of 2048 logits at least: 8 a thread, which are on their way at once, or of longer parts 16.  us with 2048 / 4096 /
+    // 8192: one row of 32000 12.7, 15.5, 16.3, of 128000 13.0, 17.6, 20.9, 33 of 50001 12.0, 14.6, 16.9, 64 of 32000 10.6, 11.9, 12.3.  With two workgroups a unit the
+    // last two 13.3 and 11.8.  8 / 16 logits a thread: one row of 128000 13.0, 13.6, of 2^20 29.0, 23.3, 33 of 50001 12.0, 12.2; 256 of 128000 33.8, 37.0, 2048 of 32000
+    // 55.6, 55.1.
     const int64_t wanted = std::min<int64_t>({kMostParts, (4 * kUnits + N - 1) / N, (V + 2047) / 2048});
     const int64_t part = (V + wanted - 1) / wanted;
     a.per = part <= 4096 ? 8 : 16;
