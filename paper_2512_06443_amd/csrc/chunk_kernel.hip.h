@@ -31,8 +31,8 @@ using namespace vlut_chunk;
 // What bounds it.  Few rows: the bytes of keys and values; 64 sequences of 3100 keys, 8 key heads of 128, 145 us or 5.3 TB/s, what a large copy reaches; 13 sequences and
 // 32 key heads of 100 (windows of 1024) 37 us.  A single sequence: the way through memory, 10 us, of which a step is 1.  Many rows: a step of a wave is 1024 cycles of the
 // matrix cores, 900 of its 32 exponentials and roundings a lane and 256 of LDS, which four waves share, so that two waves of a SIMD cover each other in part; 16384 tokens,
-// 32 and 8 heads of 128, 2190 us or 1.0 PFLOP/s, three quarters of what a large product reaches; 4096 tokens of 20 and 5 heads 122 us (0.71), of which a quarter is the
-// tiles' 11 us outside of their steps and the last tiles to end.  fp32 outputs, three products with V instead of one, twice as long.
+// 32 and 8 heads of 128, 2170 us or 1.0 PFLOP/s, three quarters of what a large product reaches; 4096 tokens of 20 and 5 heads 114 us (0.75), of which a quarter is
+// units that wait for the last tiles.  (With every other tile from the lighter end, and an XCD's tiles one stretch of them: 122 us.)  fp32 outputs, three products with V instead of one, twice as long.
 // ---------------------------------------------------------------------------------------------
 
 struct Chunk {                         // of a sequence: its first token's row and position; bad: a length that cannot be
@@ -859,25 +859,25 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int i, unsigned c
     attend_chunk<T, DP, 1, few_waves(DP), TERMS, LOAD>(p, t, lds);
 }
 
-// Workgroup `i` of those for many rows: tile `at` of the sequences' tiles, one sequence behind the other.  Of a sequence's tiles those that see the most and the least take turns,
-// so that any stretch of them is about the same work.
+// Workgroup `i` of those for many rows: tile `at` of the sequences' tiles, one sequence behind the other, of each the one that sees most first; their parts and key heads
+// side by side.
 template <class T, int DP, int KW, int TERMS, int LOAD>
 __device__ __forceinline__ void many_rows(const ChunkParams& p, int i, unsigned char* lds) {
     constexpr int RW = 4, ROWS = kManyRows;
     static_assert(ROWS == 32 * RW, "32 rows a wave");
     const int lane = (int)threadIdx.x & 63;
-    int at = i % p.many_tiles;
     Tile t;
-    t.split = i / p.many_tiles % p.many_splits;
-    t.h = i / p.many_tiles / p.many_splits;
-    if (t.h >= p.Hk) return;
+    t.h = i % p.Hk;
+    t.split = i / p.Hk % p.many_splits;
+    int at = i / p.Hk / p.many_splits;
+    if (at >= p.many_tiles) return;
     t.b = -1;
     if (p.B == 1) {
         t.seq = chunk_of(p, 0);
         const int rows = t.seq.queries * p.G, tiles = rows > p.few_rows ? (rows + ROWS - 1) / ROWS : 0;
         if (at < tiles) {
             t.b = 0;
-            at = at & 1 ? at >> 1 : tiles - 1 - (at >> 1);
+            at = tiles - 1 - at;
         }
     } else for (int b0 = 0; b0 < p.B; b0 += 64) {
         const Chunk c = b0 + lane < p.B ? chunk_of(p, b0 + lane) : Chunk{};
@@ -890,9 +890,9 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int i, unsigned 
         }
         const uint64_t past = __ballot(sum > at);
         if (past) {
-            const int f = __builtin_ctzll(past), its = __shfl(tiles, f), in = at - (__shfl(sum, f) - its);
+            const int f = __builtin_ctzll(past), t_end = __shfl(sum, f);
             t.b = b0 + f;
-            at = in & 1 ? in >> 1 : its - 1 - (in >> 1);
+            at = t_end - 1 - at;
             auto its_own = [&](int x) { return __builtin_amdgcn_readlane(x, __builtin_amdgcn_readfirstlane(f)); };
             t.seq = Chunk{its_own(c.start), its_own(c.queries), its_own(c.len), its_own(c.base), its_own(c.bad)};
             break;
@@ -914,16 +914,16 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int i, unsigned 
     attend_chunk<T, DP, RW, KW, TERMS, LOAD>(p, t, lds);
 }
 
-// Workgroups go to the 8 XCDs in turn, and tiles of one key head, which read the same keys, to one XCD (one L2) as far as that goes.  An XCD begins with its tiles that
-// see much (every other one) and ends with those that see little; where its 32 units have room for two, the second ones go the other way, so that who has the most has the
-// least beside it.
+// Workgroups go to the 8 XCDs in turn, so that an XCD has every eighth of them: those of one key head, or of few, which read the same keys, where 8 and the number of key
+// heads have a divisor, and tiles that see much and little alike.  Where its 32 units have room for two workgroups each, the second ones go the other way, so that who has
+// the most has the least beside it.
 template <class T, int DP, int KW, int TERMS, int LOAD>
 __global__ void __launch_bounds__(256 * KW, DP > 128 ? 1 : 2) many_rows_kernel(const ChunkParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
-    const int xcd = (int)blockIdx.x & 7, n = p.many_per_xcd, heavy = (n + 1) / 2, both = min(n, 64);
+    const int both = min(p.many_per_xcd, 64);
     int place = (int)blockIdx.x >> 3;
     if (KW == 1 && DP <= 128 && place >= 32 && place < both) place = both - 1 - (place - 32);
-    many_rows<T, DP, KW, TERMS, LOAD>(p, xcd * n + (place < heavy ? 2 * place : 2 * (n - 1 - place) + 1), lds);
+    many_rows<T, DP, KW, TERMS, LOAD>(p, 8 * place + ((int)blockIdx.x & 7), lds);
 }
 template <class T, int DP, int TERMS, int LOAD>
 __global__ void __launch_bounds__(64 * few_waves(DP), DP > 128 ? 1 : 2) few_rows_kernel(const ChunkParams p) {
