@@ -330,6 +330,39 @@ def test_views_and_a_workspace_of_the_callers():
     assert torch.equal(B.chunk_attention(**c, max_len=1416, workspace=ws[:need])[0], first) and bool((ws[need:] == 255).all())
 
 
+@pytest.mark.parametrize("Hq,Hk,D", [(2, 1, 128), (6, 3, 36)])
+def test_more_sequences_than_a_wave_has_lanes(Hq, Hk, D):
+    """Of all kinds in any order, long ones among them in parts, and prompts whose tiles are found among all sequences'."""
+    news = [(0, 1, 2, 45, 1, 7, 0, 130, 1, 3)[(7 * i + i // 10) % 10] for i in range(150)]
+    lens = [n + (0, 5, 3100, 64, 700)[(3 * i + i // 7) % 5] for i, n in enumerate(news)]
+    c = case(news, lens, Hq, Hk, D, BF16, 16, seed=21)
+    assert B.query_chunk_attention(sum(news) + 3, 150, Hq, Hk, D, 130, max(lens))[1] >= (2 if Hk == 1 else 1)
+    for window in (0, 200):
+        got, lse = run(c, window, max_queries=130, max_len=max(lens))
+        check(c, got, lse, window)
+
+
+def test_scale_nothing_to_do_and_pages_for_all():
+    c = case([70, 3, 1], [90, 300, 1500], 8, 2, 64, F16, 16, seed=22)
+    for scale in (1e-3, 0.02, 0.7):
+        got, lse = run(c, scale=scale)
+        check(c, got, lse, scale=scale, ref=reference(c, 0, scale))
+    # no sequence has a token: nothing is written, whatever the lengths say
+    d = dict(c, query_starts=torch.zeros(4, dtype=torch.int32, device="cuda"))
+    run(d)
+    run(d, max_queries=0)
+    # nothing is to be seen: 0
+    d = dict(c, lens=torch.zeros(3, dtype=torch.int32, device="cuda"))
+    got, lse = run(d, max_len=0)
+    assert bool((got[:74] == 0).all() and (lse[:74] == -INF).all())
+    # one row of pages for all sequences
+    d = dict(c, page_table=c["page_table"][2:3].expand(3, -1))
+    got, lse = run(d)
+    check(d, got, lse)
+    e = dict(d, page_table=d["page_table"].contiguous())
+    assert torch.equal(run(e)[0], got)
+
+
 def test_a_cache_past_32_bits():
     """Pages whose elements lie past 2^31, and with strides past what 31 bits hold (the path of addresses per key)."""
     Hk, page, D = 2, 64, 128
