@@ -234,6 +234,9 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     typedef typename Output<T, TERMS>::type O;
     constexpr bool FEW = RW == 1, WIDE = Number<T>::kWide, DIRECT = LOAD != kThroughRegisters, RUNS = LOAD == kRuns, OWN_KEYS = own_keys(RW, LOAD);
     constexpr int NW = RW * KW, WK = wave_keys(DP, RW), KT = WK / 32, KEYS = step_keys(DP, RW, KW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
+    // Of a SIMD's two waves the one with matrix instructions alone goes first, then the one whose products with V have weights between them, so that they take turns: 1024 behind
+    // 16384 298 -> 279 us, behind 8192 171 -> 162, 4096 tokens 116 -> 113.  64 features, whose products are half as long beside as many weights, 92 -> 97: not there.
+    constexpr bool TURNS = !FEW && DP == 128;
     constexpr float LIFT = 0.5f * Number<T>::kLift;            // (scores after the first step may be larger)
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
@@ -559,6 +562,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     f32x16 s[KT], o[DT];
     float m = 0.0f, l;
     auto multiply = [&](int, unsigned base) {
+        if constexpr (TURNS) __builtin_amdgcn_s_setprio(2);
 #pragma unroll
         for (int i = 0; i < KT; ++i)
 #pragma unroll
@@ -580,6 +584,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             }
         }
         in_turn<KS * KT, 1, 1, 6, 0, 0>();
+        if constexpr (TURNS) __builtin_amdgcn_s_setprio(0);
     };
     auto hide = [&](int k0) {
         if (k0 + WK > all_to || k0 < all_from) {
@@ -657,6 +662,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             for (int dt = 0; dt < DT; ++dt) vf[dt] = read_v(0, dt);
             weigh(0, pf);
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (TURNS) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int st = 0; st < 2 * KT; ++st) {
                 if (st + 1 < 2 * KT) weigh(st + 1, next);
@@ -671,6 +677,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 in_turn<DT, TERMS, 2, 0, 20 * TERMS / DT, 8 / DT>();
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if constexpr (TURNS) __builtin_amdgcn_s_setprio(0);
             pinned(l);                         // (or the sums are made behind the loop, from registers that wait for that)
         };
         sweep(multiply, weigh_up);
