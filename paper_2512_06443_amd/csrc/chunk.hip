@@ -67,9 +67,9 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
         // As many as there are if all sequences with many rows have as many as they may have.
         const int64_t tiles = std::min<int64_t>(a.many_tiles, ceil_div(rows, most_rows) * ceil_div(most_rows, kManyRows)) * Hk;
         // Two workgroups of four waves on a unit, one's waits beside the other's work, where there are tiles for that; else one whose eight waves share the keys, unless
-        // those are so many that parts of them are as good.  us, 4 x 1 / 4 x 2, 20 query and 5 key heads of 128 in bf16: 4096 tokens 113 / 128, in windows of 16 24 / 37, of
-        // 1024 79 / 93, 2500 tokens 66 / 56; 32 and 8 heads: 16384 tokens 2190 / 2410, 4096 155 / 183, of 64 features 91 / 123, 2048 59 / 58, 1024 40 / 27 (parts joined
-        // included), behind 4096 105 / 97, 8192 171 / 167, 16384 304 / 309; 256 behind 16384 89 / 89; 32 heads of 100 that are not shared, 909 tokens in windows of 1024, 67 / 46.
+        // those are so many that parts of them are as good.  us, 4 x 1 / 4 x 2, parts joined included, 20 query and 5 key heads of 128 in bf16: 4096 tokens 109 / 121, in
+        // windows of 16 24 / 37, of 1024 80 / 89, 2500 tokens 62 / 55; 32 and 8 heads: 16384 tokens 2070 / 2290, 4096 141 / 173, of 64 features 91 / 124, 2048 56 / 56, 1024
+        // 39 / 26, behind 4096 97 / 93, 8192 157 / 159, 16384 285 / 289; 256 behind 16384 82 / 84; 32 heads of 100 that are not shared, 909 tokens in windows of 1024, 53 / 50.
         a.key_waves = a.DP <= 128 && tiles < 2 * kUnits && keys < 12288 ? 2 : 1;
         const int64_t slots = (a.DP <= 128 && a.key_waves == 1 ? 2 : 1) * kUnits, step = step_keys(a.DP, 4, a.key_waves);
         const int64_t splits = std::min(std::max<int64_t>(1, slots / tiles), ceil_div(keys, 512));

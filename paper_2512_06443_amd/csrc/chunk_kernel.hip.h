@@ -31,8 +31,9 @@ using namespace vlut_chunk;
 // What bounds it.  Few rows: the bytes of keys and values; 64 sequences of 3100 keys, 8 key heads of 128, 145 us or 5.3 TB/s, what a large copy reaches; 13 sequences and
 // 32 key heads of 100 (windows of 1024) 37 us.  A single sequence: the way through memory, 10 us, of which a step is 1.  Many rows: a step of a wave is 1024 cycles of the
 // matrix cores, 900 of its 32 exponentials and roundings a lane and 256 of LDS, which four waves share, so that two waves of a SIMD cover each other in part; 16384 tokens,
-// 32 and 8 heads of 128, 2170 us or 1.0 PFLOP/s, three quarters of what a large product reaches; 4096 tokens of 20 and 5 heads 114 us (0.75), of which a quarter is
-// units that wait for the last tiles.  (With every other tile from the lighter end, and an XCD's tiles one stretch of them: 122 us.)  fp32 outputs, three products with V instead of one, twice as long.
+// 32 and 8 heads of 128, 2070 us or 1.06 PFLOP/s, four fifths of what a large product reaches; 4096 tokens of 20 and 5 heads 109 us (0.79), of which a quarter is units that
+// wait for the last tiles.  (With every other tile from the lighter end, and an XCD's tiles one stretch of them, 8 us more.)  fp32 outputs, three products with V
+// instead of one, twice as long.
 // ---------------------------------------------------------------------------------------------
 
 struct Chunk {                         // of a sequence: its first token's row and position; bad: a length that cannot be
