@@ -342,6 +342,24 @@ def test_more_sequences_than_a_wave_has_lanes(Hq, Hk, D):
         check(c, got, lse, window)
 
 
+def test_parts_of_more_keys_than_page_numbers_are_kept_for():
+    """A part whose pages' numbers come in several loads: of few rows where workgroups are many, of many rows where tiles are."""
+    gen = generator(23)
+    k, v = (torch.randn(400, 8, 16, 64, generator=gen, device="cuda").to(BF16) for _ in "kv")
+    lens = torch.tensor([{5: 5000, 700: 4097, 1199: 4096}.get(i, 1 + i % 7) for i in range(1200)], dtype=torch.int32, device="cuda")
+    table = torch.stack([torch.randperm(400, generator=gen, device="cuda")[:313] for _ in range(1200)]).int()
+    c = dict(q=torch.randn(1200, 8, 64, generator=gen, device="cuda").to(BF16), k_cache=k, v_cache=v, page_table=table,
+             query_starts=torch.arange(1201, dtype=torch.int32, device="cuda"), lens=lens)
+    assert B.query_chunk_attention(1200, 1200, 8, 8, 64, 1, 5000)[1:3] == (1, 5120)
+    got, lse = run(c, max_queries=1, max_len=5000)
+    check(c, got, lse)
+    c = case([200], [9000], 256, 256, 8, F16, 32, seed=24)
+    parts, keys = B.query_chunk_attention(203, 1, 256, 256, 8, 200, 9000)[4:]
+    assert parts == 1 and keys >= 9000
+    got, lse = run(c, max_len=9000, max_queries=200)
+    check(c, got, lse)
+
+
 def test_scale_nothing_to_do_and_pages_for_all():
     c = case([70, 3, 1], [90, 300, 1500], 8, 2, 64, F16, 16, seed=22)
     for scale in (1e-3, 0.02, 0.7):
