@@ -13,4 +13,4 @@
 #include "chunk_kernel.hip.h"
 #include "chunk_launch.hip.h"
 
-int vlut_chunk::launch_bf16(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) { return launch_chunks<__bf16, 1>(a, p, stream); }
+int vlut_chunk::launch_bf16(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) { return launch_chunks<__bf16, __bf16>(a, p, stream); }

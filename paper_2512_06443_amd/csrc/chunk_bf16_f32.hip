@@ -13,4 +13,4 @@
 #include "chunk_kernel.hip.h"
 #include "chunk_launch.hip.h"
 
-int vlut_chunk::launch_bf16_f32(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) { return launch_chunks<__bf16, Number<__bf16>::kTerms>(a, p, stream); }
+int vlut_chunk::launch_bf16_f32(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) { return launch_chunks<__bf16, float>(a, p, stream); }

@@ -13,4 +13,4 @@
 #include "chunk_kernel.hip.h"
 #include "chunk_launch.hip.h"
 
-int vlut_chunk::launch_f16(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) { return launch_chunks<_Float16, 1>(a, p, stream); }
+int vlut_chunk::launch_f16(const ChunkPlan& a, const ChunkParams& p, hipStream_t stream) { return launch_chunks<_Float16, _Float16>(a, p, stream); }

@@ -25,9 +25,8 @@ using namespace vlut_chunk;
 // m is not the running maximum: it is the largest score of the first step in which the row sees anything, and stays, so that nothing but sums is in the loop
 // and O is never multiplied.  Weights are powers of two of the scores above m and may be as large as their type's range; where that does not do (bf16: l
 // shows 2^40 or O leaves fp32; fp16: O is no number) the part is begun again with the largest of all its scores, which a sweep over K finds.
-// P goes to the second product in the cache's type.  For 16-bit outputs that is one rounding more of the size of the output's own, of terms whose errors
-// are independent (bf16 2.3e-3 of the result instead of 1.7e-3); for fp32 it is carried in further terms, each what the rounding of those before it left: 24 bits, three of bf16
-// or two of fp16.
+// P goes to the second product in terms of the cache's type, each what the rounding of those before it left: two for 16-bit outputs (one would be a second rounding of the
+// size of the output's own: bf16 2.3e-3 of the result, not 1.7e-3), for fp32 those that carry 24 bits, three of bf16 or two of fp16.
 // What bounds it.  Few rows: the bytes of keys and values; 64 sequences of 3100 keys, 8 key heads of 128, 145 us or 5.3 TB/s, what a large copy reaches; 13 sequences and
 // 32 key heads of 100 (windows of 1024) 37 us.  A single sequence: the way through memory, 10 us, of which a step is 1.  Many rows: a step of a wave is 1024 cycles of the
 // matrix cores, 900 of its 32 exponentials and roundings a lane and 256 of LDS, which four waves share, so that two waves of a SIMD cover each other in part; 16384 tokens,
@@ -62,11 +61,9 @@ __device__ __forceinline__ Range range_of(const ChunkParams& p, const Chunk& c, 
     return r;
 }
 
-// Outputs: of the cache's type where weights are carried in one term, else fp32.
-template <class T, int TERMS>
-struct Output { typedef float type; };
-template <class T>
-struct Output<T, 1> { typedef T type; };
+// Terms of the cache's type that carry the weights of one row to outputs of type O: 24 bits for fp32, two for 16 bits.
+template <class T, class O>
+__host__ __device__ constexpr int terms() { return sizeof(O) == 4 ? Number<T>::kTerms : 2; }
 template <class O>
 __device__ __forceinline__ void store_four(void* out, int64_t at, const f32x4& o) {
     if constexpr (sizeof(O) == 4) *(dword_aligned_f32x4*)((float*)out + at) = o;
@@ -229,10 +226,10 @@ struct Count { static constexpr int value = N; };
 // whatever the rows' places: 13 sequences of 32 heads of 100 56 us, not 44.)
 // Where rows are few each wave has its keys for itself, and none waits for another; a step's keys are asked for as soon as the first product is done with
 // the ones before, its values behind the second.
-template <class T, int DP, int RW, int KW, int TERMS, int LOAD>
+template <class T, class O, int DP, int RW, int KW, int LOAD>
 __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t, unsigned char* lds) {
     typedef typename Number<T>::x8 x8;
-    typedef typename Output<T, TERMS>::type O;
+    constexpr int TERMS = terms<T, O>();
     constexpr bool FEW = RW == 1, WIDE = Number<T>::kWide, DIRECT = LOAD != kThroughRegisters, RUNS = LOAD == kRuns, OWN_KEYS = own_keys(RW, LOAD);
     constexpr int NW = RW * KW, WK = wave_keys(DP, RW), KT = WK / 32, KEYS = step_keys(DP, RW, KW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
     // Of a SIMD's two waves the one with matrix instructions alone goes first, then the one whose products with V have weights between them, so that they take turns: 1024 behind
@@ -837,7 +834,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
 }
 
 // Workgroup `i` of those for few rows, sequence by sequence, key head by key head, part by part.
-template <class T, int DP, int TERMS, int LOAD>
+template <class T, class O, int DP, int LOAD>
 __device__ __forceinline__ void few_rows(const ChunkParams& p, int i, unsigned char* lds) {
     Tile t;
     t.split = i % p.few_splits;
@@ -854,7 +851,7 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int i, unsigned c
             for (int64_t x = threadIdx.x; x < (int64_t)t.row_end * (p.D / 4); x += 64 * few_waves(DP)) {
                 const int row = (int)(x / (p.D / 4)), j = row / p.G, d = 4 * (int)(x % (p.D / 4));
                 const float nan = __builtin_nanf("");
-                store_four<typename Output<T, TERMS>::type>(p.out, (t.seq.start + j) * p.out_token + (int64_t)(t.h * p.G + row - j * p.G) * p.out_head + d, f32x4{nan, nan, nan, nan});
+                store_four<O>(p.out, (t.seq.start + j) * p.out_token + (int64_t)(t.h * p.G + row - j * p.G) * p.out_head + d, f32x4{nan, nan, nan, nan});
                 if (p.lse && d == 0) p.lse[(int64_t)(t.seq.start + j) * (p.Hk * p.G) + t.h * p.G + row - j * p.G] = nan;
             }
         return;
@@ -864,12 +861,12 @@ __device__ __forceinline__ void few_rows(const ChunkParams& p, int i, unsigned c
     t.direct = r.parts == 1;
     t.first = r.first + t.split * p.few_chunk;
     t.end = t.first + min(r.end - t.first, p.few_chunk);
-    attend_chunk<T, DP, 1, few_waves(DP), TERMS, LOAD>(p, t, lds);
+    attend_chunk<T, O, DP, 1, few_waves(DP), LOAD>(p, t, lds);
 }
 
 // Workgroup `i` of those for many rows: tile `at` of the sequences' tiles, one sequence behind the other, of each the one that sees most first; their parts and key heads
 // side by side.
-template <class T, int DP, int KW, int TERMS, int LOAD>
+template <class T, class O, int DP, int KW, int LOAD>
 __device__ __forceinline__ void many_rows(const ChunkParams& p, int i, unsigned char* lds) {
     constexpr int RW = 4, ROWS = kManyRows;
     static_assert(ROWS == 32 * RW, "32 rows a wave");
@@ -919,24 +916,24 @@ __device__ __forceinline__ void many_rows(const ChunkParams& p, int i, unsigned 
     t.direct = r.parts == 1;
     t.first = r.first + t.split * p.many_chunk;
     t.end = t.first + min(r.end - t.first, p.many_chunk);
-    attend_chunk<T, DP, RW, KW, TERMS, LOAD>(p, t, lds);
+    attend_chunk<T, O, DP, RW, KW, LOAD>(p, t, lds);
 }
 
 // Workgroups go to the 8 XCDs in turn, so that an XCD has every eighth of them: those of one key head, or of few, which read the same keys, where 8 and the number of key
 // heads have a divisor, and tiles that see much and little alike.  Where its 32 units have room for two workgroups each, the second ones go the other way, so that who has
 // the most has the least beside it.
-template <class T, int DP, int KW, int TERMS, int LOAD>
+template <class T, class O, int DP, int KW, int LOAD>
 __global__ void __launch_bounds__(256 * KW, DP > 128 ? 1 : 2) many_rows_kernel(const ChunkParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
     const int both = min(p.many_per_xcd, 64);
     int place = (int)blockIdx.x >> 3;
     if (KW == 1 && DP <= 128 && place >= 32 && place < both) place = both - 1 - (place - 32);
-    many_rows<T, DP, KW, TERMS, LOAD>(p, 8 * place + ((int)blockIdx.x & 7), lds);
+    many_rows<T, O, DP, KW, LOAD>(p, 8 * place + ((int)blockIdx.x & 7), lds);
 }
-template <class T, int DP, int TERMS, int LOAD>
+template <class T, class O, int DP, int LOAD>
 __global__ void __launch_bounds__(64 * few_waves(DP), DP > 128 ? 1 : 2) few_rows_kernel(const ChunkParams p) {
     extern __shared__ __align__(16) unsigned char lds[];
-    few_rows<T, DP, TERMS, LOAD>(p, ((int)blockIdx.x & 7) * p.few_per_xcd + ((int)blockIdx.x >> 3), lds);
+    few_rows<T, O, DP, LOAD>(p, ((int)blockIdx.x & 7) * p.few_per_xcd + ((int)blockIdx.x >> 3), lds);
 }
 
 // The parts of every row joined, where there are several: DP / 4 threads have four features each.

@@ -1,0 +1,83 @@
+"""Attention of chunks, what its numbers may lose: the bits of the weights, on every way that keys come in and for few and many rows."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from test_chunk_gpu import BF16, F16, HALF, U, case, reference, run
+from paper_2512_06443_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def device():
+    torch.cuda.set_device(0)
+
+
+# How keys come in -> query heads, key heads, features, page, the pages' order.
+LOADS = {
+    "whole_64": (8, 2, 64, 16, False),
+    "whole_128": (8, 2, 128, 64, True),
+    "whole_256": (4, 1, 256, 16, False),
+    "vectors_40": (6, 2, 40, 16, False),
+    "vectors_96": (4, 4, 96, 8, False),
+    "vectors_160": (4, 2, 160, 32, True),
+    "runs_60": (5, 1, 60, 16, False),
+    "runs_100": (4, 4, 100, 32, False),
+    "dwords_36": (4, 2, 36, 16, True),
+    "dwords_100": (4, 4, 100, 16, True),
+    "dwords_132": (2, 2, 132, 16, False),
+    "registers_72": (8, 2, 72, 4, False),
+    "registers_128": (8, 2, 128, 2, True),
+}
+# Single tokens, drafts, the same in parts, tiles whose keys two groups of waves share, the same in parts.
+ROWS = {"few": ([1, 3, 2], [9, 70, 300]), "few_in_parts": ([1, 2], [3000, 77]), "many": ([60, 140], [60, 200]), "many_in_parts": ([150], [2100])}
+
+
+def sharp(c):
+    """Queries of one feature: scores are single products, of a spread of one or two, whose fp32 values are nearly exact."""
+    D = c["q"].shape[2]
+    c["q"][..., 1:] = 0
+    c["q"][..., 0] = (c["q"][..., 0].float().abs() + 0.5).mul(D ** 0.5).to(c["q"].dtype)
+    return c
+
+
+def bound_of(c, out, window=0):
+    """Weights in two terms: each is off by half a step of the rest that the first term leaves, HALF^2 of it, and in fp16, whose smallest number is 2^-24, by
+    2^-25 of a reference that is so large beside l that (16 + n / 32) U of the largest value are the most for n keys; fp32 sums and scores as in test_chunk_gpu.check; the
+    output's own half step."""
+    ref = want, _, size, spread = reference(c, window)
+    n = int(c["lens"].max())
+    kind = c["k_cache"].dtype
+    flushed = (16 + n / 32) * U * float(c["v_cache"].abs().max()) if kind == F16 else 0.0
+    bound = size * (2 * spread[..., None] + U * (24 + n / 32) + HALF[kind] ** 2) * 1.02 + HALF[out] * want.abs() * 1.01 + flushed + (2.0 ** -25 if out == F16 else 1e-40)
+    return ref, bound
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows", list(ROWS))
+@pytest.mark.parametrize("load", list(LOADS))
+def test_weights_keep_their_bits_for_outputs_of_16_bits(load, rows, dtype):
+    """Where terms cancel, the output's own rounding says nothing, and one term of the cache's type would be off by up to HALF of their magnitudes."""
+    Hq, Hk, D, page, token_major = LOADS[load]
+    news, lens = ROWS[rows]
+    c = sharp(case(news, lens, Hq, Hk, D, dtype, page, seed=D, token_major=token_major))
+    for window in (0, 50):
+        got, _ = run(c, window)
+        (want, want_lse, _, _), bound = bound_of(c, dtype, window)
+        real = ~want_lse.isnan().any(-1)
+        off = ((got.double() - want).abs() / bound)[real]
+        assert bool((off <= 1.0).all()), float(off.max())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_weights_keep_their_bits_in_tiles_enough_for_all_units(dtype):
+    """Two workgroups of four waves a unit."""
+    for D in (128, 64, 100):
+        c = sharp(case([1200], [1230], 64, 64, D, dtype, 64, seed=D))
+        assert B.query_chunk_attention(1203, 1, 64, 64, D, 1200, 1230)[3:5] == (128, 1)
+        got, _ = run(c, max_len=1230, max_queries=1200)
+        (want, _, _, _), bound = bound_of(c, dtype)
+        off = ((got.double() - want).abs() / bound)[:1200]
+        assert bool((off <= 1.0).all()), float(off.max())
