@@ -408,9 +408,12 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                                 for (unsigned of = 16u * (unsigned)lane; of < run_bytes && (its >> (OWN / 8 - 1 - g) & 1); of += BYTES)
                                     at_lds<i32x4>(stage + (unsigned)((in_stage + 8 * g) * row_k) + of) = i32x4{N, N, N, N};
                     } else if (its != 0) {
+                        // (only what is loaded again: chunks behind D are zeros for every step)
 #pragma unroll
                         for (int x = 0; x < OWN / GK; ++x) {
-                            if (its >> (OWN / 8 - 1 - GK * x / 8) & 1) at_lds<i32x4>(stage + (unsigned)((in_stage + GK * x) * ROW + 16 * lane)) = i32x4{N, N, N, N};
+                            const int r = in_stage + GK * x + lane / CH, left = LOAD == kWholeVectors ? 8 : p.D - 8 * ((lane % CH) ^ turn_k(r));
+                            if ((its >> (OWN / 8 - 1 - GK * x / 8) & 1) && left > 0)
+                                at_lds<i32x4>(stage + (unsigned)((in_stage + GK * x) * ROW + 16 * lane)) = i32x4{N, N, left > 4 ? N : 0, left > 4 ? N : 0};
                         }
                     }
                 };
