@@ -490,9 +490,9 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
  * chunks of them, drafts and single tokens in one call.  Sequence b has the rows query_starts[b] .. query_starts[b + 1] - 1 of q and out, n of them, and
  * lens[b] tokens in all, of which the n are the last: query j has position p = lens[b] - n + j and sees the tokens max(0, p - window + 1) .. p (0 .. p with a window of 0):
  *   out[row][h] = sum_t softmax_t(scale * q[row][h] . k[t][h / G]) v[t][h / G],   G = query heads / key heads.
- * A query that sees nothing, or nothing but keys that score -inf, gets 0 (and lse -inf).  Rows of no sequence are left as they are.  Keys and values that a query does
+ * A query that sees nothing, or nothing but keys that score -inf, gets 0 (and lse -inf), whatever the values.  Rows of no sequence are left as they are.  Keys and values that a query does
  * not see have no influence on it, NaN and infinities included.  An infinite value that a query sees makes that feature of its output infinite; NaN with
- * infinities of both signs, and where the key's score is -inf.
+ * infinities of both signs, and where the key's score is -inf and others' are not.
  *   q, out            N tokens; q of the cache's type, out of that type or fp32, apart from q.  Scores and sums are fp32; softmax weights go to the product with V in two
  *                     terms of the cache's type, for fp32 outputs in as many as carry 24 bits.
  *   page_table        dev [B][table_stride]: pages of each sequence, token 0 first in page 0; ceil(lens[b] / page_size) of a row are read.  NULL for max_len 0

@@ -684,9 +684,13 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         sweep(multiply, weigh_up);
         // (a lane's O is of the keys of both halves)
         const float both = l + __shfl_xor(l, 32);
-        if (!finite() || (WIDE && !(both < 0x1p40f))) again[0] = 1;
+        const bool odd = !finite();
+        if (odd || (WIDE && !(both < 0x1p40f))) again[0] = 1;
         __syncthreads();
-        if (!again[0] || known) break;
+        if (!again[0] || known) {
+            if (odd && both == both) again[1] = 1;     // something to settle (or rows that are NaN by their scores)
+            break;
+        }
         known = true;
         m = none;
         sweep(multiply, [&](int kt, unsigned) {
@@ -710,7 +714,6 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         else if (z.lse) z.lse[row_sums] = lse_of(top, total);
     };
     // COUNT rows at once: r0, r0 + step, ..., each the lane's four features from d on, read at from + i * pitch
-    float odd = 0.0f;                          // (NaN where there is something to settle)
     auto put = [&](auto count, int r0, int step, int slot0, int d, auto read) {
         constexpr int COUNT = decltype(count)::value;
         f32x4 x[COUNT];
@@ -726,8 +729,6 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         for (int i = 0; i < COUNT; ++i) {
             const f32x4 y = factor[i] == 0.0f ? f32x4{0, 0, 0, 0} : x[i] * factor[i];
             if (t.row0 + r0 + i * step < t.row_end && d < z.D) {
-                const float nothing = __builtin_fmaf(y.x, 0.0f, __builtin_fmaf(y.y, 0.0f, __builtin_fmaf(y.z, 0.0f, y.w * 0.0f)));
-                odd += factor[i] == factor[i] ? nothing : 0.0f;
                 if (t.direct) store_four<O>(z.out, to[i], y);
                 else *(f32x4*)(parts + to[i]) = y;
             }
@@ -821,7 +822,6 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             __builtin_amdgcn_wave_barrier();
         }
     }
-    if (odd != 0.0f) again[1] = 1;
     wg_barrier_lds();                          // (no wait for the stores)
     if (__builtin_expect(again[1] != 0, 0)) {
         // every wave settles its own rows, or its share of them
@@ -830,7 +830,8 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         unsigned rows = 0;
         for (int r = kw; r < 32; r += KW) {
             const float factor = row_factor[FEW ? r : 32 * wave + r];
-            if (wave_row0 + r < t.row_end && factor == factor) rows |= 1u << r;
+            // (a row that nothing is of any weight for is 0; its part says what it has seen, as others may weigh something)
+            if (wave_row0 + r < t.row_end && factor == factor && !(t.direct && factor == 0.0f)) rows |= 1u << r;
         }
         settle_chunk<T, O, DP, FEW>(z, t, wave_row0, rows);
     }
@@ -967,7 +968,7 @@ __global__ void __launch_bounds__(256) combine_chunks(const ChunkParams p) {
     const Range r = range_of(p, c, row0 / p.G, (row_end - 1) / p.G, few ? p.few_chunk : p.many_chunk);
     if (r.parts == 1) return;
     float top = -__builtin_inff(), total = 0.0f;
-    f32x4 x = f32x4{0, 0, 0, 0};
+    f32x4 x = f32x4{0, 0, 0, 0}, odd = f32x4{0, 0, 0, 0};      // odd: infinities and NaN, as they are whatever their parts weigh
     for (int s0 = 0; s0 < r.parts; s0 += 4) {
         float m[4], l[4];
         f32x4 o[4];
@@ -979,11 +980,17 @@ __global__ void __launch_bounds__(256) combine_chunks(const ChunkParams p) {
             m[i] = ml.x;
             l[i] = ml.y;
             o[i] = *(const f32x4*)((few ? p.few_o : p.many_o) + at * p.D + d);
-            if (s0 + i >= r.parts || l[i] == 0.0f) {
+            const bool none = s0 + i >= r.parts;
+            if (none || l[i] == 0.0f) {
                 m[i] = -__builtin_inff();
                 l[i] = 0.0f;
-                o[i] = f32x4{0, 0, 0, 0};
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (none || is_odd(o[i][e])) {
+                    if (!none) odd[e] += o[i][e];
+                    o[i][e] = 0.0f;
+                }
         }
         const float now = fmaxf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), top), shift = now == -__builtin_inff() ? 0.0f : now;
         const float factor = exp2_fast(top - shift);
@@ -997,7 +1004,8 @@ __global__ void __launch_bounds__(256) combine_chunks(const ChunkParams p) {
         }
         top = now;
     }
-    store_four<O>(p.out, token * p.out_token + head * p.out_head + d, total == 0.0f ? f32x4{0, 0, 0, 0} : x * (1.0f / total));
+    x = total == 0.0f ? f32x4{0, 0, 0, 0} : x * (1.0f / total) + odd;
+    store_four<O>(p.out, token * p.out_token + head * p.out_head + d, x);
     if (p.lse && d == 0) p.lse[row] = lse_of(top, total);
 }
 
