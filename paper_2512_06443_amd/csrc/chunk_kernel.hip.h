@@ -235,7 +235,9 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     // Of a SIMD's two waves the one with matrix instructions alone goes first, then the one whose products with V have weights between them, so that they take turns: 1024 behind
     // 16384 298 -> 279 us, behind 8192 171 -> 162, 4096 tokens 116 -> 113.  64 features, whose products are half as long beside as many weights, 92 -> 97: not there.
     constexpr bool TURNS = !FEW && DP == 128;
-    constexpr float LIFT = 0.5f * Number<T>::kLift;            // (scores after the first step may be larger)
+    // What a row's reference weighs.  fp16: weights below 2^-25 are lost, n 2^-25 for n keys, which beside 2^4 is what sums of n keys in 32 bits may be off, n / 32 half steps; more
+    // where that leaves room enough for scores after the first step's, and all that there is where the largest of all is known.
+    constexpr float LIFT = 0.5f * Number<T>::kLift, FIRST_LIFT = 4.0f / 14.0f * Number<T>::kLift;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int wave_row0 = t.row0 + 32 * rw, row = wave_row0 + l32;
@@ -632,12 +634,13 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         auto weigh_up = [&](int kt, unsigned v_base) {
             hide(kt + WK * kw);
             if (!known && __any(m == none)) {
-                // fp16: of a few keys the largest says little, and later ones may leave it further behind
+                // fp16: the largest of a few keys says little of later ones, which may be up to 2^12 above it; of 16 and more 2^9
                 const int k0 = kt + WK * kw, seen = min(sees_to, k0 + WK) - max(sees_from, k0);
-                const float top = largest() - (seen < 16 ? 0.0f : LIFT);
+                const float top = largest() - (seen < 16 ? FIRST_LIFT : LIFT);
                 m = m == none ? top : m;
             }
             const float shift = m == none ? 0.0f : m;
+            float sum = 0.0f;                  // of this step: l has an addition a step, not one a key, as it may be large beside a key
             // Sixteen keys at a time; the weights and V of the next are made and read while the matrix cores are on these.
             x8 vf[DT], pf[TERMS], next[TERMS];
             unsigned v_from[DT];
@@ -647,7 +650,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     float left = exp2_fast(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], scale_log2, -shift));
-                    l += left;
+                    sum += left;
 #pragma unroll
                     for (int k = 0; k < TERMS; ++k) {
                         w[k][i] = (T)left;
@@ -679,6 +682,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
                 __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (TURNS) __builtin_amdgcn_s_setprio(0);
+            l += sum;
             pinned(l);                         // (or the sums are made behind the loop, from registers that wait for that)
         };
         sweep(multiply, weigh_up);
@@ -695,7 +699,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         m = none;
         sweep(multiply, [&](int kt, unsigned) {
             hide(kt + WK * kw);
-            m = fmaxf(m, largest() - LIFT);
+            m = fmaxf(m, largest() - Number<T>::kLift);
         });
         __syncthreads();
     }

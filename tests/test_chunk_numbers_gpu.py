@@ -4,7 +4,7 @@ from __future__ import annotations
 import pytest
 import torch
 
-from test_chunk_gpu import BF16, F16, HALF, U, case, reference, run
+from test_chunk_gpu import BF16, F16, F32, HALF, U, case, check, reference, run
 from paper_2512_06443_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -81,3 +81,21 @@ def test_weights_keep_their_bits_in_tiles_enough_for_all_units(dtype):
         (want, _, _, _), bound = bound_of(c, dtype)
         off = ((got.double() - want).abs() / bound)[:1200]
         assert bool((off <= 1.0).all()), float(off.max())
+
+
+@pytest.mark.parametrize("dtype,out", [(F16, F32), (F16, F16), (BF16, F32)])
+def test_tails_far_below_a_key_that_few_others_stand_beside_at_first(dtype, out):
+    """One key 17.4 nats, 2^25.07, above all 8191 others of the windows, in whose first steps it is among 1 to 15.  The others are 2.3e-4 of the result and of the sum of
+    weights, and may be off by 4.4e-5 of it in all: in fp16 their weights are lost unless the key's own is far above 1, and each alone is less than half a step
+    of a sum in 32 bits."""
+    n, m, window = 200, 9000, 8192
+    c = case([n], [m], 256, 256, 8, dtype, 32, seed=24)
+    assert B.query_chunk_attention(n + 3, 1, 256, 256, 8, n, m, window)[3:5] == (128, 1)
+    c["q"].zero_()
+    c["q"][..., 0] = 1
+    c["k_cache"][..., 0] = -17.375
+    c["v_cache"].abs_().add_(0.5)
+    loud = m - n - window + 1 + 62                         # the first key of query 62
+    c["k_cache"][int(c["page_table"][0, loud // 32]), :, loud % 32, 0] = 0
+    got, lse = run(c, window, out, scale=1.0, max_len=m, max_queries=n)
+    check(c, got, lse, window, 1.0, reference(c, window, 1.0))
