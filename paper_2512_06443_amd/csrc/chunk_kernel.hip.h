@@ -984,17 +984,19 @@ __global__ void __launch_bounds__(256) combine_chunks(const ChunkParams p) {
             m[i] = ml.x;
             l[i] = ml.y;
             o[i] = *(const f32x4*)((few ? p.few_o : p.many_o) + at * p.D + d);
-            const bool none = s0 + i >= r.parts;
-            if (none || l[i] == 0.0f) {
-                m[i] = -__builtin_inff();
-                l[i] = 0.0f;
-            }
+        }
+        // (behind all of the loads, which are on their way together)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (none || is_odd(o[i][e])) {
-                    if (!none) odd[e] += o[i][e];
-                    o[i][e] = 0.0f;
-                }
+        for (int i = 0; i < 4; ++i) {
+            const bool none = s0 + i >= r.parts, nothing = none || l[i] == 0.0f;
+            m[i] = nothing ? -__builtin_inff() : m[i];
+            l[i] = nothing ? 0.0f : l[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool no_number = is_odd(o[i][e]);
+                odd[e] += no_number && !none ? o[i][e] : 0.0f;
+                o[i][e] = no_number || none ? 0.0f : o[i][e];
+            }
         }
         const float now = fmaxf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), top), shift = now == -__builtin_inff() ? 0.0f : now;
         const float factor = exp2_fast(top - shift);
