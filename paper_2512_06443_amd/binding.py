@@ -243,6 +243,12 @@ def lut_bytes(K: int, N: int) -> int:
     return lib().vlut_lut_bytes(K, N)
 
 
+def _workspace(t: Optional[torch.Tensor]) -> None:
+    """A caller's workspace, of which kernels write as many bytes as its elements have, from its address on."""
+    if t is not None and not (t.is_cuda and t.is_contiguous()):
+        raise ValueError("workspace: a contiguous GPU tensor is wanted")
+
+
 def workspace_bytes(M: int, K: int, N: int) -> int:
     return lib().vlut_workspace_bytes(M, K, N)
 
@@ -313,6 +319,7 @@ def mpgemm(packed: torch.Tensor, w_scale: float, a_q: torch.Tensor, a_scale: tor
         y = torch.empty((N, M), dtype=torch.float32, device=dev)
     if acc is None and want_acc:
         acc = torch.empty((M, N), dtype=torch.int32, device=dev)
+    _workspace(workspace)
     ws_bytes = lib().vlut_mfma_workspace_bytes(M, K, N) if mfma else workspace_bytes(M, K, N)
     if workspace is None and ws_bytes:
         workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
@@ -381,6 +388,7 @@ def mpgemm_rows(packed: torch.Tensor, w_scale_rows: torch.Tensor, a_q: torch.Ten
     if y is None:
         y = torch.empty((N, M), dtype=torch.float32, device=dev)
     acc = torch.empty((M, N), dtype=torch.int32, device=dev) if want_acc else None
+    _workspace(workspace)
     ws_bytes = workspace_bytes(M, K, N)
     if workspace is None and ws_bytes:
         workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
@@ -437,6 +445,7 @@ def mpgemm_f32(packed: torch.Tensor, w_scale, x: torch.Tensor, M: int, y: Option
         y = torch.empty((N, M), dtype=torch.float32, device=x.device)
     acc = torch.empty((M, N), dtype=torch.int32, device=x.device) if want_acc else None
     scales = torch.empty(N, dtype=torch.float32, device=x.device) if want_scales else None
+    _workspace(workspace)
     if workspace is None:
         ws_bytes = L.vlut_workspace_bytes_f32(M, K, N)
         if ws_bytes:
@@ -523,6 +532,7 @@ def mpgemm_g5(packed: torch.Tensor, w_scale: float, a_q: torch.Tensor, a_scale: 
     if y is None:
         y = torch.empty((N, M), dtype=torch.float32, device=dev)
     acc = torch.empty((M, N), dtype=torch.int32, device=dev) if want_acc else None
+    _workspace(workspace)
     ws_bytes = lib().vlut_workspace_bytes_g5(M, K, N)
     if workspace is None and ws_bytes:
         workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
@@ -697,6 +707,7 @@ def shared_prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     if out.shape != q.shape:
         raise ValueError("out: a tensor of q's shape is wanted")
     lse = torch.empty((B, n, Hq), dtype=torch.float32, device=q.device) if want_lse else None
+    _workspace(workspace)
     if workspace is None:
         nbytes = shared_prefix_attention_bytes(B, n, Hq, Hk, D, prefix_len, max_own_len)
         if nbytes:
@@ -762,6 +773,7 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
         raise ValueError("out: a tensor of q's shape is wanted")
     _here(q, k_cache, v_cache, page_table, query_starts, lens, out, workspace)
     lse = torch.empty((N, Hq), dtype=torch.float32, device=q.device) if want_lse else None
+    _workspace(workspace)
     if workspace is None:
         nbytes = chunk_attention_bytes(N, B, Hq, Hk, D, max_queries, max_len, window)
         if nbytes:
@@ -870,6 +882,7 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
     logprob = None if tokens is None else new(torch.float32, N)
     entropy = new(torch.float32, N) if want_entropy else None
     ids, logprobs = (new(torch.int64, N, top), new(torch.float32, N, top)) if top > 0 else (None, None)
+    _workspace(workspace)
     if workspace is None:
         nbytes = token_logprobs_bytes(N, V, top)
         if nbytes:

@@ -148,7 +148,7 @@ PyObject* py_shared_prefix_attention(PyObject*, PyObject* const* o, Py_ssize_t n
         const int64_t B = q->size(0), nq = q->size(1), Hq = q->size(2), D = q->size(3);
         const at::Tensor *kc = plain(o[1]), *vc = plain(o[2]);
         if (!cache_of(kc, vc, D, cache) || !optional(o[3], prefix) || !whole(o[4], prefix_len) || !optional(o[5], table) || !indices(lens = plain(o[6]), at::kInt, B) ||
-            !optional(o[7], queries) || !optional_features(o[11], gout, 4) || !optional(o[13], gws) || D < 1 || cache.page_size < 1)
+            !optional(o[7], queries) || !optional_features(o[11], gout, 4) || !workspace(o[13], gws) || D < 1 || cache.page_size < 1)
             Py_RETURN_NONE;
         if (table && (table->scalar_type() != at::kInt || table->dim() != 2 || table->size(0) != B || (table->size(1) > 1 && table->stride(1) != 1))) Py_RETURN_NONE;
         const int64_t room = table ? table->size(1) * cache.page_size : 0;
@@ -161,7 +161,7 @@ PyObject* py_shared_prefix_attention(PyObject*, PyObject* const* o, Py_ssize_t n
         c10::ScalarType type = q->scalar_type();
         const int want_lse = PyObject_IsTrue(o[12]);
         if (want_lse < 0) { PyErr_Clear(); Py_RETURN_NONE; }
-        if (!type_of(o[10], type) || (gout && !same_sizes(*gout, *q)) || (gws && !gws->data_ptr())) Py_RETURN_NONE;
+        if (!type_of(o[10], type) || (gout && !same_sizes(*gout, *q))) Py_RETURN_NONE;
         at::Tensor out, lse, ws;
         if (gout) out = *gout;
         if (gws) ws = *gws;

@@ -49,7 +49,7 @@ PyObject* py_chunk_attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
         c10::ScalarType type = q->scalar_type();
         const int want_lse = PyObject_IsTrue(o[12]);
         if (want_lse < 0) { PyErr_Clear(); Py_RETURN_NONE; }
-        if (!type_of(o[10], type) || !optional_features(o[11], gout, 3) || (gout && !same_sizes(*gout, *q)) || !optional(o[13], gws) || (gws && !gws->data_ptr()) ||
+        if (!type_of(o[10], type) || !optional_features(o[11], gout, 3) || (gout && !same_sizes(*gout, *q)) || !workspace(o[13], gws) ||
             !here(q, kc, vc, table, starts, lens, gout, gws))
             Py_RETURN_NONE;
         at::Tensor out, lse, ws;
@@ -160,11 +160,11 @@ PyObject* py_token_logprobs(PyObject*, PyObject* const* o, Py_ssize_t n) {
         const at::Tensor *logits, *tokens, *gws;
         int64_t top;
         float temperature;
-        if (!layer_call(n, 6) || !features(logits = plain(o[0]), 2) || !optional(o[1], tokens) || !whole(o[2], top) || !real(o[3], temperature) || !optional(o[5], gws)) Py_RETURN_NONE;
+        if (!layer_call(n, 6) || !features(logits = plain(o[0]), 2) || !optional(o[1], tokens) || !whole(o[2], top) || !real(o[3], temperature) || !workspace(o[5], gws)) Py_RETURN_NONE;
         const int64_t N = logits->size(0), V = logits->size(1);
         const int want_entropy = PyObject_IsTrue(o[4]);
         if (want_entropy < 0) { PyErr_Clear(); Py_RETURN_NONE; }
-        if ((tokens && !indices(tokens, at::kLong, N)) || top < 0 || top > VLUT_MAX_TOP || (gws && !gws->data_ptr()) || !here(logits, tokens, gws)) Py_RETURN_NONE;
+        if ((tokens && !indices(tokens, at::kLong, N)) || top < 0 || top > VLUT_MAX_TOP || !here(logits, tokens, gws)) Py_RETURN_NONE;
         at::Tensor logprob, entropy, ids, logprobs, ws;
         if (gws) ws = *gws;
         int rc;

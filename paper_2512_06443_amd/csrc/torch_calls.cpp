@@ -69,6 +69,8 @@ bool optional(PyObject* o, const at::Tensor*& t) {
     t = nullptr;
     return o == Py_None || (t = plain(o)) != nullptr;
 }
+// None, or a workspace: kernels write as many bytes as its elements have, from its address on
+bool workspace(PyObject* o, const at::Tensor*& t) { return optional(o, t) && (!t || (t->is_contiguous() && t->data_ptr())); }
 bool output(PyObject* o, const at::Tensor*& t) { return optional(o, t) && (!t || t->dim() >= 1); }
 
 at::Tensor make(c10::IntArrayRef size, c10::ScalarType type, c10::Device dev) {
@@ -153,7 +155,7 @@ PyObject* product(PyObject* const* o, Bytes used, Call call) {
         float w_scale;
         int64_t M;
         if (!packed || !q || !s || q->dim() < 2 || s->dim() < 1 || !real(o[1], w_scale) || !whole(o[4], M) || M < 0 || !output(o[5], gy) ||
-            !optional(o[6], gacc) || !optional(o[8], gws) || (gws && !gws->data_ptr()) || ((uintptr_t)packed->data_ptr() | (uintptr_t)q->data_ptr()) % 16 != 0)
+            !optional(o[6], gacc) || !workspace(o[8], gws) || ((uintptr_t)packed->data_ptr() | (uintptr_t)q->data_ptr()) % 16 != 0)
             Py_RETURN_NONE;
         const int64_t K = q->size(1), N = s->size(0);
         const int want = PyObject_IsTrue(o[7]);
@@ -200,7 +202,7 @@ PyObject* py_mpgemm_f32(PyObject*, PyObject* const* o, Py_ssize_t n) {
         float w_scale = 1.0f;
         int64_t M;
         if (!ordinary(n, 8) || !(packed = plain(o[0])) || !matrix(x = plain(o[2]), at::kFloat) || !whole(o[3], M) || M < 0 || !output(o[4], gy) ||
-            !optional(o[7], gws))
+            !workspace(o[7], gws))
             Py_RETURN_NONE;
         if (!real(o[1], w_scale) && (!(rows = plain(o[1])) || rows->scalar_type() != at::kFloat || rows->numel() != M)) Py_RETURN_NONE;
         const int want_acc = PyObject_IsTrue(o[5]), want_scales = PyObject_IsTrue(o[6]);
