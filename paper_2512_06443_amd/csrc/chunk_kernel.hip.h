@@ -24,7 +24,7 @@ using namespace vlut_chunk;
 // transposing reads.
 // m is not the running maximum: it is the largest score of the first step in which the row sees anything, and stays, so that nothing but sums is in the loop
 // and O is never multiplied.  Weights are powers of two of the scores above m and may be as large as their type's range; where that does not do (bf16: l
-// shows 2^40 or O leaves fp32; fp16: O is no number) the part is begun again with the largest of all its scores, which a sweep over K finds.
+// shows 2^40 or O 2^64; fp16: O is no number) the part is begun again with the largest of all its scores, which a sweep over K finds.
 // P goes to the second product in terms of the cache's type, each what the rounding of those before it left: two for 16-bit outputs (one would be a second rounding of the
 // size of the output's own: bf16 2.3e-3 of the result, not 1.7e-3), for fp32 those that carry 24 bits, three of bf16 or two of fp16.
 // What bounds it.  Few rows: the bytes of keys and values; 64 sequences of 3100 keys, 8 key heads of 128, 145 us or 5.3 TB/s, what a large copy reaches; 13 sequences and
@@ -237,7 +237,8 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     constexpr bool TURNS = !FEW && DP == 128;
     // What a row's reference weighs.  fp16: weights below 2^-25 are lost, n 2^-25 for n keys, which beside 2^4 is what sums of n keys in 32 bits may be off, n / 32 half steps; more
     // where that leaves room enough for scores after the first step's, and all that there is where the largest of all is known.
-    constexpr float LIFT = 0.5f * Number<T>::kLift, FIRST_LIFT = 4.0f / 14.0f * Number<T>::kLift;
+    // bf16, whose weights have fp32's range: 2^-30 there, so that the sum of as many values as there may be keys is a number where the values are.
+    constexpr float LIFT = 0.5f * Number<T>::kLift, FIRST_LIFT = 4.0f / 14.0f * Number<T>::kLift, KNOWN_LIFT = WIDE ? -30.0f : Number<T>::kLift;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int wave_row0 = t.row0 + 32 * rw, row = wave_row0 + l32;
@@ -612,16 +613,17 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
             for (int e = 0; e < 16; ++e) top = fmaxf(top, s[i][e]);
         return fmaxf(top, __shfl_xor(top, 32)) * scale_log2;
     };
+    // Every result is a number, and none above 2^64, so that those of all waves and parts together are numbers too.
     auto finite = [&]() {
-        float zero[4] = {};                    // (or NaN)
+        float squares[4] = {};                 // (or infinite, or NaN)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 if (RUNS && 32 * dt + 8 * (e >> 2) + 4 * half >= p.D) continue;
-                zero[e & 3] = __builtin_fmaf(o[dt][e], 0.0f, zero[e & 3]);
+                squares[e & 3] = __builtin_fmaf(o[dt][e], o[dt][e], squares[e & 3]);
             }
-        return zero[0] + zero[1] + zero[2] + zero[3] == 0.0f;
+        return squares[0] + squares[1] + squares[2] + squares[3] < __builtin_inff();
     };
     const float none = -__builtin_inff();
     for (bool known = false;;) {
@@ -699,7 +701,7 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         m = none;
         sweep(multiply, [&](int kt, unsigned) {
             hide(kt + WK * kw);
-            m = fmaxf(m, largest() - Number<T>::kLift);
+            m = fmaxf(m, largest() - KNOWN_LIFT);
         });
         __syncthreads();
     }

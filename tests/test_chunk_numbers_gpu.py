@@ -99,3 +99,39 @@ def test_tails_far_below_a_key_that_few_others_stand_beside_at_first(dtype, out)
     c["k_cache"][int(c["page_table"][0, loud // 32]), :, loud % 32, 0] = 0
     got, lse = run(c, window, out, scale=1.0, max_len=m, max_queries=n)
     check(c, got, lse, window, 1.0, reference(c, window, 1.0))
+
+
+@pytest.mark.parametrize("out", [BF16, F32])
+@pytest.mark.parametrize("rows", list(ROWS))
+@pytest.mark.parametrize("load", ["whole_64", "whole_128", "whole_256", "runs_100", "registers_72"])
+def test_values_near_the_types_largest(load, rows, out):
+    """Their mean is a number of the type, though their sum is none: sums of up to 3000 weights times values of 2^127."""
+    Hq, Hk, D, page, token_major = LOADS[load]
+    news, lens = ROWS[rows]
+    c = sharp(case(news, lens, Hq, Hk, D, BF16, page, seed=D, token_major=token_major))
+    c["v_cache"].sign_().add_(0.5).mul_(2.0 ** 126)        # 1.5 and -0.5 times 2^126
+    got, lse = run(c, 0, out)
+    assert bool(got[:sum(news)].isfinite().all())
+    check(c, got, lse)
+
+
+@pytest.mark.parametrize("out", [BF16, F32])
+@pytest.mark.parametrize("rows", list(ROWS))
+@pytest.mark.parametrize("load", ["whole_64", "whole_128", "whole_256", "runs_100", "registers_72"])
+def test_values_near_the_types_largest_in_two_places(load, rows, out):
+    """Two keys that count, of two waves or parts, whose values are numbers each, but not together."""
+    Hq, Hk, D, page, token_major = LOADS[load]
+    news, lens = ROWS[rows]
+    for second in (40, 69, max(lens) - 10):
+        c = case(news, lens, Hq, Hk, D, BF16, page, seed=D, token_major=token_major)
+        c["q"].zero_()
+        c["q"][..., 0] = 1
+        c["k_cache"][..., 0] = -60
+        c["v_cache"].fill_(1.875 * 2.0 ** 127)
+        for b, n in enumerate(lens):
+            for t in (5, second):
+                if t < n:
+                    c["k_cache"][int(c["page_table"][b, t // page]), :, t % page, 0] = 0
+        got, lse = run(c, 0, out, scale=1.0)
+        assert bool(got[:sum(news)].isfinite().all())
+        check(c, got, lse, scale=1.0)
