@@ -690,13 +690,13 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         sweep(multiply, weigh_up);
         // (a lane's O is of the keys of both halves)
         const float both = l + __shfl_xor(l, 32);
-        const bool odd = !finite();
-        if (odd || (WIDE && !(both < 0x1p40f))) again[0] = 1;
-        __syncthreads();
-        if (!again[0] || known) {
-            if (odd && both == both) again[1] = 1;     // something to settle (or rows that are NaN by their scores)
-            break;
+        if (!finite()) {
+            again[0] = 1;
+            if (known && both == both) again[1] = 1;       // something to settle (else scores that are no numbers)
         }
+        if (WIDE && !(both < 0x1p40f)) again[0] = 1;
+        __syncthreads();
+        if (!again[0] || known) break;
         known = true;
         m = none;
         sweep(multiply, [&](int kt, unsigned) {
