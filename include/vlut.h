@@ -494,7 +494,8 @@ int vlut_shared_prefix_attention(const vlut_heads* q, int64_t q_sequence_stride,
  * not see have no influence on it, NaN and infinities included.  An infinite value that a query sees makes that feature of its output infinite; NaN with
  * infinities of both signs, and where the key's score is -inf and others' are not.
  *   q, out            N tokens; q of the cache's type, out of that type or fp32, apart from q.  Scores and sums are fp32; softmax weights go to the product with V in two
- *                     terms of the cache's type, for fp32 outputs in as many as carry 24 bits.
+ *                     terms of the cache's type, for fp32 outputs in as many as carry 24 bits (fp16: those below 2^-29 of a row's first largest one may
+ *                     count for nothing).
  *   page_table        dev [B][table_stride]: pages of each sequence, token 0 first in page 0; ceil(lens[b] / page_size) of a row are read.  NULL for max_len 0
  *   query_starts      dev [B + 1], ascending, within 0 .. N (a sequence whose two are not has no rows)
  *   lens              dev [B], 0 <= lens[b] <= max_len

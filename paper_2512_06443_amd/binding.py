@@ -746,7 +746,7 @@ def chunk_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     """Runs vlut_chunk_attention: q [N][heads][D] (the cache's type) holds the new tokens of B sequences one behind the other, sequence b's from row
     query_starts[b] to query_starts[b + 1] (int32 [B + 1]); they are the last of its lens[b] tokens (int32 [B]), whose keys and values the pages of
     its row of `page_table` (int32 [B][pages]) hold.  Each sees the tokens up to itself, the last `window` of them where that is not 0.
-    max_queries, max_len: upper bounds (default: N, and what the table's rows hold).  scale: default D ** -0.5.  dtype: fp32 or the cache's
+    max_queries, max_len: upper bounds, which size the launches (default: N, and what the table's rows hold).  scale: default D ** -0.5.  dtype: fp32 or the cache's
     (default).  Returns (out [N][heads][D], lse fp32 [N][heads] or None); rows of no sequence are left as they are."""
     if _native is not None:
         r = _native.chunk_attention(q, k_cache, v_cache, page_table, query_starts, lens, max_queries, max_len, window, scale, dtype, out, want_lse, workspace)

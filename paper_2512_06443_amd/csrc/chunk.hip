@@ -1,4 +1,5 @@
-// Attention of chunks of new tokens over a paged cache, for MI355X (gfx950): its host side and part of the C ABI; the kernels are in two more units.
+// Attention of chunks of new tokens over a paged cache, for MI355X (gfx950): its host side and part of the C ABI; the kernels are in four more units, one
+// for each type of the cache and of the outputs.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -41,11 +42,12 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
         a.few_row_places = (int)std::min<int64_t>(kFewRows, std::max<int64_t>(1, most_rows / G) * G);
         // Parts only so that 640 waves are at work, each of four steps at least where there are many: a wave's way to its first keys and its results' way out take as long
         // as seven steps, and those that join parts 4 us.  32 steps at most, so that one long sequence among short ones does not keep the others' units waiting, or more
-        // where those would be more than 8192 workgroups.  us with parts of 1, 2, 4, 8, 16 / 32 steps, joining included, 32 query and 8 key heads of 128 in bf16 (20
-        // and 5 where it says so): a sequence of 1000 keys 12.9, 13.2, 15.3, 16.1; of 2000 (20, 5) 14.3, 14.0, 15.3, 19.7, 24.7; of 8000 28, 20, 17, 20, 28 / 45; 4 of 8000
-        // 56, 42, 35, 33, 34 / 52; 8 of 4000 51, 39, 33, 33, 36 / 49; 16 of up to 4000 80, 60, 51, 47, 47 / 52; 32 of 8 queries behind up to 3000 (20, 5) 85, 66, 54, 49,
-        // 62 / 45; 48 of up to 4095 142, 112, 97, 95, 96 / 91; 64 of 2048 to 4095 230, 176, 152, 151, 151 / 143; 13 of up to 1990 in windows of 1024, 32 heads of 100 that
-        // are not shared, 77, 57, 49, 45 / 36.
+        // where those would be more than 8192 workgroups.  us of the kernels with parts of 1, 2, 4, 8, 16 / 32 steps, joining included, 32 query and 8 key heads of 128 in bf16
+        // (20 and 5 where it says so): a sequence of 1000 keys 15.0, 15.9, 18.0, 18.9; of 2000 (20, 5) 15.5, 15.5, 18.2, 23.0, 28.8; of 8000 31, 24, 21, 24, 33 / 54; 4 of 8000
+        // 55, 40, 33, 31, 34 / 55; 8 of 4000 50, 37, 32, 31, 36 / 52; 16 of up to 4000 87, 63, 52, 49, 49 / 57; 32 of 8 queries behind up to 3000 (20, 5) 91, 68, 56, 51,
+        // 64 / 49; 48 of up to 4095 154, 119, 101, 98, 98 / 94; 64 of 2048 to 4095 252, 187, 161, 147, 147 / 147; 13 of up to 1990 in windows of 1024, 32 heads of 100 that
+        // are not shared, 79, 59, 51, 57, 37 / 37.  8 query and 2 key heads of 256 features, parts of 1, 4, 8, 16, 32 steps of two waves: a sequence of 8000 keys 42, 25, 30, 44,
+        // 74; 16 of up to 4000 63, 33, 32, 45, 75; 64 of 2048 to 4095 163, 99, 87, 80, 84.  What this takes is within 6 % of the best of each, of the last 11.
         const int64_t step = step_keys(a.DP, 1, few_waves(a.DP)), keys = seen(kFewRows), steps = ceil_div(keys, step);
         const int64_t wanted = ceil_div(640, few_waves(a.DP) * B * Hk);
         const int64_t least = std::min<int64_t>(4, ceil_div(steps, 6)), most = std::max<int64_t>(32, ceil_div(B * Hk * steps, 8192));
@@ -67,11 +69,14 @@ int plan_chunks(int64_t N, int64_t B, int64_t Hq, int64_t Hk, int64_t D, int64_t
         // As many as there are if all sequences with many rows have as many as they may have.
         const int64_t tiles = std::min<int64_t>(a.many_tiles, ceil_div(rows, most_rows) * ceil_div(most_rows, kManyRows)) * Hk;
         // Two workgroups of four waves on a unit, one's waits beside the other's work, where there are tiles for that; else one whose eight waves share the keys, unless
-        // those are so many that parts of them are as good.  us, 4 x 1 / 4 x 2, parts joined included, 20 query and 5 key heads of 128 in bf16: 4096 tokens 109 / 121, in
-        // windows of 16 24 / 37, of 1024 80 / 89, 2500 tokens 62 / 55; 32 and 8 heads: 16384 tokens 2070 / 2290, 4096 141 / 173, of 64 features 91 / 124, 2048 56 / 56, 1024
-        // 39 / 26, behind 4096 97 / 93, 8192 157 / 159, 16384 285 / 289; 256 behind 16384 82 / 84; 32 heads of 100 that are not shared, 909 tokens in windows of 1024, 53 / 50.
+        // those are so many that parts of them are as good.  us, 4 x 1 / 4 x 2, parts joined included, 20 query and 5 key heads of 128 in bf16: 4096 tokens 148 / 159, in
+        // windows of 16 24 / 39, of 1024 94 / 109, 2500 tokens 80 / 68; 32 and 8 heads: 16384 tokens 2890 / 3100, 4096 198 / 230, of 64 features 133 / 161, 2048 72 / 69, 1024
+        // 42 / 32, behind 4096 132 / 123, 8192 222 / 218, 16384 442 / 460; 256 behind 16384 111 / 112; 32 heads of 100 that are not shared, 909 tokens in windows of 1024, 61 / 58.
+        // (A cache that goes through registers is 4 x 1 in any case, which is not known here: half of the places stay empty where these are 2.)
         a.key_waves = a.DP <= 128 && tiles < 2 * kUnits && keys < 12288 ? 2 : 1;
         const int64_t slots = (a.DP <= 128 && a.key_waves == 1 ? 2 : 1) * kUnits, step = step_keys(a.DP, 4, a.key_waves);
+        // Parts of 512 keys at least.  us with 256 / 512 / 1024 / 2048: 128 behind 4096 35, 35, 37, 43, behind 1024 25, 24, 26, 30; 256 behind 4096 46, 46, 46, 51; of 256
+        // features, 8 and 2 heads, 512 behind 4096 57, 57, 71, 99.
         const int64_t splits = std::min(std::max<int64_t>(1, slots / tiles), ceil_div(keys, 512));
         a.many_chunk = (int)(ceil_div(ceil_div(keys, splits), step) * step);
         a.many_splits = (int)ceil_div(keys, a.many_chunk);

@@ -28,11 +28,10 @@ using namespace vlut_chunk;
 // P goes to the second product in terms of the cache's type, each what the rounding of those before it left: two for 16-bit outputs (one would be a second rounding of the
 // size of the output's own: bf16 2.3e-3 of the result, not 1.7e-3), for fp32 those that carry 24 bits, three of bf16 or two of fp16.
 // What bounds it.  Few rows: the bytes of keys and values; 64 sequences of 3100 keys, 8 key heads of 128, 145 us or 5.3 TB/s, what a large copy reaches; 13 sequences and
-// 32 key heads of 100 (windows of 1024) 37 us.  A single sequence: the way through memory, 10 us, of which a step is 1.  Many rows: a step of a wave is 1024 cycles of the
-// matrix cores, 900 of its 32 exponentials and roundings a lane and 256 of LDS, which four waves share, so that two waves of a SIMD cover each other in part; 16384 tokens,
-// 32 and 8 heads of 128, 2070 us or 1.06 PFLOP/s, four fifths of what a large product reaches; 4096 tokens of 20 and 5 heads 109 us (0.79), of which a quarter is units that
-// wait for the last tiles.  (With every other tile from the lighter end, and an XCD's tiles one stretch of them, 8 us more.)  fp32 outputs, three products with V
-// instead of one, twice as long.
+// 32 key heads of 100 (windows of 1024) 38 us.  A single sequence: the way through memory, 10 us, of which a step is 1.  Many rows: a step of a wave is 1536 cycles of the
+// matrix cores, some 1200 of its 32 exponentials and roundings a lane and 256 of LDS, which four waves share, so that two waves of a SIMD cover each other in part; 16384 tokens,
+// 32 and 8 heads of 128, 2850 us: 0.77 PFLOP/s of the formula's operations, 1.16 with the weights' second term, 0.86 of what a large product reaches; 4096 tokens of 20
+// and 5 heads 147 us (0.58 and 0.88), of which a quarter is units that wait for the last tiles.  fp32 outputs, three products with V instead of two, a third longer.
 // ---------------------------------------------------------------------------------------------
 
 struct Chunk {                         // of a sequence: its first token's row and position; bad: a length that cannot be
@@ -233,7 +232,8 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     constexpr bool FEW = RW == 1, WIDE = Number<T>::kWide, DIRECT = LOAD != kThroughRegisters, RUNS = LOAD == kRuns, OWN_KEYS = own_keys(RW, LOAD);
     constexpr int NW = RW * KW, WK = wave_keys(DP, RW), KT = WK / 32, KEYS = step_keys(DP, RW, KW), KS = DP / 16, CH = DP / 8, GK = 64 / CH, DT = DP / 32;
     // Of a SIMD's two waves the one with matrix instructions alone goes first, then the one whose products with V have weights between them, so that they take turns: 1024 behind
-    // 16384 298 -> 279 us, behind 8192 171 -> 162, 4096 tokens 116 -> 113.  64 features, whose products are half as long beside as many weights, 92 -> 97: not there.
+    // 16384 468 -> 429 us, behind 8192 229 -> 217, 4096 tokens 151 -> 148.  Little either way for 64 features, whose products are half as long beside as many weights (133 -> 132),
+    // and for 256, of which a SIMD has one wave (132 -> 132): not there.
     constexpr bool TURNS = !FEW && DP == 128;
     // What a row's reference weighs.  fp16: weights below 2^-25 are lost, n 2^-25 for n keys, which beside 2^4 is what sums of n keys in 32 bits may be off, n / 32 half steps; more
     // where that leaves room enough for scores after the first step's, and all that there is where the largest of all is known.

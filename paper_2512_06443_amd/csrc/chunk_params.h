@@ -1,4 +1,4 @@
-// What the host side of the attention of chunks (chunk.hip) and its kernels (chunk_kernel.hip.h, compiled once for each type of the cache) share.
+// What the host side of the attention of chunks (chunk.hip) and its kernels (chunk_kernel.hip.h, compiled once for each type of the cache and of the outputs) share.
 #pragma once
 
 #include <hip/hip_runtime.h>

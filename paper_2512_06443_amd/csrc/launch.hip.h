@@ -1,4 +1,4 @@
-// How the host side of both translation units launches a kernel.
+// How the host sides of the translation units launch a kernel.
 #pragma once
 
 #include <atomic>

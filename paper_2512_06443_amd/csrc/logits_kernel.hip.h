@@ -13,7 +13,7 @@ namespace {
 // (only terms of one sign are added in l and d).  Exponentials are powers of two of c times a difference of logits, c = log2(e) / temperature;
 // m stays a logit, since times c a row of the type's lowest values would leave 32 bits.
 // A logit of -inf is a token that is not allowed: it adds nothing.  A row of nothing else has log probabilities of -inf and an entropy of 0.
-// A thread keeps its own m, l and d over its logits; they meet at the end of the part, and those of a row's parts in join_kernel:
+// A thread keeps its own m, l and d over its logits; they meet at the end of the part, and those of a row's parts in logits_join_kernel:
 //   m = max m_i,  l = sum exp(m_i - m) l_i,  d = sum exp(m_i - m) (d_i + (m - m_i) l_i).
 // The largest: a key of 64 bits, the logit's bits in the order of its value ahead of ~index, orders tokens as they are to come out, ties by the lowest
 // index, and no two are alike.  Of a chunk of 256 threads' logits: the k-th largest of a wave's threads' own largest ones is a bound that k of the chunk's logits

@@ -1,5 +1,5 @@
 // What the attention's kernels share: the matrix instructions on either type of a cache, rows of features, and the compiler's order of things.
-// Part of the translation units attention_bf16.hip, attention_f16.hip, chunk_bf16.hip and chunk_f16.hip.
+// Part of the translation units attention_bf16.hip, attention_f16.hip, chunk_bf16.hip, chunk_bf16_f32.hip, chunk_f16.hip and chunk_f16_f32.hip.
 #pragma once
 
 namespace {
@@ -27,7 +27,7 @@ struct Number<_Float16> {
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     static constexpr unsigned kExponents = 0x7c007c00u, kNan = 0x7e007e00u;
     static constexpr bool kWide = false;
-    static constexpr float kLift = 14.0f;             // weights are up to 2^14, so that those of 2^-38 of the largest are no zeros yet
+    static constexpr float kLift = 14.0f;             // weights are up to 2^14, so that those of 2^-38 of the largest are no zeros yet (less where the largest is not known)
     static constexpr int kTerms = 2;
 };
 #if defined(__HIP_DEVICE_COMPILE__)

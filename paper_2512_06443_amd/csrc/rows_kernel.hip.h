@@ -16,8 +16,8 @@ namespace {
 // all in fp32, rounded once where it is stored; x is of the h that was not rounded.
 // A workgroup has a row, and a thread keeps its NV vectors of VEC features of everything in registers from the loads, which are on their way together, to
 // the stores: the only exchanges are the two sums of squares.
-// Bound by its bytes: 4096 rows of 4096 features in 16 bits, both norms and a gate, 134 MB in 25 us or 5.3 TB/s, what a large copy reaches; 1024 rows of 6912 in fp32 with
-// their gate 85 MB in 15.0 us (the cache holds some of them).  One row: 2.2 us, a launch and two trips to memory.
+// Bound by its bytes: 4096 rows of 4096 features in 16 bits, both norms and a gate, 134 MB in 25 us where some of them are in the cache, in calls one behind the other 30 us or
+// 4.5 TB/s (a large copy: 5.3); 1024 rows of 6912 in fp32 with their gate 85 MB in 15 us (the cache holds some of them).  One row: 2.2 us, a launch and two trips to memory.
 // Features that a thread has: launch_rows.  32 are more than its registers hold and go through scratch memory in part; only rows of more than 16384 features have them.
 // ---------------------------------------------------------------------------------------------
 struct RowsParams {
