@@ -24,7 +24,8 @@ using namespace vlut_chunk;
 // transposing reads.
 // m is not the running maximum: it is the largest score of the first step in which the row sees anything, and stays, so that nothing but sums is in the loop
 // and O is never multiplied.  Weights are powers of two of the scores above m and may be as large as their type's range; where that does not do (bf16: l
-// shows 2^40 or O 2^64; fp16: O is no number) the part is begun again with the largest of all its scores, which a sweep over K finds.
+// shows 2^40 or O 2^64; fp16: O is no number) the part is begun again with the largest of all its scores, which a sweep over K finds, and
+// (bf16) where O passes 2^64 all the same, once more with weights that add up to 1 at most.
 // P goes to the second product in terms of the cache's type, each what the rounding of those before it left: two for 16-bit outputs (one would be a second rounding of the
 // size of the output's own: bf16 2.3e-3 of the result, not 1.7e-3), for fp32 those that carry 24 bits, three of bf16 or two of fp16.
 // What bounds it.  Few rows: the bytes of keys and values; 64 sequences of 3100 keys, 8 key heads of 128, 145 us or 5.3 TB/s, what a large copy reaches; 13 sequences and
@@ -237,22 +238,23 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
     constexpr bool TURNS = !FEW && DP == 128;
     // What a row's reference weighs.  fp16: weights below 2^-25 are lost, n 2^-25 for n keys, which beside 2^4 is what sums of n keys in 32 bits may be off, n / 32 half steps; more
     // where that leaves room enough for scores after the first step's, and all that there is where the largest of all is known.
-    // bf16, whose weights have fp32's range: 2^-30 there, so that the sum of as many values as there may be keys is a number where the values are.
-    constexpr float LIFT = 0.5f * Number<T>::kLift, FIRST_LIFT = 4.0f / 14.0f * Number<T>::kLift, KNOWN_LIFT = WIDE ? -30.0f : Number<T>::kLift;
+    constexpr float LIFT = 0.5f * Number<T>::kLift, FIRST_LIFT = 4.0f / 14.0f * Number<T>::kLift;
+    // The last time that a part is worked on: with the largest of all scores; bf16, where sums of values near the type's largest are no numbers, with weights that add up to 1.
+    constexpr int LAST = WIDE ? 2 : 1;
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), rw = wave % RW, kw = wave / RW;
     const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
     const int wave_row0 = t.row0 + 32 * rw, row = wave_row0 + l32;
     const int first_key = t.first, end_key = t.end;
 
-    // behind the buffers: the waves' m and l where they share rows, where the rows' results go and their factors, two flags (the part is to be
-    // begun again; there is something to settle), pages' numbers
+    // behind the buffers: the waves' m and l where they share rows, where the rows' results go and their factors, flags (the part is to be begun again,
+    // for the first and the second time, [0] and [2]; there is something to settle, [1]), pages' numbers
     float* const row_m = (float*)(lds + tile_bytes(DP, RW, KW, LOAD));
     float* const row_l = row_m + 32 * NW;
     int64_t* const row_to = (int64_t*)(row_l + 32 * NW);
     float* const row_factor = (float*)(row_to + 32 * NW);
     int* const again = (int*)(row_factor + 32 * NW);
     int* const page_ids = again + 4;
-    if (tid == 0) again[0] = again[1] = 0;
+    if (tid == 0) again[0] = again[1] = again[2] = 0;
     if constexpr (LOAD == kDwords || LOAD == kVectors) {
         for (int x = 16 * tid; x < tile_bytes(DP, RW, KW, LOAD); x += 16 * 64 * NW) *(i32x4*)(lds + x) = i32x4{0, 0, 0, 0};
     }
@@ -626,16 +628,16 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         return squares[0] + squares[1] + squares[2] + squares[3] < __builtin_inff();
     };
     const float none = -__builtin_inff();
-    for (bool known = false;;) {
+    for (int turn = 0;; ++turn) {
         l = 0.0f;
-        if (!known) m = blind ? 0.0f : none;
+        if (turn == 0) m = blind ? 0.0f : none;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
         auto weigh_up = [&](int kt, unsigned v_base) {
             hide(kt + WK * kw);
-            if (!known && __any(m == none)) {
+            if (turn == 0 && __any(m == none)) {
                 // fp16: the largest of a few keys says little of later ones, which may be up to 2^12 above it; of 16 and more 2^9
                 const int k0 = kt + WK * kw, seen = min(sees_to, k0 + WK) - max(sees_from, k0);
                 const float top = largest() - (seen < 16 ? FIRST_LIFT : LIFT);
@@ -690,20 +692,18 @@ __device__ __forceinline__ void attend_chunk(const ChunkParams& p, const Tile& t
         sweep(multiply, weigh_up);
         // (a lane's O is of the keys of both halves)
         const float both = l + __shfl_xor(l, 32);
-        if (!finite()) {
-            again[0] = 1;
-            if (known && both == both) again[1] = 1;       // something to settle (else scores that are no numbers)
-        }
-        if (WIDE && !(both < 0x1p40f)) again[0] = 1;
+        // (rows whose scores are no numbers are what they are)
+        if ((both == both && !finite()) || (WIDE && both >= 0x1p40f)) again[turn < LAST ? 2 * turn : 1] = 1;   // the last time: something to settle
         __syncthreads();
-        if (!again[0] || known) break;
-        known = true;
-        m = none;
-        sweep(multiply, [&](int kt, unsigned) {
-            hide(kt + WK * kw);
-            m = fmaxf(m, largest() - KNOWN_LIFT);
-        });
-        __syncthreads();
+        if (turn == LAST || !again[2 * turn]) break;
+        if (turn == 0) {
+            m = none;
+            sweep(multiply, [&](int kt, unsigned) {
+                hide(kt + WK * kw);
+                m = fmaxf(m, largest() - Number<T>::kLift);
+            });
+            __syncthreads();
+        } else m += (float)(32 - __builtin_clz(t.seq.len));
     }
     l += __shfl_xor(l, 32);
     if (t.seq.bad) l = __builtin_nanf("");

@@ -135,3 +135,22 @@ def test_values_near_the_types_largest_in_two_places(load, rows, out):
         got, lse = run(c, 0, out, scale=1.0)
         assert bool(got[:sum(news)].isfinite().all())
         check(c, got, lse, scale=1.0)
+
+
+@pytest.mark.parametrize("out,exponent", [(BF16, -112), (F32, -104)])
+@pytest.mark.parametrize("rows", list(ROWS))
+@pytest.mark.parametrize("load", ["whole_64", "whole_128", "whole_256", "runs_100", "registers_72"])
+def test_small_values_behind_scores_that_rise(load, rows, out, exponent):
+    """Parts that are begun again: their weights are not so small that products with values of 2^-112 lose their bits."""
+    Hq, Hk, D, page, token_major = LOADS[load]
+    news, lens = ROWS[rows]
+    c = case(news, lens, Hq, Hk, D, BF16, page, seed=D, token_major=token_major)
+    c["q"].zero_()
+    c["q"][..., 0] = 1
+    c["v_cache"].mul_(2.0 ** exponent)
+    c["k_cache"][..., 0] = c["k_cache"][..., 0].clamp(-1, 1)
+    for b, n in enumerate(lens):
+        t = torch.arange(3, n, 7, device="cuda")
+        c["k_cache"][c["page_table"][b].long()[t // page], :, t % page, 0] += (t.clamp(max=400) / 5.0).to(BF16)[:, None]
+    got, lse = run(c, 0, out, scale=1.0)
+    check(c, got, lse, scale=1.0)
