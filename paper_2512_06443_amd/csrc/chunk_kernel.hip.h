@@ -32,7 +32,7 @@ using namespace vlut_chunk;
 // 32 key heads of 100 (windows of 1024) 38 us.  A single sequence: the way through memory, 10 us, of which a step is 1.  Many rows: a step of a wave is 1536 cycles of the
 // matrix cores, some 1200 of its 32 exponentials and roundings a lane and 256 of LDS, which four waves share, so that two waves of a SIMD cover each other in part; 16384 tokens,
 // 32 and 8 heads of 128, 2850 us: 0.77 PFLOP/s of the formula's operations, 1.16 with the weights' second term, 0.86 of what a large product reaches; 4096 tokens of 20
-// and 5 heads 147 us (0.58 and 0.88), of which a quarter is units that wait for the last tiles.  fp32 outputs, three products with V instead of two, a third longer.
+// and 5 heads 150 us (0.57 and 0.86), of which a quarter is units that wait for the last tiles.  fp32 outputs, three products with V instead of two, a third longer.
 // ---------------------------------------------------------------------------------------------
 
 struct Chunk {                         // of a sequence: its first token's row and position; bad: a length that cannot be
